@@ -213,6 +213,120 @@ int knap_ulysses_gather_chunks(const void* recv, const int32_t* row_map, int64_t
 int knap_ulysses_scatter_chunks(const void* z, const int32_t* row_map, int64_t total_tokens,
                                 int heads_local, int d, void* send, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Rotary positions of packed queries and keys, in front of knap_varlen_attn_*.
+ * The first `rot` columns of every head form rot / 2 pairs: columns (i, i + rot / 2)
+ * in the half layout, (2 i, 2 i + 1) in the interleaved one.  Pair i of a row at
+ * position p becomes
+ *     (a, b) -> factor * (a cos - b sin, a sin + b cos),  angle = p * freq[i],
+ * and the columns from rot on are copied.  knap_rope_bwd is the transpose, which takes
+ * gradients back through it: the same call with -sin.
+ *
+ * q (tokens, H, d) -> q_out, k (tokens, H_k, d) -> k_out, bf16, d fastest; both in one
+ * launch.  H_k = 0: q alone (k and k_out are not looked at).  strides: NULL for
+ * contiguous tensors, else a HOST array of eight strides in elements: of a token and
+ * of a head in q, k, q_out, k_out.  Strides of inputs are 0 or larger; rows of an
+ * output must not overlap (either the heads of a token lie between two tokens, or the
+ * tokens of a head between two heads).  An output may be its input (in place, same
+ * strides); otherwise outputs must not overlap inputs or each other (not checked).
+ * Pointers of q and k need an alignment of 2 bytes only; the fast form takes
+ * 16, strides that are multiples of 8 and units of 8 columns (rot a multiple of 8
+ * in the interleaved layout, of 16 in the half one, d of 8).
+ *
+ * Positions, one of:
+ *   positions   device int32 (tokens, n_axes), contiguous: a position on each axis
+ *               (text, row, column, frame, ...).  axis_pairs: HOST int[n_axes], how
+ *               many consecutive pairs turn by each axis, rot / 2 in all; NULL for one axis.
+ *   cu_seqlens  (positions NULL) device int32[n_seq + 1] of the bag: a row's position
+ *               is counted from its sequence's first row.  Rows from cu_seqlens[n_seq]
+ *               on (a padded bag) are left as they were.
+ * freq: device float64[rot / 2], radians per position; knap_rope_frequencies makes
+ * them.  Angles are formed in 64 bits and reduced to a fraction of a turn, so that
+ * any 32-bit position keeps a bf16 result exact to its rounding.
+ *
+ * Supported: 1 <= H, 0 <= H_k, (H + H_k) * d <= 2^24, 2 <= rot <= d <= 1024, rot even, factor
+ * finite, tokens < 2^31, 1 <= n_axes <= KNAP_ROPE_MAX_AXES, n_seq <= KNAP_MAX_SEQS.
+ * tokens = 0, or n_seq = 0 without positions, enqueues nothing.  Any number of calls may
+ * run at once; captured calls keep the values of strides, axis_pairs and factor.
+ * As for the forward, the first call of the library on a device must not be captured.
+ * ------------------------------------------------------------------------ */
+#define KNAP_ROPE_HALF        0
+#define KNAP_ROPE_INTERLEAVED 1
+#define KNAP_ROPE_MAX_AXES    4
+#define KNAP_ROPE_MAX_DIM     1024
+
+int knap_rope_fwd(const void* q, const void* k, int64_t tokens, int H, int H_k, int d,
+                  const int64_t* strides, int rot, int layout,
+                  const int32_t* positions, int n_axes, const int* axis_pairs,
+                  const int32_t* cu_seqlens, int n_seq,
+                  const double* freq, float factor,
+                  void* q_out, void* k_out, void* stream);
+int knap_rope_bwd(const void* dq_out, const void* dk_out, int64_t tokens, int H, int H_k, int d,
+                  const int64_t* strides, int rot, int layout,
+                  const int32_t* positions, int n_axes, const int* axis_pairs,
+                  const int32_t* cu_seqlens, int n_seq,
+                  const double* freq, float factor,
+                  void* dq, void* dk, void* stream);
+
+/* Frequencies of `rot` columns on one axis (HOST array freq[rot / 2]) and the factor
+ * that goes with them:  f_i = base^(-2 i / rot), for a context `scale` times the one
+ * trained on (scale >= 1):
+ *   KNAP_ROPE_PLAIN   f_i
+ *   KNAP_ROPE_LINEAR  f_i / scale (positions interpolated)
+ *   KNAP_ROPE_BASE    base * scale^(rot / (rot - 2)) for the base: the last pair turns as
+ *                     slowly as interpolated, the first as before (rot > 2)
+ *   KNAP_ROPE_PARTS   by the turns r = trained_len f_i / (2 pi) of a pair in the trained
+ *                     length: f_i where r >= high, f_i / scale where r <= low, in between
+ *                     (1 - g) f_i / scale + g f_i with g = (r - low) / (high - low);
+ *                     factor = 0.1 ln(scale) + 1, in the other kinds 1.
+ * trained_len, low and high count for the last kind alone (low < high). */
+#define KNAP_ROPE_PLAIN  0
+#define KNAP_ROPE_LINEAR 1
+#define KNAP_ROPE_BASE   2
+#define KNAP_ROPE_PARTS  3
+int knap_rope_frequencies(int rot, double base, int kind, double scale, int64_t trained_len,
+                          double low, double high, double* freq, double* factor);
+
+/* ------------------------------------------------------------------------
+ * Layer norm of rows, in front of the projections of a block and behind each
+ * head of an attention output (rows = T * H, width = d).
+ *     mean, rstd = 1 / sqrt(var + eps) of a row (var over `width` values),
+ *     xh = (x - mean) rstd,  y = xh w + b
+ * backward, with g = dy w:
+ *     dx = rstd (g - mean(g) - xh mean(g xh)),  dw = sum dy xh,  db = sum dy  (over all rows)
+ *
+ * x (rows, width): KNAP_BF16 or KNAP_F32, y of the same type or KNAP_BF16; dx has the type
+ * of x, dy that of y.  A row's columns are contiguous; strides count elements from a row to
+ * the next, >= width (not looked at for a single row).  weight and bias: `width` values of
+ * w_type, or NULL for ones and zeros.  Sums and statistics are 32-bit; mean and rstd
+ * fp32[rows], NULL in the forward where no backward follows.  dweight and dbias: fp32[width],
+ * fully overwritten, NULL where not wanted; they are summed in a fixed order, so that the
+ * same call on the same device gives the same bits.  Pointers of rows and weights need the
+ * alignment of their type only; 16 bytes, strides and widths that are multiples of 8 give
+ * the fast form.  workspace: knap_layer_norm_bwd_workspace_bytes(rows, width) bytes,
+ * 256-byte aligned, needed where dweight or dbias is wanted; one for each call that may
+ * run at the same time.  Outputs must not alias inputs.
+ *
+ * Supported: 1 <= width <= KNAP_LAYER_NORM_MAX_WIDTH, 0 <= rows < 2^31, eps finite and >= 0
+ * (a constant row with eps = 0 gives NaN).  rows = 0 enqueues nothing in the forward and
+ * zeros in dweight and dbias in the backward.  As for the forward of attention, the
+ * first call of the library on a device must not be captured.
+ * ------------------------------------------------------------------------ */
+#define KNAP_BF16 0
+#define KNAP_F32  1
+#define KNAP_LAYER_NORM_MAX_WIDTH 16384
+
+int knap_layer_norm_fwd(const void* x, int x_type, int64_t x_stride, int64_t rows, int width,
+                        const void* weight, const void* bias, int w_type, float eps,
+                        void* y, int y_type, int64_t y_stride,
+                        float* mean, float* rstd, void* stream);
+int knap_layer_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t rows, int width,
+                        const void* weight, int w_type, const float* mean, const float* rstd,
+                        const void* dy, int y_type, int64_t dy_stride,
+                        void* dx, int64_t dx_stride, float* dweight, float* dbias,
+                        void* workspace, size_t workspace_bytes, void* stream);
+size_t knap_layer_norm_bwd_workspace_bytes(int64_t rows, int width);
+
 /* Message for a KNAP_ERR_* code (static string, never NULL). */
 const char* knap_strerror(int code);
 

@@ -25,6 +25,17 @@ KNAP_ERR_SCRATCH_TOO_SMALL = -7
 KNAP_NOALLOC_MAX_ROWS = 4 * 1024 * 1024
 KNAP_MAX_SEQS = 2048
 KNAP_ULYSSES_MAX_GPUS = 64
+KNAP_ROPE_HALF = 0
+KNAP_ROPE_INTERLEAVED = 1
+KNAP_ROPE_MAX_AXES = 4
+KNAP_ROPE_MAX_DIM = 1024
+KNAP_ROPE_PLAIN = 0
+KNAP_ROPE_LINEAR = 1
+KNAP_ROPE_BASE = 2
+KNAP_ROPE_PARTS = 3
+KNAP_BF16 = 0
+KNAP_F32 = 1
+KNAP_LAYER_NORM_MAX_WIDTH = 16384
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -56,6 +67,12 @@ _SIGNATURES = {
     "knap_ulysses_gather_chunks": (_i, [_vp, _vp, _i64, _i, _i, _vp, _vp]),
     "knap_ulysses_scatter_chunks": (_i, [_vp, _vp, _i64, _i, _i, _vp, _vp]),
     "knap_ulysses_local_tokens": (_i, [_pi64, _i, _i, _pi64]),
+    "knap_rope_fwd": (_i, [_vp, _vp, _i64, _i, _i, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _vp, _f, _vp, _vp, _vp]),
+    "knap_rope_bwd": (_i, [_vp, _vp, _i64, _i, _i, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _vp, _f, _vp, _vp, _vp]),
+    "knap_rope_frequencies": (_i, [_i, _d, _i, _d, _i64, _d, _d, _pd, _pd]),
+    "knap_layer_norm_fwd": (_i, [_vp, _i, _i64, _i64, _i, _vp, _vp, _i, _f, _vp, _i, _i64, _vp, _vp, _vp]),
+    "knap_layer_norm_bwd": (_i, [_vp, _i, _i64, _i64, _i, _vp, _i, _vp, _vp, _vp, _i, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "knap_layer_norm_bwd_workspace_bytes": (_sz, [_i64, _i]),
     "knap_strerror": (C.c_char_p, [_i]),
     "knap_last_hip_error": (_i, []),
     "knap_launch_workgroups": (_i, [_i]),
@@ -256,6 +273,147 @@ def knap_ulysses_local_tokens(seq_lens, g: int):
     out = (C.c_int64 * g)()
     _check(lib.knap_ulysses_local_tokens(arr, n, g, out), "knap_ulysses_local_tokens")
     return [int(v) for v in out]
+
+
+# --------------------------------------------------------------------------- rotary positions, layer norm
+
+def _refuse(where: str, what: str) -> None:
+    err = KnapError(KNAP_ERR_INVALID_ARG, where)
+    err.args = (f"{err.args[0]}: {what}",)
+    raise err
+
+
+def _here(where: str, *tensors) -> None:
+    """Tensors that are not on the current device, whose stream the call would go to, are refused."""
+    dev = _current_device() if _current_device is not None else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            _refuse(where, f"a tensor on device {t.get_device()} while device {dev} is current")
+
+
+_KNAP_TYPES = {torch.bfloat16: KNAP_BF16, torch.float32: KNAP_F32}
+
+
+def _rope(fn, where: str, q, k, rot, layout, freq, factor, q_out, k_out, positions, axis_pairs, cu_seqlens, stream, check) -> int:
+    _here(where, q, k, q_out, k_out, freq, positions, cu_seqlens)
+    T, H, d = q.shape
+    H_k = 0 if k is None else k.shape[1]
+    bf16 = torch.bfloat16
+    for x, y in ((q, q_out), (k, k_out)):
+        if x is None:
+            continue
+        if x.dtype is not bf16 or y is None or y.dtype is not bf16 or x.shape != y.shape or x.shape[0] != T or x.shape[2] != d:
+            _refuse(where, "q, k and their outputs are bf16 (tokens, heads, d) tensors of the same tokens and d")
+        if d > 1 and (x.stride(2) != 1 or y.stride(2) != 1):
+            _refuse(where, "the columns of a head are contiguous")
+    if freq.dtype is not torch.float64 or freq.numel() != rot // 2 or not freq.is_contiguous():
+        _refuse(where, "freq is a contiguous float64 tensor of rot / 2 entries")
+    strides = None
+    if not (q.is_contiguous() and q_out.is_contiguous() and (k is None or (k.is_contiguous() and k_out.is_contiguous()))):
+        ks, kos = (k.stride(), k_out.stride()) if k is not None else ((0, 0), (0, 0))
+        qs, qos = q.stride(), q_out.stride()
+        strides = (C.c_int64 * 8)(qs[0], qs[1], ks[0], ks[1], qos[0], qos[1], kos[0], kos[1])
+    n_axes, pairs, n_seq = 0, None, 0
+    if positions is not None:
+        n_axes = 1 if positions.dim() == 1 else positions.shape[1]
+        if positions.dtype is not torch.int32 or positions.shape[0] != T or not positions.is_contiguous():
+            _refuse(where, "positions is a contiguous int32 (tokens, axes) tensor")
+        if axis_pairs:
+            if len(axis_pairs) != n_axes:
+                _refuse(where, "axis_pairs has an entry for each axis")
+            pairs = (C.c_int * n_axes)(*axis_pairs)
+    elif cu_seqlens is not None:
+        if cu_seqlens.dtype is not torch.int32 or not cu_seqlens.is_contiguous():
+            _refuse(where, "cu_seqlens is a contiguous int32 tensor")
+        n_seq = cu_seqlens.numel() - 1
+    else:
+        _refuse(where, "positions or cu_seqlens")
+    rc = fn(_ptr(q), _ptr(k), T, H, H_k, d, strides, rot, layout, _ptr(positions), n_axes, pairs, _ptr(cu_seqlens), n_seq, _ptr(freq),
+            factor, _ptr(q_out), _ptr(k_out), _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+def knap_rope_fwd(q, k, rot: int, layout: int, freq, factor: float, q_out, k_out, positions=None, axis_pairs=None, cu_seqlens=None,
+                  stream=None, check: bool = True) -> int:
+    """Rotary positions of q (T, H, d) and k (T, H_k, d) or None; any strides of tokens and heads.  positions: int32 (T,) or
+    (T, axes), else the position in the own sequence of cu_seqlens.  freq: float64 CUDA tensor of rot / 2 entries."""
+    return _rope(lib.knap_rope_fwd, "knap_rope_fwd", q, k, rot, layout, freq, factor, q_out, k_out, positions, axis_pairs, cu_seqlens,
+                 stream, check)
+
+
+def knap_rope_bwd(dq_out, dk_out, rot: int, layout: int, freq, factor: float, dq, dk, positions=None, axis_pairs=None, cu_seqlens=None,
+                  stream=None, check: bool = True) -> int:
+    """Gradients back through knap_rope_fwd: the same arguments, turned the other way."""
+    return _rope(lib.knap_rope_bwd, "knap_rope_bwd", dq_out, dk_out, rot, layout, freq, factor, dq, dk, positions, axis_pairs, cu_seqlens,
+                 stream, check)
+
+
+def knap_rope_frequencies(rot: int, base: float = 10000.0, kind: int = KNAP_ROPE_PLAIN, scale: float = 1.0, trained_len: int = 1,
+                          low: float = 1.0, high: float = 32.0) -> Tuple[List[float], float]:
+    """Frequencies of rot / 2 pairs (radians per position) and the factor that goes with them."""
+    freq, factor = (C.c_double * max(1, rot // 2))(), C.c_double()
+    _check(lib.knap_rope_frequencies(rot, base, kind, scale, trained_len, low, high, freq, C.byref(factor)), "knap_rope_frequencies")
+    return list(freq), factor.value
+
+
+def _rows(where: str, name: str, t, rows: int, width: int, dtype=None) -> int:
+    """The row stride of a (rows, width) tensor with contiguous rows, checked."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        _refuse(where, f"{name} is a (rows, width) tensor with contiguous rows")
+    if t.dtype not in _KNAP_TYPES or (dtype is not None and t.dtype is not dtype):
+        _refuse(where, f"the type of {name}")
+    return t.stride(0)
+
+
+def _vector(where: str, name: str, t, n: int, dtype=None) -> None:
+    if t is not None and (t.numel() != n or not t.is_contiguous() or (t.dtype is not dtype if dtype is not None else t.dtype not in _KNAP_TYPES)):
+        _refuse(where, f"{name} is a contiguous vector of {n} values of its type")
+
+
+def knap_layer_norm_fwd(x, weight, bias, eps: float, y, mean=None, rstd=None, stream=None, check: bool = True) -> int:
+    """y = (x - mean) rstd weight + bias of every row of x (rows, width); weight and bias (of one type) may be None."""
+    where = "knap_layer_norm_fwd"
+    _here(where, x, weight, bias, y, mean, rstd)
+    rows, width = x.shape
+    xs, ys = _rows(where, "x", x, rows, width), _rows(where, "y", y, rows, width)
+    _vector(where, "weight", weight, width)
+    _vector(where, "bias", bias, width, None if weight is None else weight.dtype)
+    _vector(where, "mean", mean, rows, torch.float32)
+    _vector(where, "rstd", rstd, rows, torch.float32)
+    w = weight if weight is not None else bias
+    rc = lib.knap_layer_norm_fwd(_ptr(x), _KNAP_TYPES[x.dtype], xs, rows, width, _ptr(weight), _ptr(bias),
+                                 KNAP_F32 if w is None else _KNAP_TYPES[w.dtype], eps, _ptr(y), _KNAP_TYPES[y.dtype], ys, _ptr(mean),
+                                 _ptr(rstd), _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+def knap_layer_norm_bwd_workspace_bytes(rows: int, width: int) -> int:
+    return int(lib.knap_layer_norm_bwd_workspace_bytes(rows, width))
+
+
+def knap_layer_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, workspace_bytes: Optional[int] = None, stream=None,
+                        check: bool = True) -> int:
+    """dx (of x's type), dweight and dbias (fp32, or None) of knap_layer_norm_fwd, whose mean and rstd it takes."""
+    where = "knap_layer_norm_bwd"
+    _here(where, x, weight, mean, rstd, dy, dx, dweight, dbias, workspace)
+    rows, width = x.shape
+    xs, dys, dxs = _rows(where, "x", x, rows, width), _rows(where, "dy", dy, rows, width), _rows(where, "dx", dx, rows, width, x.dtype)
+    _vector(where, "weight", weight, width)
+    for name, t, n in (("mean", mean, rows), ("rstd", rstd, rows), ("dweight", dweight, width), ("dbias", dbias, width)):
+        _vector(where, name, t, n, torch.float32)
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib.knap_layer_norm_bwd(_ptr(x), _KNAP_TYPES[x.dtype], xs, rows, width, _ptr(weight),
+                                 KNAP_F32 if weight is None else _KNAP_TYPES[weight.dtype], _ptr(mean), _ptr(rstd), _ptr(dy),
+                                 _KNAP_TYPES[dy.dtype], dys, _ptr(dx), dxs, _ptr(dweight), _ptr(dbias), _ptr(workspace), workspace_bytes,
+                                 _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
 
 
 # --------------------------------------------------------------------------- host model / balancer

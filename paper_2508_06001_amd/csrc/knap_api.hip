@@ -310,6 +310,173 @@ int knap_ulysses_scatter_chunks(const void* z, const int32_t* row_map, int64_t t
   return ulysses_rows(z, send, row_map, total_tokens, heads_local, d, false, stream);
 }
 
+// ---------------------------------------------------------------------------
+// Rotary positions
+// ---------------------------------------------------------------------------
+
+namespace {
+
+// rows of an output must not overlap: the heads of a token lie between two tokens, or the tokens of a head between two heads
+bool rows_apart(int64_t tokens, int heads, int d, int64_t token, int64_t head) {
+  if (token < 0 || head < 0) return false;
+  if ((heads == 1 || head >= d) && (tokens == 1 || (token >= d && token - d >= (heads - 1) * head))) return true;
+  return (tokens == 1 || token >= d) && (heads == 1 || (head >= d && (head - d) / token >= tokens - 1));
+}
+
+int rope_impl(const void* q, const void* k, int64_t tokens, int H, int H_k, int d, const int64_t* strides, int rot, int layout,
+              const int32_t* positions, int n_axes, const int* axis_pairs, const int32_t* cu_seqlens, int n_seq,
+              const double* freq, float factor, void* q_out, void* k_out, bool backward, void* stream) {
+  if (tokens < 0 || tokens > INT32_MAX || H < 1 || H_k < 0 || d < 2 || d > KNAP_ROPE_MAX_DIM || rot < 2 || rot > d || rot % 2)
+    return KNAP_ERR_INVALID_ARG;
+  if (((int64_t)H + H_k) * d > (1 << 24) || (layout != KNAP_ROPE_HALF && layout != KNAP_ROPE_INTERLEAVED)) return KNAP_ERR_INVALID_ARG;
+  if (!(factor > -3.0e38f && factor < 3.0e38f)) return KNAP_ERR_INVALID_ARG;
+  knap::RopeArgs a{};
+  if (positions) {
+    if (n_axes < 1 || n_axes > KNAP_ROPE_MAX_AXES || (n_axes > 1 && !axis_pairs)) return KNAP_ERR_INVALID_ARG;
+    int64_t end = 0;
+    for (int x = 0; x < KNAP_ROPE_MAX_AXES; ++x) {
+      if (x < n_axes && axis_pairs) {
+        if (axis_pairs[x] < 0) return KNAP_ERR_INVALID_ARG;
+        end += axis_pairs[x];
+      } else if (x == 0) {
+        end = rot / 2;
+      }
+      if (end > rot / 2) return KNAP_ERR_INVALID_ARG;
+      a.axis_end[x] = (int)end;
+    }
+    if (end != rot / 2) return KNAP_ERR_INVALID_ARG;
+  } else {
+    if (n_seq < 0) return KNAP_ERR_INVALID_ARG;
+    if (n_seq > KNAP_MAX_SEQS) return KNAP_ERR_TOO_MANY_SEQS;
+    if (n_seq == 0) return KNAP_OK;
+  }
+  if (tokens == 0) return KNAP_OK;
+  if (!q || !q_out || !freq || (H_k > 0 && (!k || !k_out)) || (!positions && !cu_seqlens)) return KNAP_ERR_INVALID_ARG;
+  if (!aligned(q, 2) || !aligned(q_out, 2) || !aligned(freq, 8) || !aligned(positions, 4) || !aligned(cu_seqlens, 4)) return KNAP_ERR_INVALID_ARG;
+  if (H_k > 0 && (!aligned(k, 2) || !aligned(k_out, 2) || q_out == k_out || q_out == k || k_out == q)) return KNAP_ERR_INVALID_ARG;
+  const int64_t row_q = (int64_t)H * d, row_k = (int64_t)H_k * d;
+  const int64_t packed[8] = {row_q, d, row_k, d, row_q, d, row_k, d};
+  const int64_t* s = strides ? strides : packed;
+  constexpr int64_t kMostStride = (int64_t)1 << 40;         // (row, stride) products stay far from 64 bits
+  for (int i = 0; i < 8; ++i)
+    if ((H_k > 0 || (i & 2) == 0) && (s[i] < 0 || s[i] > kMostStride)) return KNAP_ERR_INVALID_ARG;
+  if (!rows_apart(tokens, H, d, s[4], s[5]) || (H_k > 0 && !rows_apart(tokens, H_k, d, s[6], s[7]))) return KNAP_ERR_INVALID_ARG;
+  const bool in_place_q = q_out == q, in_place_k = H_k > 0 && k_out == k;
+  if ((in_place_q && (s[0] != s[4] || s[1] != s[5])) || (in_place_k && (s[2] != s[6] || s[3] != s[7]))) return KNAP_ERR_INVALID_ARG;
+  a.q = static_cast<const __bf16*>(q);
+  a.q_out = static_cast<__bf16*>(q_out);
+  a.q_token = s[0]; a.q_head = s[1]; a.qo_token = s[4]; a.qo_head = s[5];
+  const bool half = layout == KNAP_ROPE_HALF;
+  bool wide = d % 8 == 0 && rot % (half ? 16 : 8) == 0 && aligned(q, 16) && aligned(q_out, 16) && (s[0] | s[1] | s[4] | s[5]) % 8 == 0;
+  if (H_k > 0) {
+    a.k = static_cast<const __bf16*>(k);
+    a.k_out = static_cast<__bf16*>(k_out);
+    a.k_token = s[2]; a.k_head = s[3]; a.ko_token = s[6]; a.ko_head = s[7];
+    wide = wide && aligned(k, 16) && aligned(k_out, 16) && (s[2] | s[3] | s[6] | s[7]) % 8 == 0;
+  }
+  a.T = (int)tokens; a.H = H; a.Hk = H_k; a.d = d; a.rot = rot;
+  a.positions = positions; a.n_axes = n_axes;
+  a.cu = cu_seqlens; a.n_seq = n_seq;
+  a.freq = freq;
+  a.factor = factor;
+  a.sign = backward ? -1.f : 1.f;
+  a.copies = rot < d && !(in_place_q && (in_place_k || H_k == 0));
+  DeviceInfo* di = device_info();
+  if (!di) return KNAP_ERR_LAUNCH_FAILED;
+  const hipError_t e = knap::launch_rope(a, half, wide, di->cus, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
+  return KNAP_OK;
+}
+
+// type codes, strides and pointers of one tensor of rows
+bool rows_ok(const void* p, int type, int64_t stride, int64_t rows, int width) {
+  return p && aligned(p, type == KNAP_BF16 ? 2 : 4) && (rows == 1 || (stride >= width && stride <= ((int64_t)1 << 30)));
+}
+bool rows_wide(const void* p, int64_t stride, int64_t rows) { return aligned(p, 16) && (rows == 1 || stride % 8 == 0); }
+bool type_ok(int type) { return type == KNAP_BF16 || type == KNAP_F32; }
+
+}  // namespace
+
+int knap_rope_fwd(const void* q, const void* k, int64_t tokens, int H, int H_k, int d, const int64_t* strides, int rot, int layout,
+                  const int32_t* positions, int n_axes, const int* axis_pairs, const int32_t* cu_seqlens, int n_seq,
+                  const double* freq, float factor, void* q_out, void* k_out, void* stream) {
+  return rope_impl(q, k, tokens, H, H_k, d, strides, rot, layout, positions, n_axes, axis_pairs, cu_seqlens, n_seq, freq, factor, q_out,
+                   k_out, false, stream);
+}
+
+int knap_rope_bwd(const void* dq_out, const void* dk_out, int64_t tokens, int H, int H_k, int d, const int64_t* strides, int rot,
+                  int layout, const int32_t* positions, int n_axes, const int* axis_pairs, const int32_t* cu_seqlens, int n_seq,
+                  const double* freq, float factor, void* dq, void* dk, void* stream) {
+  return rope_impl(dq_out, dk_out, tokens, H, H_k, d, strides, rot, layout, positions, n_axes, axis_pairs, cu_seqlens, n_seq, freq, factor,
+                   dq, dk, true, stream);
+}
+
+// ---------------------------------------------------------------------------
+// Layer norm
+// ---------------------------------------------------------------------------
+
+int knap_layer_norm_fwd(const void* x, int x_type, int64_t x_stride, int64_t rows, int width, const void* weight, const void* bias,
+                        int w_type, float eps, void* y, int y_type, int64_t y_stride, float* mean, float* rstd, void* stream) {
+  if (!type_ok(x_type) || !type_ok(y_type) || !type_ok(w_type) || (x_type == KNAP_BF16 && y_type == KNAP_F32)) return KNAP_ERR_INVALID_ARG;
+  if (rows < 0 || rows > INT32_MAX || width < 1 || width > KNAP_LAYER_NORM_MAX_WIDTH || !(eps >= 0.f) || !(eps < 3.0e38f)) return KNAP_ERR_INVALID_ARG;
+  if (rows == 0) return KNAP_OK;
+  if (!rows_ok(x, x_type, x_stride, rows, width) || !rows_ok(y, y_type, y_stride, rows, width) || x == y) return KNAP_ERR_INVALID_ARG;
+  const size_t w_align = w_type == KNAP_BF16 ? 2 : 4;
+  if (!aligned(weight, w_align) || !aligned(bias, w_align) || !aligned(mean, 4) || !aligned(rstd, 4)) return KNAP_ERR_INVALID_ARG;
+  knap::NormArgs a{};
+  a.x = x; a.weight = weight; a.bias = bias; a.y = y;
+  a.mean = mean; a.rstd = rstd;
+  a.x_stride = x_stride; a.y_stride = y_stride; a.rows = rows;
+  a.width = width; a.eps = eps; a.w_bf16 = w_type == KNAP_BF16;
+  DeviceInfo* di = device_info();
+  if (!di) return KNAP_ERR_LAUNCH_FAILED;
+  const bool wide = width % 8 == 0 && rows_wide(x, x_stride, rows) && rows_wide(y, y_stride, rows);
+  const hipError_t e = knap::launch_layer_norm_fwd(a, x_type == KNAP_BF16, y_type == KNAP_BF16, wide, di->cus, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
+  return KNAP_OK;
+}
+
+size_t knap_layer_norm_bwd_workspace_bytes(int64_t rows, int width) {
+  if (rows <= 0 || width <= 0) return 0;
+  const size_t groups = rows < knap::kNormMaxGroups ? (size_t)rows : (size_t)knap::kNormMaxGroups;
+  return round_up(groups * 2 * (size_t)width * sizeof(float), 256);
+}
+
+int knap_layer_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t rows, int width, const void* weight, int w_type,
+                        const float* mean, const float* rstd, const void* dy, int y_type, int64_t dy_stride, void* dx, int64_t dx_stride,
+                        float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!type_ok(x_type) || !type_ok(y_type) || !type_ok(w_type) || (x_type == KNAP_BF16 && y_type == KNAP_F32)) return KNAP_ERR_INVALID_ARG;
+  if (rows < 0 || rows > INT32_MAX || width < 1 || width > KNAP_LAYER_NORM_MAX_WIDTH) return KNAP_ERR_INVALID_ARG;
+  if (!aligned(dweight, 4) || !aligned(dbias, 4) || (dweight && dweight == dbias)) return KNAP_ERR_INVALID_ARG;
+  const bool sums = dweight || dbias;
+  hipError_t e;
+  if (rows == 0) {
+    if (!sums) return KNAP_OK;
+    e = knap::launch_layer_norm_zero(dweight, dbias, width, static_cast<hipStream_t>(stream));
+  } else {
+    if (!rows_ok(x, x_type, x_stride, rows, width) || !rows_ok(dy, y_type, dy_stride, rows, width) ||
+        !rows_ok(dx, x_type, dx_stride, rows, width) || dx == x || dx == dy)
+      return KNAP_ERR_INVALID_ARG;
+    if (!mean || !rstd || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, w_type == KNAP_BF16 ? 2 : 4)) return KNAP_ERR_INVALID_ARG;
+    if (sums) {
+      if (!workspace || !aligned(workspace, 256)) return KNAP_ERR_INVALID_ARG;
+      if (workspace_bytes < knap_layer_norm_bwd_workspace_bytes(rows, width)) return KNAP_ERR_WORKSPACE_TOO_SMALL;
+    }
+    knap::NormArgs a{};
+    a.x = x; a.weight = weight; a.dy = dy; a.dx = dx;
+    a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+    a.partial = sums ? static_cast<float*>(workspace) : nullptr;
+    a.x_stride = x_stride; a.y_stride = dy_stride; a.dx_stride = dx_stride; a.rows = rows;
+    a.width = width; a.w_bf16 = w_type == KNAP_BF16;
+    DeviceInfo* di = device_info();
+    if (!di) return KNAP_ERR_LAUNCH_FAILED;
+    const bool wide = width % 8 == 0 && rows_wide(x, x_stride, rows) && rows_wide(dy, dy_stride, rows) && rows_wide(dx, dx_stride, rows);
+    e = knap::launch_layer_norm_bwd(a, dweight, dbias, x_type == KNAP_BF16, y_type == KNAP_BF16, wide, di->cus, static_cast<hipStream_t>(stream));
+  }
+  if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
+  return KNAP_OK;
+}
+
 const char* knap_strerror(int code) {
   switch (code) {
     case KNAP_OK: return "success";

@@ -183,6 +183,29 @@ int knap_ulysses_local_tokens(const int64_t* seq_len, int n_seq, int g, int64_t*
   return KNAP_OK;
 }
 
+/* Each kind changes the frequencies alone, in 64 bits; the factor belongs to the last. */
+int knap_rope_frequencies(int rot, double base, int kind, double scale, int64_t trained_len,
+                          double low, double high, double* freq, double* factor) {
+  if (rot < 2 || rot % 2 || !freq || !factor || !(base > 0.0) || !isfinite(base) || !(scale >= 1.0) || !isfinite(scale))
+    return KNAP_ERR_INVALID_ARG;
+  if (kind < KNAP_ROPE_PLAIN || kind > KNAP_ROPE_PARTS || (kind == KNAP_ROPE_BASE && rot == 2)) return KNAP_ERR_INVALID_ARG;
+  if (kind == KNAP_ROPE_PARTS && (trained_len < 1 || !(low < high) || !isfinite(low) || !isfinite(high))) return KNAP_ERR_INVALID_ARG;
+  if (kind == KNAP_ROPE_BASE) base *= pow(scale, (double)rot / (double)(rot - 2));
+  for (int i = 0; i < rot / 2; ++i) {
+    double f = pow(base, -2.0 * i / rot);
+    if (kind == KNAP_ROPE_LINEAR) f /= scale;
+    if (kind == KNAP_ROPE_PARTS) {
+      const double turns = (double)trained_len * f / 6.283185307179586476925;
+      double keep = (turns - low) / (high - low);
+      keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+      f = keep * f + (1.0 - keep) * f / scale;
+    }
+    freq[i] = f;
+  }
+  *factor = kind == KNAP_ROPE_PARTS ? 0.1 * log(scale) + 1.0 : 1.0;
+  return KNAP_OK;
+}
+
 double knap_wir(const double* bag_load, const int* bag_gpus, int n_bags) {
   if (!bag_load || !bag_gpus || n_bags <= 0) return NAN;
   double hi = 0.0, lo = 0.0;

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "knap_dispatch.h"
+#include "knapattn.h"
 
 namespace knap {
 
@@ -48,6 +49,38 @@ hipError_t launch_ulysses_heads(const void* src, void* dst, uint32_t T, uint32_t
 hipError_t launch_ulysses_rows(const void* src, void* dst, const int32_t* row_map, uint32_t T, uint32_t U,
                                bool gather, hipStream_t stream);
 hipError_t launch_ulysses_plan(const int32_t* cu, int n_seq, int g, int T, int32_t* row_map, hipStream_t stream);
+
+// Rotary positions: everything but the launch geometry comes from the caller
+struct RopeArgs {
+  const __bf16 *q, *k;
+  __bf16 *q_out, *k_out;
+  int64_t q_token, q_head, k_token, k_head, qo_token, qo_head, ko_token, ko_head;      // strides in elements
+  int T, H, Hk, d, rot;
+  const int32_t* positions;      // (T, n_axes), or nullptr: by cu
+  int n_axes, axis_end[KNAP_ROPE_MAX_AXES];      // the first pair that is not of the axis
+  const int32_t* cu;
+  int n_seq;
+  const double* freq;
+  float factor, sign;      // sign: of the sine
+  bool copies;             // columns from rot on go to another tensor
+  int tokens_per_group;    // set by the launch
+};
+hipError_t launch_rope(RopeArgs a, bool half, bool wide, int cus, hipStream_t stream);
+
+// Layer norm
+struct NormArgs {
+  const void *x, *weight, *bias, *dy;
+  void *y, *dx;
+  float *mean, *rstd, *partial;      // partial: (workgroups, 2, width), the sums of dy xh and of dy
+  int64_t x_stride, y_stride, dx_stride, rows;      // y_stride: of y or dy
+  int width;
+  float eps;
+  bool w_bf16;
+};
+constexpr int kNormMaxGroups = 1024;      // workgroups of a backward
+hipError_t launch_layer_norm_fwd(const NormArgs& a, bool x_bf16, bool y_bf16, bool wide, int cus, hipStream_t stream);
+hipError_t launch_layer_norm_bwd(const NormArgs& a, float* dw, float* db, bool x_bf16, bool y_bf16, bool wide, int cus, hipStream_t stream);
+hipError_t launch_layer_norm_zero(float* dw, float* db, int width, hipStream_t stream);
 
 // resident workgroups per compute unit of the persistent kernels
 int fwd_workgroups_per_cu(int d);

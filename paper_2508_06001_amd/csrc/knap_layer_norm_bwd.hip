@@ -1,0 +1,142 @@
+// Layer norm, backward (knap_layer_norm.h), with g = dy w and xh = (x - mean) rstd:
+//   dx = rstd (g - mean(g) - xh mean(g xh)),  dw = sum over rows of dy xh,  db = sum over rows of dy.
+// Bound by HBM: x and dy are read once, dx is written once.  A workgroup stays for its share of the rows and holds its dw and db in
+// registers; they go to the workspace as one row of sums a workgroup, which a second kernel adds up in a fixed order: no atomics,
+// the same bits every time.
+#include "knap_layer_norm.h"
+
+#include <algorithm>
+
+namespace knap {
+
+template <class C, class TX, class TY>
+__global__ __launch_bounds__(C::THREADS, 2) void layer_norm_bwd_kernel(NormArgs a) {
+  __shared__ float s_sum[2][2 * C::ROWS * 8];
+  __shared__ float s_cols[C::GROUPS > 1 ? C::THREADS * C::COLS : 1];
+  const int g = threadIdx.x % C::LANES, group = threadIdx.x / C::LANES;
+  const int width = a.width;
+  const float share = 1.0f / (float)width;
+  float w[C::COLS], dw[C::COLS], db[C::COLS];
+  load_weight<C>(a.weight, a.w_bf16, 1.f, g, width, w);
+#pragma unroll
+  for (int i = 0; i < C::COLS; ++i) dw[i] = db[i] = 0.f;
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * C::PASS; r0 < a.rows; r0 += (int64_t)gridDim.x * C::PASS, turn ^= 1) {
+    float x[C::ROWS][C::COLS], dy[C::ROWS][C::COLS], sums[2 * C::ROWS], rstd[C::ROWS];
+    int64_t row[C::ROWS];
+#pragma unroll
+    for (int k = 0; k < C::ROWS; ++k) {
+      row[k] = r0 + k * C::GROUPS + group;
+      const bool there = row[k] < a.rows;
+      load_row<C>(static_cast<const TX*>(a.x) + row[k] * a.x_stride, there, g, width, x[k]);
+      load_row<C>(static_cast<const TY*>(a.dy) + row[k] * a.y_stride, there, g, width, dy[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < C::ROWS; ++k) {
+      const bool there = row[k] < a.rows;
+      const float mean = there ? a.mean[row[k]] : 0.f;
+      rstd[k] = there ? a.rstd[row[k]] : 0.f;
+      float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int i = 0; i < C::COLS; ++i) {
+        x[k][i] = norm_has<C>(g, i, width) ? (x[k][i] - mean) * rstd[k] : 0.f;
+        dw[i] = __builtin_fmaf(dy[k][i], x[k][i], dw[i]);
+        db[i] += dy[k][i];
+        dy[k][i] *= w[i];
+        s1 += dy[k][i];
+        s2 = __builtin_fmaf(dy[k][i], x[k][i], s2);
+      }
+      sums[2 * k] = s1;
+      sums[2 * k + 1] = s2;
+    }
+    row_sums<C>(sums, s_sum[turn]);
+#pragma unroll
+    for (int k = 0; k < C::ROWS; ++k) {
+      const float m1 = sums[2 * k] * share, m2 = sums[2 * k + 1] * share;
+#pragma unroll
+      for (int i = 0; i < C::COLS; ++i) x[k][i] = rstd[k] * (dy[k][i] - m1 - x[k][i] * m2);
+      store_row<C>(static_cast<TX*>(a.dx) + row[k] * a.dx_stride, row[k] < a.rows, g, width, x[k]);
+    }
+  }
+  if (!a.partial) return;
+  float* mine = a.partial + (size_t)blockIdx.x * 2 * width;
+  if constexpr (C::GROUPS == 1) {
+#pragma unroll
+    for (int i = 0; i < C::COLS; ++i)
+      if (norm_has<C>(g, i, width)) {
+        mine[norm_col<C>(g, i)] = dw[i];
+        mine[width + norm_col<C>(g, i)] = db[i];
+      }
+  } else {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < C::COLS; ++i)
+        if (norm_has<C>(g, i, width)) s_cols[group * width + norm_col<C>(g, i)] = half == 0 ? dw[i] : db[i];
+      __syncthreads();
+      for (int c = threadIdx.x; c < width; c += C::THREADS) {
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < C::GROUPS; ++k) sum += s_cols[k * width + c];
+        mine[half * width + c] = sum;
+      }
+    }
+  }
+}
+
+// sums[c] = sum over `n` rows of partial[.][c], for 2 width columns: COLS columns of a workgroup, its 1024 threads' rows joined in LDS
+template <int COLS>
+__global__ __launch_bounds__(1024) void layer_norm_sum_kernel(const float* __restrict__ partial, int n, int width, float* __restrict__ dw,
+                                                              float* __restrict__ db) {
+  constexpr int SLICES = 1024 / COLS;
+  __shared__ float s_part[SLICES][COLS];
+  const int c = threadIdx.x % COLS, slice = threadIdx.x / COLS;
+  const int col = (int)blockIdx.x * COLS + c;
+  float sum = 0.f;
+  if (col < 2 * width) {
+#pragma unroll 8
+    for (int r = slice; r < n; r += SLICES) sum += partial[(size_t)r * 2 * width + col];
+  }
+  s_part[slice][c] = sum;
+  __syncthreads();
+  if (slice == 0 && col < 2 * width) {
+    sum = 0.f;
+    for (int k = 0; k < SLICES; ++k) sum += s_part[k][c];
+    if (col < width) { if (dw) dw[col] = sum; }
+    else if (db) db[col - width] = sum;
+  }
+}
+
+template <class TX, class TY, bool WIDE>
+static hipError_t launch_bwd_t(const NormArgs& a, float* dw, float* db, int cus, hipStream_t stream) {
+  return norm_form<WIDE>(a.width, [&](auto cfg) {
+    using C = decltype(cfg);
+    const int64_t passes = (a.rows + C::PASS - 1) / C::PASS;
+    const int most = (int)std::min<int64_t>(passes, std::min(4 * cus, kNormMaxGroups));
+    const int64_t each = (passes + most - 1) / most;          // as many for every workgroup, but for the last
+    const int groups = (int)((passes + each - 1) / each);
+    hipLaunchKernelGGL((layer_norm_bwd_kernel<C, TX, TY>), dim3(groups), dim3(C::THREADS), 0, stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.partial) return e;
+    if (a.width <= 2048)
+      hipLaunchKernelGGL(layer_norm_sum_kernel<16>, dim3((2 * a.width + 15) / 16), dim3(1024), 0, stream, a.partial, groups, a.width, dw, db);
+    else
+      hipLaunchKernelGGL(layer_norm_sum_kernel<64>, dim3((2 * a.width + 63) / 64), dim3(1024), 0, stream, a.partial, groups, a.width, dw, db);
+    return hipGetLastError();
+  });
+}
+
+// gradients of no rows
+hipError_t launch_layer_norm_zero(float* dw, float* db, int width, hipStream_t stream) {
+  hipLaunchKernelGGL(layer_norm_sum_kernel<64>, dim3((2 * width + 63) / 64), dim3(1024), 0, stream, nullptr, 0, width, dw, db);
+  return hipGetLastError();
+}
+
+hipError_t launch_layer_norm_bwd(const NormArgs& a, float* dw, float* db, bool x_bf16, bool y_bf16, bool wide, int cus, hipStream_t stream) {
+  if (x_bf16) return wide ? launch_bwd_t<__bf16, __bf16, true>(a, dw, db, cus, stream) : launch_bwd_t<__bf16, __bf16, false>(a, dw, db, cus, stream);
+  if (y_bf16) return wide ? launch_bwd_t<float, __bf16, true>(a, dw, db, cus, stream) : launch_bwd_t<float, __bf16, false>(a, dw, db, cus, stream);
+  return wide ? launch_bwd_t<float, float, true>(a, dw, db, cus, stream) : launch_bwd_t<float, float, false>(a, dw, db, cus, stream);
+}
+
+}  // namespace knap
