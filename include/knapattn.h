@@ -168,6 +168,56 @@ int knap_varlen_attn_causal_bwd(const void* q, const void* k, const void* v,
                                 void* stream);
 
 /* ------------------------------------------------------------------------
+ * Differential attention over a packed bag: the difference of two softmax maps
+ * with a learned weight for each head, forward and backward, under either mask.
+ * The d columns of a head's q and k rows are two maps of d / 2 columns each:
+ *     P_m = softmax(scale q_m k_m^T),  O_m = P_m v  (m = 1, 2; v has d columns),
+ *     out = O_1 - lambda_h O_2.
+ * scale is applied to the products of d / 2 columns (1 / sqrt(d / 2) as a rule).
+ *
+ * Layouts, masks, supported sizes, alignment, errors, streams, concurrency and capture are
+ * those of knap_varlen_attn_fwd / _bwd (forward calls of either kind take the same
+ * counter sets in turn and count together).  Besides:
+ *   lambda   fp32[H], any sign; it is read on the device, so that a captured call follows it.
+ *   out2     bf16 (T, H, d): O_2, which the backward takes; NULL in the forward where no backward
+ *            follows.
+ *   lse      fp32 (2, H, T): the log-sums of map 1, then of map 2.
+ *   dlambda  fp32[H] = -sum over rows of dout . O_2, summed in 32 bits over the probabilities
+ *            as they are, in a fixed order; zeros where total_tokens is 0 and n_seq is not.
+ * Between bags a result differs within its rounding errors only by the tiling of
+ * the sequence itself: the kernels have one form for each d, so that a sequence's results depend
+ * neither on the other sequences of the bag nor on H.  */
+int knap_varlen_diff_attn_fwd(const void* q, const void* k, const void* v,
+                              const int32_t* cu_seqlens, int n_seq,
+                              int H, int d, float scale, const float* lambda,
+                              void* out, void* out2, float* lse,
+                              void* stream);
+int knap_varlen_diff_attn_causal_fwd(const void* q, const void* k, const void* v,
+                                     const int32_t* cu_seqlens, int n_seq,
+                                     int H, int d, float scale, const float* lambda,
+                                     void* out, void* out2, float* lse,
+                                     void* stream);
+int knap_varlen_diff_attn_bwd(const void* q, const void* k, const void* v,
+                              const int32_t* cu_seqlens, int n_seq,
+                              int H, int d, float scale, const float* lambda,
+                              const void* out, const void* out2, const float* lse,
+                              const void* dout,
+                              void* dq, void* dk, void* dv, float* dlambda,
+                              int64_t total_tokens,
+                              void* workspace, size_t workspace_bytes,
+                              void* stream);
+int knap_varlen_diff_attn_causal_bwd(const void* q, const void* k, const void* v,
+                                     const int32_t* cu_seqlens, int n_seq,
+                                     int H, int d, float scale, const float* lambda,
+                                     const void* out, const void* out2, const float* lse,
+                                     const void* dout,
+                                     void* dq, void* dk, void* dv, float* dlambda,
+                                     int64_t total_tokens,
+                                     void* workspace, size_t workspace_bytes,
+                                     void* stream);
+size_t knap_varlen_diff_attn_bwd_workspace_bytes(int64_t total_tokens, int n_seq, int H, int d);
+
+/* ------------------------------------------------------------------------
  * Local data movement of the Ulysses layout switch (Sec. 3.4).  A g-GPU bag
  * goes from (partial sequences, full heads) to (full sequences, partial heads)
  * with one all-to-all before attention and back with one after it.  Around

@@ -4,4 +4,4 @@ balancer of KnapFormer.  Thin Python binding over the C ABI in include/knapattn.
 """
 from .binding import *  # noqa: F401,F403
 from .binding import EXPORTS, LIB_PATH, KnapError, lib  # noqa: F401
-from .runtime import LayerNorm, RotaryPositions, VarlenAttention  # noqa: F401
+from .runtime import LayerNorm, RotaryPositions, VarlenAttention, VarlenDiffAttention  # noqa: F401

@@ -60,6 +60,11 @@ _SIGNATURES = {
     "knap_varlen_attn_bwd_noalloc": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
     "knap_varlen_attn_causal_fwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp]),
     "knap_varlen_attn_causal_bwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "knap_varlen_diff_attn_fwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp]),
+    "knap_varlen_diff_attn_causal_fwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp]),
+    "knap_varlen_diff_attn_bwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f] + [_vp] * 9 + [_i64, _vp, _sz, _vp]),
+    "knap_varlen_diff_attn_causal_bwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _f] + [_vp] * 9 + [_i64, _vp, _sz, _vp]),
+    "knap_varlen_diff_attn_bwd_workspace_bytes": (_sz, [_i64, _i, _i, _i]),
     "knap_ulysses_pack_heads": (_i, [_vp, _i64, _i, _i, _i, _vp, _vp]),
     "knap_ulysses_unpack_heads": (_i, [_vp, _i64, _i, _i, _i, _vp, _vp]),
     "knap_ulysses_plan_workspace_bytes": (_sz, [_i, _i]),
@@ -275,8 +280,6 @@ def knap_ulysses_local_tokens(seq_lens, g: int):
     return [int(v) for v in out]
 
 
-# --------------------------------------------------------------------------- rotary positions, layer norm
-
 def _refuse(where: str, what: str) -> None:
     err = KnapError(KNAP_ERR_INVALID_ARG, where)
     err.args = (f"{err.args[0]}: {what}",)
@@ -293,6 +296,79 @@ def _here(where: str, *tensors) -> None:
 
 _KNAP_TYPES = {torch.bfloat16: KNAP_BF16, torch.float32: KNAP_F32}
 
+
+# --------------------------------------------------------------------------- differential attention
+
+def _diff_tensors(where: str, bf16, f32) -> None:
+    for t, shape in bf16:
+        if t is not None and (t.dtype is not torch.bfloat16 or t.numel() != shape or not t.is_contiguous()):
+            _refuse(where, "q, k, v, the outputs and their gradients are contiguous bf16 (T, H, d) tensors")
+    for t, n in f32:
+        if t is not None and (t.dtype is not torch.float32 or t.numel() < n or not t.is_contiguous()):
+            _refuse(where, "lambda and dlambda are contiguous fp32 (H,) tensors, lse is an fp32 (2, H, T) one")
+
+
+def _diff_fwd(fn, where: str, q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse, stream, check) -> int:
+    _here(where, q, k, v, cu_seqlens, lam, out, out2, lse)
+    n = q.numel()
+    _diff_tensors(where, ((q, n), (k, n), (v, n), (out, n), (out2, n)), ((lam, H), (lse, 0)))
+    rc = fn(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), n_seq, H, d, scale, _ptr(lam), _ptr(out), _ptr(out2), _ptr(lse), _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+def knap_varlen_diff_attn_fwd(q, k, v, cu_seqlens, n_seq: int, H: int, d: int, scale: float, lam, out, out2, lse, stream=None,
+                              check: bool = True) -> int:
+    """Enqueue the forward of differential attention.  q, k, v, out, out2 (or None): bf16 (T, H, d); lam: fp32 (H,); lse: fp32 (2, H, T)."""
+    return _diff_fwd(lib.knap_varlen_diff_attn_fwd, "knap_varlen_diff_attn_fwd", q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse,
+                     stream, check)
+
+
+def knap_varlen_diff_attn_causal_fwd(q, k, v, cu_seqlens, n_seq: int, H: int, d: int, scale: float, lam, out, out2, lse, stream=None,
+                                     check: bool = True) -> int:
+    """knap_varlen_diff_attn_fwd with the causal mask inside every sequence."""
+    return _diff_fwd(lib.knap_varlen_diff_attn_causal_fwd, "knap_varlen_diff_attn_causal_fwd", q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out,
+                     out2, lse, stream, check)
+
+
+def knap_varlen_diff_attn_bwd_workspace_bytes(total_tokens: int, n_seq: int, H: int, d: int) -> int:
+    return int(lib.knap_varlen_diff_attn_bwd_workspace_bytes(total_tokens, n_seq, H, d))
+
+
+def _diff_bwd(fn, where: str, q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse, dout, dq, dk, dv, dlam, total_tokens, workspace,
+              workspace_bytes, stream, check) -> int:
+    _here(where, q, k, v, cu_seqlens, lam, out, out2, lse, dout, dq, dk, dv, dlam, workspace)
+    n = q.numel()
+    _diff_tensors(where, [(t, n) for t in (q, k, v, out, out2, dout, dq, dk, dv)],
+                  ((lam, H), (dlam, H), (lse, 2 * H * total_tokens)))
+    if total_tokens * H * d > n:
+        _refuse(where, "total_tokens is more than the tensors hold")
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = fn(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), n_seq, H, d, scale, _ptr(lam), _ptr(out), _ptr(out2), _ptr(lse), _ptr(dout), _ptr(dq),
+            _ptr(dk), _ptr(dv), _ptr(dlam), total_tokens, _ptr(workspace), workspace_bytes, _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+def knap_varlen_diff_attn_bwd(q, k, v, cu_seqlens, n_seq: int, H: int, d: int, scale: float, lam, out, out2, lse, dout, dq, dk, dv, dlam,
+                              total_tokens: int, workspace, workspace_bytes: Optional[int] = None, stream=None, check: bool = True) -> int:
+    """Enqueue the backward of differential attention; dlam: fp32 (H,)."""
+    return _diff_bwd(lib.knap_varlen_diff_attn_bwd, "knap_varlen_diff_attn_bwd", q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse,
+                     dout, dq, dk, dv, dlam, total_tokens, workspace, workspace_bytes, stream, check)
+
+
+def knap_varlen_diff_attn_causal_bwd(q, k, v, cu_seqlens, n_seq: int, H: int, d: int, scale: float, lam, out, out2, lse, dout, dq, dk, dv, dlam,
+                                     total_tokens: int, workspace, workspace_bytes: Optional[int] = None, stream=None,
+                                     check: bool = True) -> int:
+    """knap_varlen_diff_attn_bwd with the causal mask inside every sequence."""
+    return _diff_bwd(lib.knap_varlen_diff_attn_causal_bwd, "knap_varlen_diff_attn_causal_bwd", q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out,
+                     out2, lse, dout, dq, dk, dv, dlam, total_tokens, workspace, workspace_bytes, stream, check)
+
+
+# --------------------------------------------------------------------------- rotary positions, layer norm
 
 def _rope(fn, where: str, q, k, rot, layout, freq, factor, q_out, k_out, positions, axis_pairs, cu_seqlens, stream, check) -> int:
     _here(where, q, k, q_out, k_out, freq, positions, cu_seqlens)

@@ -88,6 +88,17 @@ bool capturing(void* stream) {
   return capture != hipStreamCaptureStatusNone;
 }
 
+// the counters that a forward launch draws from: the next set in turn
+hipError_t next_counters(DeviceInfo* di, void* stream, unsigned** counters) {
+  if (capturing(stream)) {
+    *counters = di->queues + 8 * knap::captured_set(di->fwd_captured.fetch_add(1));
+    return hipSuccess;
+  }
+  const knap::EagerSet s = knap::eager_set(di->fwd_calls.fetch_add(1));
+  *counters = di->queues + 8 * s.set;
+  return s.clear >= 0 ? knap::clear_queue_sets(di->queues + 8 * s.clear, knap::kSetsPerThird, static_cast<hipStream_t>(stream)) : hipSuccess;
+}
+
 int fwd_impl(const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int n_seq,
              int H, int d, float scale, bool causal, void* out, float* lse, void* stream) {
   const int rc = check_common(q, k, v, cu_seqlens, n_seq, H, d, scale);
@@ -98,17 +109,9 @@ int fwd_impl(const void* q, const void* k, const void* v, const int32_t* cu_seql
   DeviceInfo* di = device_info();
   if (!di) return KNAP_ERR_LAUNCH_FAILED;
   const int grid = di->cus * di->fwd_wg[d == 128];
-  unsigned set;
-  hipError_t e = hipSuccess;
-  if (capturing(stream)) {
-    set = knap::captured_set(di->fwd_captured.fetch_add(1));
-  } else {
-    const knap::EagerSet s = knap::eager_set(di->fwd_calls.fetch_add(1));
-    set = s.set;
-    if (s.clear >= 0) e = knap::clear_queue_sets(di->queues + 8 * s.clear, knap::kSetsPerThird, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
-  }
-  unsigned* counters = di->queues + 8 * set;
+  unsigned* counters;
+  hipError_t e = next_counters(di, stream, &counters);
+  if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
   e = (causal ? knap::launch_fwd_causal : knap::launch_fwd_full)(q, k, v, cu_seqlens, n_seq, H, d, scale, out, lse, counters, grid,
                                                                  static_cast<hipStream_t>(stream));
   if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
@@ -308,6 +311,96 @@ int knap_ulysses_gather_chunks(const void* recv, const int32_t* row_map, int64_t
 int knap_ulysses_scatter_chunks(const void* z, const int32_t* row_map, int64_t total_tokens,
                                 int heads_local, int d, void* send, void* stream) {
   return ulysses_rows(z, send, row_map, total_tokens, heads_local, d, false, stream);
+}
+
+// ---------------------------------------------------------------------------
+// Differential attention
+// ---------------------------------------------------------------------------
+
+namespace {
+
+int diff_fwd_impl(const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int n_seq, int H, int d, float scale,
+                  const float* lambda, bool causal, void* out, void* out2, float* lse, void* stream) {
+  const int rc = check_common(q, k, v, cu_seqlens, n_seq, H, d, scale);
+  if (rc != KNAP_OK || n_seq == 0) return rc;
+  if (!lambda || !out || !lse || !aligned(lambda, 4) || !aligned(out, 16) || !aligned(out2, 16) || !aligned(lse, 4)) return KNAP_ERR_INVALID_ARG;
+  if (out == q || out == k || out == v || out == out2 || (out2 && (out2 == q || out2 == k || out2 == v))) return KNAP_ERR_INVALID_ARG;
+  DeviceInfo* di = device_info();
+  if (!di) return KNAP_ERR_LAUNCH_FAILED;
+  knap::DiffFwdArgs a = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(k), static_cast<const __bf16*>(v), cu_seqlens, n_seq, H, scale,
+                         lambda, static_cast<__bf16*>(out), static_cast<__bf16*>(out2), lse, nullptr};
+  hipError_t e = next_counters(di, stream, &a.counters);
+  if (e == hipSuccess) e = knap::launch_diff_fwd(a, d, causal, di->cus, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
+  return KNAP_OK;
+}
+
+int diff_bwd_impl(const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int n_seq, int H, int d, float scale,
+                  const float* lambda, bool causal, const void* out, const void* out2, const float* lse, const void* dout, void* dq, void* dk,
+                  void* dv, float* dlambda, int64_t total_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_common(q, k, v, cu_seqlens, n_seq, H, d, scale);
+  if (rc != KNAP_OK) return rc;
+  if (total_tokens < 0 || total_tokens > INT32_MAX) return KNAP_ERR_INVALID_ARG;
+  if (n_seq == 0) return KNAP_OK;
+  if (!dlambda || !aligned(dlambda, 4)) return KNAP_ERR_INVALID_ARG;
+  hipError_t e;
+  if (total_tokens == 0) {
+    e = knap::launch_layer_norm_zero(dlambda, nullptr, H, static_cast<hipStream_t>(stream));
+  } else {
+    if (!lambda || !out || !out2 || !lse || !dout || !dq || !dk || !dv) return KNAP_ERR_INVALID_ARG;
+    if (!aligned(lambda, 4) || !aligned(out, 16) || !aligned(out2, 16) || !aligned(lse, 4) || !aligned(dout, 16) || !aligned(dq, 16) ||
+        !aligned(dk, 16) || !aligned(dv, 16))
+      return KNAP_ERR_INVALID_ARG;
+    if (dq == dk || dq == dv || dk == dv || dq == q || dk == k || dv == v) return KNAP_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256)) return KNAP_ERR_INVALID_ARG;
+    if (workspace_bytes < knap_varlen_diff_attn_bwd_workspace_bytes(total_tokens, n_seq, H, d)) return KNAP_ERR_WORKSPACE_TOO_SMALL;
+    DeviceInfo* di = device_info();
+    if (!di) return KNAP_ERR_LAUNCH_FAILED;
+    const size_t part = round_up(static_cast<size_t>(total_tokens) * H * sizeof(float), 256);
+    char* ws = static_cast<char*>(workspace);
+    auto at = [&](int i) { return reinterpret_cast<float*>(ws + i * part); };
+    const knap::DiffBwdArgs a = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(k), static_cast<const __bf16*>(v),
+                                 static_cast<const __bf16*>(out), static_cast<const __bf16*>(out2), static_cast<const __bf16*>(dout), cu_seqlens,
+                                 n_seq, H, scale, lambda, lse, static_cast<__bf16*>(dq), static_cast<__bf16*>(dk), static_cast<__bf16*>(dv),
+                                 dlambda, at(0), at(1), at(2), at(3), at(4), reinterpret_cast<unsigned*>(ws + 5 * part)};
+    e = knap::launch_diff_bwd(a, d, causal, (int)total_tokens, di->cus, static_cast<hipStream_t>(stream));
+  }
+  if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
+  return KNAP_OK;
+}
+
+}  // namespace
+
+int knap_varlen_diff_attn_fwd(const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int n_seq, int H, int d, float scale,
+                              const float* lambda, void* out, void* out2, float* lse, void* stream) {
+  return diff_fwd_impl(q, k, v, cu_seqlens, n_seq, H, d, scale, lambda, false, out, out2, lse, stream);
+}
+
+int knap_varlen_diff_attn_causal_fwd(const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int n_seq, int H, int d, float scale,
+                                     const float* lambda, void* out, void* out2, float* lse, void* stream) {
+  return diff_fwd_impl(q, k, v, cu_seqlens, n_seq, H, d, scale, lambda, true, out, out2, lse, stream);
+}
+
+size_t knap_varlen_diff_attn_bwd_workspace_bytes(int64_t total_tokens, int n_seq, int H, int d) {
+  (void)n_seq;
+  if (total_tokens <= 0 || H <= 0 || d <= 0) return 0;
+  // five values of each (row, head), then 256 bytes of work-queue counters
+  return 5 * round_up(static_cast<size_t>(total_tokens) * H * sizeof(float), 256) + 256;
+}
+
+int knap_varlen_diff_attn_bwd(const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int n_seq, int H, int d, float scale,
+                              const float* lambda, const void* out, const void* out2, const float* lse, const void* dout, void* dq, void* dk,
+                              void* dv, float* dlambda, int64_t total_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+  return diff_bwd_impl(q, k, v, cu_seqlens, n_seq, H, d, scale, lambda, false, out, out2, lse, dout, dq, dk, dv, dlambda, total_tokens, workspace,
+                       workspace_bytes, stream);
+}
+
+int knap_varlen_diff_attn_causal_bwd(const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int n_seq, int H, int d, float scale,
+                                     const float* lambda, const void* out, const void* out2, const float* lse, const void* dout, void* dq,
+                                     void* dk, void* dv, float* dlambda, int64_t total_tokens, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  return diff_bwd_impl(q, k, v, cu_seqlens, n_seq, H, d, scale, lambda, true, out, out2, lse, dout, dq, dk, dv, dlambda, total_tokens, workspace,
+                       workspace_bytes, stream);
 }
 
 // ---------------------------------------------------------------------------

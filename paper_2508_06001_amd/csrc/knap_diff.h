@@ -1,0 +1,59 @@
+// Differential attention: what its kernels share.
+#pragma once
+
+#include "knap_attn_fwd_part.h"
+
+namespace knap {
+
+template <int D>
+struct DiffCfg {
+  static constexpr int BM = 128;         // query rows per work item
+  static constexpr int BN = 64;          // key/value rows per LDS tile
+  static constexpr int KC = D / 16;      // contraction chunks over d, the first half of them of map 1
+  static constexpr int DB = D / 32;      // 32-wide blocks of d
+  static constexpr int TILE_ELEMS = BN * Tile<D>::LD;
+};
+
+// One map's softmax of a lane's query: the exponent reference (raw score units), it times c, and this lane's share of the row sum
+// (32 of every 64 keys).  The reference moves only when a half tile's probabilities against it are too large, as in the forward of plain
+// attention.
+struct DiffSoftmax {
+  float m_ref = -INFINITY, mc = -INFINITY, l = 0.f;
+
+  static __device__ __forceinline__ float exps(const f32x16& s, float c, float mc, bf16x8 (&pb)[2]) {
+    float p[16], sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = fast_exp2(__builtin_fmaf(s[r], c, -mc));
+      sum += p[r];
+    }
+#pragma unroll
+    for (int ck = 0; ck < 2; ++ck) {
+      const int r0 = 8 * ck;
+      pb[ck] = pack8(p[r0], p[r0 + 1], p[r0 + 2], p[r0 + 3], p[r0 + 4], p[r0 + 5], p[r0 + 6], p[r0 + 7]);
+    }
+    return sum;
+  }
+
+  template <int DB>
+  __device__ __forceinline__ void step(const f32x16& s, float c, bf16x8 (&pb)[2], f32x16 (&o)[DB], int hh) {
+    float sum = exps(s, c, mc, pb);
+    if (__builtin_amdgcn_ballot_w64(!(sum <= kMaxHalfSum)) != 0) {
+      const float m_loc = half_max(s, 64, hh);
+      const float m_new = fmaxf(m_ref, fmaxf(m_loc, xor32(m_loc)));
+      const float alpha = m_new == m_ref ? 1.f : fast_exp2((m_ref - m_new) * c);
+      m_ref = m_new;
+      mc = m_new == -INFINITY ? 0.f : m_new * c;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+      sum = exps(s, c, mc, pb);
+      if (m_new == -INFINITY) mc = -INFINITY;      // scores of -inf alone set no reference: the next half has to settle too
+    }
+    l += sum;
+  }
+};
+
+}  // namespace knap

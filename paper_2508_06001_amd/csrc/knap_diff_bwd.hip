@@ -1,0 +1,547 @@
+// Differential attention, backward.  With P_m recomputed from q, k and the forward's log-sums, dP = dout v^T and D_m = sum_c dout_c O_m,c:
+//   dS_1 = P_1 (dP - D_1),  dS_2 = -lambda P_2 (dP - D_2),  dq_m = scale dS_m k_m,  dk_m = scale dS_m^T q_m,
+//   dv = (P_1 - lambda P_2)^T dout,  dlambda = - sum over rows of D_2.
+// The products are as many as those of plain attention of the same d: the scores, dq and dk are two halves of the columns, dP and dv are
+// one for both maps.  What is twice as much are the exponentials.  As there, dQ (by query tiles) and dK, dV (by key tiles) are kernels of
+// their own that keep their sums in registers, and nothing is added up across workgroups but dlambda.
+//
+//   diff_delta_kernel   D_1 = sum dout out + lambda D_2 and D_2 = sum dout out2 of every row, from the rounded outputs, which is as exact
+//                       as dS in bf16 can use; and the log-sums in base 2
+//   diff_dq_kernel      dQ, and D_2 again in 32 bits, as sum_j P_2 dP: what dlambda is summed from (dout times the rounded out2 is off
+//                       by 2^-9 a row, which a sum over rows of either sign does not average out against its own size)
+//   diff_dkdv_kernel    dK, dV
+//   diff_lambda_kernel  dlambda, one workgroup a head, in a fixed order
+// Probabilities are carried times 2^15 (the log-sums are stored that much smaller), which fp16 holds with 11 bits down to 2^-29: so
+// that the waves that form dK get them from the waves that form dV with no rounding worth counting.  The results' factors take it out.
+#include "knap_attn_dkdv.h"
+#include "knap_attn_dq.h"
+#include "knap_diff.h"
+
+namespace knap {
+
+constexpr float kDiffUp = 15.f;                       // log2 of what probabilities are carried times
+constexpr float kDiffDown = 1.0f / 32768.f;
+
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// 128 rows of one head; the D / 8 lanes of a row hold 8 columns each
+template <int D>
+__global__ __launch_bounds__(kThreads) void diff_delta_kernel(DiffBwdArgs a) {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 16) a.counters[threadIdx.x] = 0u;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int t0 = blockIdx.x * 128, head = blockIdx.y, T = a.cu[a.n_seq], H = a.H;
+  if (t0 >= T) return;
+  const uint32_t row_bytes = (uint32_t)((size_t)H * D * sizeof(__bf16));
+  const size_t at = ((size_t)t0 * H + head) * D;
+  const uint32_t bytes = (uint32_t)min(T - t0, 128) * row_bytes;
+  const auto ro = make_rsrc(a.out + at, bytes), r2 = make_rsrc(a.out2 + at, bytes), rd = make_rsrc(a.dout + at, bytes);
+  constexpr int LANES = D / 8, ROWS = 64 / LANES, N = 32 / ROWS;      // lanes of a row, rows of a load, loads of a wave
+  const uint32_t off = (uint32_t)(wave * 32 + lane / LANES) * row_bytes + (uint32_t)(lane % LANES) * 16u;
+  const float lambda = a.lambda[head];
+  float d1 = 0.f, d2 = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t o = off + (uint32_t)(i * ROWS) * row_bytes;
+    const bf16x8 of = __builtin_bit_cast(bf16x8, buffer_load16(ro, o)), o2 = __builtin_bit_cast(bf16x8, buffer_load16(r2, o)),
+                 dof = __builtin_bit_cast(bf16x8, buffer_load16(rd, o));
+    float x = 0.f, y = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x = __builtin_fmaf((float)dof[e], (float)of[e], x);
+      y = __builtin_fmaf((float)dof[e], (float)o2[e], y);
+    }
+#pragma unroll
+    for (int s = 1; s < LANES; s <<= 1) {
+      x += __shfl_xor(x, s, 64);
+      y += __shfl_xor(y, s, 64);
+    }
+    if (lane % LANES == i) {                // row ROWS i + lane / LANES of the wave's 32, kept by lane i of its row
+      d1 = x;
+      d2 = y;
+    }
+  }
+  const int t = t0 + wave * 32 + ROWS * (lane % LANES) + lane / LANES;
+  if (lane % LANES < N && t < T) {
+    const size_t row_at = (size_t)head * T + t, second = (size_t)H * T;
+    d1 = __builtin_fmaf(lambda, d2, d1);
+    a.nd1[row_at] = -d1;
+    a.diff[row_at] = d1 - d2;
+    a.lse_a[row_at] = __builtin_fmaf(a.lse[row_at], kLog2e, -kDiffUp);
+    a.lse_b[row_at] = __builtin_fmaf(a.lse[second + row_at], kLog2e, -kDiffUp);
+  }
+}
+
+// dQ: the forward's structure.  S_m^T = K_m Q_m^T and dP^T = V dO^T put one query in each lane; dS_m^T is, unchanged, the operand of
+// dQ_m^T += K_m^T dS_m^T with K^T read transposed from LDS.
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
+  using C = DiffCfg<D>;
+  extern __shared__ int s_dyn[];
+  int* s_order = s_dyn;
+  int* s_start = s_dyn + a.n_seq;
+  __shared__ __attribute__((aligned(1024))) __bf16 sK0[C::TILE_ELEMS];
+  __shared__ __attribute__((aligned(1024))) __bf16 sK1[C::TILE_ELEMS];
+  __shared__ __attribute__((aligned(1024))) __bf16 sV0[C::TILE_ELEMS];
+  __shared__ __attribute__((aligned(1024))) __bf16 sV1[C::TILE_ELEMS];
+  __shared__ int s_ticket;
+  static_assert(sizeof(__bf16) * C::TILE_ELEMS >= sizeof(int) * kThreads, "scan scratch must fit in a tile");
+
+  const int T = a.cu[a.n_seq], H = a.H;
+  const int n_items = build_schedule<C::BM, kThreads, CAUSAL>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const float c = a.scale * kLog2e;
+  const size_t row_stride = (size_t)H * D;
+  const uint32_t row_bytes = (uint32_t)(row_stride * sizeof(__bf16));
+  RowReader<D> rows;
+  ColReader<D> cols;
+  rows.init(lane);
+  cols.init(lane);
+  ItemQueue<0> queue;
+  queue.init(a.counters, s_start, a.n_seq, n_items);
+  int ticket = queue.first_ticket();
+  while (ticket < queue.wide) {
+    const WorkItem it = decode_item<C::BM, CAUSAL>(queue.item(ticket), a.cu, a.n_seq, s_order, s_start);
+    const int L = it.len, head = __builtin_amdgcn_readfirstlane(it.head);
+    const int other = (L + C::BM - 1) / C::BM - 1 - it.tile;
+    const float lambda = a.lambda[head];
+    unsigned next_ticket;      // thread 0 only
+    for (int sub = 0; sub < (CAUSAL && it.tile != other ? 2 : 1); ++sub) {
+      const int q_tile = __builtin_amdgcn_readfirstlane(!CAUSAL ? it.tile : sub == 0 ? other : it.tile);
+      const int q0 = q_tile * C::BM, q_row = q0 + 32 * wave + l32;
+      const bool q_valid = q_row < L;
+      const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
+      const int n_tiles = (kv_end + C::BN - 1) / C::BN;
+      const int first_masked = CAUSAL ? 2 * q_tile : L / C::BN;
+      const int kv_lim = CAUSAL ? q_row + 1 : L;
+      const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
+      auto load_tile = [&](int t, __bf16* dK, __bf16* dV) {
+        const int kv0 = t * C::BN;
+        const uint32_t bytes = (uint32_t)max(0, min(kv_end - kv0, C::BN)) * row_bytes;
+        tile_load_async<D>(dK, make_rsrc(a.k + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, C::BN, wave, lane);
+        tile_load_async<D>(dV, make_rsrc(a.v + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, C::BN, wave, lane);
+      };
+      const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
+      const uint32_t off = (uint32_t)(32 * wave + l32) * row_bytes + (uint32_t)(16 * hh);
+      const size_t row_at = (size_t)head * T + it.row0 + (q_valid ? q_row : 0);
+      const float nd1 = a.nd1[row_at], nd2 = nd1 + a.diff[row_at];
+      // +inf for rows past the end: P = 0
+      const float lse_a = q_valid ? a.lse_a[row_at] : INFINITY, lse_b = q_valid ? a.lse_b[row_at] : INFINITY;
+      bf16x8 qf[C::KC], dof[C::KC];
+      {
+        const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
+        const auto rd = make_rsrc(a.dout + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+        for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
+        KNAP_SCHED_FENCE();
+#pragma unroll
+        for (int cc = 0; cc < C::KC; ++cc) dof[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rd, off + 32u * cc));
+        KNAP_SCHED_FENCE();
+      }
+      load_tile(0, sK0, sV0);
+      f32x16 acc[C::DB];
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db) acc[db] = zero16();
+      float d2 = 0.f;
+      wait_async_loads();
+      if (sub == 0 && queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
+      lds_barrier();
+
+      auto tile = [&](int t, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) {
+        load_tile(t + 1, nK, nV);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int k0 = t * C::BN + 32 * half;
+          if (k0 >= kv_end || (CAUSAL && k0 > q0 + 32 * wave + 31)) break;
+          f32x16 dp = zero16();
+#pragma unroll
+          for (int cc = 0; cc < C::KC; ++cc) dp = mfma32(rows.get(tV, 32 * half, cc), dof[cc], dp);
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            f32x16 s = zero16();
+#pragma unroll
+            for (int cc = 0; cc < C::KC / 2; ++cc) s = mfma32(rows.get(tK, 32 * half, m * C::KC / 2 + cc), qf[m * C::KC / 2 + cc], s);
+            // keys that this query does not see score -inf: rows past the end arrive as zeros, and exp2(-log-sum) of a score of zero may
+            // be infinite
+            if (t >= first_masked) mask_half(s, kv_lim - k0, hh);
+            float ds[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float p = fast_exp2(__builtin_fmaf(s[r], c, -(m == 0 ? lse_a : lse_b)));
+              if (m == 1) d2 = __builtin_fmaf(p, dp[r], d2);
+              ds[r] = p * (dp[r] + (m == 0 ? nd1 : nd2));
+            }
+            const bf16x8 x0 = pack8(ds[0], ds[1], ds[2], ds[3], ds[4], ds[5], ds[6], ds[7]);
+            const bf16x8 x1 = pack8(ds[8], ds[9], ds[10], ds[11], ds[12], ds[13], ds[14], ds[15]);
+#pragma unroll
+            for (int db = m * C::DB / 2; db < (m + 1) * C::DB / 2; ++db) {
+              acc[db] = mfma32(cols.get(tK, 32 * half, db), x0, acc[db]);
+              acc[db] = mfma32(cols.get(tK, 32 * half + 16, db), x1, acc[db]);
+            }
+          }
+        }
+        wait_async_loads();
+        lds_barrier();
+      };
+      for (int t = 0; t < n_tiles; t += 2) {
+        tile(t, sK0, sV0, sK1, sV1);
+        if (t + 1 < n_tiles) tile(t + 1, sK1, sV1, sK0, sV0);
+      }
+      d2 += xor32(d2);
+      if (q_valid && hh == 0) a.d2[row_at] = d2 * kDiffDown;
+      const auto rg = make_rsrc(a.dq + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db)
+        store_block(rg, off + 64u * db, acc[db], db < C::DB / 2 ? a.scale * kDiffDown : -lambda * a.scale * kDiffDown);
+    }
+    if (!queue.draws) return;
+    if (tid == 0) s_ticket = queue.later_ticket(next_ticket);
+    lds_barrier();
+    ticket = __builtin_amdgcn_readfirstlane(s_ticket);
+    lds_barrier();        // everyone has the ticket before the next one is put down
+  }
+}
+
+// dK, dV: the structure of plain attention's kernel (knap_attn_dkdv.h), PAIRS pairs of waves, each pair with 64 keys of the tile and the
+// two waves of a pair with a role each:
+//   dV wave: keeps its K rows in registers; S_1, P_1, then S_2, P_2, both handed over as fp16 through LDS; dV += (P_1 - lambda P_2)^T dO;
+//   dK wave: keeps its V rows in registers and runs one tile behind: dP - D_1 = dO V^T - D_1, dS_1 = P_1 (dP - D_1),
+//            dS_2 = P_2 (dP - D_1 + (D_1 - D_2)), dK_m += dS_m^T Q_m; -lambda is taken in at the end.
+// The dV wave's registers hold the scores of one map at a time: its P_1 comes back from the LDS that it was handed over through.
+template <int D, int PAIRS>
+struct DiffLane : DkdvLane<D, PAIRS> {
+  using C = Bwd2Cfg<D, PAIRS>;
+  static constexpr int P_BLOCK = 64 * 16, P_MAP = 2 * C::KB * P_BLOCK, P_TILE = 2 * P_MAP, P_PAIR = 2 * P_TILE;      // bytes
+  __device__ __forceinline__ void init(int lane, int wave_, int role_, uint32_t row_bytes) {
+    DkdvLane<D, PAIRS>::init(lane, wave_, role_, row_bytes);
+    this->at.word = P_PAIR * this->pair + 16 * lane;
+  }
+};
+
+// one slot of the ring: 32 rows of Q and dO and four values of each
+struct DiffSlot {
+  __bf16 *q, *dout;
+  float *lse_a, *lse_b, *nd1, *diff;
+};
+
+template <int D, int PAIRS, bool CAUSAL>
+__device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffSlot& r0, const DiffSlot& r1, const DiffSlot& r2, float* sink, char* sP,
+                                               const DiffLane<D, PAIRS>& me, const WorkItem& it, int head, int kv_tile, int T) {
+  using C = Bwd2Cfg<D, PAIRS>;
+  using W = DiffLane<D, PAIRS>;
+  constexpr int KH = C::KC / 2, NH = C::NB / 2;
+  const int L = it.len, role = me.role, pair = me.pair, wave = me.wave;
+  const float c = g.scale * kLog2e, lambda = g.lambda[head];
+  const size_t row_stride = (size_t)g.H * D;
+  const uint32_t row_bytes = (uint32_t)(row_stride * sizeof(__bf16));
+  const int kv0 = kv_tile * C::BN;
+  const int q_first = CAUSAL ? kv0 : 0;       // queries this key tile meets: rows q_first .. L - 1; tiles and rows below count from it
+  const int Lq = L - q_first;
+  const size_t q_at = (size_t)(it.row0 + q_first) * row_stride + (size_t)head * D;
+  const size_t v_at = (size_t)head * T + it.row0 + q_first;
+  const int n_tiles = (Lq + C::BM - 1) / C::BM;
+
+  bf16x8 kvf[C::KB][C::KC];
+  {
+    const auto r = make_rsrc((role == 0 ? g.k : g.v) + (size_t)(it.row0 + kv0) * row_stride + (size_t)head * D,
+                             (uint32_t)min(L - kv0, C::BN) * row_bytes);
+    const int w = me.at.fresh();
+#pragma unroll
+    for (int kb = 0; kb < C::KB; ++kb) {
+      const uint32_t off = (uint32_t)(64 * pair + 32 * kb + LaneWord::l32(w)) * row_bytes + (uint32_t)LaneWord::hh16(w);
+#pragma unroll
+      for (int cc = 0; cc < C::KC; ++cc) kvf[kb][cc] = __builtin_bit_cast(bf16x8, buffer_load16(r, off + 32u * cc));
+    }
+  }
+  f32x16 acc[C::KB][C::NB];
+#pragma unroll
+  for (int kb = 0; kb < C::KB; ++kb)
+#pragma unroll
+    for (int nb = 0; nb < C::NB; ++nb) acc[kb][nb] = zero16();
+
+  // CAUSAL: step t works on query tile n_tiles - 1 - t, from the sequence's last one down to the diagonal
+  auto issue_tile = [&](int t, const DiffSlot& to) {
+    int q0, n_rows;
+    if constexpr (CAUSAL) {
+      q0 = max(0, n_tiles - 1 - t) * C::BM;
+      n_rows = t < n_tiles ? min(Lq - q0, C::BM) : 0;
+    } else {
+      q0 = t * C::BM;
+      n_rows = max(0, min(L - q0, C::BM));
+    }
+    const auto rq = make_rsrc(g.q + q_at + (size_t)q0 * row_stride, (uint32_t)n_rows * row_bytes);
+    const auto rd = make_rsrc(g.dout + q_at + (size_t)q0 * row_stride, (uint32_t)n_rows * row_bytes);
+#pragma unroll
+    for (int r = 0; r < C::BM; r += 2 * PAIRS * W::ROWS_PER_INSTR) {
+      uint32_t off = me.cp_off;
+      if (r) asm volatile("" : "+v"(off));
+      off += (uint32_t)r * row_bytes;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (__attribute__((address_space(3))) void*)(to.q + (me.cp_row0 + r) * Tile<D>::LD), 16, (int)off, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rd, (__attribute__((address_space(3))) void*)(to.dout + (me.cp_row0 + r) * Tile<D>::LD), 16, (int)off, 0, 0, 0);
+    }
+    const float* src = (wave == 0 ? g.lse_a : wave == 1 ? g.lse_b : wave == 2 ? g.nd1 : g.diff) + v_at + q0;
+    float* dst = wave == 0 ? to.lse_a : wave == 1 ? to.lse_b : wave == 2 ? to.nd1 : wave == 3 ? to.diff : sink;
+    const auto rs = make_rsrc(src, wave < 4 ? (uint32_t)n_rows * 4u : 0u);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)dst, 4, LaneWord::lane4(me.at.fresh()), 0, 0, 0);
+  };
+  auto step_sync = [&]() {
+    wait_async_loads();
+    lds_barrier();
+  };
+  constexpr int AHEAD = 2;
+  // x[kb] += tile rows (A, from LDS) x this wave's K or V rows, columns 16 FROM .. 16 TO
+  auto first_product = [&](auto from_tag, auto to_tag, const __bf16* tA, int rb, f32x16 (&x)[C::KB]) {
+    constexpr int FROM = decltype(from_tag)::value, TO = decltype(to_tag)::value;
+    bf16x8 af[C::KC];
+#pragma unroll
+    for (int cc = FROM; cc < FROM + AHEAD && cc < TO; ++cc) af[cc] = me.rows.get(tA, rb, cc);
+    KNAP_SCHED_FENCE();
+#pragma unroll
+    for (int cc = FROM; cc < TO; ++cc) {
+#pragma unroll
+      for (int kb = 0; kb < C::KB; ++kb) x[kb] = mfma32(af[cc], kvf[kb][cc], x[kb]);
+      if (cc + AHEAD < TO) af[cc + AHEAD] = me.rows.get(tA, rb, cc + AHEAD);
+      KNAP_SCHED_FENCE();
+    }
+  };
+  // acc[kb][nb] += op[kb] x tile columns over the 16 queries of chunk cq, column blocks FROM .. TO
+  auto second_product = [&](auto from_tag, auto to_tag, const __bf16* tB, int cb, int cq, const bf16x8 (&op)[C::KB]) {
+    constexpr int FROM = decltype(from_tag)::value, TO = decltype(to_tag)::value;
+    bf16x8 bf[C::NB];
+#pragma unroll
+    for (int nb = FROM; nb < TO; ++nb) bf[nb] = me.cols.get(tB, cb, 16 * cq, nb);
+    KNAP_SCHED_FENCE();
+#pragma unroll
+    for (int nb = FROM; nb < TO; ++nb)
+#pragma unroll
+      for (int kb = 0; kb < C::KB; ++kb) acc[kb][nb] = mfma32(bf[nb], op[kb], acc[kb][nb]);
+    KNAP_SCHED_FENCE();
+  };
+  constexpr std::integral_constant<int, 0> n0{};
+  constexpr std::integral_constant<int, KH> kh{};
+  constexpr std::integral_constant<int, C::KC> kc{};
+  constexpr std::integral_constant<int, NH> nh{};
+  constexpr std::integral_constant<int, C::NB> nb_all{};
+  // 16 bytes of this lane in block `b` of its pair's P of map m, tile t
+  auto p_at = [&](int w, int t, int m, int b) {
+    return reinterpret_cast<f16x8*>(sP + W::P_MAP * m + W::P_BLOCK * b + (w + (t & 1) * W::P_TILE));
+  };
+  auto dv_step = [&](int t, const DiffSlot& at) {
+    const int rb = me.rows.fresh(), cb = me.cols.fresh(), w = me.at.fresh();
+    bool diag = false;
+    int first_seen[C::KB];
+    if constexpr (CAUSAL) {
+      diag = n_tiles - 1 - t < C::BN / C::BM;
+#pragma unroll
+      for (int kb = 0; kb < C::KB; ++kb) first_seen[kb] = 64 * pair + 32 * kb + LaneWord::l32(w) - (n_tiles - 1 - t) * C::BM - LaneWord::hh16(w) / 4;
+    }
+    // P_m of chunk cq and key block kb: register e of half h is query 8 (2 cq + h) + 4 hh + e
+    auto exps = [&](const f32x16& s, const float* lse, int cq, int kb, float (&p)[8]) {
+      const char* row = reinterpret_cast<const char*>(lse + 16 * cq) + LaneWord::hh16(w);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 lq = *reinterpret_cast<const f32x4*>(row + 32 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[4 * h + e] = fast_exp2(__builtin_fmaf(s[8 * cq + 4 * h + e], c, -lq[e]));
+          if (CAUSAL && diag) p[4 * h + e] = 8 * (2 * cq + h) + e < first_seen[kb] ? 0.f : p[4 * h + e];
+        }
+      }
+    };
+    f32x16 s[C::KB];
+#pragma unroll
+    for (int kb = 0; kb < C::KB; ++kb) s[kb] = zero16();
+    first_product(n0, kh, at.q, rb, s);
+#pragma unroll
+    for (int kb = 0; kb < C::KB; ++kb)
+#pragma unroll
+      for (int cq = 0; cq < 2; ++cq) {
+        float p[8];
+        exps(s[kb], at.lse_a, cq, kb, p);
+        f16x8 x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (_Float16)p[e];
+        *p_at(w, t, 0, 2 * kb + cq) = x;
+      }
+#pragma unroll
+    for (int kb = 0; kb < C::KB; ++kb) s[kb] = zero16();
+    first_product(kh, kc, at.q, rb, s);
+#pragma unroll
+    for (int cq = 0; cq < 2; ++cq) {
+      bf16x8 pa[C::KB];
+#pragma unroll
+      for (int kb = 0; kb < C::KB; ++kb) {
+        float p[8];
+        exps(s[kb], at.lse_b, cq, kb, p);
+        const f16x8 one = *p_at(w, t, 0, 2 * kb + cq);
+        f16x8 x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] = (_Float16)p[e];
+          pa[kb][e] = (__bf16)__builtin_fmaf(-lambda, p[e], (float)one[e]);
+        }
+        *p_at(w, t, 1, 2 * kb + cq) = x;
+      }
+      second_product(n0, nb_all, at.dout, cb, cq, pa);
+    }
+  };
+  auto dk_step = [&](int u, const DiffSlot& at) {
+    const int rb = me.rows.fresh(), cb = me.cols.fresh(), w = me.at.fresh();
+    f32x16 dp[C::KB];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(at.nd1) + LaneWord::hh16(w) + 32 * j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int kb = 0; kb < C::KB; ++kb) dp[kb][4 * j + e] = x[e];
+    }
+    first_product(n0, kc, at.dout, rb, dp);
+#pragma unroll
+    for (int cq = 0; cq < 2; ++cq) {
+      bf16x8 da[C::KB];
+#pragma unroll
+      for (int kb = 0; kb < C::KB; ++kb) {
+        const f16x8 p = *p_at(w, u, 0, 2 * kb + cq);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) da[kb][e] = (__bf16)((float)p[e] * dp[kb][8 * cq + e]);
+      }
+      second_product(n0, nh, at.q, cb, cq, da);
+      const char* row = reinterpret_cast<const char*>(at.diff + 16 * cq) + LaneWord::hh16(w);
+      const f32x4 e0 = *reinterpret_cast<const f32x4*>(row), e1 = *reinterpret_cast<const f32x4*>(row + 32);
+#pragma unroll
+      for (int kb = 0; kb < C::KB; ++kb) {
+        const f16x8 p = *p_at(w, u, 1, 2 * kb + cq);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) da[kb][e] = (__bf16)((float)p[e] * (dp[kb][8 * cq + e] + (e < 4 ? e0[e & 3] : e1[e & 3])));
+      }
+      second_product(nh, nb_all, at.q, cb, cq, da);
+    }
+  };
+  const int n_own = 64 * pair >= L - kv0 ? 0 : CAUSAL ? n_tiles - 2 * pair : n_tiles;      // see knap_attn_dkdv.h
+#define KNAP_STEP(ROLE, t, cur, prev, nxt)                            \
+  do {                                                                \
+    issue_tile((t) + 1, r##nxt);                                      \
+    if constexpr (ROLE == 0) {                                        \
+      if ((t) < n_own) dv_step((t), r##cur);                          \
+    } else {                                                          \
+      if ((t) >= 1 && (t) <= n_own) dk_step((t) - 1, r##prev);        \
+    }                                                                 \
+    step_sync();                                                      \
+  } while (0)
+#define KNAP_ROLE_LOOP(ROLE)                                          \
+  do {                                                                \
+    int t = 0;                                                        \
+    for (; t + 2 <= n_tiles; t += 3) {                                \
+      KNAP_STEP(ROLE, t, 0, 2, 1);                                    \
+      KNAP_STEP(ROLE, t + 1, 1, 0, 2);                                \
+      KNAP_STEP(ROLE, t + 2, 2, 1, 0);                                \
+    }                                                                 \
+    if (t <= n_tiles) {                                               \
+      KNAP_STEP(ROLE, t, 0, 2, 1);                                    \
+      if (t + 1 <= n_tiles) KNAP_STEP(ROLE, t + 1, 1, 0, 2);          \
+    }                                                                 \
+  } while (0)
+  issue_tile(0, r0);
+  step_sync();
+  if (role == 0) KNAP_ROLE_LOOP(0);
+  else KNAP_ROLE_LOOP(1);
+#undef KNAP_ROLE_LOOP
+#undef KNAP_STEP
+
+  const auto rg = make_rsrc((role == 0 ? g.dv : g.dk) + (size_t)(it.row0 + kv0) * row_stride + (size_t)head * D,
+                            (uint32_t)min(L - kv0, C::BN) * row_bytes);
+  const int w_out = me.at.fresh();
+#pragma unroll
+  for (int kb = 0; kb < C::KB; ++kb) {
+    const uint32_t off = (uint32_t)(64 * pair + 32 * kb + LaneWord::l32(w_out)) * row_bytes + (uint32_t)LaneWord::hh16(w_out);
+#pragma unroll
+    for (int nb = 0; nb < C::NB; ++nb)
+      store_block(rg, off + 64u * nb, acc[kb][nb], kDiffDown * (role == 0 ? 1.0f : nb < NH ? g.scale : -lambda * g.scale));
+  }
+}
+
+template <int D, int PAIRS, bool CAUSAL>
+__global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a) {
+  using C = Bwd2Cfg<D, PAIRS>;
+  extern __shared__ int s_dyn[];
+  int* s_order = s_dyn;
+  int* s_start = s_dyn + a.n_seq;
+#define KNAP_RING(i)                                                                    \
+  __shared__ __attribute__((aligned(1024))) __bf16 sQ##i[C::TILE_ELEMS];                \
+  __shared__ __attribute__((aligned(1024))) __bf16 sdO##i[C::TILE_ELEMS];               \
+  __shared__ __attribute__((aligned(256))) float sLa##i[64], sLb##i[64], sNd##i[64], sDf##i[64];
+  KNAP_RING(0) KNAP_RING(1) KNAP_RING(2)
+#undef KNAP_RING
+  __shared__ __attribute__((aligned(256))) float sSink[64];
+  __shared__ __attribute__((aligned(1024))) char sP[PAIRS * DiffLane<D, PAIRS>::P_PAIR];
+  __shared__ int s_ticket;
+
+  const int T = a.cu[a.n_seq];
+  const int n_items = build_schedule<C::BN, C::THREADS, CAUSAL>(a.cu, a.n_seq, a.H, s_order, s_start, reinterpret_cast<int*>(&sP[0]));
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // the two waves of a pair sit on one SIMD where there are four pairs; at two pairs the second half of the grid swaps roles
+  const int role = (wave / PAIRS) ^ (PAIRS == 2 ? (int)(blockIdx.x * 2 / gridDim.x) & 1 : 0);
+  DiffLane<D, PAIRS> me;
+  me.init(lane, wave, role, (uint32_t)((size_t)a.H * D * sizeof(__bf16)));
+  const DiffSlot r0 = {sQ0, sdO0, sLa0, sLb0, sNd0, sDf0}, r1 = {sQ1, sdO1, sLa1, sLb1, sNd1, sDf1}, r2 = {sQ2, sdO2, sLa2, sLb2, sNd2, sDf2};
+  ItemQueue<0> queue;
+  queue.init(a.counters + 8, s_start, a.n_seq, n_items);
+  for (int ticket = queue.first_ticket(); ticket < queue.wide;) {
+    const WorkItem it = decode_item<C::BN, CAUSAL>(queue.item(ticket), a.cu, a.n_seq, s_order, s_start);
+    const int head = __builtin_amdgcn_readfirstlane(it.head), first = __builtin_amdgcn_readfirstlane(it.tile);
+    const int last = (it.len + C::BN - 1) / C::BN - 1 - first;      // CAUSAL: the pair of key tiles {first, last}
+    unsigned next_ticket;      // thread 0 only
+    if (tid == 0 && queue.draws) next_ticket = atomicAdd(queue.ctr, 1u);
+    for (int sub = 0; sub < (CAUSAL && first != last ? 2 : 1); ++sub)
+      diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sSink, sP, me, it, head, sub == 0 ? first : last, T);
+    if (!queue.draws) break;
+    if (tid == 0) s_ticket = queue.later_ticket(next_ticket);
+    lds_barrier();
+    ticket = __builtin_amdgcn_readfirstlane(s_ticket);
+    lds_barrier();        // everyone has the ticket before the next one is put down
+  }
+}
+
+// dlambda of a head: minus the sum of its rows' D_2
+__global__ __launch_bounds__(1024) void diff_lambda_kernel(DiffBwdArgs a) {
+  __shared__ float s_sum[16];
+  const int T = a.cu[a.n_seq];
+  const float* row = a.d2 + (size_t)blockIdx.x * T;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int t = threadIdx.x; t < T; t += 1024) sum += row[t];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = 0.f;
+    for (int w = 0; w < 16; ++w) sum += s_sum[w];
+    a.dlambda[blockIdx.x] = -sum;
+  }
+}
+
+template <int D, bool CAUSAL>
+static hipError_t launch_diff_bwd_t(const DiffBwdArgs& a, int tokens, int cus, hipStream_t stream) {
+  constexpr int PAIRS = D == 128 ? 4 : 2;
+  const size_t dyn = (size_t)(2 * a.n_seq + 1) * sizeof(int);
+  hipLaunchKernelGGL(diff_delta_kernel<D>, dim3((tokens + 127) / 128, a.H), dim3(kThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((diff_dq_kernel<D, CAUSAL>), dim3(2 * cus), dim3(kThreads), dyn, stream, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL((diff_dkdv_kernel<D, PAIRS, CAUSAL>), dim3(cus * 4 / PAIRS), dim3(128 * PAIRS), dyn, stream, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(diff_lambda_kernel, dim3(a.H), dim3(1024), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int tokens, int cus, hipStream_t stream) {
+  if (d == 64) return causal ? launch_diff_bwd_t<64, true>(a, tokens, cus, stream) : launch_diff_bwd_t<64, false>(a, tokens, cus, stream);
+  return causal ? launch_diff_bwd_t<128, true>(a, tokens, cus, stream) : launch_diff_bwd_t<128, false>(a, tokens, cus, stream);
+}
+
+}  // namespace knap

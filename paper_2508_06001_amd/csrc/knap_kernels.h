@@ -50,6 +50,31 @@ hipError_t launch_ulysses_rows(const void* src, void* dst, const int32_t* row_ma
                                bool gather, hipStream_t stream);
 hipError_t launch_ulysses_plan(const int32_t* cu, int n_seq, int g, int T, int32_t* row_map, hipStream_t stream);
 
+// Differential attention
+struct DiffFwdArgs {
+  const __bf16 *q, *k, *v;
+  const int32_t* cu;
+  int n_seq, H;
+  float scale;
+  const float* lambda;      // (H)
+  __bf16 *out, *out2;       // out2 (the second map's output) or nullptr
+  float* lse;               // (2, H, T)
+  unsigned* counters;
+};
+struct DiffBwdArgs {
+  const __bf16 *q, *k, *v, *out, *out2, *dout;
+  const int32_t* cu;
+  int n_seq, H;
+  float scale;
+  const float *lambda, *lse;
+  __bf16 *dq, *dk, *dv;
+  float* dlambda;
+  float *nd1, *diff, *lse_a, *lse_b, *d2;      // (H, T) each: -D_1, D_1 - D_2, the log-sums in base 2 less 15, D_2 in 32 bits
+  unsigned* counters;                          // 8 for the dQ kernel, 8 for the dK/dV kernel; the launch clears them
+};
+hipError_t launch_diff_fwd(const DiffFwdArgs& a, int d, bool causal, int cus, hipStream_t stream);
+hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int tokens, int cus, hipStream_t stream);
+
 // Rotary positions: everything but the launch geometry comes from the caller
 struct RopeArgs {
   const __bf16 *q, *k;

@@ -125,3 +125,62 @@ class VarlenAttention:
         if self.rope is not None:
             self.rope.backward(self.dq, self.dk, self.dq, self.dk, stream)
         return self.dq, self.dk, self.dv
+
+
+class VarlenDiffAttention:
+    """Buffers + calls of differential attention over one packed bag: `lam` is the fp32 (H,) weight of the second map; `train=False`
+    keeps nothing for a backward.  `rope` turns the q and k of each map in front, as heads of d / 2 columns (rot <= d / 2).  `norm`, a
+    LayerNorm of T * H rows of d, is applied to every head's output row behind the difference."""
+
+    def __init__(self, cu_seqlens: Sequence[int], H: int, d: int, scale: float, lam, device="cuda", causal: bool = False, train: bool = True,
+                 rope: Optional[RotaryPositions] = None, norm: Optional[LayerNorm] = None):
+        self.causal, self.rope, self.norm = bool(causal), rope, norm
+        cu = np.asarray(cu_seqlens, dtype=np.int32)
+        self.n_seq = int(cu.shape[0] - 1)
+        self.T = int(cu[-1]) if cu.shape[0] else 0
+        self.H, self.d, self.scale, self.lam = int(H), int(d), float(scale), lam
+        self.device = torch.device(device)
+        self.cu = torch.from_numpy(cu).to(self.device)
+        shape = (self.T, self.H, self.d)
+
+        def new():
+            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+
+        self.out = new()
+        self.lse = torch.empty((2, self.H, self.T), dtype=torch.float32, device=self.device)
+        self.out2 = self.dq = self.dk = self.dv = self.dlam = self.workspace = None
+        if train:
+            self.out2, self.dq, self.dk, self.dv = new(), new(), new(), new()
+            self.dlam = torch.zeros((self.H,), dtype=torch.float32, device=self.device)
+            nbytes = B.knap_varlen_diff_attn_bwd_workspace_bytes(self.T, self.n_seq, self.H, self.d)
+            self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        if rope is not None:
+            self.q_turned, self.k_turned = new(), new()
+
+    def _maps(self, *tensors):
+        return [t.view(self.T, 2 * self.H, self.d // 2) for t in tensors]
+
+    def forward(self, q, k, v, stream=None):
+        if self.rope is not None:
+            self.rope.forward(*self._maps(q, k, self.q_turned, self.k_turned), stream)
+            q, k = self.q_turned, self.k_turned
+        fwd = B.knap_varlen_diff_attn_causal_fwd if self.causal else B.knap_varlen_diff_attn_fwd
+        fwd(q, k, v, self.cu, self.n_seq, self.H, self.d, self.scale, self.lam, self.out, self.out2, self.lse, stream)
+        if self.norm is None:
+            return self.out, self.lse
+        return self.norm.forward(self.out.view(self.T * self.H, self.d), stream).view(self.T, self.H, self.d), self.lse
+
+    def backward(self, q, k, v, dout, stream=None):
+        """dq, dk, dv, dlambda; the norm's own gradients are in `norm.dweight` and `norm.dbias`."""
+        if self.norm is not None:
+            rows = self.T * self.H
+            dout = self.norm.backward(self.out.view(rows, self.d), dout.view(rows, self.d), stream)[0].view(self.T, self.H, self.d)
+        if self.rope is not None:        # as the forward left them
+            q, k = self.q_turned, self.k_turned
+        bwd = B.knap_varlen_diff_attn_causal_bwd if self.causal else B.knap_varlen_diff_attn_bwd
+        bwd(q, k, v, self.cu, self.n_seq, self.H, self.d, self.scale, self.lam, self.out, self.out2, self.lse, dout, self.dq, self.dk, self.dv,
+            self.dlam, self.T, self.workspace, None, stream)
+        if self.rope is not None:
+            grads = self._maps(self.dq, self.dk)
+            self.rope.backward(*grads, *grads, stream)
+        return self.dq, self.dk, self.dv, self.dlam
