@@ -482,10 +482,11 @@ int rope_impl(const void* q, const void* k, int64_t tokens, int H, int H_k, int 
 }
 
 // type codes, strides and pointers of one tensor of rows
-bool rows_ok(const void* p, int type, int64_t stride, int64_t rows, int width) {
-  return p && aligned(p, type == KNAP_BF16 ? 2 : 4) && (rows == 1 || (stride >= width && stride <= ((int64_t)1 << 30)));
+bool rows_ok(const void* p, int type, int64_t stride, int width) {
+  return p && aligned(p, type == KNAP_BF16 ? 2 : 4) && stride >= width && stride <= ((int64_t)1 << 30);
 }
-bool rows_wide(const void* p, int64_t stride, int64_t rows) { return aligned(p, 16) && (rows == 1 || stride % 8 == 0); }
+// whether 16-byte accesses reach every row; rows further apart than 2^22 columns take the other form, whose offsets count one row alone
+bool rows_wide(const void* p, int64_t stride, int64_t rows) { return aligned(p, 16) && (rows == 1 || (stride % 8 == 0 && stride <= (1 << 22))); }
 bool type_ok(int type) { return type == KNAP_BF16 || type == KNAP_F32; }
 
 }  // namespace
@@ -513,7 +514,8 @@ int knap_layer_norm_fwd(const void* x, int x_type, int64_t x_stride, int64_t row
   if (!type_ok(x_type) || !type_ok(y_type) || !type_ok(w_type) || (x_type == KNAP_BF16 && y_type == KNAP_F32)) return KNAP_ERR_INVALID_ARG;
   if (rows < 0 || rows > INT32_MAX || width < 1 || width > KNAP_LAYER_NORM_MAX_WIDTH || !(eps >= 0.f) || !(eps < 3.0e38f)) return KNAP_ERR_INVALID_ARG;
   if (rows == 0) return KNAP_OK;
-  if (!rows_ok(x, x_type, x_stride, rows, width) || !rows_ok(y, y_type, y_stride, rows, width) || x == y) return KNAP_ERR_INVALID_ARG;
+  if (rows == 1) x_stride = y_stride = width;
+  if (!rows_ok(x, x_type, x_stride, width) || !rows_ok(y, y_type, y_stride, width) || x == y) return KNAP_ERR_INVALID_ARG;
   const size_t w_align = w_type == KNAP_BF16 ? 2 : 4;
   if (!aligned(weight, w_align) || !aligned(bias, w_align) || !aligned(mean, 4) || !aligned(rstd, 4)) return KNAP_ERR_INVALID_ARG;
   knap::NormArgs a{};
@@ -547,8 +549,9 @@ int knap_layer_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t row
     if (!sums) return KNAP_OK;
     e = knap::launch_layer_norm_zero(dweight, dbias, width, static_cast<hipStream_t>(stream));
   } else {
-    if (!rows_ok(x, x_type, x_stride, rows, width) || !rows_ok(dy, y_type, dy_stride, rows, width) ||
-        !rows_ok(dx, x_type, dx_stride, rows, width) || dx == x || dx == dy)
+    if (rows == 1) x_stride = dy_stride = dx_stride = width;
+    if (!rows_ok(x, x_type, x_stride, width) || !rows_ok(dy, y_type, dy_stride, width) ||
+        !rows_ok(dx, x_type, dx_stride, width) || dx == x || dx == dy)
       return KNAP_ERR_INVALID_ARG;
     if (!mean || !rstd || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, w_type == KNAP_BF16 ? 2 : 4)) return KNAP_ERR_INVALID_ARG;
     if (sums) {

@@ -9,6 +9,8 @@
 #include "knap_device.h"
 #include "knap_kernels.h"
 
+#include <type_traits>
+
 namespace knap {
 
 template <int LANES_, int UNITS_, int ROWS_, bool WIDE_>
@@ -42,46 +44,94 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) { v[e] = x[e]; v[4 + e] = y[e]; }
 }
-__device__ __forceinline__ void store8(__bf16* p, const float* v) {
-  *reinterpret_cast<bf16x8*>(p) = pack8(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void store8(float* p, const float* v) {
-  const f32x4 x = {v[0], v[1], v[2], v[3]}, y = {v[4], v[5], v[6], v[7]};
-  *reinterpret_cast<f32x4*>(p) = x;
-  *reinterpret_cast<f32x4*>(p + 4) = y;
-}
 
-// a row's columns of this thread; zeros where it has none
+// A thread's columns of a row as they lie in memory, so that the loads of the next rows can be under way while this one is worked on
+// and columns of 16 bits take half a register each.  Columns behind the row's end are zeros: accesses go through a descriptor of the
+// row (of the rows of the waves, where several share one), which costs no branches.
 template <class C, class T>
-__device__ __forceinline__ void load_row(const T* row, bool there, int g, int width, float (&v)[C::COLS]) {
+struct RowRaw {
+  static constexpr bool PACKED = C::WIDE && sizeof(T) == 2;
+  static constexpr int WORDS = PACKED ? 4 * C::UNITS : C::COLS;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (PACKED) return __builtin_bit_cast(float, (i & 1) ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    else if constexpr (sizeof(T) == 2) return __builtin_bit_cast(float, w[i] << 16);
+    else return __builtin_bit_cast(float, w[i]);
+  }
+};
+
+// rows [row, row + GROUPS) of which the thread's group has the `group`-th; `rows` and `stride` of the tensor
+template <class C, class T>
+struct RowPlace {
+  __amdgpu_buffer_rsrc_t r;
+  uint32_t off, end;      // byte offsets of the row and behind it
+  __device__ __forceinline__ RowPlace(const T* base, int64_t stride, int64_t row0, int group, int64_t rows, int width) {
+    if constexpr (C::LANES >= 64) {
+      const int64_t row = row0 + __builtin_amdgcn_readfirstlane(group);
+      r = make_rsrc(base + row * stride, row < rows ? (uint32_t)width * (uint32_t)sizeof(T) : 0u);
+      off = 0;
+      end = (uint32_t)width * (uint32_t)sizeof(T);
+    } else {              // the groups of a wave and those of the others: their rows are at most 64 KB apart, or the form is not taken
+      const int64_t left = min((int64_t)C::GROUPS, rows - row0);
+      r = make_rsrc(base + row0 * stride, left > 0 ? (uint32_t)((left - 1) * stride + width) * (uint32_t)sizeof(T) : 0u);
+      off = (uint32_t)group * (uint32_t)stride * (uint32_t)sizeof(T);
+      end = group < left ? off + (uint32_t)width * (uint32_t)sizeof(T) : 0u;
+    }
+  }
+  // the byte offset of column c, or one behind everything for columns that the row does not have
+  __device__ __forceinline__ int at(int c) const {
+    const uint32_t o = off + (uint32_t)c * (uint32_t)sizeof(T);
+    if constexpr (C::LANES >= 64) return (int)o;
+    else return o < end ? (int)o : 0x7ffffff0;
+  }
+};
+
+template <class C, class T>
+__device__ __forceinline__ void load_row(const RowPlace<C, T>& p, int g, RowRaw<C, T>& v) {
 #pragma unroll
   for (int u = 0; u < C::UNITS; ++u) {
-    float x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
     if constexpr (C::WIDE) {
-      if (there && norm_has<C>(g, 8 * u, width)) load8(row + norm_col<C>(g, 8 * u), x);
+      const int o = p.at(norm_col<C>(g, 8 * u));
+#pragma unroll
+      for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(p.r, o + 16 * h, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v.w[(sizeof(T) == 2 ? 4 : 8) * u + 4 * h + e] = x[e];
+      }
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (there && norm_has<C>(g, 8 * u + e, width)) x[e] = (float)row[norm_col<C>(g, 8 * u + e)];
+      for (int e = 0; e < 8; ++e) {
+        const int o = p.at(norm_col<C>(g, 8 * u + e));
+        v.w[8 * u + e] = sizeof(T) == 2 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(p.r, o, 0, 0) : __builtin_amdgcn_raw_buffer_load_b32(p.r, o, 0, 0);
+      }
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[8 * u + e] = x[e];
   }
 }
 
 template <class C, class T>
-__device__ __forceinline__ void store_row(T* row, bool there, int g, int width, const float (&v)[C::COLS]) {
-  if (!there) return;
+__device__ __forceinline__ void store_row(const RowPlace<C, T>& p, int g, const float (&v)[C::COLS]) {
 #pragma unroll
   for (int u = 0; u < C::UNITS; ++u) {
     if constexpr (C::WIDE) {
-      if (norm_has<C>(g, 8 * u, width)) store8(row + norm_col<C>(g, 8 * u), v + 8 * u);
+      const int o = p.at(norm_col<C>(g, 8 * u));
+      const float* x = v + 8 * u;
+      if constexpr (sizeof(T) == 2) {
+        const bf16x8 b = pack8(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, b), p.r, o, 0, 0);
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 y = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), p.r, o + 16 * h, 0, 0);
+        }
+      }
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (norm_has<C>(g, 8 * u + e, width)) row[norm_col<C>(g, 8 * u + e)] = (T)v[8 * u + e];
+      for (int e = 0; e < 8; ++e) {
+        const int o = p.at(norm_col<C>(g, 8 * u + e));
+        if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (__bf16)v[8 * u + e]), p.r, o, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v[8 * u + e]), p.r, o, 0, 0);
+      }
     }
   }
 }
@@ -114,13 +164,34 @@ __device__ __forceinline__ void load_weight(const void* w, bool w_bf16, float no
     }
 }
 
+// x and the lanes it is joined with: DPP inside 16 lanes, swaps of rows of 16 and of halves of the wave beyond
+template <int LANES>
+__device__ __forceinline__ float lane_sum(float x) {
+  auto dpp = [&](auto ctrl) {
+    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  dpp(std::integral_constant<int, 0xb1>{});         // quad_perm 1, 0, 3, 2
+  dpp(std::integral_constant<int, 0x4e>{});         // quad_perm 2, 3, 0, 1
+  dpp(std::integral_constant<int, 0x141>{});        // row_half_mirror: the other four of eight
+  dpp(std::integral_constant<int, 0x140>{});        // row_mirror: the other eight of sixteen
+  if constexpr (LANES > 16) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    const auto p = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    x = __builtin_bit_cast(float, (uint32_t)p[0]) + __builtin_bit_cast(float, (uint32_t)p[1]);
+  }
+  if constexpr (LANES > 32) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    const auto p = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    x = __builtin_bit_cast(float, (uint32_t)p[0]) + __builtin_bit_cast(float, (uint32_t)p[1]);
+  }
+  return x;
+}
+
 // N sums over the threads of a row, in every one of them.  s_sum: waves x N floats, another place than that of the call before.
 template <class C, int N>
 __device__ __forceinline__ void row_sums(float (&x)[N], float* s_sum) {
 #pragma unroll
-  for (int o = 1; o < (C::LANES < 64 ? C::LANES : 64); o <<= 1)
-#pragma unroll
-    for (int n = 0; n < N; ++n) x[n] += __shfl_xor(x[n], o, 64);
+  for (int n = 0; n < N; ++n) x[n] = lane_sum<C::LANES>(x[n]);
   if constexpr (C::LANES > 64) {
     constexpr int WAVES = C::THREADS / 64;
     const int wave = threadIdx.x >> 6;

@@ -15,36 +15,53 @@ __global__ __launch_bounds__(C::THREADS, 2) void layer_norm_bwd_kernel(NormArgs 
   __shared__ float s_cols[C::GROUPS > 1 ? C::THREADS * C::COLS : 1];
   const int g = threadIdx.x % C::LANES, group = threadIdx.x / C::LANES;
   const int width = a.width;
-  const float share = 1.0f / (float)width;
+  const float n = (float)width;
   float w[C::COLS], dw[C::COLS], db[C::COLS];
   load_weight<C>(a.weight, a.w_bf16, 1.f, g, width, w);
 #pragma unroll
   for (int i = 0; i < C::COLS; ++i) dw[i] = db[i] = 0.f;
-  int turn = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * C::PASS; r0 < a.rows; r0 += (int64_t)gridDim.x * C::PASS, turn ^= 1) {
-    float x[C::ROWS][C::COLS], dy[C::ROWS][C::COLS], sums[2 * C::ROWS], rstd[C::ROWS];
-    int64_t row[C::ROWS];
+  const TX* x_base = static_cast<const TX*>(a.x);
+  const TY* dy_base = static_cast<const TY*>(a.dy);
+  TX* dx_base = static_cast<TX*>(a.dx);
+  const int64_t step = (int64_t)gridDim.x * C::PASS;
+  RowRaw<C, TX> next_x[C::ROWS];
+  RowRaw<C, TY> next_dy[C::ROWS];
+  float next_mean[C::ROWS], next_rstd[C::ROWS];
+  auto load = [&](int64_t r0) {
 #pragma unroll
     for (int k = 0; k < C::ROWS; ++k) {
-      row[k] = r0 + k * C::GROUPS + group;
-      const bool there = row[k] < a.rows;
-      load_row<C>(static_cast<const TX*>(a.x) + row[k] * a.x_stride, there, g, width, x[k]);
-      load_row<C>(static_cast<const TY*>(a.dy) + row[k] * a.y_stride, there, g, width, dy[k]);
+      const int64_t first = r0 + k * C::GROUPS, row = first + group;
+      load_row<C, TX>(RowPlace<C, TX>(x_base, a.x_stride, first, group, a.rows, width), g, next_x[k]);
+      load_row<C, TY>(RowPlace<C, TY>(dy_base, a.y_stride, first, group, a.rows, width), g, next_dy[k]);
+      next_mean[k] = row < a.rows ? a.mean[row] : 0.f;
+      next_rstd[k] = row < a.rows ? a.rstd[row] : 0.f;
     }
+  };
+  load((int64_t)blockIdx.x * C::PASS);
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * C::PASS; r0 < a.rows; r0 += step, turn ^= 1) {
+    RowRaw<C, TX> x[C::ROWS];
+    RowRaw<C, TY> dy[C::ROWS];
+    float sums[2 * C::ROWS], rstd[C::ROWS], shift[C::ROWS];
 #pragma unroll
     for (int k = 0; k < C::ROWS; ++k) {
-      const bool there = row[k] < a.rows;
-      const float mean = there ? a.mean[row[k]] : 0.f;
-      rstd[k] = there ? a.rstd[row[k]] : 0.f;
+      x[k] = next_x[k];
+      dy[k] = next_dy[k];
+      rstd[k] = next_rstd[k];
+      shift[k] = next_mean[k];
+    }
+    load(r0 + step);
+    // columns behind the row's end have dy = 0 and add nothing
+#pragma unroll
+    for (int k = 0; k < C::ROWS; ++k) {
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
       for (int i = 0; i < C::COLS; ++i) {
-        x[k][i] = norm_has<C>(g, i, width) ? (x[k][i] - mean) * rstd[k] : 0.f;
-        dw[i] = __builtin_fmaf(dy[k][i], x[k][i], dw[i]);
-        db[i] += dy[k][i];
-        dy[k][i] *= w[i];
-        s1 += dy[k][i];
-        s2 = __builtin_fmaf(dy[k][i], x[k][i], s2);
+        const float xh = (x[k].get(i) - shift[k]) * rstd[k], y = dy[k].get(i), gi = y * w[i];
+        dw[i] = __builtin_fmaf(y, xh, dw[i]);
+        db[i] += y;
+        s1 += gi;
+        s2 = __builtin_fmaf(gi, xh, s2);
       }
       sums[2 * k] = s1;
       sums[2 * k + 1] = s2;
@@ -52,10 +69,14 @@ __global__ __launch_bounds__(C::THREADS, 2) void layer_norm_bwd_kernel(NormArgs 
     row_sums<C>(sums, s_sum[turn]);
 #pragma unroll
     for (int k = 0; k < C::ROWS; ++k) {
-      const float m1 = sums[2 * k] * share, m2 = sums[2 * k + 1] * share;
+      const float m1 = sums[2 * k] / n, m2 = sums[2 * k + 1] / n;
+      float dx[C::COLS];
 #pragma unroll
-      for (int i = 0; i < C::COLS; ++i) x[k][i] = rstd[k] * (dy[k][i] - m1 - x[k][i] * m2);
-      store_row<C>(static_cast<TX*>(a.dx) + row[k] * a.dx_stride, row[k] < a.rows, g, width, x[k]);
+      for (int i = 0; i < C::COLS; ++i) {
+        const float xh = (x[k].get(i) - shift[k]) * rstd[k];
+        dx[i] = rstd[k] * (__builtin_fmaf(dy[k].get(i), w[i], -m1) - xh * m2);
+      }
+      store_row<C, TX>(RowPlace<C, TX>(dx_base, a.dx_stride, r0 + k * C::GROUPS, group, a.rows, width), g, dx);
     }
   }
   if (!a.partial) return;

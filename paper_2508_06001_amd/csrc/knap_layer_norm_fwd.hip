@@ -15,42 +15,50 @@ __global__ __launch_bounds__(C::THREADS, 2) void layer_norm_fwd_kernel(NormArgs 
   float w[C::COLS], b[C::COLS];
   load_weight<C>(a.weight, a.w_bf16, 1.f, g, width, w);
   load_weight<C>(a.bias, a.w_bf16, 0.f, g, width, b);
-  for (int64_t r0 = (int64_t)blockIdx.x * C::PASS; r0 < a.rows; r0 += (int64_t)gridDim.x * C::PASS) {
-    float x[C::ROWS][C::COLS], sum[C::ROWS];
-    int64_t row[C::ROWS];
+  const TX* x_base = static_cast<const TX*>(a.x);
+  TY* y_base = static_cast<TY*>(a.y);
+  const int64_t step = (int64_t)gridDim.x * C::PASS;
+  RowRaw<C, TX> next[C::ROWS];
+  auto load = [&](int64_t r0) {
 #pragma unroll
-    for (int k = 0; k < C::ROWS; ++k) {
-      row[k] = r0 + k * C::GROUPS + group;
-      load_row<C>(static_cast<const TX*>(a.x) + row[k] * a.x_stride, row[k] < a.rows, g, width, x[k]);
-    }
+    for (int k = 0; k < C::ROWS; ++k) load_row<C, TX>(RowPlace<C, TX>(x_base, a.x_stride, r0 + k * C::GROUPS, group, a.rows, width), g, next[k]);
+  };
+  load((int64_t)blockIdx.x * C::PASS);
+  for (int64_t r0 = (int64_t)blockIdx.x * C::PASS; r0 < a.rows; r0 += step) {
+    RowRaw<C, TX> x[C::ROWS];
+    float sum[C::ROWS], mean[C::ROWS];
+#pragma unroll
+    for (int k = 0; k < C::ROWS; ++k) x[k] = next[k];
+    load(r0 + step);
 #pragma unroll
     for (int k = 0; k < C::ROWS; ++k) {
       sum[k] = 0.f;
 #pragma unroll
-      for (int i = 0; i < C::COLS; ++i) sum[k] += x[k][i];
+      for (int i = 0; i < C::COLS; ++i) sum[k] += x[k].get(i);
     }
     row_sums<C>(sum, s_sum[0]);
-    float mean[C::ROWS];
 #pragma unroll
     for (int k = 0; k < C::ROWS; ++k) {
       mean[k] = sum[k] / n;
       sum[k] = 0.f;
 #pragma unroll
       for (int i = 0; i < C::COLS; ++i) {
-        x[k][i] = norm_has<C>(g, i, width) ? x[k][i] - mean[k] : 0.f;
-        sum[k] = __builtin_fmaf(x[k][i], x[k][i], sum[k]);
+        const float d = norm_has<C>(g, i, width) ? x[k].get(i) - mean[k] : 0.f;
+        sum[k] = __builtin_fmaf(d, d, sum[k]);
       }
     }
     row_sums<C>(sum, s_sum[1]);
 #pragma unroll
     for (int k = 0; k < C::ROWS; ++k) {
       const float rstd = 1.0f / sqrtf(sum[k] / n + a.eps);
+      float y[C::COLS];
 #pragma unroll
-      for (int i = 0; i < C::COLS; ++i) x[k][i] = __builtin_fmaf(x[k][i] * rstd, w[i], b[i]);
-      store_row<C>(static_cast<TY*>(a.y) + row[k] * a.y_stride, row[k] < a.rows, g, width, x[k]);
-      if (g == 0 && row[k] < a.rows) {
-        if (a.mean) a.mean[row[k]] = mean[k];
-        if (a.rstd) a.rstd[row[k]] = rstd;
+      for (int i = 0; i < C::COLS; ++i) y[i] = __builtin_fmaf((x[k].get(i) - mean[k]) * rstd, w[i], b[i]);
+      store_row<C, TY>(RowPlace<C, TY>(y_base, a.y_stride, r0 + k * C::GROUPS, group, a.rows, width), g, y);
+      const int64_t row = r0 + k * C::GROUPS + group;
+      if (g == 0 && row < a.rows) {
+        if (a.mean) a.mean[row] = mean[k];
+        if (a.rstd) a.rstd[row] = rstd;
       }
     }
   }
