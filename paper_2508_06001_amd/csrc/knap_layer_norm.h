@@ -218,9 +218,12 @@ hipError_t norm_form(int width, F f) {
   }
   if (width <= 512) return f(NormCfg<64, 1, 4, WIDE>{});
   if (width <= 1024) return f(NormCfg<64, 2, 2, WIDE>{});
+  if (width <= 1536) return f(NormCfg<64, 3, 1, WIDE>{});
   if (width <= 2048) return f(NormCfg<64, 4, 1, WIDE>{});
   if (width <= 4096) return f(NormCfg<256, 2, 2, WIDE>{});
+  if (width <= 6144) return f(NormCfg<256, 3, 1, WIDE>{});
   if (width <= 8192) return f(NormCfg<256, 4, 1, WIDE>{});
+  if (width <= 12288) return f(NormCfg<512, 3, 1, WIDE>{});
   return f(NormCfg<512, 4, 1, WIDE>{});
 }
 
