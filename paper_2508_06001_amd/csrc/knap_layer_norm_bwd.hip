@@ -134,7 +134,9 @@ static hipError_t launch_bwd_t(const NormArgs& a, float* dw, float* db, int cus,
   return norm_form<WIDE>(a.width, [&](auto cfg) {
     using C = decltype(cfg);
     const int64_t passes = (a.rows + C::PASS - 1) / C::PASS;
-    const int most = (int)std::min<int64_t>(passes, std::min(4 * cus, kNormMaxGroups));
+    // two workgroups a CU, which is what the registers of the wider forms allow: more of them only leave more sums to add up (8191 rows of
+    // 4099 in 32 bits, four -> two, us: 65.0 -> 60.0 and 9.4 -> 5.6 for the sums; 103008 of 128 19.4 -> 18.6; 31464 of 1536 the same, 6.4 -> 5.4)
+    const int most = (int)std::min<int64_t>(passes, std::min(2 * cus, kNormMaxGroups));
     const int64_t each = (passes + most - 1) / most;          // as many for every workgroup, but for the last
     const int groups = (int)((passes + each - 1) / each);
     hipLaunchKernelGGL((layer_norm_bwd_kernel<C, TX, TY>), dim3(groups), dim3(C::THREADS), 0, stream, a);
