@@ -279,9 +279,9 @@ int knap_ulysses_scatter_chunks(const void* z, const int32_t* row_map, int64_t t
  * output must not overlap (either the heads of a token lie between two tokens, or the
  * tokens of a head between two heads).  An output may be its input (in place, same
  * strides); otherwise outputs must not overlap inputs or each other (not checked).
- * Pointers of q and k need an alignment of 2 bytes only; the fast form takes
- * 16, strides that are multiples of 8 and units of 8 columns (rot a multiple of 8
- * in the interleaved layout, of 16 in the half one, d of 8).
+ * Pointers of q and k need an alignment of 2 bytes only; the fast forms take
+ * 16 and strides and d that are multiples of 8, the fastest also rot a multiple of 8 in
+ * the interleaved layout, in the half one of 16 and d a power of two up to 512.
  *
  * Positions, one of:
  *   positions   device int32 (tokens, n_axes), contiguous: a position on each axis

@@ -460,12 +460,12 @@ int rope_impl(const void* q, const void* k, int64_t tokens, int H, int H_k, int 
   a.q_out = static_cast<__bf16*>(q_out);
   a.q_token = s[0]; a.q_head = s[1]; a.qo_token = s[4]; a.qo_head = s[5];
   const bool half = layout == KNAP_ROPE_HALF;
-  bool wide = d % 8 == 0 && rot % (half ? 16 : 8) == 0 && aligned(q, 16) && aligned(q_out, 16) && (s[0] | s[1] | s[4] | s[5]) % 8 == 0;
+  bool on16 = d % 8 == 0 && aligned(q, 16) && aligned(q_out, 16) && (s[0] | s[1] | s[4] | s[5]) % 8 == 0;
   if (H_k > 0) {
     a.k = static_cast<const __bf16*>(k);
     a.k_out = static_cast<__bf16*>(k_out);
     a.k_token = s[2]; a.k_head = s[3]; a.ko_token = s[6]; a.ko_head = s[7];
-    wide = wide && aligned(k, 16) && aligned(k_out, 16) && (s[2] | s[3] | s[6] | s[7]) % 8 == 0;
+    on16 = on16 && aligned(k, 16) && aligned(k_out, 16) && (s[2] | s[3] | s[6] | s[7]) % 8 == 0;
   }
   a.T = (int)tokens; a.H = H; a.Hk = H_k; a.d = d; a.rot = rot;
   a.positions = positions; a.n_axes = n_axes;
@@ -476,7 +476,7 @@ int rope_impl(const void* q, const void* k, int64_t tokens, int H, int H_k, int 
   a.copies = rot < d && !(in_place_q && (in_place_k || H_k == 0));
   DeviceInfo* di = device_info();
   if (!di) return KNAP_ERR_LAUNCH_FAILED;
-  const hipError_t e = knap::launch_rope(a, half, wide, di->cus, static_cast<hipStream_t>(stream));
+  const hipError_t e = knap::launch_rope(a, half, on16, di->cus, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
   return KNAP_OK;
 }

@@ -90,7 +90,7 @@ struct RopeArgs {
   bool copies;             // columns from rot on go to another tensor
   int tokens_per_group;    // set by the launch
 };
-hipError_t launch_rope(RopeArgs a, bool half, bool wide, int cus, hipStream_t stream);
+hipError_t launch_rope(RopeArgs a, bool half, bool aligned, int cus, hipStream_t stream);
 
 // Layer norm
 struct NormArgs {

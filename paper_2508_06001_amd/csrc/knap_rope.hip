@@ -39,15 +39,44 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, p);
 }
 
-// WIDE: every row starts on 16 bytes and no 16-byte unit holds columns of two kinds (rotated first half, second half, copied);
-// otherwise pairs and columns are moved one by one.
-template <bool HALF, bool WIDE>
+// How columns are moved:
+//   kPairs   one pair, or one copied column, at a time: rows that start on 2 bytes only
+//   kStaged  rows on 16 bytes, but units of 8 columns of which some are turned and some not, or whose partners lie across units: rows go
+//            through LDS, 16 bytes at a time either way, and are turned there pair by pair (5810 tokens, 16 heads of 64 of which 20
+//            columns turn, us: 10.7, and 24 pair by pair from memory)
+//   kUnits   units hold columns of one kind (rotated first half, second half, copied), a thread has one; in the half layout its partner is
+//            another unit of the row, which the wave's lanes trade, so that every access of a wave is whole rows (196608 tokens, 6 heads of
+//            128 of which 64 columns turn, us: 110 (5.5 TB/s), and 127 with both units of a pair in a thread)
+// Loads and stores past the caches: 31464 tokens, 48 heads of 128, us: 139 -> 128, now 124 (6.2 TB/s).
+enum RopeForm { kPairs, kStaged, kUnits };
+constexpr int kStageColumns = 16384;      // of the rows of a turn through LDS
+
+struct RopeRow {
+  const __bf16* src;
+  __bf16* dst;
+};
+// row `head` of a token, heads of q in front of those of k.  Both rows are formed and one is taken: a choice between the strides becomes
+// loads of kernel arguments that wait for each other (31464 tokens, 48 heads of 128, us: 128 -> 137).
+__device__ __forceinline__ RopeRow rope_row(const RopeArgs& a, int64_t t, uint32_t head) {
+  const bool is_q = head < (uint32_t)a.H;
+  const int64_t hq = head, hk = (int64_t)head - a.H;
+  const __bf16 *sq = a.q + t * a.q_token + hq * a.q_head, *sk = a.k + t * a.k_token + hk * a.k_head;
+  __bf16 *dq = a.q_out + t * a.qo_token + hq * a.qo_head, *dk = a.k_out + t * a.ko_token + hk * a.ko_head;
+  return {is_q ? sq : sk, is_q ? dq : dk};
+}
+
+__device__ __forceinline__ u32x4 unit_load(const __bf16* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+__device__ __forceinline__ void unit_store(__bf16* p, u32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p)); }
+
+template <bool HALF, RopeForm FORM>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
   extern __shared__ float2 s_trig[];                 // (tokens, pairs)
   __shared__ int s_first[kRopeMaxTokens];
   const int tid = threadIdx.x, pairs = a.rot / 2;
   const int t0 = (int)blockIdx.x * a.tokens_per_group;
   const int n_tok = min(a.tokens_per_group, a.T - t0);
+  const uint32_t heads = (uint32_t)(a.H + a.Hk);
+
   if (!a.positions) {
     for (int i = __builtin_amdgcn_readfirstlane(tid >> 6); i < n_tok; i += kRopeThreads / 64) {
       const int first = first_row_of(a.cu, a.n_seq, t0 + i, tid & 63);
@@ -74,56 +103,92 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
   }
   __syncthreads();
 
-  // slots of a head: units of 8 columns (of the half layout: two of them, a unit and its partner), or single pairs and columns
-  const int turned = WIDE ? (HALF ? a.rot / 16 : a.rot / 8) : pairs;
-  const int slots = turned + (a.copies ? (WIDE ? (a.d - a.rot) / 8 : a.d - a.rot) : 0);
-  const uint32_t per_tok = (uint32_t)(a.H + a.Hk) * (uint32_t)slots;
-  for (uint32_t i = tid; i < (uint32_t)n_tok * per_tok; i += kRopeThreads) {
-    const uint32_t tok = i / per_tok, rest = i - tok * per_tok, head = rest / (uint32_t)slots;
-    const int slot = (int)(rest - head * (uint32_t)slots);
-    if (!a.positions && s_first[tok] < 0) continue;
-    const bool is_q = head < (uint32_t)a.H;
-    const int64_t t = t0 + (int)tok, h = is_q ? head : head - (uint32_t)a.H;
-    const __bf16* src = is_q ? a.q + t * a.q_token + h * a.q_head : a.k + t * a.k_token + h * a.k_head;
-    __bf16* dst = is_q ? a.q_out + t * a.qo_token + h * a.qo_head : a.k_out + t * a.ko_token + h * a.ko_head;
-    const float2* trig = s_trig + (int)tok * pairs;
-    if constexpr (WIDE) {
-      if (slot >= turned) {
-        const int c = a.rot + 8 * (slot - turned);
-        *reinterpret_cast<u32x4*>(dst + c) = *reinterpret_cast<const u32x4*>(src + c);
-      } else if constexpr (HALF) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(src + 8 * slot), y = *reinterpret_cast<const u32x4*>(src + pairs + 8 * slot);
-        u32x4 ox, oy;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 u = trig[8 * slot + 2 * e], v = trig[8 * slot + 2 * e + 1];
-          const float a0 = lo_of(x[e]), a1 = hi_of(x[e]), b0 = lo_of(y[e]), b1 = hi_of(y[e]);
-          ox[e] = pack2(a0 * u.x - b0 * u.y, a1 * v.x - b1 * v.y);
-          oy[e] = pack2(a0 * u.y + b0 * u.x, a1 * v.y + b1 * v.x);
-        }
-        *reinterpret_cast<u32x4*>(dst + 8 * slot) = ox;
-        *reinterpret_cast<u32x4*>(dst + pairs + 8 * slot) = oy;
-      } else {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(src + 8 * slot);
-        u32x4 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 u = trig[4 * slot + e];
-          const float a0 = lo_of(x[e]), b0 = hi_of(x[e]);
-          o[e] = pack2(a0 * u.x - b0 * u.y, a0 * u.y + b0 * u.x);
-        }
-        *reinterpret_cast<u32x4*>(dst + 8 * slot) = o;
+  if constexpr (FORM == kUnits) {
+    // A thread keeps its unit and goes from row to row, `side` of them side by side, without a division for each.  HALF: a row's units are
+    // a power of two of lanes of one wave.
+    const uint32_t units = (uint32_t)a.d / 8, turned = (uint32_t)a.rot / 8, away = turned / 2;
+    const uint32_t side = kRopeThreads / units, u = tid % units, rows = (uint32_t)n_tok * heads;
+    if (u >= turned && !a.copies) return;
+    uint32_t r = tid / units, tok = r / heads, head = r - tok * heads;
+    const uint32_t more_tok = side / heads, more_head = side - more_tok * heads;
+    if (r >= side) return;
+    // (Two, three or six rows' loads in front of their stores: 196608 tokens, 6 heads, us: 110 -> 125, 131, 139.)
+    for (; r < rows; r += side, tok += more_tok, head += more_head) {
+      if (head >= heads) {
+        head -= heads;
+        ++tok;
       }
-    } else {
-      if (slot >= turned) {
-        const int c = a.rot + slot - turned;
-        dst[c] = src[c];
+      if (!a.positions && s_first[tok] < 0) continue;
+      const RopeRow row = rope_row(a, t0 + (int)tok, head);
+      const u32x4 x = unit_load(row.src + 8 * u);
+      u32x4 o = x;
+      if (u < turned) {
+        const float2* trig = s_trig + tok * (uint32_t)pairs;
+        if constexpr (HALF) {
+          const bool second = u >= away;
+          trig += 8 * (second ? u - away : u);
+          const int partner = tid + (second ? -(int)away : (int)away);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t y = (uint32_t)__shfl((int)x[e], partner & 63, 64);
+            const float2 p = trig[2 * e], q = trig[2 * e + 1];
+            const float s0 = second ? p.y : -p.y, s1 = second ? q.y : -q.y;
+            o[e] = pack2(lo_of(x[e]) * p.x + lo_of(y) * s0, hi_of(x[e]) * q.x + hi_of(y) * s1);
+          }
+        } else {
+          trig += 4 * u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 p = trig[e];
+            const float a0 = lo_of(x[e]), b0 = hi_of(x[e]);
+            o[e] = pack2(a0 * p.x - b0 * p.y, a0 * p.y + b0 * p.x);
+          }
+        }
+      }
+      unit_store(row.dst + 8 * u, o);
+    }
+  } else if constexpr (FORM == kStaged) {
+    __bf16* stage = reinterpret_cast<__bf16*>(s_trig + n_tok * pairs + (n_tok * pairs & 1));
+    const uint32_t n_rows = (uint32_t)n_tok * heads, most = (uint32_t)(kStageColumns / a.d), units = (uint32_t)a.d / 8;
+    for (uint32_t r0 = 0; r0 < n_rows; r0 += most) {
+      const uint32_t rows = min(most, n_rows - r0);
+      auto row_of = [&](uint32_t r) { return rope_row(a, t0 + (int)((r0 + r) / heads), (r0 + r) % heads); };
+      for (uint32_t i = tid; i < rows * units; i += kRopeThreads)
+        *reinterpret_cast<u32x4*>(stage + 8 * i) = unit_load(row_of(i / units).src + 8 * (i % units));
+      __syncthreads();
+      for (uint32_t i = tid; i < rows * (uint32_t)pairs; i += kRopeThreads) {
+        const uint32_t r = i / (uint32_t)pairs, p = i - r * (uint32_t)pairs;
+        __bf16* at = stage + r * (uint32_t)a.d;
+        const uint32_t ca = HALF ? p : 2 * p, cb = HALF ? p + (uint32_t)pairs : 2 * p + 1;
+        const float x = (float)at[ca], y = (float)at[cb];
+        const float2 u = s_trig[((r0 + r) / heads) * (uint32_t)pairs + p];
+        at[ca] = (__bf16)(x * u.x - y * u.y);
+        at[cb] = (__bf16)(x * u.y + y * u.x);
+      }
+      __syncthreads();
+      for (uint32_t i = tid; i < rows * units; i += kRopeThreads) {
+        if (!a.positions && s_first[(r0 + i / units) / heads] < 0) continue;
+        unit_store(row_of(i / units).dst + 8 * (i % units), *reinterpret_cast<const u32x4*>(stage + 8 * i));
+      }
+      __syncthreads();
+    }
+  } else {
+    const int slots = pairs + (a.copies ? a.d - a.rot : 0);      // of a head: pairs, then single columns
+    const uint32_t per_tok = heads * (uint32_t)slots, n_slots = (uint32_t)n_tok * per_tok;
+    for (uint32_t i = tid; i < n_slots; i += kRopeThreads) {
+      const uint32_t tok = i / per_tok, rest = i - tok * per_tok, head = rest / (uint32_t)slots;
+      const int at = (int)(rest - head * (uint32_t)slots);
+      if (!a.positions && s_first[tok] < 0) continue;
+      const RopeRow row = rope_row(a, t0 + (int)tok, head);
+      if (at >= pairs) {
+        const int c = a.rot + at - pairs;
+        row.dst[c] = row.src[c];
       } else {
-        const int ca = HALF ? slot : 2 * slot, cb = HALF ? slot + pairs : 2 * slot + 1;
-        const float x = (float)src[ca], y = (float)src[cb];
-        const float2 u = trig[slot];
-        dst[ca] = (__bf16)(x * u.x - y * u.y);
-        dst[cb] = (__bf16)(x * u.y + y * u.x);
+        const int ca = HALF ? at : 2 * at, cb = HALF ? at + pairs : 2 * at + 1;
+        const float x = (float)row.src[ca], y = (float)row.src[cb];
+        const float2 u = s_trig[(int)tok * pairs + at];
+        row.dst[ca] = (__bf16)(x * u.x - y * u.y);
+        row.dst[cb] = (__bf16)(x * u.y + y * u.x);
       }
     }
   }
@@ -131,16 +196,19 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
 
 }  // namespace
 
-hipError_t launch_rope(RopeArgs a, bool half, bool wide, int cus, hipStream_t stream) {
-  const int turned = wide ? (half ? a.rot / 16 : a.rot / 8) : a.rot / 2;
-  const int slots = turned + (a.copies ? (wide ? (a.d - a.rot) / 8 : a.d - a.rot) : 0);
-  const int64_t per_tok = (int64_t)(a.H + a.Hk) * slots;
-  // tokens of a workgroup: enough slots that its threads have four each, but not so many that the CUs run out of workgroups
+hipError_t launch_rope(RopeArgs a, bool half, bool aligned, int cus, hipStream_t stream) {
+  const int units = a.d / 8;
+  const bool whole = half ? a.rot % 16 == 0 && units <= 64 && (units & (units - 1)) == 0 : a.rot % 8 == 0;
+  const RopeForm form = !aligned ? kPairs : whole ? kUnits : kStaged;
+  const int64_t per_tok = (int64_t)(a.H + a.Hk) * (form == kPairs ? a.d : units);
+  // tokens of a workgroup: enough units that its threads have three or four each, but not so many that the CUs run out of workgroups
   int tokens = (int)std::max<int64_t>(1, std::min<int64_t>(kRopeMaxTokens, 4 * kRopeThreads / per_tok));
   while (tokens > 1 && (a.T + tokens - 1) / tokens < 4 * cus) tokens /= 2;
   a.tokens_per_group = tokens;
-  const size_t lds = (size_t)tokens * (a.rot / 2) * sizeof(float2);
-  auto* kernel = half ? (wide ? rope_kernel<true, true> : rope_kernel<true, false>) : (wide ? rope_kernel<false, true> : rope_kernel<false, false>);
+  size_t lds = (size_t)tokens * (a.rot / 2) * sizeof(float2);
+  if (form == kStaged) lds = (lds + 15) / 16 * 16 + kStageColumns * sizeof(__bf16);
+  auto* kernel = half ? (form == kUnits ? rope_kernel<true, kUnits> : form == kStaged ? rope_kernel<true, kStaged> : rope_kernel<true, kPairs>)
+                      : (form == kUnits ? rope_kernel<false, kUnits> : form == kStaged ? rope_kernel<false, kStaged> : rope_kernel<false, kPairs>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)((a.T + (int64_t)tokens - 1) / tokens)), dim3(kRopeThreads), lds, stream, a);
   return hipGetLastError();
 }
