@@ -219,14 +219,16 @@ struct DiffLane : DkdvLane<D, PAIRS> {
   }
 };
 
-// one slot of the ring: 32 rows of Q and dO and four values of each
+// one slot of the ring: 32 rows of Q and dO, and 64 places each for their log-sums (two), -D_1 and D_1 - D_2 (wave w copies the w-th of them,
+// the other waves nothing into the fifth)
 struct DiffSlot {
   __bf16 *q, *dout;
-  float *lse_a, *lse_b, *nd1, *diff;
+  float* values;
 };
+constexpr int kDiffValues = 5 * 64;
 
 template <int D, int PAIRS, bool CAUSAL>
-__device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffSlot& r0, const DiffSlot& r1, const DiffSlot& r2, float* sink, char* sP,
+__device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffSlot& r0, const DiffSlot& r1, const DiffSlot& r2, char* sP, char* sPark,
                                                const DiffLane<D, PAIRS>& me, const WorkItem& it, int head, int kv_tile, int T) {
   using C = Bwd2Cfg<D, PAIRS>;
   using W = DiffLane<D, PAIRS>;
@@ -239,10 +241,15 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
   const int q_first = CAUSAL ? kv0 : 0;       // queries this key tile meets: rows q_first .. L - 1; tiles and rows below count from it
   const int Lq = L - q_first;
   const size_t q_at = (size_t)(it.row0 + q_first) * row_stride + (size_t)head * D;
-  const size_t v_at = (size_t)head * T + it.row0 + q_first;
+  const float* values = (wave == 0 ? g.lse_a : wave == 1 ? g.lse_b : wave == 2 ? g.nd1 : g.diff) + (size_t)head * T + it.row0 + q_first;
+  const uint32_t value_bytes = wave < 4 ? 4u : 0u;
   const int n_tiles = (Lq + C::BM - 1) / C::BM;
 
-  bf16x8 kvf[C::KB][C::KC];
+  // PARKED: the last 16 columns lie in LDS, for which there is no register: spilled, their reloads would wait for the tile copies issued in
+  // front of them (vector memory completes in issue order)
+  constexpr int PARKED = D == 128 ? 1 : 0, KEPT = C::KC - PARKED;
+  bf16x8 kvf[C::KB][KEPT];
+  auto parked = [&](int kb, int w) { return reinterpret_cast<bf16x8*>(sPark + 1024 * (2 * wave + kb) + (LaneWord::lane4(w) << 2)); };
   {
     const auto r = make_rsrc((role == 0 ? g.k : g.v) + (size_t)(it.row0 + kv0) * row_stride + (size_t)head * D,
                              (uint32_t)min(L - kv0, C::BN) * row_bytes);
@@ -251,7 +258,8 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
     for (int kb = 0; kb < C::KB; ++kb) {
       const uint32_t off = (uint32_t)(64 * pair + 32 * kb + LaneWord::l32(w)) * row_bytes + (uint32_t)LaneWord::hh16(w);
 #pragma unroll
-      for (int cc = 0; cc < C::KC; ++cc) kvf[kb][cc] = __builtin_bit_cast(bf16x8, buffer_load16(r, off + 32u * cc));
+      for (int cc = 0; cc < KEPT; ++cc) kvf[kb][cc] = __builtin_bit_cast(bf16x8, buffer_load16(r, off + 32u * cc));
+      if constexpr (PARKED) *parked(kb, w) = __builtin_bit_cast(bf16x8, buffer_load16(r, off + 32u * KEPT));
     }
   }
   f32x16 acc[C::KB][C::NB];
@@ -280,10 +288,9 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (__attribute__((address_space(3))) void*)(to.q + (me.cp_row0 + r) * Tile<D>::LD), 16, (int)off, 0, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rd, (__attribute__((address_space(3))) void*)(to.dout + (me.cp_row0 + r) * Tile<D>::LD), 16, (int)off, 0, 0, 0);
     }
-    const float* src = (wave == 0 ? g.lse_a : wave == 1 ? g.lse_b : wave == 2 ? g.nd1 : g.diff) + v_at + q0;
-    float* dst = wave == 0 ? to.lse_a : wave == 1 ? to.lse_b : wave == 2 ? to.nd1 : wave == 3 ? to.diff : sink;
-    const auto rs = make_rsrc(src, wave < 4 ? (uint32_t)n_rows * 4u : 0u);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)dst, 4, LaneWord::lane4(me.at.fresh()), 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(values + q0, (uint32_t)n_rows * value_bytes),
+                                             (__attribute__((address_space(3))) void*)(to.values + 64 * min(wave, 4)), 4,
+                                             LaneWord::lane4(me.at.fresh()), 0, 0, 0);
   };
   auto step_sync = [&]() {
     wait_async_loads();
@@ -291,17 +298,21 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
   };
   constexpr int AHEAD = 2;
   // x[kb] += tile rows (A, from LDS) x this wave's K or V rows, columns 16 FROM .. 16 TO
-  auto first_product = [&](auto from_tag, auto to_tag, const __bf16* tA, int rb, f32x16 (&x)[C::KB]) {
+  auto first_product = [&](auto from_tag, auto to_tag, const __bf16* tA, int rb, int w, f32x16 (&x)[C::KB]) {
     constexpr int FROM = decltype(from_tag)::value, TO = decltype(to_tag)::value;
-    bf16x8 af[C::KC];
+    bf16x8 af[C::KC], last[C::KB];
 #pragma unroll
     for (int cc = FROM; cc < FROM + AHEAD && cc < TO; ++cc) af[cc] = me.rows.get(tA, rb, cc);
     KNAP_SCHED_FENCE();
 #pragma unroll
     for (int cc = FROM; cc < TO; ++cc) {
 #pragma unroll
-      for (int kb = 0; kb < C::KB; ++kb) x[kb] = mfma32(af[cc], kvf[kb][cc], x[kb]);
+      for (int kb = 0; kb < C::KB; ++kb) x[kb] = mfma32(af[cc], cc < KEPT ? kvf[kb][cc < KEPT ? cc : 0] : last[kb], x[kb]);
       if (cc + AHEAD < TO) af[cc + AHEAD] = me.rows.get(tA, rb, cc + AHEAD);
+      if (cc + AHEAD == KEPT && cc + AHEAD < TO) {
+#pragma unroll
+        for (int kb = 0; kb < C::KB; ++kb) last[kb] = *parked(kb, w);
+      }
       KNAP_SCHED_FENCE();
     }
   };
@@ -310,13 +321,15 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
     constexpr int FROM = decltype(from_tag)::value, TO = decltype(to_tag)::value;
     bf16x8 bf[C::NB];
 #pragma unroll
-    for (int nb = FROM; nb < TO; ++nb) bf[nb] = me.cols.get(tB, cb, 16 * cq, nb);
+    for (int nb = FROM; nb < FROM + 2 && nb < TO; ++nb) bf[nb] = me.cols.get(tB, cb, 16 * cq, nb);
     KNAP_SCHED_FENCE();
 #pragma unroll
-    for (int nb = FROM; nb < TO; ++nb)
+    for (int nb = FROM; nb < TO; ++nb) {
 #pragma unroll
       for (int kb = 0; kb < C::KB; ++kb) acc[kb][nb] = mfma32(bf[nb], op[kb], acc[kb][nb]);
-    KNAP_SCHED_FENCE();
+      if (nb + 2 < TO) bf[nb + 2] = me.cols.get(tB, cb, 16 * cq, nb + 2);
+      KNAP_SCHED_FENCE();
+    }
   };
   constexpr std::integral_constant<int, 0> n0{};
   constexpr std::integral_constant<int, KH> kh{};
@@ -352,13 +365,13 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
     f32x16 s[C::KB];
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb) s[kb] = zero16();
-    first_product(n0, kh, at.q, rb, s);
+    first_product(n0, kh, at.q, rb, w, s);
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb)
 #pragma unroll
       for (int cq = 0; cq < 2; ++cq) {
         float p[8];
-        exps(s[kb], at.lse_a, cq, kb, p);
+        exps(s[kb], at.values, cq, kb, p);
         f16x8 x;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = (_Float16)p[e];
@@ -366,14 +379,14 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
       }
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb) s[kb] = zero16();
-    first_product(kh, kc, at.q, rb, s);
+    first_product(kh, kc, at.q, rb, w, s);
 #pragma unroll
     for (int cq = 0; cq < 2; ++cq) {
       bf16x8 pa[C::KB];
 #pragma unroll
       for (int kb = 0; kb < C::KB; ++kb) {
         float p[8];
-        exps(s[kb], at.lse_b, cq, kb, p);
+        exps(s[kb], at.values + 64, cq, kb, p);
         const f16x8 one = *p_at(w, t, 0, 2 * kb + cq);
         f16x8 x;
 #pragma unroll
@@ -386,18 +399,19 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
       second_product(n0, nb_all, at.dout, cb, cq, pa);
     }
   };
+  // (a product with an fp16 factor is one instruction as a fused one)
   auto dk_step = [&](int u, const DiffSlot& at) {
     const int rb = me.rows.fresh(), cb = me.cols.fresh(), w = me.at.fresh();
     f32x16 dp[C::KB];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(at.nd1) + LaneWord::hh16(w) + 32 * j);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(at.values + 128) + LaneWord::hh16(w) + 32 * j);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int kb = 0; kb < C::KB; ++kb) dp[kb][4 * j + e] = x[e];
     }
-    first_product(n0, kc, at.dout, rb, dp);
+    first_product(n0, kc, at.dout, rb, w, dp);
 #pragma unroll
     for (int cq = 0; cq < 2; ++cq) {
       bf16x8 da[C::KB];
@@ -405,16 +419,16 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
       for (int kb = 0; kb < C::KB; ++kb) {
         const f16x8 p = *p_at(w, u, 0, 2 * kb + cq);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) da[kb][e] = (__bf16)((float)p[e] * dp[kb][8 * cq + e]);
+        for (int e = 0; e < 8; ++e) da[kb][e] = (__bf16)__builtin_fmaf((float)p[e], dp[kb][8 * cq + e], 0.f);
       }
       second_product(n0, nh, at.q, cb, cq, da);
-      const char* row = reinterpret_cast<const char*>(at.diff + 16 * cq) + LaneWord::hh16(w);
+      const char* row = reinterpret_cast<const char*>(at.values + 192 + 16 * cq) + LaneWord::hh16(w);
       const f32x4 e0 = *reinterpret_cast<const f32x4*>(row), e1 = *reinterpret_cast<const f32x4*>(row + 32);
 #pragma unroll
       for (int kb = 0; kb < C::KB; ++kb) {
         const f16x8 p = *p_at(w, u, 1, 2 * kb + cq);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) da[kb][e] = (__bf16)((float)p[e] * (dp[kb][8 * cq + e] + (e < 4 ? e0[e & 3] : e1[e & 3])));
+        for (int e = 0; e < 8; ++e) da[kb][e] = (__bf16)__builtin_fmaf((float)p[e], dp[kb][8 * cq + e] + (e < 4 ? e0[e & 3] : e1[e & 3]), 0.f);
       }
       second_product(nh, nb_all, at.q, cb, cq, da);
     }
@@ -471,11 +485,11 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
 #define KNAP_RING(i)                                                                    \
   __shared__ __attribute__((aligned(1024))) __bf16 sQ##i[C::TILE_ELEMS];                \
   __shared__ __attribute__((aligned(1024))) __bf16 sdO##i[C::TILE_ELEMS];               \
-  __shared__ __attribute__((aligned(256))) float sLa##i[64], sLb##i[64], sNd##i[64], sDf##i[64];
+  __shared__ __attribute__((aligned(256))) float sValues##i[kDiffValues];
   KNAP_RING(0) KNAP_RING(1) KNAP_RING(2)
 #undef KNAP_RING
-  __shared__ __attribute__((aligned(256))) float sSink[64];
   __shared__ __attribute__((aligned(1024))) char sP[PAIRS * DiffLane<D, PAIRS>::P_PAIR];
+  __shared__ __attribute__((aligned(1024))) char sPark[D == 128 ? 2 * PAIRS * 2048 : 16];
   __shared__ int s_ticket;
 
   const int T = a.cu[a.n_seq];
@@ -486,7 +500,7 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
   const int role = (wave / PAIRS) ^ (PAIRS == 2 ? (int)(blockIdx.x * 2 / gridDim.x) & 1 : 0);
   DiffLane<D, PAIRS> me;
   me.init(lane, wave, role, (uint32_t)((size_t)a.H * D * sizeof(__bf16)));
-  const DiffSlot r0 = {sQ0, sdO0, sLa0, sLb0, sNd0, sDf0}, r1 = {sQ1, sdO1, sLa1, sLb1, sNd1, sDf1}, r2 = {sQ2, sdO2, sLa2, sLb2, sNd2, sDf2};
+  const DiffSlot r0 = {sQ0, sdO0, sValues0}, r1 = {sQ1, sdO1, sValues1}, r2 = {sQ2, sdO2, sValues2};
   ItemQueue<0> queue;
   queue.init(a.counters + 8, s_start, a.n_seq, n_items);
   for (int ticket = queue.first_ticket(); ticket < queue.wide;) {
@@ -496,7 +510,7 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
     unsigned next_ticket;      // thread 0 only
     if (tid == 0 && queue.draws) next_ticket = atomicAdd(queue.ctr, 1u);
     for (int sub = 0; sub < (CAUSAL && first != last ? 2 : 1); ++sub)
-      diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sSink, sP, me, it, head, sub == 0 ? first : last, T);
+      diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sP, sPark, me, it, head, sub == 0 ? first : last, T);
     if (!queue.draws) break;
     if (tid == 0) s_ticket = queue.later_ticket(next_ticket);
     lds_barrier();
