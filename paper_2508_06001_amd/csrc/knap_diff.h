@@ -56,4 +56,33 @@ struct DiffSoftmax {
   }
 };
 
+// Every XCD takes every eighth item of the list, in order, its workgroups by drawing from its counter (at zero before the launch).
+struct StridedQueue {
+  unsigned* ctr;
+  int q, n_q, per, wide;
+  bool draws;       // more tickets than workgroups: somebody has to draw
+  __device__ __forceinline__ void init(unsigned* counters, int n_items) {
+    n_q = (gridDim.x % 8 == 0) ? 8 : 1;
+    q = (int)(blockIdx.x % n_q);                  // workgroups go to the XCDs round-robin
+    per = (int)gridDim.x / n_q;
+    ctr = counters + q;
+    wide = __builtin_amdgcn_readfirstlane((n_items - q + n_q - 1) / n_q);
+    draws = wide > per;
+  }
+  __device__ __forceinline__ int first_ticket() const { return (int)blockIdx.x / n_q; }
+  __device__ __forceinline__ int later_ticket(unsigned drawn) const { return per + (int)drawn; }
+  __device__ __forceinline__ int item(int ticket) const { return q + ticket * n_q; }
+};
+
+// item w of a list that holds, for each sequence, its tiles of TILE rows in turn, and for each of them all heads
+template <int TILE>
+__device__ __forceinline__ WorkItem decode_tile_major(int w, const int32_t* __restrict__ cu, int n_seq, int H, const int* s_order, const int* s_start) {
+  const int r = rank_of_item(s_start, n_seq, w);
+  const int rem = w - __builtin_amdgcn_readfirstlane(s_start[r]);
+  WorkItem it = sequence_of_rank(r, cu, s_order);
+  it.tile = __builtin_amdgcn_readfirstlane(rem / H);
+  it.head = __builtin_amdgcn_readfirstlane(rem - it.tile * H);
+  return it;
+}
+
 }  // namespace knap

@@ -343,11 +343,10 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
   auto dv_step = [&](int t, const DiffSlot& at) {
     const int rb = me.rows.fresh(), cb = me.cols.fresh(), w = me.at.fresh();
     bool diag = false;
-    int first_seen[C::KB];
+    int first_seen = 0;      // of key block 0, 32 later of key block 1
     if constexpr (CAUSAL) {
       diag = n_tiles - 1 - t < C::BN / C::BM;
-#pragma unroll
-      for (int kb = 0; kb < C::KB; ++kb) first_seen[kb] = 64 * pair + 32 * kb + LaneWord::l32(w) - (n_tiles - 1 - t) * C::BM - LaneWord::hh16(w) / 4;
+      first_seen = 64 * pair + LaneWord::l32(w) - (n_tiles - 1 - t) * C::BM - LaneWord::hh16(w) / 4;
     }
     // P_m of chunk cq and key block kb: register e of half h is query 8 (2 cq + h) + 4 hh + e
     auto exps = [&](const f32x16& s, const float* lse, int cq, int kb, float (&p)[8]) {
@@ -358,7 +357,7 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           p[4 * h + e] = fast_exp2(__builtin_fmaf(s[8 * cq + 4 * h + e], c, -lq[e]));
-          if (CAUSAL && diag) p[4 * h + e] = 8 * (2 * cq + h) + e < first_seen[kb] ? 0.f : p[4 * h + e];
+          if (CAUSAL && diag) p[4 * h + e] = 8 * (2 * cq + h) + e - 32 * kb < first_seen ? 0.f : p[4 * h + e];
         }
       }
     };
@@ -493,7 +492,7 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
   __shared__ int s_ticket;
 
   const int T = a.cu[a.n_seq];
-  const int n_items = build_schedule<C::BN, C::THREADS, CAUSAL>(a.cu, a.n_seq, a.H, s_order, s_start, reinterpret_cast<int*>(&sP[0]));
+  const int n_items = build_schedule<C::BN, C::THREADS, false>(a.cu, a.n_seq, a.H, s_order, s_start, reinterpret_cast<int*>(&sP[0]));
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the two waves of a pair sit on one SIMD where there are four pairs; at two pairs the second half of the grid swaps roles
@@ -501,16 +500,13 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
   DiffLane<D, PAIRS> me;
   me.init(lane, wave, role, (uint32_t)((size_t)a.H * D * sizeof(__bf16)));
   const DiffSlot r0 = {sQ0, sdO0, sValues0}, r1 = {sQ1, sdO1, sValues1}, r2 = {sQ2, sdO2, sValues2};
-  ItemQueue<0> queue;
-  queue.init(a.counters + 8, s_start, a.n_seq, n_items);
+  StridedQueue queue;
+  queue.init(a.counters + 8, n_items);
   for (int ticket = queue.first_ticket(); ticket < queue.wide;) {
-    const WorkItem it = decode_item<C::BN, CAUSAL>(queue.item(ticket), a.cu, a.n_seq, s_order, s_start);
-    const int head = __builtin_amdgcn_readfirstlane(it.head), first = __builtin_amdgcn_readfirstlane(it.tile);
-    const int last = (it.len + C::BN - 1) / C::BN - 1 - first;      // CAUSAL: the pair of key tiles {first, last}
+    const WorkItem it = decode_tile_major<C::BN>(queue.item(ticket), a.cu, a.n_seq, a.H, s_order, s_start);
     unsigned next_ticket;      // thread 0 only
     if (tid == 0 && queue.draws) next_ticket = atomicAdd(queue.ctr, 1u);
-    for (int sub = 0; sub < (CAUSAL && first != last ? 2 : 1); ++sub)
-      diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sP, sPark, me, it, head, sub == 0 ? first : last, T);
+    diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sP, sPark, me, it, it.head, it.tile, T);
     if (!queue.draws) break;
     if (tid == 0) s_ticket = queue.later_ticket(next_ticket);
     lds_barrier();
