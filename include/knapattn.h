@@ -176,8 +176,8 @@ int knap_varlen_attn_causal_bwd(const void* q, const void* k, const void* v,
  * scale is applied to the products of d / 2 columns (1 / sqrt(d / 2) as a rule).
  *
  * Layouts, masks, supported sizes, alignment, errors, streams, concurrency and capture are
- * those of knap_varlen_attn_fwd / _bwd (forward calls of either kind take the same
- * counter sets in turn and count together).  Besides:
+ * those of knap_varlen_attn_fwd / _bwd.  Every one of these calls, the backward ones too,
+ * draws from a set of the forward's counters, and counts as one of its calls.  Besides:
  *   lambda   fp32[H], any sign; it is read on the device, so that a captured call follows it.
  *   out2     bf16 (T, H, d): O_2, which the backward takes; NULL in the forward where no backward
  *            follows.

@@ -359,11 +359,12 @@ int diff_bwd_impl(const void* q, const void* k, const void* v, const int32_t* cu
     const size_t part = round_up(static_cast<size_t>(total_tokens) * H * sizeof(float), 256);
     char* ws = static_cast<char*>(workspace);
     auto at = [&](int i) { return reinterpret_cast<float*>(ws + i * part); };
-    const knap::DiffBwdArgs a = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(k), static_cast<const __bf16*>(v),
+    knap::DiffBwdArgs a = {static_cast<const __bf16*>(q), static_cast<const __bf16*>(k), static_cast<const __bf16*>(v),
                                  static_cast<const __bf16*>(out), static_cast<const __bf16*>(out2), static_cast<const __bf16*>(dout), cu_seqlens,
                                  n_seq, H, scale, lambda, lse, static_cast<__bf16*>(dq), static_cast<__bf16*>(dk), static_cast<__bf16*>(dv),
-                                 dlambda, at(0), at(1), at(2), at(3), at(4), reinterpret_cast<unsigned*>(ws + 5 * part)};
-    e = knap::launch_diff_bwd(a, d, causal, (int)total_tokens, di->cus, static_cast<hipStream_t>(stream));
+                                 dlambda, at(0), at(1), at(2), at(3), at(4), reinterpret_cast<unsigned*>(ws + 5 * part), nullptr};
+    e = next_counters(di, stream, &a.dq_counters);
+    if (e == hipSuccess) e = knap::launch_diff_bwd(a, d, causal, di->cus, static_cast<hipStream_t>(stream));
   }
   if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
   return KNAP_OK;

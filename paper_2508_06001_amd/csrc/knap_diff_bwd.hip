@@ -5,12 +5,11 @@
 // one for both maps.  What is twice as much are the exponentials.  As there, dQ (by query tiles) and dK, dV (by key tiles) are kernels of
 // their own that keep their sums in registers, and nothing is added up across workgroups but dlambda.
 //
-//   diff_delta_kernel   D_1 = sum dout out + lambda D_2 and D_2 = sum dout out2 of every row, from the rounded outputs, which is as exact
-//                       as dS in bf16 can use; and the log-sums in base 2
-//   diff_dq_kernel      dQ, and D_2 again in 32 bits, as sum_j P_2 dP: what dlambda is summed from (dout times the rounded out2 is off
-//                       by 2^-9 a row, which a sum over rows of either sign does not average out against its own size)
-//   diff_dkdv_kernel    dK, dV
-//   diff_lambda_kernel  dlambda, one workgroup a head, in a fixed order
+//   diff_dq_kernel      on the way in D_1 = sum dout out + lambda D_2 and D_2 = sum dout out2 of every row, from the rounded outputs, which is
+//                       as exact as dS in bf16 can use, and the log-sums in base 2, both handed on in memory; dQ; and D_2 again in 32 bits,
+//                       as sum_j P_2 dP, for dlambda (dout times the rounded out2 is off by 2^-9 a row, which a sum over rows of either
+//                       sign does not average out against its own size)
+//   diff_dkdv_kernel    dK, dV; behind its items dlambda, one workgroup a head, in a fixed order
 // Probabilities are carried times 2^15 (the log-sums are stored that much smaller), which fp16 holds with 11 bits down to 2^-29: so
 // that the waves that form dK get them from the waves that form dV with no rounding worth counting.  The results' factors take it out.
 #include "knap_attn_dkdv.h"
@@ -24,53 +23,6 @@ constexpr float kDiffDown = 1.0f / 32768.f;
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-// 128 rows of one head; the D / 8 lanes of a row hold 8 columns each
-template <int D>
-__global__ __launch_bounds__(kThreads) void diff_delta_kernel(DiffBwdArgs a) {
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 16) a.counters[threadIdx.x] = 0u;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int t0 = blockIdx.x * 128, head = blockIdx.y, T = a.cu[a.n_seq], H = a.H;
-  if (t0 >= T) return;
-  const uint32_t row_bytes = (uint32_t)((size_t)H * D * sizeof(__bf16));
-  const size_t at = ((size_t)t0 * H + head) * D;
-  const uint32_t bytes = (uint32_t)min(T - t0, 128) * row_bytes;
-  const auto ro = make_rsrc(a.out + at, bytes), r2 = make_rsrc(a.out2 + at, bytes), rd = make_rsrc(a.dout + at, bytes);
-  constexpr int LANES = D / 8, ROWS = 64 / LANES, N = 32 / ROWS;      // lanes of a row, rows of a load, loads of a wave
-  const uint32_t off = (uint32_t)(wave * 32 + lane / LANES) * row_bytes + (uint32_t)(lane % LANES) * 16u;
-  const float lambda = a.lambda[head];
-  float d1 = 0.f, d2 = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t o = off + (uint32_t)(i * ROWS) * row_bytes;
-    const bf16x8 of = __builtin_bit_cast(bf16x8, buffer_load16(ro, o)), o2 = __builtin_bit_cast(bf16x8, buffer_load16(r2, o)),
-                 dof = __builtin_bit_cast(bf16x8, buffer_load16(rd, o));
-    float x = 0.f, y = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x = __builtin_fmaf((float)dof[e], (float)of[e], x);
-      y = __builtin_fmaf((float)dof[e], (float)o2[e], y);
-    }
-#pragma unroll
-    for (int s = 1; s < LANES; s <<= 1) {
-      x += __shfl_xor(x, s, 64);
-      y += __shfl_xor(y, s, 64);
-    }
-    if (lane % LANES == i) {                // row ROWS i + lane / LANES of the wave's 32, kept by lane i of its row
-      d1 = x;
-      d2 = y;
-    }
-  }
-  const int t = t0 + wave * 32 + ROWS * (lane % LANES) + lane / LANES;
-  if (lane % LANES < N && t < T) {
-    const size_t row_at = (size_t)head * T + t, second = (size_t)H * T;
-    d1 = __builtin_fmaf(lambda, d2, d1);
-    a.nd1[row_at] = -d1;
-    a.diff[row_at] = d1 - d2;
-    a.lse_a[row_at] = __builtin_fmaf(a.lse[row_at], kLog2e, -kDiffUp);
-    a.lse_b[row_at] = __builtin_fmaf(a.lse[second + row_at], kLog2e, -kDiffUp);
-  }
-}
 
 // dQ: the forward's structure.  S_m^T = K_m Q_m^T and dP^T = V dO^T put one query in each lane; dS_m^T is, unchanged, the operand of
 // dQ_m^T += K_m^T dS_m^T with K^T read transposed from LDS.
@@ -88,7 +40,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
   static_assert(sizeof(__bf16) * C::TILE_ELEMS >= sizeof(int) * kThreads, "scan scratch must fit in a tile");
 
   const int T = a.cu[a.n_seq], H = a.H;
-  const int n_items = build_schedule<C::BM, kThreads, CAUSAL>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
+  build_schedule<C::BM, kThreads, CAUSAL>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float c = a.scale * kLog2e;
@@ -98,11 +50,15 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
   ColReader<D> cols;
   rows.init(lane);
   cols.init(lane);
-  ItemQueue<0> queue;
-  queue.init(a.counters, s_start, a.n_seq, n_items);
+  if (blockIdx.x == 0 && tid < 8) a.counters[tid] = 0u;      // of the launch behind this one
+  EvenQueue<0, 1> queue;
+  queue.init(a.dq_counters);
+  if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
+  __syncthreads();
+  deal_even<C::BM, CAUSAL>(queue, a.cu, a.n_seq, s_order, s_start);
   int ticket = queue.first_ticket();
   while (ticket < queue.wide) {
-    const WorkItem it = decode_item<C::BM, CAUSAL>(queue.item(ticket), a.cu, a.n_seq, s_order, s_start);
+    const WorkItem it = decode_even<C::BM, CAUSAL>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
     const int L = it.len, head = __builtin_amdgcn_readfirstlane(it.head);
     const int other = (L + C::BM - 1) / C::BM - 1 - it.tile;
     const float lambda = a.lambda[head];
@@ -125,27 +81,48 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
       const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
       const uint32_t off = (uint32_t)(32 * wave + l32) * row_bytes + (uint32_t)(16 * hh);
       const size_t row_at = (size_t)head * T + it.row0 + (q_valid ? q_row : 0);
-      const float nd1 = a.nd1[row_at], nd2 = nd1 + a.diff[row_at];
+      const size_t second = (size_t)H * T;
+      const float own_a = __builtin_fmaf(a.lse[row_at], kLog2e, -kDiffUp), own_b = __builtin_fmaf(a.lse[second + row_at], kLog2e, -kDiffUp);
       // +inf for rows past the end: P = 0
-      const float lse_a = q_valid ? a.lse_a[row_at] : INFINITY, lse_b = q_valid ? a.lse_b[row_at] : INFINITY;
+      const float lse_a = q_valid ? own_a : INFINITY, lse_b = q_valid ? own_b : INFINITY;
+      // One tensor after the other (knap_attn_dq.h).  The lane holds half of its query's columns, its partner at lane ^ 32 the other half.
       bf16x8 qf[C::KC], dof[C::KC];
+      float nd1, nd2;
       {
         const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
         const auto rd = make_rsrc(a.dout + seq_at + (size_t)q0 * row_stride, rows_bytes);
+        const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
+        const auto r2 = make_rsrc(a.out2 + seq_at + (size_t)q0 * row_stride, rows_bytes);
+        bf16x8 of[C::KC], o2[C::KC];
 #pragma unroll
         for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
         KNAP_SCHED_FENCE();
 #pragma unroll
         for (int cc = 0; cc < C::KC; ++cc) dof[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rd, off + 32u * cc));
         KNAP_SCHED_FENCE();
+#pragma unroll
+        for (int cc = 0; cc < C::KC; ++cc) of[cc] = __builtin_bit_cast(bf16x8, buffer_load16(ro, off + 32u * cc));
+        KNAP_SCHED_FENCE();
+#pragma unroll
+        for (int cc = 0; cc < C::KC; ++cc) o2[cc] = __builtin_bit_cast(bf16x8, buffer_load16(r2, off + 32u * cc));
+        KNAP_SCHED_FENCE();
+        load_tile(0, sK0, sV0);
+        KNAP_SCHED_FENCE();
+        const float d2_rounded = row_delta<D>(dof, o2);
+        nd1 = -__builtin_fmaf(lambda, d2_rounded, row_delta<D>(dof, of));
+        nd2 = -d2_rounded;
       }
-      load_tile(0, sK0, sV0);
       f32x16 acc[C::DB];
 #pragma unroll
       for (int db = 0; db < C::DB; ++db) acc[db] = zero16();
       float d2 = 0.f;
       wait_async_loads();
-      if (sub == 0 && queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
+      if (q_valid && hh == 0) {     // for the dK/dV kernel, behind the wait, which would wait for these stores as well
+        a.nd1[row_at] = nd1;
+        a.diff[row_at] = nd2 - nd1;
+        a.lse_a[row_at] = own_a;
+        a.lse_b[row_at] = own_b;
+      }
       lds_barrier();
 
       auto tile = [&](int t, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) {
@@ -188,6 +165,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
         tile(t, sK0, sV0, sK1, sV1);
         if (t + 1 < n_tiles) tile(t + 1, sK1, sV1, sK0, sV0);
       }
+      if (sub == 0 && queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
       d2 += xor32(d2);
       if (q_valid && hh == 0) a.d2[row_at] = d2 * kDiffDown;
       const auto rg = make_rsrc(a.dq + seq_at + (size_t)q0 * row_stride, rows_bytes);
@@ -196,7 +174,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
         store_block(rg, off + 64u * db, acc[db], db < C::DB / 2 ? a.scale * kDiffDown : -lambda * a.scale * kDiffDown);
     }
     if (!queue.draws) return;
-    if (tid == 0) s_ticket = queue.later_ticket(next_ticket);
+    if (tid == 0) s_ticket = drawn_ticket(queue, next_ticket);
     lds_barrier();
     ticket = __builtin_amdgcn_readfirstlane(s_ticket);
     lds_barrier();        // everyone has the ticket before the next one is put down
@@ -475,6 +453,25 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
   }
 }
 
+// dlambda of a head: minus the sum of its rows' D_2, by one workgroup
+template <int THREADS>
+__device__ __forceinline__ void diff_lambda(const DiffBwdArgs& a, int head, int T, float* s_sum) {
+  const float* row = a.d2 + (size_t)head * T;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int t = threadIdx.x; t < T; t += THREADS) sum += row[t];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = 0.f;
+    for (int w = 0; w < THREADS / 64; ++w) sum += s_sum[w];
+    a.dlambda[head] = -sum;
+  }
+  __syncthreads();
+}
+
 template <int D, int PAIRS, bool CAUSAL>
 __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a) {
   using C = Bwd2Cfg<D, PAIRS>;
@@ -501,7 +498,7 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
   me.init(lane, wave, role, (uint32_t)((size_t)a.H * D * sizeof(__bf16)));
   const DiffSlot r0 = {sQ0, sdO0, sValues0}, r1 = {sQ1, sdO1, sValues1}, r2 = {sQ2, sdO2, sValues2};
   StridedQueue queue;
-  queue.init(a.counters + 8, n_items);
+  queue.init(a.counters, n_items);
   for (int ticket = queue.first_ticket(); ticket < queue.wide;) {
     const WorkItem it = decode_tile_major<C::BN>(queue.item(ticket), a.cu, a.n_seq, a.H, s_order, s_start);
     unsigned next_ticket;      // thread 0 only
@@ -512,46 +509,25 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
     lds_barrier();
     ticket = __builtin_amdgcn_readfirstlane(s_ticket);
     lds_barrier();        // everyone has the ticket before the next one is put down
-  }
-}
-
-// dlambda of a head: minus the sum of its rows' D_2
-__global__ __launch_bounds__(1024) void diff_lambda_kernel(DiffBwdArgs a) {
-  __shared__ float s_sum[16];
-  const int T = a.cu[a.n_seq];
-  const float* row = a.d2 + (size_t)blockIdx.x * T;
-  float sum = 0.f;
-#pragma unroll 8
-  for (int t = threadIdx.x; t < T; t += 1024) sum += row[t];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
-  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+  }  // the workgroups from the last one on, which have the cheapest items or none
   __syncthreads();
-  if (threadIdx.x == 0) {
-    sum = 0.f;
-    for (int w = 0; w < 16; ++w) sum += s_sum[w];
-    a.dlambda[blockIdx.x] = -sum;
-  }
+  for (int head = (int)(gridDim.x - 1 - blockIdx.x); head < a.H; head += (int)gridDim.x) diff_lambda<C::THREADS>(a, head, T, reinterpret_cast<float*>(&sP[0]));
 }
 
 template <int D, bool CAUSAL>
-static hipError_t launch_diff_bwd_t(const DiffBwdArgs& a, int tokens, int cus, hipStream_t stream) {
+static hipError_t launch_diff_bwd_t(const DiffBwdArgs& a, int cus, hipStream_t stream) {
   constexpr int PAIRS = D == 128 ? 4 : 2;
   const size_t dyn = (size_t)(2 * a.n_seq + 1) * sizeof(int);
-  hipLaunchKernelGGL(diff_delta_kernel<D>, dim3((tokens + 127) / 128, a.H), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((diff_dq_kernel<D, CAUSAL>), dim3(2 * cus), dim3(kThreads), dyn, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((diff_dq_kernel<D, CAUSAL>), dim3(2 * cus), dim3(kThreads), dyn, stream, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL((diff_dkdv_kernel<D, PAIRS, CAUSAL>), dim3(cus * 4 / PAIRS), dim3(128 * PAIRS), dyn, stream, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(diff_lambda_kernel, dim3(a.H), dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
 
-hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int tokens, int cus, hipStream_t stream) {
-  if (d == 64) return causal ? launch_diff_bwd_t<64, true>(a, tokens, cus, stream) : launch_diff_bwd_t<64, false>(a, tokens, cus, stream);
-  return causal ? launch_diff_bwd_t<128, true>(a, tokens, cus, stream) : launch_diff_bwd_t<128, false>(a, tokens, cus, stream);
+hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int cus, hipStream_t stream) {
+  if (d == 64) return causal ? launch_diff_bwd_t<64, true>(a, cus, stream) : launch_diff_bwd_t<64, false>(a, cus, stream);
+  return causal ? launch_diff_bwd_t<128, true>(a, cus, stream) : launch_diff_bwd_t<128, false>(a, cus, stream);
 }
 
 }  // namespace knap

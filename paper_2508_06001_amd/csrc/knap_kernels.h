@@ -70,10 +70,11 @@ struct DiffBwdArgs {
   __bf16 *dq, *dk, *dv;
   float* dlambda;
   float *nd1, *diff, *lse_a, *lse_b, *d2;      // (H, T) each: -D_1, D_1 - D_2, the log-sums in base 2 less 15, D_2 in 32 bits
-  unsigned* counters;                          // 8 for the dQ kernel, 8 for the dK/dV kernel; the launch clears them
+  unsigned* counters;                          // 8 for the dK/dV kernel, which the dQ kernel clears
+  unsigned* dq_counters;                       // a set of the forward's, at zero
 };
 hipError_t launch_diff_fwd(const DiffFwdArgs& a, int d, bool causal, int cus, hipStream_t stream);
-hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int tokens, int cus, hipStream_t stream);
+hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int cus, hipStream_t stream);
 
 // Rotary positions: everything but the launch geometry comes from the caller
 struct RopeArgs {

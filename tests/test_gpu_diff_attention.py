@@ -205,6 +205,27 @@ def test_same_bits_without_a_backward_captured_and_beside_each_other(causal):
 @pytest.mark.gpu
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("d", [64, 128])
+def test_more_items_than_workgroups_whatever_the_workspace_holds(d, causal):
+    """Bags whose items are drawn from counters, by either kernel of the backward: the same bits whatever the workspace held, and right
+    in a head that comes late in every list."""
+    import torch
+    import paper_2508_06001_amd as K
+    run = Run([700, 130, 257, 512, 1, 333, 900, 64] * 4, 24, d, causal, seed=17)
+    run.check(heads=[23])
+    attn = K.VarlenDiffAttention(run.cu, 24, d, run.scale, run.lam, causal=causal)
+    x = run.x
+    for fill in (0, 1, 0x7f, 0xff):
+        attn.workspace.fill_(fill)
+        attn.forward(x["q"], x["k"], x["v"])
+        got = dict(zip(("dq", "dk", "dv", "dlam"), attn.backward(x["q"], x["k"], x["v"], x["dout"])))
+        torch.cuda.synchronize()
+        for n, t in got.items():
+            assert torch.equal(t, run.y[n][:run.T] if n != "dlam" else run.y[n]), (fill, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
 def test_the_operators_together(d, causal):
     """A differential attention layer as a model has it: layer norm of the rows, rotary positions of both maps, the attention, layer norm of every
     head's row; the gradients go the way back.  Against the same chain in 64 bits.  Each of the up to six bf16 tensors on the way is rounded
