@@ -327,28 +327,37 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
       first_seen = 64 * pair + LaneWord::l32(w) - (n_tiles - 1 - t) * C::BM - LaneWord::hh16(w) / 4;
     }
     // P_m of chunk cq and key block kb: register e of half h is query 8 (2 cq + h) + 4 hh + e
-    auto exps = [&](const f32x16& s, const float* lse, int cq, int kb, float (&p)[8]) {
+    auto exps = [&](const f32x16& s, const float* lse, int cq, float (&p)[8]) {
       const char* row = reinterpret_cast<const char*>(lse + 16 * cq) + LaneWord::hh16(w);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const f32x4 lq = *reinterpret_cast<const f32x4*>(row + 32 * h);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[4 * h + e] = fast_exp2(__builtin_fmaf(s[8 * cq + 4 * h + e], c, -lq[e]));
-          if (CAUSAL && diag) p[4 * h + e] = 8 * (2 * cq + h) + e - 32 * kb < first_seen ? 0.f : p[4 * h + e];
-        }
+        for (int e = 0; e < 4; ++e) p[4 * h + e] = fast_exp2(__builtin_fmaf(s[8 * cq + 4 * h + e], c, -lq[e]));
       }
     };
     f32x16 s[C::KB];
+    // scores of queries before this lane's key are -inf: in one branch, not one for each probability
+    auto mask = [&]() __attribute__((always_inline)) {
+      if constexpr (CAUSAL) {
+        if (diag) {
+#pragma unroll
+          for (int kb = 0; kb < C::KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kb][r] = 8 * (r >> 2) + (r & 3) - 32 * kb < first_seen ? -INFINITY : s[kb][r];
+        }
+      }
+    };
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb) s[kb] = zero16();
     first_product(n0, kh, at.q, rb, w, s);
+    mask();
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb)
 #pragma unroll
       for (int cq = 0; cq < 2; ++cq) {
         float p[8];
-        exps(s[kb], at.values, cq, kb, p);
+        exps(s[kb], at.values, cq, p);
         f16x8 x;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = (_Float16)p[e];
@@ -357,13 +366,14 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
 #pragma unroll
     for (int kb = 0; kb < C::KB; ++kb) s[kb] = zero16();
     first_product(kh, kc, at.q, rb, w, s);
+    mask();
 #pragma unroll
     for (int cq = 0; cq < 2; ++cq) {
       bf16x8 pa[C::KB];
 #pragma unroll
       for (int kb = 0; kb < C::KB; ++kb) {
         float p[8];
-        exps(s[kb], at.values + 64, cq, kb, p);
+        exps(s[kb], at.values + 64, cq, p);
         const f16x8 one = *p_at(w, t, 0, 2 * kb + cq);
         f16x8 x;
 #pragma unroll
