@@ -125,12 +125,15 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
       }
       lds_barrier();
 
-      auto tile = [&](int t, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) {
+      // MASKED: a tile that crosses the sequence's end or the diagonal.  Keys that a query does not see score -inf: rows past the end
+      // arrive as zeros, and exp2(-log-sum) of a score of zero may be infinite.  Halves that none of the wave's queries sees are left out.
+      auto tile = [&](auto masked_tag, int t, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked_tag)::value;
         load_tile(t + 1, nK, nV);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const int k0 = t * C::BN + 32 * half;
-          if (k0 >= kv_end || (CAUSAL && k0 > q0 + 32 * wave + 31)) break;
+          if (MASKED && (k0 >= kv_end || (CAUSAL && k0 > q0 + 32 * wave + 31))) break;
           f32x16 dp = zero16();
 #pragma unroll
           for (int cc = 0; cc < C::KC; ++cc) dp = mfma32(rows.get(tV, 32 * half, cc), dof[cc], dp);
@@ -139,9 +142,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
             f32x16 s = zero16();
 #pragma unroll
             for (int cc = 0; cc < C::KC / 2; ++cc) s = mfma32(rows.get(tK, 32 * half, m * C::KC / 2 + cc), qf[m * C::KC / 2 + cc], s);
-            // keys that this query does not see score -inf: rows past the end arrive as zeros, and exp2(-log-sum) of a score of zero may
-            // be infinite
-            if (t >= first_masked) mask_half(s, kv_lim - k0, hh);
+            if constexpr (MASKED) mask_half(s, kv_lim - k0, hh);
             float ds[16];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -161,9 +162,15 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
         wait_async_loads();
         lds_barrier();
       };
-      for (int t = 0; t < n_tiles; t += 2) {
-        tile(t, sK0, sV0, sK1, sV1);
-        if (t + 1 < n_tiles) tile(t + 1, sK1, sV1, sK0, sV0);
+      // (an even number of tiles in front of the masked ones under the mask, any otherwise)
+      const int n_plain = min(n_tiles, first_masked);
+      for (int t = 0; t < n_plain; t += 2) {
+        tile(std::false_type{}, t, sK0, sV0, sK1, sV1);
+        if (t + 1 < n_plain) tile(std::false_type{}, t + 1, sK1, sV1, sK0, sV0);
+      }
+      for (int t = n_plain; t < n_tiles; ++t) {
+        const bool odd = t & 1;
+        tile(std::true_type{}, t, odd ? sK1 : sK0, odd ? sV1 : sV0, odd ? sK0 : sK1, odd ? sV0 : sV1);
       }
       if (sub == 0 && queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
       d2 += xor32(d2);
