@@ -20,25 +20,11 @@ struct DiffCfg {
 struct DiffSoftmax {
   float m_ref = -INFINITY, mc = -INFINITY, l = 0.f;
 
-  static __device__ __forceinline__ float exps(const f32x16& s, float c, float mc, bf16x8 (&pb)[2]) {
-    float p[16], sum = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      p[r] = fast_exp2(__builtin_fmaf(s[r], c, -mc));
-      sum += p[r];
-    }
-#pragma unroll
-    for (int ck = 0; ck < 2; ++ck) {
-      const int r0 = 8 * ck;
-      pb[ck] = pack8(p[r0], p[r0 + 1], p[r0 + 2], p[r0 + 3], p[r0 + 4], p[r0 + 5], p[r0 + 6], p[r0 + 7]);
-    }
-    return sum;
-  }
-
+  // takes in the half whose probabilities sum to `sum` in this lane
   template <int DB>
-  __device__ __forceinline__ void step(const f32x16& s, float c, bf16x8 (&pb)[2], f32x16 (&o)[DB], int hh) {
-    float sum = exps(s, c, mc, pb);
-    if (__builtin_amdgcn_ballot_w64(!(sum <= kMaxHalfSum)) != 0) {
+  __device__ __forceinline__ void settle(const f32x16& s, float c, float sum, bf16x8 (&pb)[2], f32x16 (&o)[DB], int hh) {
+    const bool moves = __builtin_amdgcn_ballot_w64(!(sum <= kMaxHalfSum)) != 0;
+    if (__builtin_expect(moves, 0)) {
       const float m_loc = half_max(s, 64, hh);
       const float m_new = fmaxf(m_ref, fmaxf(m_loc, xor32(m_loc)));
       const float alpha = m_new == m_ref ? 1.f : fast_exp2((m_ref - m_new) * c);
@@ -49,10 +35,17 @@ struct DiffSoftmax {
       for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
-      sum = exps(s, c, mc, pb);
+      sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = fast_exp2(__builtin_fmaf(s[r], c, -mc));
+        sum += p;
+        pb[r >> 3][r & 7] = (__bf16)p;
+      }
       if (m_new == -INFINITY) mc = -INFINITY;      // scores of -inf alone set no reference: the next half has to settle too
     }
     l += sum;
+    KNAP_SCHED_FENCE();
   }
 };
 

@@ -3,9 +3,8 @@
 // where q_1, k_1 are the first d / 2 columns of a head's rows and q_2, k_2 the others.
 //
 // The structure is that of the forward of plain attention (knap_attn_fwd.hip): S_m^T = K_m Q_m^T with one query per lane, P_m^T as it
-// comes out of that, packed, as the operand of O_m^T += V^T P_m^T, tiles of 64 keys through LDS, two buffers each.  Both maps are formed in
-// one pass: the score products are as many as plain attention's (two halves of the columns), a fragment of V read from LDS feeds both
-// maps' products, and nothing is formed twice.  6 L^2 d flops in all where four calls of plain attention (two maps, two halves of the values)
+// comes out of that, packed, as the operand of O_m^T += V^T P_m^T, the keys through LDS, two buffers each.  Both maps are formed in
+// one pass: the score products are as many as plain attention's (two halves of the columns), and nothing is formed twice.  6 L^2 d flops in all where four calls of plain attention (two maps, two halves of the values)
 // would take 8.
 //
 // Row sums are taken over the probabilities as they are, in 32 bits, not over what is left of them in bf16: the log-sum is then as exact
@@ -14,18 +13,24 @@
 
 namespace knap {
 
+// The keys go through in halves of 32.  A stage is a half and a map; three stages that follow each other are in work at a time, in one slot of
+// the pipeline: the scores of the last one, the probabilities of the middle one, the product with the values of the first one.  No
+// product of a slot waits for its arithmetic, nor the other way round; the stage whose sums a moving reference rescales is of the other
+// map than the one whose products run.  K runs half a tile ahead of V: a turn (two slots, one barrier) reads the keys of half h + 1 and
+// the values of half h, while the keys of h + 2 and the values of h + 1 are copied.
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   using C = DiffCfg<D>;
+  constexpr int KH = C::KC / 2, DB = C::DB, ROWS = 32, TILE = ROWS * Tile<D>::LD;
   extern __shared__ int s_dyn[];
   int* s_order = s_dyn;
   int* s_start = s_dyn + a.n_seq;
-  __shared__ __attribute__((aligned(1024))) __bf16 sK0[C::TILE_ELEMS];
-  __shared__ __attribute__((aligned(1024))) __bf16 sK1[C::TILE_ELEMS];
-  __shared__ __attribute__((aligned(1024))) __bf16 sV0[C::TILE_ELEMS];
-  __shared__ __attribute__((aligned(1024))) __bf16 sV1[C::TILE_ELEMS];
+  __shared__ __attribute__((aligned(1024))) __bf16 sK0[TILE];
+  __shared__ __attribute__((aligned(1024))) __bf16 sK1[TILE];
+  __shared__ __attribute__((aligned(1024))) __bf16 sV0[TILE];
+  __shared__ __attribute__((aligned(1024))) __bf16 sV1[TILE];
   __shared__ int s_ticket;
-  static_assert(sizeof(__bf16) * C::TILE_ELEMS >= sizeof(int) * kThreads, "scan scratch must fit in a tile");
+  static_assert(sizeof(__bf16) * TILE >= sizeof(int) * kThreads, "scan scratch must fit in a tile");
 
   const int T = a.cu[a.n_seq], H = a.H;
   build_schedule<C::BM, kThreads, CAUSAL>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
@@ -34,8 +39,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   const float c = a.scale * kLog2e;
   const size_t row_stride = (size_t)H * D;
   const uint32_t row_bytes = (uint32_t)(row_stride * sizeof(__bf16));
-  RowReader<D> k_rows;
-  ColReader<D> v_cols;
+  RowReaderX<D> k_rows;
+  ColReaderX<D> v_cols;
   k_rows.init(lane);
   v_cols.init(lane);
   EvenQueue<0, 1> queue;
@@ -53,19 +58,19 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
     unsigned next_ticket;      // thread 0 only
     for (int sub = 0; sub < (CAUSAL && it.tile != other ? 2 : 1); ++sub) {
       const int q_tile = __builtin_amdgcn_readfirstlane(!CAUSAL ? it.tile : sub == 0 ? other : it.tile);
-      const int q0 = q_tile * C::BM, q_row = q0 + 32 * wave + l32;
+      const int q0 = q_tile * C::BM;
       const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
-      const int n_tiles = (kv_end + C::BN - 1) / C::BN;
-      const int first_masked = CAUSAL ? 2 * q_tile : L / C::BN;
-      const int kv_lim = CAUSAL ? q_row + 1 : L;
+      const int n_half = (kv_end + ROWS - 1) / ROWS;
+      // halves that this wave's queries see, none where its rows lie past the end: it then only copies; the last one is masked under the
+      // mask (its diagonal) and where the sequence ends in it
+      const int n_own = q0 + 32 * wave >= L ? 0 : CAUSAL ? min(n_half, q0 / ROWS + wave + 1) : n_half;
       const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
-      auto load_tile = [&](int t, __bf16* dK, __bf16* dV) {
-        const int kv0 = t * C::BN;
-        const uint32_t bytes = (uint32_t)max(0, min(kv_end - kv0, C::BN)) * row_bytes;
-        tile_load_async<D>(dK, make_rsrc(a.k + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, C::BN, wave, lane);
-        tile_load_async<D>(dV, make_rsrc(a.v + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, C::BN, wave, lane);
+      auto copy = [&](const __bf16* src, int h, __bf16* dst) __attribute__((always_inline)) {
+        const int kv0 = h * ROWS;
+        const uint32_t bytes = (uint32_t)max(0, min(kv_end - kv0, ROWS)) * row_bytes;
+        tile_load_async<D>(dst, make_rsrc(src + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, ROWS, wave, lane);
       };
-      load_tile(0, sK0, sV0);       // a barrier stands between the last reads of the buffers and this
+      copy(a.k, 0, sK0);       // a barrier stands between the last reads of the buffers and this
       const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
       const uint32_t off = (uint32_t)(32 * wave + l32) * row_bytes + (uint32_t)(16 * hh);
       bf16x8 qf[C::KC];
@@ -74,45 +79,139 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
 #pragma unroll
         for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
       }
-      f32x16 o[2][C::DB];
+      f32x16 o[2][DB];
       DiffSoftmax st[2];
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int db = 0; db < C::DB; ++db) o[m][db] = zero16();
+        for (int db = 0; db < DB; ++db) o[m][db] = zero16();
       wait_async_loads();
       lds_barrier();
+      copy(a.v, 0, sV0);
+      copy(a.k, 1, sK1);
 
-      auto tile = [&](int t, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) {
-        load_tile(t + 1, nK, nV);
+      bf16x8 ak[KH];
+      auto keys = [&](const __bf16* tK, int kb, int m, int i) __attribute__((always_inline)) { ak[i] = k_rows.get(tK, kb, m * KH + i); };
+      // One slot: the scores sn of map NEXT (QK: its keys in `ak`), the probabilities pn of scores s against map NOW's reference (PR), the
+      // product of map NEXT's probabilities pb with the values tV (PV).  Groups of a product each, fences between them, so that the order
+      // below is the order issued; `behind(i)` goes into the groups of the second product.
+      auto slot = [&](auto qk_tag, auto pr_tag, auto pv_tag, auto next_tag, const f32x16& s, f32x16& sn, const bf16x8 (&pb)[2], bf16x8 (&pn)[2],
+                      const __bf16* tV, int vb, float& sum, auto behind) __attribute__((always_inline)) {
+        constexpr bool QK = decltype(qk_tag)::value, PR = decltype(pr_tag)::value, PV = decltype(pv_tag)::value;
+        constexpr int NEXT = decltype(next_tag)::value, NOW = 1 - NEXT;
+        constexpr int GROUPS = (QK ? KH : 0) + (PV ? 2 * DB : 0), PER = PR ? (16 + GROUPS - 1) / GROUPS : 0;
+        const float mc = st[NOW].mc;
+        float p[16];
+        int r = 0;
+        auto form = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int k0 = t * C::BN + 32 * half;
-          if (k0 >= kv_end || (CAUSAL && k0 > q0 + 32 * wave + 31)) break;
-          bf16x8 pb[2][2];
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            f32x16 s = zero16();
-#pragma unroll
-            for (int cc = 0; cc < C::KC / 2; ++cc) s = mfma32(k_rows.get(tK, 32 * half, m * C::KC / 2 + cc), qf[m * C::KC / 2 + cc], s);
-            if (t >= first_masked) mask_half(s, kv_lim - k0, hh);
-            st[m].template step<C::DB>(s, c, pb[m], o[m], hh);
-          }
-#pragma unroll
-          for (int ck = 0; ck < 2; ++ck)
-#pragma unroll
-            for (int db = 0; db < C::DB; ++db) {
-              const bf16x8 vt = v_cols.get(tV, 32 * half + 16 * ck, db);
-              o[0][db] = mfma32(vt, pb[0][ck], o[0][db]);
-              o[1][db] = mfma32(vt, pb[1][ck], o[1][db]);
+          for (int e = 0; e < PER; ++e) {
+            if (r < 16) {
+              p[r] = fast_exp2(__builtin_fmaf(s[r], c, -mc));
+              sum += p[r];
+              pn[r >> 3][r & 7] = (__bf16)p[r];
             }
+            ++r;
+          }
+        };
+        bf16x8 vt[2 * DB];
+        auto value = [&](int j) __attribute__((always_inline)) { vt[j] = v_cols.get(tV, vb, 16 * (j / DB), j % DB); };
+        sum = 0.f;
+        if constexpr (PV && !QK) { value(0); value(1); KNAP_SCHED_FENCE(); }
+        if constexpr (QK) {
+#pragma unroll
+          for (int i = 0; i < KH; ++i) {
+            sn = mfma32(ak[i], qf[NEXT * KH + i], i == 0 ? zero16() : sn);
+            if (PV && i >= KH - 2) value(i - (KH - 2));
+            form();
+            KNAP_SCHED_FENCE();
+          }
         }
+        if constexpr (PV) {
+#pragma unroll
+          for (int j = 0; j < 2 * DB; ++j) {
+            o[NEXT][j % DB] = mfma32(vt[j], pb[j / DB], o[NEXT][j % DB]);
+            if (j + 2 < 2 * DB) value(j + 2);
+            behind(j);
+            form();
+            KNAP_SCHED_FENCE();
+          }
+        }
+      };
+      constexpr std::true_type yes{};
+      constexpr std::false_type no{};
+      constexpr std::integral_constant<int, 0> map0{};
+      constexpr std::integral_constant<int, 1> map1{};
+      f32x16 s0, s1;            // scores of the maps
+      bf16x8 pb0[2], pb1[2];    // their probabilities
+      auto nothing = [](int) {};
+      const bool masked = CAUSAL || (n_own == n_half && kv_end % ROWS != 0);
+      const int kv_lim = CAUSAL ? q0 + 32 * wave + l32 + 1 : L;
+      auto mask = [&](f32x16& s, int h) __attribute__((always_inline)) {
+        if (masked && h == n_own - 1) mask_half(s, kv_lim - h * ROWS, hh);
+        KNAP_SCHED_FENCE();
+      };
+      if (n_own > 0) {
+        float sum;
+        {
+          const int kb = k_rows.fresh();
+#pragma unroll
+          for (int i = 0; i < KH; ++i) keys(sK0, kb, 0, i);
+#pragma unroll
+          for (int i = 0; i < KH; ++i) s0 = mfma32(ak[i], qf[i], i == 0 ? zero16() : s0);
+#pragma unroll
+          for (int i = 0; i < KH; ++i) keys(sK0, kb, 1, i);
+        }
+        mask(s0, 0);
+        slot(yes, yes, no, map1, s0, s1, pb1, pb0, sV0, 0, sum, nothing);
+        st[0].template settle<DB>(s0, c, sum, pb0, o[0], hh);
+        mask(s1, 0);
+      }
+      // the second map of half h and the first of half h + 1 go through the softmax
+      auto turn = [&](int h, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) __attribute__((always_inline)) {
         wait_async_loads();
         lds_barrier();
+        const int kb = k_rows.fresh(), vb = v_cols.fresh();
+#pragma unroll
+        for (int i = 0; i < KH; ++i) keys(tK, kb, 0, i);
+        copy(a.k, h + 2, nK);
+        copy(a.v, h + 1, nV);
+        float sum;
+        slot(yes, yes, yes, map0, s1, s0, pb0, pb1, tV, vb, sum, [&](int j) __attribute__((always_inline)) { if (j >= 2 * DB - KH) keys(tK, kb, 1, j - (2 * DB - KH)); });
+        st[1].template settle<DB>(s1, c, sum, pb1, o[1], hh);
+        mask(s0, h + 1);
+        slot(yes, yes, yes, map1, s0, s1, pb1, pb0, tV, vb, sum, nothing);
+        st[0].template settle<DB>(s0, c, sum, pb0, o[0], hh);
+        mask(s1, h + 1);
       };
-      for (int t = 0; t < n_tiles; t += 2) {
-        tile(t, sK0, sV0, sK1, sV1);
-        if (t + 1 < n_tiles) tile(t + 1, sK1, sV1, sK0, sV0);
+      int h = 0;
+      for (; h < n_own - 1; h += 2) {
+        turn(h, sK1, sV0, sK0, sV1);
+        if (h + 2 < n_own) turn(h + 1, sK0, sV1, sK1, sV0);
+      }
+      h = max(n_own - 1, 0);
+      // the last half's second map, and its products; then, and for waves without rows from the start, the others' turns: copies alone
+      wait_async_loads();
+      lds_barrier();
+      if (h + 1 < n_half) {
+        copy(a.k, h + 2, (h & 1) ? sK1 : sK0);
+        copy(a.v, h + 1, (h & 1) ? sV0 : sV1);
+      }
+      if (n_own > 0) {
+        const __bf16* tV = (h & 1) ? sV1 : sV0;
+        const int vb = v_cols.fresh();
+        float sum;
+        slot(no, yes, yes, map0, s1, s0, pb0, pb1, tV, vb, sum, nothing);
+        st[1].template settle<DB>(s1, c, sum, pb1, o[1], hh);
+        slot(no, no, yes, map1, s0, s1, pb1, pb0, tV, vb, sum, nothing);
+      }
+      for (++h; h < n_half; ++h) {
+        wait_async_loads();
+        lds_barrier();
+        if (h + 1 < n_half) {
+          copy(a.k, h + 2, (h & 1) ? sK1 : sK0);
+          copy(a.v, h + 1, (h & 1) ? sV0 : sV1);
+        }
       }
       if (sub == 0 && queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
 
@@ -127,7 +226,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
       }
       const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
 #pragma unroll
-      for (int db = 0; db < C::DB; ++db) {
+      for (int db = 0; db < DB; ++db) {
         f32x16 x;
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[r] = o[0][db][r] * inv[0] - lambda * (o[1][db][r] * inv[1]);
@@ -136,8 +235,9 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
       if (a.out2) {
         const auto r2 = make_rsrc(a.out2 + seq_at + (size_t)q0 * row_stride, rows_bytes);
 #pragma unroll
-        for (int db = 0; db < C::DB; ++db) store_block(r2, off + 64u * db, o[1][db], inv[1]);
+        for (int db = 0; db < DB; ++db) store_block(r2, off + 64u * db, o[1][db], inv[1]);
       }
+      lds_barrier();        // nobody reads a tile any longer
     }
     if (!queue.draws) return;
     if (tid == 0) s_ticket = drawn_ticket(queue, next_ticket);
