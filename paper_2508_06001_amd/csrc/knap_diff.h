@@ -22,10 +22,12 @@ struct DiffSoftmax {
 
   // takes in the half whose probabilities sum to `sum` in this lane
   template <int DB>
-  __device__ __forceinline__ void settle(const f32x16& s, float c, float sum, bf16x8 (&pb)[2], f32x16 (&o)[DB], int hh) {
+  __device__ __forceinline__ void settle(const f32x16& s, float c, float sum, bf16x8 (&pb)[2], f32x16 (&o)[DB]) {
     const bool moves = __builtin_amdgcn_ballot_w64(!(sum <= kMaxHalfSum)) != 0;
     if (__builtin_expect(moves, 0)) {
-      const float m_loc = half_max(s, 64, hh);
+      float m_loc = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) m_loc = fmaxf(m_loc, s[r]);
       const float m_new = fmaxf(m_ref, fmaxf(m_loc, xor32(m_loc)));
       const float alpha = m_new == m_ref ? 1.f : fast_exp2((m_ref - m_new) * c);
       m_ref = m_new;

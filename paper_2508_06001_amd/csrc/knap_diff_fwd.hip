@@ -34,8 +34,10 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
 
   const int T = a.cu[a.n_seq], H = a.H;
   build_schedule<C::BM, kThreads, CAUSAL>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // what follows from the lane is formed where it is used, from this one register: the loop has none to spare
+  auto here = [&]() __attribute__((always_inline)) { int x = lane; asm volatile("" : "+v"(x)); return x; };
   const float c = a.scale * kLog2e;
   const size_t row_stride = (size_t)H * D;
   const uint32_t row_bytes = (uint32_t)(row_stride * sizeof(__bf16));
@@ -43,6 +45,12 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   ColReaderX<D> v_cols;
   k_rows.init(lane);
   v_cols.init(lane);
+  // where this lane's 16 bytes of a copied half lie in the tensor: a wave's instruction copies CP_ROWS rows, the waves and then the
+  // instructions in turn; the swizzle looks at a row's low four bits alone, which a second instruction has in common
+  constexpr int CP_ROWS = 512 / D;
+  static_assert(4 * CP_ROWS % 16 == 0 && ROWS % (4 * CP_ROWS) == 0, "");
+  const int cp_row = wave * CP_ROWS + lane / Tile<D>::CPR;
+  const uint32_t cp_off = (uint32_t)cp_row * row_bytes + (uint32_t)Tile<D>::chunk_pos(cp_row, lane % Tile<D>::CPR) * 16u;
   EvenQueue<0, 1> queue;
   queue.init(a.counters);
   if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
@@ -67,14 +75,21 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
       const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
       auto copy = [&](const __bf16* src, int h, __bf16* dst) __attribute__((always_inline)) {
         const int kv0 = h * ROWS;
-        const uint32_t bytes = (uint32_t)max(0, min(kv_end - kv0, ROWS)) * row_bytes;
-        tile_load_async<D>(dst, make_rsrc(src + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, ROWS, wave, lane);
+        const auto r = make_rsrc(src + seq_at + (size_t)kv0 * row_stride, (uint32_t)max(0, min(kv_end - kv0, ROWS)) * row_bytes);
+#pragma unroll
+        for (int i = 0; i < ROWS / (4 * CP_ROWS); ++i) {
+          uint32_t o = cp_off;
+          if (i) asm volatile("" : "+v"(o));     // formed here, not kept in a register of its own through the loop
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(dst + (4 * i + wave) * CP_ROWS * Tile<D>::LD), 16,
+                                                   (int)(o + (uint32_t)(4 * i * CP_ROWS) * row_bytes), 0, 0, 0);
+        }
       };
       copy(a.k, 0, sK0);       // a barrier stands between the last reads of the buffers and this
       const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
-      const uint32_t off = (uint32_t)(32 * wave + l32) * row_bytes + (uint32_t)(16 * hh);
       bf16x8 qf[C::KC];
       {
+        const int ln = here();
+        const uint32_t off = (uint32_t)(32 * wave + (ln & 31)) * row_bytes + (uint32_t)(16 * (ln >> 5));
         const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
 #pragma unroll
         for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
@@ -146,9 +161,11 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
       bf16x8 pb0[2], pb1[2];    // their probabilities
       auto nothing = [](int) {};
       const bool masked = CAUSAL || (n_own == n_half && kv_end % ROWS != 0);
-      const int kv_lim = CAUSAL ? q0 + 32 * wave + l32 + 1 : L;
       auto mask = [&](f32x16& s, int h) __attribute__((always_inline)) {
-        if (masked && h == n_own - 1) mask_half(s, kv_lim - h * ROWS, hh);
+        if (masked && h == n_own - 1) {
+          const int ln = here();
+          mask_half(s, (CAUSAL ? q0 + 32 * wave + (ln & 31) + 1 : L) - h * ROWS, ln >> 5);
+        }
         KNAP_SCHED_FENCE();
       };
       if (n_own > 0) {
@@ -164,7 +181,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
         }
         mask(s0, 0);
         slot(yes, yes, no, map1, s0, s1, pb1, pb0, sV0, 0, sum, nothing);
-        st[0].template settle<DB>(s0, c, sum, pb0, o[0], hh);
+        st[0].template settle<DB>(s0, c, sum, pb0, o[0]);
         mask(s1, 0);
       }
       // the second map of half h and the first of half h + 1 go through the softmax
@@ -178,10 +195,10 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
         copy(a.v, h + 1, nV);
         float sum;
         slot(yes, yes, yes, map0, s1, s0, pb0, pb1, tV, vb, sum, [&](int j) __attribute__((always_inline)) { if (j >= 2 * DB - KH) keys(tK, kb, 1, j - (2 * DB - KH)); });
-        st[1].template settle<DB>(s1, c, sum, pb1, o[1], hh);
+        st[1].template settle<DB>(s1, c, sum, pb1, o[1]);
         mask(s0, h + 1);
         slot(yes, yes, yes, map1, s0, s1, pb1, pb0, tV, vb, sum, nothing);
-        st[0].template settle<DB>(s0, c, sum, pb0, o[0], hh);
+        st[0].template settle<DB>(s0, c, sum, pb0, o[0]);
         mask(s1, h + 1);
       };
       int h = 0;
@@ -202,7 +219,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
         const int vb = v_cols.fresh();
         float sum;
         slot(no, yes, yes, map0, s1, s0, pb0, pb1, tV, vb, sum, nothing);
-        st[1].template settle<DB>(s1, c, sum, pb1, o[1], hh);
+        st[1].template settle<DB>(s1, c, sum, pb1, o[1]);
         slot(no, no, yes, map1, s0, s1, pb1, pb0, tV, vb, sum, nothing);
       }
       for (++h; h < n_half; ++h) {
@@ -215,6 +232,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
       }
       if (sub == 0 && queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
 
+      const int ln = here();
+      const uint32_t off = (uint32_t)(32 * wave + (ln & 31)) * row_bytes + (uint32_t)(16 * (ln >> 5));
       float inv[2];
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
@@ -222,7 +241,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
         inv[m] = 1.0f / l;
         const auto rl = make_rsrc(a.lse + ((size_t)m * H + head) * T + it.row0 + q0, (uint32_t)min(L - q0, C::BM) * 4u);
         __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, st[m].m_ref * a.scale + __logf(l)), rl,
-                                              hh == 0 ? (32 * wave + l32) * 4 : 4 * C::BM, 0, 0);
+                                              ln < 32 ? (32 * wave + ln) * 4 : 4 * C::BM, 0, 0);
       }
       const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
 #pragma unroll
