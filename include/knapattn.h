@@ -184,9 +184,8 @@ int knap_varlen_attn_causal_bwd(const void* q, const void* k, const void* v,
  *   lse      fp32 (2, H, T): the log-sums of map 1, then of map 2.
  *   dlambda  fp32[H] = -sum over rows of dout . O_2, summed in 32 bits over the probabilities
  *            as they are, in a fixed order; zeros where total_tokens is 0 and n_seq is not.
- * Between bags a result differs within its rounding errors only by the tiling of
- * the sequence itself: the kernels have one form for each d, so that a sequence's results depend
- * neither on the other sequences of the bag nor on H.  */
+ * The same calls on the same bag give the same bits; between bags a sequence's results may
+ * differ within their rounding errors, as those of knap_varlen_attn_fwd may.  */
 int knap_varlen_diff_attn_fwd(const void* q, const void* k, const void* v,
                               const int32_t* cu_seqlens, int n_seq,
                               int H, int d, float scale, const float* lambda,

@@ -13,6 +13,146 @@
 
 namespace knap {
 
+// 64 query rows of a sequence and head, from q0 on: waves w and w + 2 share 32 of them, one taking the first 32 keys of every 64, the other the
+// second; the two halves of each softmax are merged through LDS at the end.  A barrier has to stand between this and whatever reads or
+// fills the tiles before or behind it.
+struct DiffTiles {
+  __bf16 *k[4], *v[4];      // 32 rows each; two pairs in turn
+};
+
+template <int D, bool CAUSAL>
+__device__ __forceinline__ void diff_fwd_part(const DiffFwdArgs& a, const DiffTiles& lds, const WorkItem& it, int head, int q0, int T, int lane, int wave) {
+  using C = DiffCfg<D>;
+  constexpr int KH = C::KC / 2, DB = C::DB, ROWS = 32;
+  const int L = it.len, l32 = lane & 31, hh = lane >> 5;
+  const int rb = __builtin_amdgcn_readfirstlane(wave & 1), kh = __builtin_amdgcn_readfirstlane(wave >> 1);
+  const float c = a.scale * kLog2e, lambda = a.lambda[head];
+  const size_t row_stride = (size_t)a.H * D;
+  const uint32_t row_bytes = (uint32_t)(row_stride * sizeof(__bf16));
+  const int kv_end = CAUSAL ? min(L, q0 + 64) : L, n_tiles = (kv_end + 63) / 64;
+  const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
+  auto copy = [&](const __bf16* src, int kv0, __bf16* dst) {
+    tile_load_async<D>(dst, make_rsrc(src + seq_at + (size_t)kv0 * row_stride, (uint32_t)max(0, min(kv_end - kv0, ROWS)) * row_bytes), row_bytes, ROWS,
+                       wave, lane);
+  };
+  RowReaderX<D> k_rows;
+  ColReaderX<D> v_cols;
+  k_rows.init(lane);
+  v_cols.init(lane);
+  const uint32_t rows_bytes = (uint32_t)min(L - q0, 64) * row_bytes;
+  const uint32_t off = (uint32_t)(32 * rb + l32) * row_bytes + (uint32_t)(16 * hh);
+  bf16x8 qf[C::KC];
+  const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+  for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
+  f32x16 o[2][DB];
+  DiffSoftmax st[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[m][db] = zero16();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    copy(a.k, 32 * i, lds.k[i]);
+    copy(a.v, 32 * i, lds.v[i]);
+  }
+  wait_async_loads();
+  lds_barrier();
+  const int kv_lim = CAUSAL ? q0 + 32 * rb + l32 + 1 : L, all_see = CAUSAL ? q0 + 32 * rb + 1 : L, none_see = CAUSAL ? q0 + 32 * rb + 32 : L;
+  auto tile = [&](int t, const __bf16* tK, const __bf16* tV, __bf16* nK0, __bf16* nK1, __bf16* nV0, __bf16* nV1) __attribute__((always_inline)) {
+    copy(a.k, 64 * t + 64, nK0);
+    copy(a.k, 64 * t + 96, nK1);
+    copy(a.v, 64 * t + 64, nV0);
+    copy(a.v, 64 * t + 96, nV1);
+    const int k0 = 64 * t + 32 * kh;
+    if (k0 < min(none_see, kv_end)) {
+      const int kb = k_rows.fresh(), vb = v_cols.fresh();
+      bf16x8 pb[2][2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        f32x16 s = zero16();
+#pragma unroll
+        for (int cc = 0; cc < KH; ++cc) s = mfma32(k_rows.get(tK, kb, m * KH + cc), qf[m * KH + cc], s);
+        if (k0 + ROWS > all_see) mask_half(s, kv_lim - k0, hh);
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = fast_exp2(__builtin_fmaf(s[r], c, -st[m].mc));
+          sum += p;
+          pb[m][r >> 3][r & 7] = (__bf16)p;
+        }
+        st[m].template settle<DB>(s, c, sum, pb[m], o[m]);
+      }
+#pragma unroll
+      for (int j = 0; j < 2 * DB; ++j) {
+        const bf16x8 vt = v_cols.get(tV, vb, 16 * (j / DB), j % DB);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) o[m][j % DB] = mfma32(vt, pb[m][j / DB], o[m][j % DB]);
+      }
+    }
+    wait_async_loads();
+    lds_barrier();
+  };
+  for (int t = 0; t < n_tiles; t += 2) {
+    tile(t, kh == 0 ? lds.k[0] : lds.k[1], kh == 0 ? lds.v[0] : lds.v[1], lds.k[2], lds.k[3], lds.v[2], lds.v[3]);
+    if (t + 1 < n_tiles) tile(t + 1, kh == 0 ? lds.k[2] : lds.k[3], kh == 0 ? lds.v[2] : lds.v[3], lds.k[0], lds.k[1], lds.v[0], lds.v[1]);
+  }
+
+  // merge, a map at a time: the waves of the second keys put down reference, sum and output, those of the first take them up
+  constexpr int PER = DB / 2;       // blocks of 32 columns that a buffer of 32 rows holds in 32 bits
+  float* part_ml = reinterpret_cast<float*>(lds.k[0]) + 128 * rb;
+  auto part_o = [&](int db) { return reinterpret_cast<float*>(rb == 0 ? lds.k[2 + db / PER] : lds.v[2 + db / PER]) + 1024 * (db % PER); };
+  float inv[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    if (kh == 1) {
+      part_ml[lane] = st[m].m_ref;
+      part_ml[64 + lane] = st[m].l;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 x = {o[m][db][4 * j], o[m][db][4 * j + 1], o[m][db][4 * j + 2], o[m][db][4 * j + 3]};
+          *reinterpret_cast<f32x4*>(part_o(db) + (64 * j + lane) * 4) = x;
+        }
+    }
+    lds_barrier();
+    if (kh == 0) {
+      const float m_ref = st[m].m_ref, m_other = part_ml[lane], l_other = part_ml[64 + lane];
+      const float m_new = fmaxf(m_ref, m_other);
+      const float a_own = m_new == m_ref ? 1.f : fast_exp2((m_ref - m_new) * c), a_other = m_new == m_other ? 1.f : fast_exp2((m_other - m_new) * c);
+      const float l_half = st[m].l * a_own + l_other * a_other, l = l_half + xor32(l_half);
+      inv[m] = 1.0f / l;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(part_o(db) + (64 * j + lane) * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[m][db][4 * j + e] = o[m][db][4 * j + e] * a_own + x[e] * a_other;
+        }
+      const auto rl = make_rsrc(a.lse + ((size_t)m * a.H + head) * T + it.row0 + q0, (uint32_t)min(L - q0, 64) * 4u);
+      __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, m_new * a.scale + __logf(l)), rl, hh == 0 ? (32 * rb + l32) * 4 : 4 * 64, 0, 0);
+    }
+    lds_barrier();
+  }
+  if (kh == 0) {
+    const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      f32x16 x;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = o[0][db][r] * inv[0] - lambda * (o[1][db][r] * inv[1]);
+      store_block(ro, off + 64u * db, x, 1.0f);
+    }
+    if (a.out2) {
+      const auto r2 = make_rsrc(a.out2 + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store_block(r2, off + 64u * db, o[1][db], inv[1]);
+    }
+  }
+}
+
 // The keys go through in halves of 32.  A stage is a half and a map; three stages that follow each other are in work at a time, in one slot of
 // the pipeline: the scores of the last one, the probabilities of the middle one, the product with the values of the first one.  No
 // product of a slot waits for its arithmetic, nor the other way round; the stage whose sums a moving reference rescales is of the other
@@ -29,6 +169,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   __shared__ __attribute__((aligned(1024))) __bf16 sK1[TILE];
   __shared__ __attribute__((aligned(1024))) __bf16 sV0[TILE];
   __shared__ __attribute__((aligned(1024))) __bf16 sV1[TILE];
+  __shared__ __attribute__((aligned(1024))) __bf16 sK2[TILE], sK3[TILE], sV2[TILE], sV3[TILE];      // of the parts alone
   __shared__ int s_ticket;
   static_assert(sizeof(__bf16) * TILE >= sizeof(int) * kThreads, "scan scratch must fit in a tile");
 
@@ -51,7 +192,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   static_assert(4 * CP_ROWS % 16 == 0 && ROWS % (4 * CP_ROWS) == 0, "");
   const int cp_row = wave * CP_ROWS + lane / Tile<D>::CPR;
   const uint32_t cp_off = (uint32_t)cp_row * row_bytes + (uint32_t)Tile<D>::chunk_pos(cp_row, lane % Tile<D>::CPR) * 16u;
-  EvenQueue<0, 1> queue;
+  constexpr int SPLIT = CAUSAL ? 4 : 2;     // narrow items (64 queries) of a wide one
+  EvenQueue<SPLIT, 1> queue;
   queue.init(a.counters);
   if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
   __syncthreads();
@@ -263,6 +405,22 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
     lds_barrier();
     ticket = __builtin_amdgcn_readfirstlane(s_ticket);
     lds_barrier();        // everyone has the ticket before the next one is put down
+  }
+  // few items, or those of a thin last round: in parts of 64 queries (EvenQueue::deal)
+  const DiffTiles tiles = {{sK0, sK1, sK2, sK3}, {sV0, sV1, sV2, sV3}};
+  for (int part = ticket - queue.wide; part >= 0 && part < queue.parts;) {
+    const WorkItem it = decode_even<C::BM, CAUSAL>(queue.item_of_part(part), queue, a.cu, a.n_seq, H, s_order, s_start);
+    const int head = __builtin_amdgcn_readfirstlane(it.head), other = (it.len + C::BM - 1) / C::BM - 1 - it.tile, sub = (part % SPLIT) >> 1;
+    const int q0 = __builtin_amdgcn_readfirstlane((CAUSAL && sub == 0 ? other : it.tile) * C::BM + 64 * (part & 1));
+    if (q0 < it.len && !(CAUSAL && sub == 1 && it.tile == other)) diff_fwd_part<D, CAUSAL>(a, tiles, it, head, q0, T, lane, wave);
+    if (!queue.draws) return;         // every part was a first ticket
+    if (tid == 0) {
+      const unsigned drawn = atomicAdd(queue.ctr, 1u);
+      s_ticket = drawn_ticket(queue, drawn);
+    }
+    lds_barrier();                    // (and the tiles are no longer read)
+    part = __builtin_amdgcn_readfirstlane(s_ticket) - queue.wide;
+    lds_barrier();                    // everyone has the ticket before it is drawn again
   }
 }
 
