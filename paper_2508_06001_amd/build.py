@@ -33,6 +33,7 @@ HIP_FLAGS = [
 
 # flags of single sources
 FILE_FLAGS = {
+    "knap_diff_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     # the scheduler's exact register-pressure tracking: without it the causal dQ kernel is up to 4 % slower (17 sequences
     # of 328..4533 tokens, 24 x 128: 844 us against 871); the causal dK/dV kernel is the same with it, the bidirectional one
     # 1 % slower on long sequences

@@ -364,7 +364,7 @@ int diff_bwd_impl(const void* q, const void* k, const void* v, const int32_t* cu
                                  n_seq, H, scale, lambda, lse, static_cast<__bf16*>(dq), static_cast<__bf16*>(dk), static_cast<__bf16*>(dv),
                                  dlambda, at(0), at(1), at(2), at(3), at(4), reinterpret_cast<unsigned*>(ws + 5 * part), nullptr};
     e = next_counters(di, stream, &a.dq_counters);
-    if (e == hipSuccess) e = knap::launch_diff_bwd(a, d, causal, di->cus, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) e = knap::launch_diff_bwd(a, d, causal, (int)total_tokens, di->cus, static_cast<hipStream_t>(stream));
   }
   if (e != hipSuccess) { g_last_hip_error = static_cast<int>(e); return KNAP_ERR_LAUNCH_FAILED; }
   return KNAP_OK;

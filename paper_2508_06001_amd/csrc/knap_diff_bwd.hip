@@ -531,20 +531,29 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
   for (int head = (int)(gridDim.x - 1 - blockIdx.x); head < a.H; head += (int)gridDim.x) diff_lambda<C::THREADS>(a, head, T, reinterpret_cast<float*>(&sP[0]));
 }
 
-template <int D, bool CAUSAL>
-static hipError_t launch_diff_bwd_t(const DiffBwdArgs& a, int cus, hipStream_t stream) {
-  constexpr int PAIRS = D == 128 ? 4 : 2;
+template <int D, int PAIRS, bool CAUSAL>
+static hipError_t launch_diff_dkdv_t(const DiffBwdArgs& a, int grid, hipStream_t stream) {
   const size_t dyn = (size_t)(2 * a.n_seq + 1) * sizeof(int);
-  hipLaunchKernelGGL((diff_dq_kernel<D, CAUSAL>), dim3(2 * cus), dim3(kThreads), dyn, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((diff_dkdv_kernel<D, PAIRS, CAUSAL>), dim3(cus * 4 / PAIRS), dim3(128 * PAIRS), dyn, stream, a);
+  hipLaunchKernelGGL((diff_dkdv_kernel<D, PAIRS, CAUSAL>), dim3(grid), dim3(128 * PAIRS), dyn, stream, a);
   return hipGetLastError();
 }
 
-hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int cus, hipStream_t stream) {
-  if (d == 64) return causal ? launch_diff_bwd_t<64, true>(a, cus, stream) : launch_diff_bwd_t<64, false>(a, cus, stream);
-  return causal ? launch_diff_bwd_t<128, true>(a, cus, stream) : launch_diff_bwd_t<128, false>(a, cus, stream);
+template <int D, bool CAUSAL>
+static hipError_t launch_diff_bwd_t(const DiffBwdArgs& a, int tokens, int cus, hipStream_t stream) {
+  const size_t dyn = (size_t)(2 * a.n_seq + 1) * sizeof(int);
+  hipLaunchKernelGGL((diff_dq_kernel<D, CAUSAL>), dim3(2 * cus), dim3(kThreads), dyn, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if constexpr (D == 64) return launch_diff_dkdv_t<64, 2, CAUSAL>(a, 2 * cus, stream);
+  // d = 128: four pairs, 256 keys, fill a CU; two, 128 keys, leave half of its SIMDs' time unused, but spread few items over twice as many
+  // CUs, as long as each finds one of its own
+  if (rounds(tokens, a.n_seq, a.H, 128, cus) <= 1.0) return launch_diff_dkdv_t<128, 2, CAUSAL>(a, cus, stream);
+  return launch_diff_dkdv_t<128, 4, CAUSAL>(a, cus, stream);
+}
+
+hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int tokens, int cus, hipStream_t stream) {
+  if (d == 64) return causal ? launch_diff_bwd_t<64, true>(a, tokens, cus, stream) : launch_diff_bwd_t<64, false>(a, tokens, cus, stream);
+  return causal ? launch_diff_bwd_t<128, true>(a, tokens, cus, stream) : launch_diff_bwd_t<128, false>(a, tokens, cus, stream);
 }
 
 }  // namespace knap

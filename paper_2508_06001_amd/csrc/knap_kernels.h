@@ -74,7 +74,7 @@ struct DiffBwdArgs {
   unsigned* dq_counters;                       // a set of the forward's, at zero
 };
 hipError_t launch_diff_fwd(const DiffFwdArgs& a, int d, bool causal, int cus, hipStream_t stream);
-hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int cus, hipStream_t stream);
+hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool causal, int tokens, int cus, hipStream_t stream);
 
 // Rotary positions: everything but the launch geometry comes from the caller
 struct RopeArgs {
