@@ -546,7 +546,9 @@ static hipError_t launch_diff_bwd_t(const DiffBwdArgs& a, int tokens, int cus, h
   if (e != hipSuccess) return e;
   if constexpr (D == 64) return launch_diff_dkdv_t<64, 2, CAUSAL>(a, 2 * cus, stream);
   // d = 128: four pairs, 256 keys, fill a CU; two, 128 keys, leave half of its SIMDs' time unused, but spread few items over twice as many
-  // CUs, as long as each finds one of its own
+  // CUs, as long as each finds one of its own.  us at four pairs and at two: one sequence of 2000, 12 x 128, 131 and 108; of 5000, 6 x 128,
+  // 309 and 266; of 1000, 24 x 128, 75 and 60; 200, 150 and 90, 24 x 128, 24 and 19.  Not beyond one round: two pairs on CUs that all have
+  // work take the time of four on half of them.
   if (rounds(tokens, a.n_seq, a.H, 128, cus) <= 1.0) return launch_diff_dkdv_t<128, 2, CAUSAL>(a, cus, stream);
   return launch_diff_dkdv_t<128, 4, CAUSAL>(a, cus, stream);
 }
