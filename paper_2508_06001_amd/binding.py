@@ -299,7 +299,9 @@ _KNAP_TYPES = {torch.bfloat16: KNAP_BF16, torch.float32: KNAP_F32}
 
 # --------------------------------------------------------------------------- differential attention
 
-def _diff_tensors(where: str, bf16, f32) -> None:
+def _diff_tensors(where: str, cu_seqlens, n_seq, bf16, f32) -> None:
+    if cu_seqlens is not None and (cu_seqlens.dtype is not torch.int32 or cu_seqlens.numel() <= n_seq or not cu_seqlens.is_contiguous()):
+        _refuse(where, "cu_seqlens is a contiguous int32 tensor of n_seq + 1 entries")
     for t, shape in bf16:
         if t is not None and (t.dtype is not torch.bfloat16 or t.numel() != shape or not t.is_contiguous()):
             _refuse(where, "q, k, v, the outputs and their gradients are contiguous bf16 (T, H, d) tensors")
@@ -311,7 +313,7 @@ def _diff_tensors(where: str, bf16, f32) -> None:
 def _diff_fwd(fn, where: str, q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse, stream, check) -> int:
     _here(where, q, k, v, cu_seqlens, lam, out, out2, lse)
     n = q.numel()
-    _diff_tensors(where, ((q, n), (k, n), (v, n), (out, n), (out2, n)), ((lam, H), (lse, 0)))
+    _diff_tensors(where, cu_seqlens, n_seq, ((q, n), (k, n), (v, n), (out, n), (out2, n)), ((lam, H), (lse, 0)))
     rc = fn(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), n_seq, H, d, scale, _ptr(lam), _ptr(out), _ptr(out2), _ptr(lse), _stream_handle(stream))
     if check:
         _check(rc, where)
@@ -340,7 +342,7 @@ def _diff_bwd(fn, where: str, q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out,
               workspace_bytes, stream, check) -> int:
     _here(where, q, k, v, cu_seqlens, lam, out, out2, lse, dout, dq, dk, dv, dlam, workspace)
     n = q.numel()
-    _diff_tensors(where, [(t, n) for t in (q, k, v, out, out2, dout, dq, dk, dv)],
+    _diff_tensors(where, cu_seqlens, n_seq, [(t, n) for t in (q, k, v, out, out2, dout, dq, dk, dv)],
                   ((lam, H), (dlam, H), (lse, 2 * H * total_tokens)))
     if total_tokens * H * d > n:
         _refuse(where, "total_tokens is more than the tensors hold")
@@ -371,29 +373,35 @@ def knap_varlen_diff_attn_causal_bwd(q, k, v, cu_seqlens, n_seq: int, H: int, d:
 # --------------------------------------------------------------------------- rotary positions, layer norm
 
 def _rope(fn, where: str, q, k, rot, layout, freq, factor, q_out, k_out, positions, axis_pairs, cu_seqlens, stream, check) -> int:
+    # the host's time bounds the smallest calls: each property is asked for once, strides only where something is not contiguous
     _here(where, q, k, q_out, k_out, freq, positions, cu_seqlens)
-    T, H, d = q.shape
-    H_k = 0 if k is None else k.shape[1]
     bf16 = torch.bfloat16
-    for x, y in ((q, q_out), (k, k_out)):
-        if x is None:
-            continue
-        if x.dtype is not bf16 or y is None or y.dtype is not bf16 or x.shape != y.shape or x.shape[0] != T or x.shape[2] != d:
+    q_shape, k_shape = q.shape, None if k is None else k.shape
+    if len(q_shape) != 3 or q.dtype is not bf16 or q_out.dtype is not bf16 or q_out.shape != q_shape:
+        _refuse(where, "q, k and their outputs are bf16 (tokens, heads, d) tensors of the same tokens and d")
+    T, H, d = q_shape
+    plain, H_k, k_at, k_out_at = q.is_contiguous() and q_out.is_contiguous(), 0, 0, 0
+    if k is not None:
+        if (len(k_shape) != 3 or k.dtype is not bf16 or k_out is None or k_out.dtype is not bf16 or k_out.shape != k_shape or k_shape[0] != T
+                or k_shape[2] != d):
             _refuse(where, "q, k and their outputs are bf16 (tokens, heads, d) tensors of the same tokens and d")
-        if d > 1 and (x.stride(2) != 1 or y.stride(2) != 1):
+        plain = plain and k.is_contiguous() and k_out.is_contiguous()
+        H_k, k_at, k_out_at = k_shape[1], k.data_ptr(), k_out.data_ptr()
+    strides = None
+    if not plain:
+        qs, qos = q.stride(), q_out.stride()
+        ks, kos = (k.stride(), k_out.stride()) if k is not None else ((0, 0, 1), (0, 0, 1))
+        if d > 1 and (qs[2] != 1 or qos[2] != 1 or ks[2] != 1 or kos[2] != 1):
             _refuse(where, "the columns of a head are contiguous")
+        strides = (C.c_int64 * 8)(qs[0], qs[1], ks[0], ks[1], qos[0], qos[1], kos[0], kos[1])
     if freq.dtype is not torch.float64 or freq.numel() != rot // 2 or not freq.is_contiguous():
         _refuse(where, "freq is a contiguous float64 tensor of rot / 2 entries")
-    strides = None
-    if not (q.is_contiguous() and q_out.is_contiguous() and (k is None or (k.is_contiguous() and k_out.is_contiguous()))):
-        ks, kos = (k.stride(), k_out.stride()) if k is not None else ((0, 0), (0, 0))
-        qs, qos = q.stride(), q_out.stride()
-        strides = (C.c_int64 * 8)(qs[0], qs[1], ks[0], ks[1], qos[0], qos[1], kos[0], kos[1])
-    n_axes, pairs, n_seq = 0, None, 0
+    n_axes, pairs, n_seq, pos_at, cu_at = 0, None, 0, 0, 0
     if positions is not None:
-        n_axes = 1 if positions.dim() == 1 else positions.shape[1]
-        if positions.dtype is not torch.int32 or positions.shape[0] != T or not positions.is_contiguous():
-            _refuse(where, "positions is a contiguous int32 (tokens, axes) tensor")
+        n_axes = 1 if positions.dim() == 1 else positions.shape[-1]
+        if positions.dtype is not torch.int32 or positions.numel() != T * n_axes or positions.shape[0] != T or not positions.is_contiguous():
+            _refuse(where, "positions is a contiguous int32 (tokens,) or (tokens, axes) tensor")
+        pos_at = positions.data_ptr()
         if axis_pairs:
             if len(axis_pairs) != n_axes:
                 _refuse(where, "axis_pairs has an entry for each axis")
@@ -401,11 +409,11 @@ def _rope(fn, where: str, q, k, rot, layout, freq, factor, q_out, k_out, positio
     elif cu_seqlens is not None:
         if cu_seqlens.dtype is not torch.int32 or not cu_seqlens.is_contiguous():
             _refuse(where, "cu_seqlens is a contiguous int32 tensor")
-        n_seq = cu_seqlens.numel() - 1
+        n_seq, cu_at = cu_seqlens.numel() - 1, cu_seqlens.data_ptr()
     else:
         _refuse(where, "positions or cu_seqlens")
-    rc = fn(_ptr(q), _ptr(k), T, H, H_k, d, strides, rot, layout, _ptr(positions), n_axes, pairs, _ptr(cu_seqlens), n_seq, _ptr(freq),
-            factor, _ptr(q_out), _ptr(k_out), _stream_handle(stream))
+    rc = fn(q.data_ptr(), k_at, T, H, H_k, d, strides, rot, layout, pos_at, n_axes, pairs, cu_at, n_seq, freq.data_ptr(), factor,
+            q_out.data_ptr(), k_out_at, _stream_handle(stream))
     if check:
         _check(rc, where)
     return rc
@@ -434,17 +442,23 @@ def knap_rope_frequencies(rot: int, base: float = 10000.0, kind: int = KNAP_ROPE
     return list(freq), factor.value
 
 
-def _rows(where: str, name: str, t, rows: int, width: int, dtype=None) -> int:
+def _rows(where: str, name: str, t, shape, dtype=None) -> int:
     """The row stride of a (rows, width) tensor with contiguous rows, checked."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
-        _refuse(where, f"{name} is a (rows, width) tensor with contiguous rows")
     if t.dtype not in _KNAP_TYPES or (dtype is not None and t.dtype is not dtype):
         _refuse(where, f"the type of {name}")
+    if len(shape) != 2 or t.shape != shape:
+        _refuse(where, f"{name} is a (rows, width) tensor")
+    if t.is_contiguous():
+        return shape[1]
+    if shape[1] > 1 and t.stride(1) != 1:
+        _refuse(where, f"the rows of {name} are contiguous")
     return t.stride(0)
 
 
 def _vector(where: str, name: str, t, n: int, dtype=None) -> None:
-    if t is not None and (t.numel() != n or not t.is_contiguous() or (t.dtype is not dtype if dtype is not None else t.dtype not in _KNAP_TYPES)):
+    if t is None:
+        return
+    if t.numel() != n or not t.is_contiguous() or (t.dtype not in _KNAP_TYPES if dtype is None else t.dtype is not dtype):
         _refuse(where, f"{name} is a contiguous vector of {n} values of its type")
 
 
@@ -452,8 +466,9 @@ def knap_layer_norm_fwd(x, weight, bias, eps: float, y, mean=None, rstd=None, st
     """y = (x - mean) rstd weight + bias of every row of x (rows, width); weight and bias (of one type) may be None."""
     where = "knap_layer_norm_fwd"
     _here(where, x, weight, bias, y, mean, rstd)
-    rows, width = x.shape
-    xs, ys = _rows(where, "x", x, rows, width), _rows(where, "y", y, rows, width)
+    shape = x.shape
+    xs, ys = _rows(where, "x", x, shape), _rows(where, "y", y, shape)
+    rows, width = shape
     _vector(where, "weight", weight, width)
     _vector(where, "bias", bias, width, None if weight is None else weight.dtype)
     _vector(where, "mean", mean, rows, torch.float32)
@@ -476,8 +491,9 @@ def knap_layer_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace
     """dx (of x's type), dweight and dbias (fp32, or None) of knap_layer_norm_fwd, whose mean and rstd it takes."""
     where = "knap_layer_norm_bwd"
     _here(where, x, weight, mean, rstd, dy, dx, dweight, dbias, workspace)
-    rows, width = x.shape
-    xs, dys, dxs = _rows(where, "x", x, rows, width), _rows(where, "dy", dy, rows, width), _rows(where, "dx", dx, rows, width, x.dtype)
+    shape = x.shape
+    xs, dys, dxs = _rows(where, "x", x, shape), _rows(where, "dy", dy, shape), _rows(where, "dx", dx, shape, x.dtype)
+    rows, width = shape
     _vector(where, "weight", weight, width)
     for name, t, n in (("mean", mean, rows), ("rstd", rstd, rows), ("dweight", dweight, width), ("dbias", dbias, width)):
         _vector(where, name, t, n, torch.float32)
