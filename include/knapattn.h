@@ -177,13 +177,16 @@ int knap_varlen_attn_causal_bwd(const void* q, const void* k, const void* v,
  *
  * Layouts, masks, supported sizes, alignment, errors, streams, concurrency and capture are
  * those of knap_varlen_attn_fwd / _bwd.  Every one of these calls, the backward ones too,
- * draws from a set of the forward's counters, and counts as one of its calls.  Besides:
+ * draws from a set of the forward's counters, and counts as one of its calls.  Values that
+ * are not finite stay in their sequence and head; under the causal mask they may reach up to
+ * 127 rows on the side that their mask hides (a probability of zero times them).  Besides:
  *   lambda   fp32[H], any sign; it is read on the device, so that a captured call follows it.
  *   out2     bf16 (T, H, d): O_2, which the backward takes; NULL in the forward where no backward
  *            follows.
  *   lse      fp32 (2, H, T): the log-sums of map 1, then of map 2.
  *   dlambda  fp32[H] = -sum over rows of dout . O_2, summed in 32 bits over the probabilities
- *            as they are, in a fixed order; zeros where total_tokens is 0 and n_seq is not.
+ *            as they are, in a fixed order; zeros where total_tokens is 0 and n_seq is not.  Not
+ *            the array of lambda.
  * The same calls on the same bag give the same bits; between bags a sequence's results may
  * differ within their rounding errors, as those of knap_varlen_attn_fwd may.  */
 int knap_varlen_diff_attn_fwd(const void* q, const void* k, const void* v,

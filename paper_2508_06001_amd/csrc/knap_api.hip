@@ -342,7 +342,7 @@ int diff_bwd_impl(const void* q, const void* k, const void* v, const int32_t* cu
   if (rc != KNAP_OK) return rc;
   if (total_tokens < 0 || total_tokens > INT32_MAX) return KNAP_ERR_INVALID_ARG;
   if (n_seq == 0) return KNAP_OK;
-  if (!dlambda || !aligned(dlambda, 4)) return KNAP_ERR_INVALID_ARG;
+  if (!dlambda || !aligned(dlambda, 4) || dlambda == lambda) return KNAP_ERR_INVALID_ARG;
   hipError_t e;
   if (total_tokens == 0) {
     e = knap::launch_layer_norm_zero(dlambda, nullptr, H, static_cast<hipStream_t>(stream));

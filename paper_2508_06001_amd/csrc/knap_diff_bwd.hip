@@ -526,7 +526,8 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
     lds_barrier();
     ticket = __builtin_amdgcn_readfirstlane(s_ticket);
     lds_barrier();        // everyone has the ticket before the next one is put down
-  }  // the workgroups from the last one on, which have the cheapest items or none
+  }
+  // dlambda by the workgroups from the last one on, which have the cheapest items or none
   __syncthreads();
   for (int head = (int)(gridDim.x - 1 - blockIdx.x); head < a.H; head += (int)gridDim.x) diff_lambda<C::THREADS>(a, head, T, reinterpret_cast<float*>(&sP[0]));
 }

@@ -191,6 +191,7 @@ int knap_rope_frequencies(int rot, double base, int kind, double scale, int64_t 
   if (kind < KNAP_ROPE_PLAIN || kind > KNAP_ROPE_PARTS || (kind == KNAP_ROPE_BASE && rot == 2)) return KNAP_ERR_INVALID_ARG;
   if (kind == KNAP_ROPE_PARTS && (trained_len < 1 || !(low < high) || !isfinite(low) || !isfinite(high))) return KNAP_ERR_INVALID_ARG;
   if (kind == KNAP_ROPE_BASE) base *= pow(scale, (double)rot / (double)(rot - 2));
+  if (!isfinite(base)) return KNAP_ERR_INVALID_ARG;
   for (int i = 0; i < rot / 2; ++i) {
     double f = pow(base, -2.0 * i / rot);
     if (kind == KNAP_ROPE_LINEAR) f /= scale;

@@ -71,7 +71,7 @@ struct RowPlace {
       r = make_rsrc(base + row * stride, row < rows ? (uint32_t)width * (uint32_t)sizeof(T) : 0u);
       off = 0;
       end = (uint32_t)width * (uint32_t)sizeof(T);
-    } else {              // the groups of a wave and those of the others: their rows are at most 64 KB apart, or the form is not taken
+    } else {              // the rows of all groups, at most 2^22 columns apart, or the form is not taken: offsets of 16 of them in 32 bits
       const int64_t left = min((int64_t)C::GROUPS, rows - row0);
       r = make_rsrc(base + row0 * stride, left > 0 ? (uint32_t)((left - 1) * stride + width) * (uint32_t)sizeof(T) : 0u);
       off = (uint32_t)group * (uint32_t)stride * (uint32_t)sizeof(T);

@@ -155,6 +155,31 @@ def test_rows_behind_the_last_sequence_and_other_sequences(d, causal):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_bad_values_that_the_mask_hides(d):
+    """NaN and infinities in rows 700 of k and v, 300 of q and dout, and -inf scores, reach at most 127 rows that do not see them."""
+    import torch
+    import paper_2508_06001_amd as K
+    run = Run([1000], 2, d, True)
+    x = {n: t.clone() for n, t in run.x.items()}
+    attn = K.VarlenDiffAttention(run.cu, 2, d, run.scale, run.lam, causal=True)
+    for row, names in ((700, ("k", "v")), (300, ("q", "dout"))):
+        y = {n: t.clone() for n, t in x.items()}
+        for n in names:
+            y[n][row, 0, 1], y[n][row, 1, d - 1] = float("nan"), float("-inf")
+        attn.forward(y["q"], y["k"], y["v"])
+        attn.backward(y["q"], y["k"], y["v"], y["dout"])
+        torch.cuda.synchronize()
+        for n, t in (("out", attn.out), ("out2", attn.out2), ("dq", attn.dq), ("dk", attn.dk), ("dv", attn.dv)):
+            if row == 700:        # queries before the key; their keys' gradients come from all queries behind them
+                keep = slice(0, row - 127) if n in ("out", "out2", "dq") else None
+            else:                 # the query's own rows, and gradients of the keys that it does not see
+                keep = slice(row + 128, None)
+            if keep is not None:
+                assert torch.equal(t[keep], run.y[n][keep]), (row, n)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("causal", [False, True])
 def test_same_bits_without_a_backward_captured_and_beside_each_other(causal):
     import torch
@@ -307,7 +332,7 @@ def test_bad_arguments_are_refused_without_touching_a_gpu():
         for wrong in common + [dict(out=256), dict(out=512), dict(out=768), dict(out2=2048), dict(out2=256)]:
             assert fwd(**wrong) == bad, wrong
         for wrong in common + [dict(out2=0), dict(do=0), dict(dq=0), dict(dk=0), dict(dv=0), dict(dlam=0), dict(dlam=2), dict(do=16388), dict(dq=256 * 66),
-                               dict(dv=256 * 66), dict(dq=256), dict(dk=512), dict(dv=768), dict(T=-1), dict(T=1 << 31), dict(ws=0), dict(ws=128)]:
+                               dict(dv=256 * 66), dict(dq=256), dict(dk=512), dict(dv=768), dict(dlam=64), dict(T=-1), dict(T=1 << 31), dict(ws=0), dict(ws=128)]:
             assert bwd(**wrong) == bad, wrong
         assert fwd(n=K.KNAP_MAX_SEQS + 1) == bwd(n=K.KNAP_MAX_SEQS + 1) == K.KNAP_ERR_TOO_MANY_SEQS
         need = K.knap_varlen_diff_attn_bwd_workspace_bytes(100, 1, 2, 64)
@@ -327,6 +352,6 @@ def test_the_binding_refuses_what_the_library_cannot_see():
                                                               out=torch.empty_like(x), out2=None, lse=lse), **kw})
     call()
     for wrong in (dict(q=x.float()), dict(k=x[:4]), dict(v=x.transpose(0, 1)), dict(lam=lam[:1]), dict(lam=lam.double()), dict(lse=lse.double()),
-                  dict(out=x.cpu()), dict(lam=lam.cpu())):
+                  dict(out=x.cpu()), dict(lam=lam.cpu()), dict(cu_seqlens=cu.long()), dict(cu_seqlens=cu[:1]), dict(n_seq=2)):
         with pytest.raises(K.KnapError):
             call(**wrong)

@@ -40,7 +40,7 @@ def f64(t):
 @pytest.mark.parametrize("half", [True, False])
 @pytest.mark.parametrize("T,H,Hk,d,rot", [(1, 1, 1, 64, 64), (1, 24, 24, 128, 128), (5, 2, 1, 128, 32), (67, 3, 2, 64, 20), (130, 2, 0, 128, 128),
                                           (333, 6, 6, 80, 80), (33, 4, 4, 10, 6), (1000, 12, 4, 64, 48), (257, 1, 1, 1024, 1024), (7, 5, 1, 2, 2),
-                                          (4099, 3, 3, 128, 96)])
+                                          (4099, 3, 3, 128, 96), (9001, 1, 0, 1024, 1024)])
 def test_turned_columns(T, H, Hk, d, rot, half, bwd):
     import torch
     import paper_2508_06001_amd as K
@@ -290,7 +290,7 @@ def test_bad_arguments_are_refused_without_touching_a_gpu():
         assert call(**wrong) == bad, wrong
     assert call(pos=0, n_seq=K.KNAP_MAX_SEQS + 1, cu=64) == K.KNAP_ERR_TOO_MANY_SEQS
     for args in ((0, 1e4, 0, 1.0), (3, 1e4, 0, 1.0), (64, 0.0, 0, 1.0), (64, 1e4, 4, 1.0), (64, 1e4, -1, 1.0), (64, 1e4, 1, 0.5),
-                 (64, float("nan"), 0, 1.0), (2, 1e4, K.KNAP_ROPE_BASE, 2.0), (64, 1e4, 1, float("inf"))):
+                 (64, float("nan"), 0, 1.0), (2, 1e4, K.KNAP_ROPE_BASE, 2.0), (64, 1e4, 1, float("inf")), (4, 1e4, K.KNAP_ROPE_BASE, 1e160)):
         with pytest.raises(K.KnapError):
             K.knap_rope_frequencies(*args)
     for trained, low, high in ((0, 1.0, 32.0), (4096, 32.0, 32.0), (4096, float("nan"), 1.0)):
@@ -311,6 +311,7 @@ def test_the_binding_refuses_what_the_library_cannot_see():
                            (x, torch.empty_like(x), dict(freq=freq.float())), (x, torch.empty_like(x), dict(freq=freq[:31])),
                            (x, torch.empty_like(x), dict(positions=pos.long())), (x, torch.empty_like(x), dict(positions=pos[:3])),
                            (x, torch.empty_like(x), dict(positions=None)), (x.cpu(), torch.empty_like(x), {}),
-                           (x, torch.empty_like(x), dict(axis_pairs=[16, 16]))):
+                           (x, torch.empty_like(x), dict(axis_pairs=[16, 16])), (x[0], torch.empty_like(x[0]), {}),
+                           (x, torch.empty_like(x), dict(positions=pos.view(4, 1, 1).expand(4, 1, 2).contiguous()))):
         with pytest.raises(K.KnapError):
             K.knap_rope_fwd(q, None, q_out=q_out, k_out=None, **{**ok, **more})
