@@ -212,9 +212,10 @@ struct DiffSlot {
 };
 constexpr int kDiffValues = 5 * 64;
 
-template <int D, int PAIRS, bool CAUSAL>
+// `draw` is called behind the last product, in front of the stores.
+template <int D, int PAIRS, bool CAUSAL, class Draw>
 __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffSlot& r0, const DiffSlot& r1, const DiffSlot& r2, char* sP, char* sPark,
-                                               const DiffLane<D, PAIRS>& me, const WorkItem& it, int head, int kv_tile, int T) {
+                                               const DiffLane<D, PAIRS>& me, const WorkItem& it, int head, int kv_tile, int T, Draw draw) {
   using C = Bwd2Cfg<D, PAIRS>;
   using W = DiffLane<D, PAIRS>;
   constexpr int KH = C::KC / 2, NH = C::NB / 2;
@@ -457,6 +458,7 @@ __device__ __forceinline__ void diff_dkdv_tile(const DiffBwdArgs& g, const DiffS
   else KNAP_ROLE_LOOP(1);
 #undef KNAP_ROLE_LOOP
 #undef KNAP_STEP
+  draw();
 
   const auto rg = make_rsrc((role == 0 ? g.dv : g.dk) + (size_t)(it.row0 + kv0) * row_stride + (size_t)head * D,
                             (uint32_t)min(L - kv0, C::BN) * row_bytes);
@@ -519,8 +521,9 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
   for (int ticket = queue.first_ticket(); ticket < queue.wide;) {
     const WorkItem it = decode_tile_major<C::BN>(queue.item(ticket), a.cu, a.n_seq, a.H, s_order, s_start);
     unsigned next_ticket;      // thread 0 only
-    if (tid == 0 && queue.draws) next_ticket = atomicAdd(queue.ctr, 1u);
-    diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sP, sPark, me, it, it.head, it.tile, T);
+    diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sP, sPark, me, it, it.head, it.tile, T, [&] {
+      if (tid == 0 && queue.draws) next_ticket = atomicAdd(queue.ctr, 1u);
+    });
     if (!queue.draws) break;
     if (tid == 0) s_ticket = queue.later_ticket(next_ticket);
     lds_barrier();
