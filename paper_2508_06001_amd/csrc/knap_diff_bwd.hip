@@ -519,7 +519,11 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
   StridedQueue queue;
   queue.init(a.counters, n_items);
   for (int ticket = queue.first_ticket(); ticket < queue.wide;) {
-    const WorkItem it = decode_tile_major<C::BN>(queue.item(ticket), a.cu, a.n_seq, a.H, s_order, s_start);
+    // longest items first: by what is left of the sequence under the mask (tile by tile of one sequence after the other, us: 4 of 4096, 6 x 128,
+    // 383 -> 325; 32 of 450, 12 x 128, 155 -> 142; 17 of 328 .. 4533, 12 x 64, 542 -> 522), by sequence without it
+    const int w = queue.item(ticket);
+    const WorkItem it = CAUSAL ? decode_most_left<C::BN>(w, a.cu, a.n_seq, a.H, s_order, s_start)
+                               : decode_tile_major<C::BN>(w, a.cu, a.n_seq, a.H, s_order, s_start);
     unsigned next_ticket;      // thread 0 only
     diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sP, sPark, me, it, it.head, it.tile, T, [&] {
       if (tid == 0 && queue.draws) next_ticket = atomicAdd(queue.ctr, 1u);
@@ -549,11 +553,15 @@ static hipError_t launch_diff_bwd_t(const DiffBwdArgs& a, int tokens, int cus, h
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if constexpr (D == 64) return launch_diff_dkdv_t<64, 2, CAUSAL>(a, 2 * cus, stream);
-  // d = 128: four pairs, 256 keys, fill a CU; two, 128 keys, leave half of its SIMDs' time unused, but spread few items over twice as many
-  // CUs, as long as each finds one of its own.  us at four pairs and at two: one sequence of 2000, 12 x 128, 131 and 108; of 5000, 6 x 128,
-  // 309 and 266; of 1000, 24 x 128, 75 and 60; 200, 150 and 90, 24 x 128, 24 and 19.  Not beyond one round: two pairs on CUs that all have
-  // work take the time of four on half of them.
-  if (rounds(tokens, a.n_seq, a.H, 128, cus) <= 1.0) return launch_diff_dkdv_t<128, 2, CAUSAL>(a, cus, stream);
+  // d = 128: four pairs, 256 keys, fill a CU; two, 128 keys, leave half of its SIMDs' time unused (a step takes 0.86 of the time), but spread
+  // few items over twice as many CUs.  Without the mask as long as each finds one of its own, us at four pairs and at two: one sequence of
+  // 2000, 12 x 128, 131 and 108; of 5000, 6 x 128, 309 and 266; of 1000, 24 x 128, 75 and 60; 200, 150 and 90, 24 x 128, 24 and 19.
+  // Under the mask, where items are half as long in the mean and the longest decide, up to two rounds of them, but for short sequences, whose
+  // 256 keys are few items anyway: 16384, 3 x 128, 1018 and 883; 8000, 6 x 128, 510 and 445; 4 of 1000, 12 x 128, 86 and 72; 6 of
+  // 768, 12 x 128, 71 and 67; 7 of 640 63 and 59; but 9 of 512 54 and 57; 12 of 300 41 and 45; 20 of 256 40 and 47.  The mean does not show a
+  // long one among many short ones: 3000 and 20 of 100 take four, 209, where two would take 176.
+  const double most = CAUSAL && tokens > 600 * (int64_t)a.n_seq ? 2.0 : 1.0;
+  if (rounds(tokens, a.n_seq, a.H, 128, cus) <= most) return launch_diff_dkdv_t<128, 2, CAUSAL>(a, cus, stream);
   return launch_diff_dkdv_t<128, 4, CAUSAL>(a, cus, stream);
 }
 
