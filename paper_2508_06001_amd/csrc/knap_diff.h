@@ -69,6 +69,8 @@ struct StridedQueue {
   __device__ __forceinline__ int first_ticket() const { return (int)blockIdx.x / n_q; }
   __device__ __forceinline__ int later_ticket(unsigned drawn) const { return per + (int)drawn; }
   __device__ __forceinline__ int item(int ticket) const { return q + ticket * n_q; }
+  // every workgroup draws until it gets a ticket past the last: `wide` draws in all
+  __device__ __forceinline__ bool last_draw(unsigned drawn) const { return drawn + 1 == (unsigned)wide; }
 };
 
 // item w of a list that holds, for each sequence, its tiles of TILE rows in turn, and for each of them all heads

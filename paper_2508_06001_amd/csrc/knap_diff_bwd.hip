@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
   static_assert(sizeof(__bf16) * C::TILE_ELEMS >= sizeof(int) * kThreads, "scan scratch must fit in a tile");
 
   const int T = a.cu[a.n_seq], H = a.H;
-  build_schedule<C::BM, kThreads, CAUSAL>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
+  const int n_items = build_schedule<C::BM, kThreads, false>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float c = a.scale * kLog2e;
@@ -51,20 +51,27 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
   rows.init(lane);
   cols.init(lane);
   if (blockIdx.x == 0 && tid < 8) a.counters[tid] = 0u;      // of the launch behind this one
-  EvenQueue<0, 1> queue;
-  queue.init(a.dq_counters);
-  if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
-  __syncthreads();
-  deal_even<C::BM, CAUSAL>(queue, a.cu, a.n_seq, s_order, s_start);
+  std::conditional_t<CAUSAL, StridedQueue, EvenQueue<0, 1>> queue;
+  if constexpr (CAUSAL) {
+    queue.init(a.dq_counters, n_items);
+  } else {
+    queue.init(a.dq_counters);
+    if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
+    __syncthreads();
+    deal_even<C::BM, false>(queue, a.cu, a.n_seq, s_order, s_start);
+  }
   int ticket = queue.first_ticket();
   while (ticket < queue.wide) {
-    const WorkItem it = decode_even<C::BM, CAUSAL>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
+    // under the mask the query tiles with most keys first, as in the forward (pairs in even shares, us: 17 of 328 .. 4533, 6 x 128, 320 -> 265; 4 of
+    // 4096 235 -> 194; 32 of 200 33 -> 24; 8000, 12 x 64, 305 -> 239; 17 of 328 .. 4533, 24 x 128, 1038 -> 1045)
+    WorkItem it;
+    if constexpr (CAUSAL) it = decode_most_left<C::BM>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
+    else it = decode_even<C::BM, false>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
     const int L = it.len, head = __builtin_amdgcn_readfirstlane(it.head);
-    const int other = (L + C::BM - 1) / C::BM - 1 - it.tile;
     const float lambda = a.lambda[head];
     unsigned next_ticket;      // thread 0 only
-    for (int sub = 0; sub < (CAUSAL && it.tile != other ? 2 : 1); ++sub) {
-      const int q_tile = __builtin_amdgcn_readfirstlane(!CAUSAL ? it.tile : sub == 0 ? other : it.tile);
+    {
+      const int q_tile = __builtin_amdgcn_readfirstlane(CAUSAL ? (L + C::BM - 1) / C::BM - 1 - it.tile : it.tile);
       const int q0 = q_tile * C::BM, q_row = q0 + 32 * wave + l32;
       const bool q_valid = q_row < L;
       const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
@@ -172,7 +179,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
         const bool odd = t & 1;
         tile(std::true_type{}, t, odd ? sK1 : sK0, odd ? sV1 : sV0, odd ? sK0 : sK1, odd ? sV0 : sV1);
       }
-      if (sub == 0 && queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
+      if (queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
       d2 += xor32(d2);
       if (q_valid && hh == 0) a.d2[row_at] = d2 * kDiffDown;
       const auto rg = make_rsrc(a.dq + seq_at + (size_t)q0 * row_stride, rows_bytes);

@@ -8,8 +8,13 @@
 // in all, where four calls of plain attention (two maps, two halves of the values) would take 8.
 //
 // What bounds it: two exponentials a score pair where plain attention has one, beside 24 matrix instructions a half of 32 keys and wave;
-// the vector unit has 1.5 times plain attention's work a product.  Measured, us (credited TFLOP/s): 2 x 4292 and 37 .. 384, 24 x 128, 655
-// (960); 12 x 64 under the mask, tiny 10.6; 8192 x 2 and 16384, 3 x 128, 716 (770 of them on the 75 % of the workgroups that have an item).
+// 7.5 vector instructions a matrix one, the matrix units busy 49 % of the time.  Measured, us (TFLOP/s): 4173 and 4096, 24 x 128, 650 (970); 17 of
+// 328 .. 4533 under the mask, 6 x 128, 231 (890), 24 x 128, 880 (930); 16384, 3 x 128, 680 (910, on the 75 % of the workgroups that have an
+// item); 37 .. 311, 2 x 64, 11.
+// Under the mask items are single query tiles, those with most keys first, drawn one by one (pairs of a long and a short tile in even shares, as
+// plain attention has them, us: 17 of 328 .. 4533, 6 x 128, 255 -> 231; 4 of 4096 200 -> 170; 32 of 200, 6 x 128, 28 -> 19; 8000, 12 x 64, 260 -> 203;
+// the longest items alone decide for 16384, 3 x 128, 433 -> 473).  Parts of 64 queries for few items, as plain attention has them, cost more
+// than they gain here: one of 2000, 12 x 128, 73 in parts and 66; of 1000, 24 x 128, 43 and 39.
 // With probabilities in bf16 out is off by 2.5e-3 in the 2-norm where its own rounding alone is 1.7e-3: they are the operand of a matrix
 // product with v, whose type they take.
 //
@@ -18,146 +23,6 @@
 #include "knap_diff.h"
 
 namespace knap {
-
-// 64 query rows of a sequence and head, from q0 on: waves w and w + 2 share 32 of them, one taking the first 32 keys of every 64, the other the
-// second; the two halves of each softmax are merged through LDS at the end.  A barrier has to stand between this and whatever reads or
-// fills the tiles before or behind it.
-struct DiffTiles {
-  __bf16 *k[4], *v[4];      // 32 rows each; two pairs in turn
-};
-
-template <int D, bool CAUSAL>
-__device__ __forceinline__ void diff_fwd_part(const DiffFwdArgs& a, const DiffTiles& lds, const WorkItem& it, int head, int q0, int T, int lane, int wave) {
-  using C = DiffCfg<D>;
-  constexpr int KH = C::KC / 2, DB = C::DB, ROWS = 32;
-  const int L = it.len, l32 = lane & 31, hh = lane >> 5;
-  const int rb = __builtin_amdgcn_readfirstlane(wave & 1), kh = __builtin_amdgcn_readfirstlane(wave >> 1);
-  const float c = a.scale * kLog2e, lambda = a.lambda[head];
-  const size_t row_stride = (size_t)a.H * D;
-  const uint32_t row_bytes = (uint32_t)(row_stride * sizeof(__bf16));
-  const int kv_end = CAUSAL ? min(L, q0 + 64) : L, n_tiles = (kv_end + 63) / 64;
-  const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
-  auto copy = [&](const __bf16* src, int kv0, __bf16* dst) {
-    tile_load_async<D>(dst, make_rsrc(src + seq_at + (size_t)kv0 * row_stride, (uint32_t)max(0, min(kv_end - kv0, ROWS)) * row_bytes), row_bytes, ROWS,
-                       wave, lane);
-  };
-  RowReaderX<D> k_rows;
-  ColReaderX<D> v_cols;
-  k_rows.init(lane);
-  v_cols.init(lane);
-  const uint32_t rows_bytes = (uint32_t)min(L - q0, 64) * row_bytes;
-  const uint32_t off = (uint32_t)(32 * rb + l32) * row_bytes + (uint32_t)(16 * hh);
-  bf16x8 qf[C::KC];
-  const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
-#pragma unroll
-  for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
-  f32x16 o[2][DB];
-  DiffSoftmax st[2];
-#pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int db = 0; db < DB; ++db) o[m][db] = zero16();
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    copy(a.k, 32 * i, lds.k[i]);
-    copy(a.v, 32 * i, lds.v[i]);
-  }
-  wait_async_loads();
-  lds_barrier();
-  const int kv_lim = CAUSAL ? q0 + 32 * rb + l32 + 1 : L, all_see = CAUSAL ? q0 + 32 * rb + 1 : L, none_see = CAUSAL ? q0 + 32 * rb + 32 : L;
-  auto tile = [&](int t, const __bf16* tK, const __bf16* tV, __bf16* nK0, __bf16* nK1, __bf16* nV0, __bf16* nV1) __attribute__((always_inline)) {
-    copy(a.k, 64 * t + 64, nK0);
-    copy(a.k, 64 * t + 96, nK1);
-    copy(a.v, 64 * t + 64, nV0);
-    copy(a.v, 64 * t + 96, nV1);
-    const int k0 = 64 * t + 32 * kh;
-    if (k0 < min(none_see, kv_end)) {
-      const int kb = k_rows.fresh(), vb = v_cols.fresh();
-      bf16x8 pb[2][2];
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        f32x16 s = zero16();
-#pragma unroll
-        for (int cc = 0; cc < KH; ++cc) s = mfma32(k_rows.get(tK, kb, m * KH + cc), qf[m * KH + cc], s);
-        if (k0 + ROWS > all_see) mask_half(s, kv_lim - k0, hh);
-        float sum = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float p = fast_exp2(__builtin_fmaf(s[r], c, -st[m].mc));
-          sum += p;
-          pb[m][r >> 3][r & 7] = (__bf16)p;
-        }
-        st[m].template settle<DB>(s, c, sum, pb[m], o[m]);
-      }
-#pragma unroll
-      for (int j = 0; j < 2 * DB; ++j) {
-        const bf16x8 vt = v_cols.get(tV, vb, 16 * (j / DB), j % DB);
-#pragma unroll
-        for (int m = 0; m < 2; ++m) o[m][j % DB] = mfma32(vt, pb[m][j / DB], o[m][j % DB]);
-      }
-    }
-    wait_async_loads();
-    lds_barrier();
-  };
-  for (int t = 0; t < n_tiles; t += 2) {
-    tile(t, kh == 0 ? lds.k[0] : lds.k[1], kh == 0 ? lds.v[0] : lds.v[1], lds.k[2], lds.k[3], lds.v[2], lds.v[3]);
-    if (t + 1 < n_tiles) tile(t + 1, kh == 0 ? lds.k[2] : lds.k[3], kh == 0 ? lds.v[2] : lds.v[3], lds.k[0], lds.k[1], lds.v[0], lds.v[1]);
-  }
-
-  // merge, a map at a time: the waves of the second keys put down reference, sum and output, those of the first take them up
-  constexpr int PER = DB / 2;       // blocks of 32 columns that a buffer of 32 rows holds in 32 bits
-  float* part_ml = reinterpret_cast<float*>(lds.k[0]) + 128 * rb;
-  auto part_o = [&](int db) { return reinterpret_cast<float*>(rb == 0 ? lds.k[2 + db / PER] : lds.v[2 + db / PER]) + 1024 * (db % PER); };
-  float inv[2];
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    if (kh == 1) {
-      part_ml[lane] = st[m].m_ref;
-      part_ml[64 + lane] = st[m].l;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4 x = {o[m][db][4 * j], o[m][db][4 * j + 1], o[m][db][4 * j + 2], o[m][db][4 * j + 3]};
-          *reinterpret_cast<f32x4*>(part_o(db) + (64 * j + lane) * 4) = x;
-        }
-    }
-    lds_barrier();
-    if (kh == 0) {
-      const float m_ref = st[m].m_ref, m_other = part_ml[lane], l_other = part_ml[64 + lane];
-      const float m_new = fmaxf(m_ref, m_other);
-      const float a_own = m_new == m_ref ? 1.f : fast_exp2((m_ref - m_new) * c), a_other = m_new == m_other ? 1.f : fast_exp2((m_other - m_new) * c);
-      const float l_half = st[m].l * a_own + l_other * a_other, l = l_half + xor32(l_half);
-      inv[m] = 1.0f / l;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(part_o(db) + (64 * j + lane) * 4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[m][db][4 * j + e] = o[m][db][4 * j + e] * a_own + x[e] * a_other;
-        }
-      const auto rl = make_rsrc(a.lse + ((size_t)m * a.H + head) * T + it.row0 + q0, (uint32_t)min(L - q0, 64) * 4u);
-      __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, m_new * a.scale + __logf(l)), rl, hh == 0 ? (32 * rb + l32) * 4 : 4 * 64, 0, 0);
-    }
-    lds_barrier();
-  }
-  if (kh == 0) {
-    const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      f32x16 x;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = o[0][db][r] * inv[0] - lambda * (o[1][db][r] * inv[1]);
-      store_block(ro, off + 64u * db, x, 1.0f);
-    }
-    if (a.out2) {
-      const auto r2 = make_rsrc(a.out2 + seq_at + (size_t)q0 * row_stride, rows_bytes);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) store_block(r2, off + 64u * db, o[1][db], inv[1]);
-    }
-  }
-}
 
 // The keys go through in halves of 32.  A stage is a half and a map; three stages that follow each other are in work at a time, in one slot of
 // the pipeline: the scores of the last one, the probabilities of the middle one, the product with the values of the first one.  No
@@ -175,17 +40,20 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   __shared__ __attribute__((aligned(1024))) __bf16 sK1[TILE];
   __shared__ __attribute__((aligned(1024))) __bf16 sV0[TILE];
   __shared__ __attribute__((aligned(1024))) __bf16 sV1[TILE];
-  __shared__ __attribute__((aligned(1024))) __bf16 sK2[TILE], sK3[TILE], sV2[TILE], sV3[TILE];      // of the parts alone
+  // The last columns of each map's q, KH - KEPT chunks of 16, lie in LDS: there are no registers for them, and spilled, their reloads in
+  // every turn would wait for the copies in front of them (4173 and 4096, 24 x 128, us: 702 -> 662; 32 of 450 234 -> 184)
+  constexpr int KEPT = D == 128 ? KH - (CAUSAL ? 2 : 1) : KH;
+  __shared__ __attribute__((aligned(1024))) char sPark[KEPT < KH ? 2 * (KH - KEPT) * 4096 : 16];
   __shared__ int s_ticket;
   static_assert(sizeof(__bf16) * TILE >= sizeof(int) * kThreads, "scan scratch must fit in a tile");
 
   const int T = a.cu[a.n_seq], H = a.H;
-  build_schedule<C::BM, kThreads, CAUSAL>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
+  const int n_items = build_schedule<C::BM, kThreads, false>(a.cu, a.n_seq, H, s_order, s_start, reinterpret_cast<int*>(&sK0[0]));
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // what follows from the lane is formed where it is used, from this one register: the loop has none to spare
   auto here = [&]() __attribute__((always_inline)) { int x = lane; asm volatile("" : "+v"(x)); return x; };
-  const float c = a.scale * kLog2e;
+  const float c = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.scale * kLog2e)));      // (a scalar register)
   const size_t row_stride = (size_t)H * D;
   const uint32_t row_bytes = (uint32_t)(row_stride * sizeof(__bf16));
   RowReaderX<D> k_rows;
@@ -198,22 +66,26 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   static_assert(4 * CP_ROWS % 16 == 0 && ROWS % (4 * CP_ROWS) == 0, "");
   const int cp_row = wave * CP_ROWS + lane / Tile<D>::CPR;
   const uint32_t cp_off = (uint32_t)cp_row * row_bytes + (uint32_t)Tile<D>::chunk_pos(cp_row, lane % Tile<D>::CPR) * 16u;
-  constexpr int SPLIT = CAUSAL ? 4 : 2;     // narrow items (64 queries) of a wide one
-  EvenQueue<SPLIT, 1> queue;
-  queue.init(a.counters);
-  if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
-  __syncthreads();
-  deal_even<C::BM, CAUSAL>(queue, a.cu, a.n_seq, s_order, s_start);
+  std::conditional_t<CAUSAL, StridedQueue, EvenQueue<0, 1>> queue;
+  if constexpr (CAUSAL) {
+    queue.init(a.counters, n_items);
+  } else {
+    queue.init(a.counters);
+    if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
+    __syncthreads();
+    deal_even<C::BM, false>(queue, a.cu, a.n_seq, s_order, s_start);
+  }
 
   int ticket = queue.first_ticket();
   while (ticket < queue.wide) {
-    const WorkItem it = decode_even<C::BM, CAUSAL>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
+    WorkItem it;
+    if constexpr (!CAUSAL) it = decode_even<C::BM, false>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
+    else it = decode_most_left<C::BM>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
     const int L = it.len, head = __builtin_amdgcn_readfirstlane(it.head);
-    const int other = (L + C::BM - 1) / C::BM - 1 - it.tile;     // CAUSAL: the pair of query tiles {other, tile}, the long one first
     const float lambda = a.lambda[head];
     unsigned next_ticket;      // thread 0 only
-    for (int sub = 0; sub < (CAUSAL && it.tile != other ? 2 : 1); ++sub) {
-      const int q_tile = __builtin_amdgcn_readfirstlane(!CAUSAL ? it.tile : sub == 0 ? other : it.tile);
+    {
+      const int q_tile = __builtin_amdgcn_readfirstlane(CAUSAL ? (L + C::BM - 1) / C::BM - 1 - it.tile : it.tile);
       const int q0 = q_tile * C::BM;
       const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
       const int n_half = (kv_end + ROWS - 1) / ROWS;
@@ -234,13 +106,19 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
       };
       copy(a.k, 0, sK0);       // a barrier stands between the last reads of the buffers and this
       const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
-      bf16x8 qf[C::KC];
+      bf16x8 qf[2][KEPT];
+      auto parked = [&](int m, int i) { return reinterpret_cast<bf16x8*>(sPark + 4096 * (m * (KH - KEPT) + i - KEPT) + 1024 * wave + 16 * here()); };
       {
         const int ln = here();
         const uint32_t off = (uint32_t)(32 * wave + (ln & 31)) * row_bytes + (uint32_t)(16 * (ln >> 5));
         const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
 #pragma unroll
-        for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
+        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+          for (int i = 0; i < KEPT; ++i) qf[m][i] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * (m * KH + i)));
+#pragma unroll
+          for (int i = KEPT; i < KH; ++i) *parked(m, i) = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * (m * KH + i)));
+        }
       }
       f32x16 o[2][DB];
       DiffSoftmax st[2];
@@ -282,9 +160,11 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
         sum = 0.f;
         if constexpr (PV && !QK) { value(0); value(1); KNAP_SCHED_FENCE(); }
         if constexpr (QK) {
+          bf16x8 last[KH];
 #pragma unroll
           for (int i = 0; i < KH; ++i) {
-            sn = mfma32(ak[i], qf[NEXT * KH + i], i == 0 ? zero16() : sn);
+            sn = mfma32(ak[i], i < KEPT ? qf[NEXT][i < KEPT ? i : 0] : last[i], i == 0 ? zero16() : sn);
+            if (i + 2 >= KEPT && i + 2 < KH) last[i + 2] = *parked(NEXT, i + 2);
             if (PV && i >= KH - 2) value(i - (KH - 2));
             form();
             KNAP_SCHED_FENCE();
@@ -323,7 +203,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
 #pragma unroll
           for (int i = 0; i < KH; ++i) keys(sK0, kb, 0, i);
 #pragma unroll
-          for (int i = 0; i < KH; ++i) s0 = mfma32(ak[i], qf[i], i == 0 ? zero16() : s0);
+          for (int i = 0; i < KH; ++i) s0 = mfma32(ak[i], i < KEPT ? qf[0][i < KEPT ? i : 0] : *parked(0, i), i == 0 ? zero16() : s0);
 #pragma unroll
           for (int i = 0; i < KH; ++i) keys(sK0, kb, 1, i);
         }
@@ -378,7 +258,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
           copy(a.v, h + 1, (h & 1) ? sV0 : sV1);
         }
       }
-      if (sub == 0 && queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
+      if (queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
 
       const int ln = here();
       const uint32_t off = (uint32_t)(32 * wave + (ln & 31)) * row_bytes + (uint32_t)(16 * (ln >> 5));
@@ -411,22 +291,6 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
     lds_barrier();
     ticket = __builtin_amdgcn_readfirstlane(s_ticket);
     lds_barrier();        // everyone has the ticket before the next one is put down
-  }
-  // few items, or those of a thin last round: in parts of 64 queries (EvenQueue::deal)
-  const DiffTiles tiles = {{sK0, sK1, sK2, sK3}, {sV0, sV1, sV2, sV3}};
-  for (int part = ticket - queue.wide; part >= 0 && part < queue.parts;) {
-    const WorkItem it = decode_even<C::BM, CAUSAL>(queue.item_of_part(part), queue, a.cu, a.n_seq, H, s_order, s_start);
-    const int head = __builtin_amdgcn_readfirstlane(it.head), other = (it.len + C::BM - 1) / C::BM - 1 - it.tile, sub = (part % SPLIT) >> 1;
-    const int q0 = __builtin_amdgcn_readfirstlane((CAUSAL && sub == 0 ? other : it.tile) * C::BM + 64 * (part & 1));
-    if (q0 < it.len && !(CAUSAL && sub == 1 && it.tile == other)) diff_fwd_part<D, CAUSAL>(a, tiles, it, head, q0, T, lane, wave);
-    if (!queue.draws) return;         // every part was a first ticket
-    if (tid == 0) {
-      const unsigned drawn = atomicAdd(queue.ctr, 1u);
-      s_ticket = drawn_ticket(queue, drawn);
-    }
-    lds_barrier();                    // (and the tiles are no longer read)
-    part = __builtin_amdgcn_readfirstlane(s_ticket) - queue.wide;
-    lds_barrier();                    // everyone has the ticket before it is drawn again
   }
 }
 
