@@ -65,13 +65,13 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
     // under the mask the query tiles with most keys first, as in the forward (pairs in even shares, us: 17 of 328 .. 4533, 6 x 128, 320 -> 265; 4 of
     // 4096 235 -> 194; 32 of 200 33 -> 24; 8000, 12 x 64, 305 -> 239; 17 of 328 .. 4533, 24 x 128, 1038 -> 1045)
     WorkItem it;
-    if constexpr (CAUSAL) it = decode_most_left<C::BM>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
+    if constexpr (CAUSAL) it = decode_most_left<C::BM, true>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
     else it = decode_even<C::BM, false>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
     const int L = it.len, head = __builtin_amdgcn_readfirstlane(it.head);
     const float lambda = a.lambda[head];
     unsigned next_ticket;      // thread 0 only
     {
-      const int q_tile = __builtin_amdgcn_readfirstlane(CAUSAL ? (L + C::BM - 1) / C::BM - 1 - it.tile : it.tile);
+      const int q_tile = __builtin_amdgcn_readfirstlane(it.tile);
       const int q0 = q_tile * C::BM, q_row = q0 + 32 * wave + l32;
       const bool q_valid = q_row < L;
       const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
@@ -529,7 +529,7 @@ __global__ __launch_bounds__(128 * PAIRS, 2) void diff_dkdv_kernel(DiffBwdArgs a
     // longest items first: by what is left of the sequence under the mask (tile by tile of one sequence after the other, us: 4 of 4096, 6 x 128,
     // 383 -> 325; 32 of 450, 12 x 128, 155 -> 142; 17 of 328 .. 4533, 12 x 64, 542 -> 522), by sequence without it
     const int w = queue.item(ticket);
-    const WorkItem it = CAUSAL ? decode_most_left<C::BN>(w, a.cu, a.n_seq, a.H, s_order, s_start)
+    const WorkItem it = CAUSAL ? decode_most_left<C::BN, false>(w, a.cu, a.n_seq, a.H, s_order, s_start)
                                : decode_tile_major<C::BN>(w, a.cu, a.n_seq, a.H, s_order, s_start);
     unsigned next_ticket;      // thread 0 only
     diff_dkdv_tile<D, PAIRS, CAUSAL>(a, r0, r1, r2, sP, sPark, me, it, it.head, it.tile, T, [&] {

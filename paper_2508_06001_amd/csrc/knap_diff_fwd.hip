@@ -80,12 +80,12 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   while (ticket < queue.wide) {
     WorkItem it;
     if constexpr (!CAUSAL) it = decode_even<C::BM, false>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
-    else it = decode_most_left<C::BM>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
+    else it = decode_most_left<C::BM, true>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
     const int L = it.len, head = __builtin_amdgcn_readfirstlane(it.head);
     const float lambda = a.lambda[head];
     unsigned next_ticket;      // thread 0 only
     {
-      const int q_tile = __builtin_amdgcn_readfirstlane(CAUSAL ? (L + C::BM - 1) / C::BM - 1 - it.tile : it.tile);
+      const int q_tile = __builtin_amdgcn_readfirstlane(it.tile);
       const int q0 = q_tile * C::BM;
       const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
       const int n_half = (kv_end + ROWS - 1) / ROWS;
