@@ -155,6 +155,28 @@ def test_rows_behind_the_last_sequence_and_other_sequences(d, causal):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_sequences_without_tokens_alone(d, causal):
+    """The host cannot see that there are none: pointers are there, and what they point at stays as it was, but for dlambda."""
+    import torch
+    import paper_2508_06001_amd as K
+    H, n = 3, 3
+    say(f"[gpu] diff without tokens d={d} causal={causal}")
+    rows = [torch.full((5, H, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(9)]
+    lse, lam, dlam = torch.full((64,), float("nan"), device="cuda"), torch.ones((H,), device="cuda"), torch.full((H,), float("nan"), device="cuda")
+    cu, ws = torch.zeros((n + 1,), dtype=torch.int32, device="cuda"), torch.zeros((256,), dtype=torch.uint8, device="cuda")
+    fwd, bwd = ((K.knap_varlen_diff_attn_causal_fwd, K.knap_varlen_diff_attn_causal_bwd) if causal
+                else (K.knap_varlen_diff_attn_fwd, K.knap_varlen_diff_attn_bwd))
+    q, k, v, out, out2, dout, dq, dk, dv = rows
+    fwd(q, k, v, cu, n, H, d, 0.1, lam, out, out2, lse)
+    bwd(q, k, v, cu, n, H, d, 0.1, lam, out, out2, lse, dout, dq, dk, dv, dlam, 0, ws)
+    torch.cuda.synchronize()
+    assert not bool(dlam.any())
+    assert all(bool(torch.isnan(t).all()) for t in rows + [lse])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
 def test_bad_values_that_the_mask_hides(d):
     """NaN and infinities in rows 700 of k and v, 300 of q and dout, and -inf scores, reach at most 127 rows that do not see them."""
