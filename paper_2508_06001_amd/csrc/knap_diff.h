@@ -15,6 +15,9 @@ struct DiffCfg {
   static constexpr int TILE_ELEMS = BN * Tile<D>::LD;
 };
 
+// workgroups a CU of the forward and of dQ, which their registers allow
+constexpr int diff_workgroups(int d) { return d == 64 ? 3 : 2; }
+
 // One map's softmax of a lane's query: the exponent reference (raw score units), it times c, and this lane's share of the row sum
 // (32 of every 64 keys).  The reference moves only when a half tile's probabilities against it are too large, as in the forward of plain
 // attention.

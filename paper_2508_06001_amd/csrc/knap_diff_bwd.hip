@@ -24,10 +24,10 @@ constexpr float kDiffDown = 1.0f / 32768.f;
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// dQ: the forward's structure.  S_m^T = K_m Q_m^T and dP^T = V dO^T put one query in each lane; dS_m^T is, unchanged, the operand of
+// dQ: plain attention's structure.  S_m^T = K_m Q_m^T and dP^T = V dO^T put one query in each lane; dS_m^T is, unchanged, the operand of
 // dQ_m^T += K_m^T dS_m^T with K^T read transposed from LDS.
 template <int D, bool CAUSAL>
-__global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
+__global__ __launch_bounds__(kThreads, diff_workgroups(D)) void diff_dq_kernel(DiffBwdArgs a) {
   using C = DiffCfg<D>;
   extern __shared__ int s_dyn[];
   int* s_order = s_dyn;
@@ -51,142 +51,132 @@ __global__ __launch_bounds__(kThreads, 2) void diff_dq_kernel(DiffBwdArgs a) {
   rows.init(lane);
   cols.init(lane);
   if (blockIdx.x == 0 && tid < 8) a.counters[tid] = 0u;      // of the launch behind this one
-  std::conditional_t<CAUSAL, StridedQueue, EvenQueue<0, 1>> queue;
-  if constexpr (CAUSAL) {
-    queue.init(a.dq_counters, n_items);
-  } else {
-    queue.init(a.dq_counters);
-    if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
-    __syncthreads();
-    deal_even<C::BM, false>(queue, a.cu, a.n_seq, s_order, s_start);
-  }
+  StridedQueue queue;
+  queue.init(a.dq_counters, n_items);
   int ticket = queue.first_ticket();
   while (ticket < queue.wide) {
     // under the mask the query tiles with most keys first, as in the forward (pairs in even shares, us: 17 of 328 .. 4533, 6 x 128, 320 -> 265; 4 of
     // 4096 235 -> 194; 32 of 200 33 -> 24; 8000, 12 x 64, 305 -> 239; 17 of 328 .. 4533, 24 x 128, 1038 -> 1045)
     WorkItem it;
     if constexpr (CAUSAL) it = decode_most_left<C::BM, true>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
-    else it = decode_even<C::BM, false>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
+    else it = decode_tile_major<C::BM>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
     const int L = it.len, head = __builtin_amdgcn_readfirstlane(it.head);
     const float lambda = a.lambda[head];
     unsigned next_ticket;      // thread 0 only
+    const int q_tile = __builtin_amdgcn_readfirstlane(it.tile), q0 = q_tile * C::BM, q_row = q0 + 32 * wave + l32;
+    const bool q_valid = q_row < L;
+    const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
+    const int n_tiles = (kv_end + C::BN - 1) / C::BN;
+    const int first_masked = CAUSAL ? 2 * q_tile : L / C::BN;
+    const int kv_lim = CAUSAL ? q_row + 1 : L;
+    const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
+    auto load_tile = [&](int t, __bf16* dK, __bf16* dV) {
+      const int kv0 = t * C::BN;
+      const uint32_t bytes = (uint32_t)max(0, min(kv_end - kv0, C::BN)) * row_bytes;
+      tile_load_async<D>(dK, make_rsrc(a.k + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, C::BN, wave, lane);
+      tile_load_async<D>(dV, make_rsrc(a.v + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, C::BN, wave, lane);
+    };
+    const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
+    const uint32_t off = (uint32_t)(32 * wave + l32) * row_bytes + (uint32_t)(16 * hh);
+    const size_t row_at = (size_t)head * T + it.row0 + (q_valid ? q_row : 0);
+    const size_t second = (size_t)H * T;
+    const float own_a = __builtin_fmaf(a.lse[row_at], kLog2e, -kDiffUp), own_b = __builtin_fmaf(a.lse[second + row_at], kLog2e, -kDiffUp);
+    // +inf for rows past the end: P = 0
+    const float lse_a = q_valid ? own_a : INFINITY, lse_b = q_valid ? own_b : INFINITY;
+    // One tensor after the other (knap_attn_dq.h).  The lane holds half of its query's columns, its partner at lane ^ 32 the other half.
+    bf16x8 qf[C::KC], dof[C::KC];
+    float nd1, nd2;
     {
-      const int q_tile = __builtin_amdgcn_readfirstlane(it.tile);
-      const int q0 = q_tile * C::BM, q_row = q0 + 32 * wave + l32;
-      const bool q_valid = q_row < L;
-      const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
-      const int n_tiles = (kv_end + C::BN - 1) / C::BN;
-      const int first_masked = CAUSAL ? 2 * q_tile : L / C::BN;
-      const int kv_lim = CAUSAL ? q_row + 1 : L;
-      const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
-      auto load_tile = [&](int t, __bf16* dK, __bf16* dV) {
-        const int kv0 = t * C::BN;
-        const uint32_t bytes = (uint32_t)max(0, min(kv_end - kv0, C::BN)) * row_bytes;
-        tile_load_async<D>(dK, make_rsrc(a.k + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, C::BN, wave, lane);
-        tile_load_async<D>(dV, make_rsrc(a.v + seq_at + (size_t)kv0 * row_stride, bytes), row_bytes, C::BN, wave, lane);
-      };
-      const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
-      const uint32_t off = (uint32_t)(32 * wave + l32) * row_bytes + (uint32_t)(16 * hh);
-      const size_t row_at = (size_t)head * T + it.row0 + (q_valid ? q_row : 0);
-      const size_t second = (size_t)H * T;
-      const float own_a = __builtin_fmaf(a.lse[row_at], kLog2e, -kDiffUp), own_b = __builtin_fmaf(a.lse[second + row_at], kLog2e, -kDiffUp);
-      // +inf for rows past the end: P = 0
-      const float lse_a = q_valid ? own_a : INFINITY, lse_b = q_valid ? own_b : INFINITY;
-      // One tensor after the other (knap_attn_dq.h).  The lane holds half of its query's columns, its partner at lane ^ 32 the other half.
-      bf16x8 qf[C::KC], dof[C::KC];
-      float nd1, nd2;
-      {
-        const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
-        const auto rd = make_rsrc(a.dout + seq_at + (size_t)q0 * row_stride, rows_bytes);
-        const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
-        const auto r2 = make_rsrc(a.out2 + seq_at + (size_t)q0 * row_stride, rows_bytes);
-        bf16x8 of[C::KC], o2[C::KC];
+      const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
+      const auto rd = make_rsrc(a.dout + seq_at + (size_t)q0 * row_stride, rows_bytes);
+      const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
+      const auto r2 = make_rsrc(a.out2 + seq_at + (size_t)q0 * row_stride, rows_bytes);
+      bf16x8 of[C::KC], o2[C::KC];
 #pragma unroll
-        for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
-        KNAP_SCHED_FENCE();
+      for (int cc = 0; cc < C::KC; ++cc) qf[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * cc));
+      KNAP_SCHED_FENCE();
 #pragma unroll
-        for (int cc = 0; cc < C::KC; ++cc) dof[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rd, off + 32u * cc));
-        KNAP_SCHED_FENCE();
+      for (int cc = 0; cc < C::KC; ++cc) dof[cc] = __builtin_bit_cast(bf16x8, buffer_load16(rd, off + 32u * cc));
+      KNAP_SCHED_FENCE();
 #pragma unroll
-        for (int cc = 0; cc < C::KC; ++cc) of[cc] = __builtin_bit_cast(bf16x8, buffer_load16(ro, off + 32u * cc));
-        KNAP_SCHED_FENCE();
+      for (int cc = 0; cc < C::KC; ++cc) of[cc] = __builtin_bit_cast(bf16x8, buffer_load16(ro, off + 32u * cc));
+      KNAP_SCHED_FENCE();
 #pragma unroll
-        for (int cc = 0; cc < C::KC; ++cc) o2[cc] = __builtin_bit_cast(bf16x8, buffer_load16(r2, off + 32u * cc));
-        KNAP_SCHED_FENCE();
-        load_tile(0, sK0, sV0);
-        KNAP_SCHED_FENCE();
-        const float d2_rounded = row_delta<D>(dof, o2);
-        nd1 = -__builtin_fmaf(lambda, d2_rounded, row_delta<D>(dof, of));
-        nd2 = -d2_rounded;
-      }
-      f32x16 acc[C::DB];
+      for (int cc = 0; cc < C::KC; ++cc) o2[cc] = __builtin_bit_cast(bf16x8, buffer_load16(r2, off + 32u * cc));
+      KNAP_SCHED_FENCE();
+      load_tile(0, sK0, sV0);
+      KNAP_SCHED_FENCE();
+      const float d2_rounded = row_delta<D>(dof, o2);
+      nd1 = -__builtin_fmaf(lambda, d2_rounded, row_delta<D>(dof, of));
+      nd2 = -d2_rounded;
+    }
+    f32x16 acc[C::DB];
 #pragma unroll
-      for (int db = 0; db < C::DB; ++db) acc[db] = zero16();
-      float d2 = 0.f;
-      wait_async_loads();
-      if (q_valid && hh == 0) {     // for the dK/dV kernel, behind the wait, which would wait for these stores as well
-        a.nd1[row_at] = nd1;
-        a.diff[row_at] = nd2 - nd1;
-        a.lse_a[row_at] = own_a;
-        a.lse_b[row_at] = own_b;
-      }
-      lds_barrier();
+    for (int db = 0; db < C::DB; ++db) acc[db] = zero16();
+    float d2 = 0.f;
+    wait_async_loads();
+    if (q_valid && hh == 0) {     // for the dK/dV kernel, behind the wait, which would wait for these stores as well
+      a.nd1[row_at] = nd1;
+      a.diff[row_at] = nd2 - nd1;
+      a.lse_a[row_at] = own_a;
+      a.lse_b[row_at] = own_b;
+    }
+    lds_barrier();
 
-      // MASKED: a tile that crosses the sequence's end or the diagonal.  Keys that a query does not see score -inf: rows past the end
-      // arrive as zeros, and exp2(-log-sum) of a score of zero may be infinite.  Halves that none of the wave's queries sees are left out.
-      auto tile = [&](auto masked_tag, int t, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) __attribute__((always_inline)) {
-        constexpr bool MASKED = decltype(masked_tag)::value;
-        load_tile(t + 1, nK, nV);
+    // MASKED: a tile that crosses the sequence's end or the diagonal.  Keys that a query does not see score -inf: rows past the end
+    // arrive as zeros, and exp2(-log-sum) of a score of zero may be infinite.  Halves that none of the wave's queries sees are left out.
+    auto tile = [&](auto masked_tag, int t, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) __attribute__((always_inline)) {
+      constexpr bool MASKED = decltype(masked_tag)::value;
+      load_tile(t + 1, nK, nV);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int k0 = t * C::BN + 32 * half;
-          if (MASKED && (k0 >= kv_end || (CAUSAL && k0 > q0 + 32 * wave + 31))) break;
-          f32x16 dp = zero16();
+      for (int half = 0; half < 2; ++half) {
+        const int k0 = t * C::BN + 32 * half;
+        if (MASKED && (k0 >= kv_end || (CAUSAL && k0 > q0 + 32 * wave + 31))) break;
+        f32x16 dp = zero16();
 #pragma unroll
-          for (int cc = 0; cc < C::KC; ++cc) dp = mfma32(rows.get(tV, 32 * half, cc), dof[cc], dp);
+        for (int cc = 0; cc < C::KC; ++cc) dp = mfma32(rows.get(tV, 32 * half, cc), dof[cc], dp);
 #pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            f32x16 s = zero16();
+        for (int m = 0; m < 2; ++m) {
+          f32x16 s = zero16();
 #pragma unroll
-            for (int cc = 0; cc < C::KC / 2; ++cc) s = mfma32(rows.get(tK, 32 * half, m * C::KC / 2 + cc), qf[m * C::KC / 2 + cc], s);
-            if constexpr (MASKED) mask_half(s, kv_lim - k0, hh);
-            float ds[16];
+          for (int cc = 0; cc < C::KC / 2; ++cc) s = mfma32(rows.get(tK, 32 * half, m * C::KC / 2 + cc), qf[m * C::KC / 2 + cc], s);
+          if constexpr (MASKED) mask_half(s, kv_lim - k0, hh);
+          float ds[16];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float p = fast_exp2(__builtin_fmaf(s[r], c, -(m == 0 ? lse_a : lse_b)));
-              if (m == 1) d2 = __builtin_fmaf(p, dp[r], d2);
-              ds[r] = p * (dp[r] + (m == 0 ? nd1 : nd2));
-            }
-            const bf16x8 x0 = pack8(ds[0], ds[1], ds[2], ds[3], ds[4], ds[5], ds[6], ds[7]);
-            const bf16x8 x1 = pack8(ds[8], ds[9], ds[10], ds[11], ds[12], ds[13], ds[14], ds[15]);
+          for (int r = 0; r < 16; ++r) {
+            const float p = fast_exp2(__builtin_fmaf(s[r], c, -(m == 0 ? lse_a : lse_b)));
+            if (m == 1) d2 = __builtin_fmaf(p, dp[r], d2);
+            ds[r] = p * (dp[r] + (m == 0 ? nd1 : nd2));
+          }
+          const bf16x8 x0 = pack8(ds[0], ds[1], ds[2], ds[3], ds[4], ds[5], ds[6], ds[7]);
+          const bf16x8 x1 = pack8(ds[8], ds[9], ds[10], ds[11], ds[12], ds[13], ds[14], ds[15]);
 #pragma unroll
-            for (int db = m * C::DB / 2; db < (m + 1) * C::DB / 2; ++db) {
-              acc[db] = mfma32(cols.get(tK, 32 * half, db), x0, acc[db]);
-              acc[db] = mfma32(cols.get(tK, 32 * half + 16, db), x1, acc[db]);
-            }
+          for (int db = m * C::DB / 2; db < (m + 1) * C::DB / 2; ++db) {
+            acc[db] = mfma32(cols.get(tK, 32 * half, db), x0, acc[db]);
+            acc[db] = mfma32(cols.get(tK, 32 * half + 16, db), x1, acc[db]);
           }
         }
-        wait_async_loads();
-        lds_barrier();
-      };
-      // (an even number of tiles in front of the masked ones under the mask, any otherwise)
-      const int n_plain = min(n_tiles, first_masked);
-      for (int t = 0; t < n_plain; t += 2) {
-        tile(std::false_type{}, t, sK0, sV0, sK1, sV1);
-        if (t + 1 < n_plain) tile(std::false_type{}, t + 1, sK1, sV1, sK0, sV0);
       }
-      for (int t = n_plain; t < n_tiles; ++t) {
-        const bool odd = t & 1;
-        tile(std::true_type{}, t, odd ? sK1 : sK0, odd ? sV1 : sV0, odd ? sK0 : sK1, odd ? sV0 : sV1);
-      }
-      if (queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
-      d2 += xor32(d2);
-      if (q_valid && hh == 0) a.d2[row_at] = d2 * kDiffDown;
-      const auto rg = make_rsrc(a.dq + seq_at + (size_t)q0 * row_stride, rows_bytes);
-#pragma unroll
-      for (int db = 0; db < C::DB; ++db)
-        store_block(rg, off + 64u * db, acc[db], db < C::DB / 2 ? a.scale * kDiffDown : -lambda * a.scale * kDiffDown);
+      wait_async_loads();
+      lds_barrier();
+    };
+    // (an even number of tiles in front of the masked ones under the mask, any otherwise)
+    const int n_plain = min(n_tiles, first_masked);
+    for (int t = 0; t < n_plain; t += 2) {
+      tile(std::false_type{}, t, sK0, sV0, sK1, sV1);
+      if (t + 1 < n_plain) tile(std::false_type{}, t + 1, sK1, sV1, sK0, sV0);
     }
+    for (int t = n_plain; t < n_tiles; ++t) {
+      const bool odd = t & 1;
+      tile(std::true_type{}, t, odd ? sK1 : sK0, odd ? sV1 : sV0, odd ? sK0 : sK1, odd ? sV0 : sV1);
+    }
+    if (queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
+    d2 += xor32(d2);
+    if (q_valid && hh == 0) a.d2[row_at] = d2 * kDiffDown;
+    const auto rg = make_rsrc(a.dq + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+    for (int db = 0; db < C::DB; ++db)
+      store_block(rg, off + 64u * db, acc[db], db < C::DB / 2 ? a.scale * kDiffDown : -lambda * a.scale * kDiffDown);
     if (!queue.draws) return;
     if (tid == 0) s_ticket = drawn_ticket(queue, next_ticket);
     lds_barrier();
@@ -554,7 +544,7 @@ static hipError_t launch_diff_dkdv_t(const DiffBwdArgs& a, int grid, hipStream_t
 template <int D, bool CAUSAL>
 static hipError_t launch_diff_bwd_t(const DiffBwdArgs& a, int tokens, int cus, hipStream_t stream) {
   const size_t dyn = (size_t)(2 * a.n_seq + 1) * sizeof(int);
-  hipLaunchKernelGGL((diff_dq_kernel<D, CAUSAL>), dim3(2 * cus), dim3(kThreads), dyn, stream, a);
+  hipLaunchKernelGGL((diff_dq_kernel<D, CAUSAL>), dim3(diff_workgroups(D) * cus), dim3(kThreads), dyn, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if constexpr (D == 64) return launch_diff_dkdv_t<64, 2, CAUSAL>(a, 2 * cus, stream);

@@ -29,8 +29,10 @@ namespace knap {
 // product of a slot waits for its arithmetic, nor the other way round; the stage whose sums a moving reference rescales is of the other
 // map than the one whose products run.  K runs half a tile ahead of V: a turn (two slots, one barrier) reads the keys of half h + 1 and
 // the values of half h, while the keys of h + 2 and the values of h + 1 are copied.
+// Workgroups a CU, two and three at d = 64, us: 16384, 12 heads, 1635 and 1393; 10 of 310 .. 6795, 48 heads, 2009 and 1906; 17 of 328 .. 4533, 12 heads, under
+// the mask, 302 and 269 (8000, 12 heads, 201 and 210: its longest items alone decide).
 template <int D, bool CAUSAL>
-__global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
+__global__ __launch_bounds__(kThreads, diff_workgroups(D)) void diff_fwd_kernel(DiffFwdArgs a) {
   using C = DiffCfg<D>;
   constexpr int KH = C::KC / 2, DB = C::DB, ROWS = 32, TILE = ROWS * Tile<D>::LD;
   extern __shared__ int s_dyn[];
@@ -66,226 +68,215 @@ __global__ __launch_bounds__(kThreads, 2) void diff_fwd_kernel(DiffFwdArgs a) {
   static_assert(4 * CP_ROWS % 16 == 0 && ROWS % (4 * CP_ROWS) == 0, "");
   const int cp_row = wave * CP_ROWS + lane / Tile<D>::CPR;
   const uint32_t cp_off = (uint32_t)cp_row * row_bytes + (uint32_t)Tile<D>::chunk_pos(cp_row, lane % Tile<D>::CPR) * 16u;
-  std::conditional_t<CAUSAL, StridedQueue, EvenQueue<0, 1>> queue;
-  if constexpr (CAUSAL) {
-    queue.init(a.counters, n_items);
-  } else {
-    queue.init(a.counters);
-    if (tid < 64) even_shares(queue, a.n_seq, s_start, lane);
-    __syncthreads();
-    deal_even<C::BM, false>(queue, a.cu, a.n_seq, s_order, s_start);
-  }
-
+  StridedQueue queue;
+  queue.init(a.counters, n_items);
   int ticket = queue.first_ticket();
   while (ticket < queue.wide) {
     WorkItem it;
-    if constexpr (!CAUSAL) it = decode_even<C::BM, false>(ticket, queue, a.cu, a.n_seq, H, s_order, s_start);
-    else it = decode_most_left<C::BM, true>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
+    if constexpr (CAUSAL) it = decode_most_left<C::BM, true>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
+    else it = decode_tile_major<C::BM>(queue.item(ticket), a.cu, a.n_seq, H, s_order, s_start);
     const int L = it.len, head = __builtin_amdgcn_readfirstlane(it.head);
     const float lambda = a.lambda[head];
     unsigned next_ticket;      // thread 0 only
-    {
-      const int q_tile = __builtin_amdgcn_readfirstlane(it.tile);
-      const int q0 = q_tile * C::BM;
-      const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
-      const int n_half = (kv_end + ROWS - 1) / ROWS;
-      // halves that this wave's queries see, none where its rows lie past the end: it then only copies; the last one is masked under the
-      // mask (its diagonal) and where the sequence ends in it
-      const int n_own = q0 + 32 * wave >= L ? 0 : CAUSAL ? min(n_half, q0 / ROWS + wave + 1) : n_half;
-      const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
-      auto copy = [&](const __bf16* src, int h, __bf16* dst) __attribute__((always_inline)) {
-        const int kv0 = h * ROWS;
-        const auto r = make_rsrc(src + seq_at + (size_t)kv0 * row_stride, (uint32_t)max(0, min(kv_end - kv0, ROWS)) * row_bytes);
+    const int q0 = __builtin_amdgcn_readfirstlane(it.tile) * C::BM;
+    const int kv_end = CAUSAL ? min(L, q0 + C::BM) : L;
+    const int n_half = (kv_end + ROWS - 1) / ROWS;
+    // halves that this wave's queries see, none where its rows lie past the end: it then only copies; the last one is masked under the
+    // mask (its diagonal) and where the sequence ends in it
+    const int n_own = q0 + 32 * wave >= L ? 0 : CAUSAL ? min(n_half, q0 / ROWS + wave + 1) : n_half;
+    const size_t seq_at = (size_t)it.row0 * row_stride + (size_t)head * D;
+    auto copy = [&](const __bf16* src, int h, __bf16* dst) __attribute__((always_inline)) {
+      const int kv0 = h * ROWS;
+      const auto r = make_rsrc(src + seq_at + (size_t)kv0 * row_stride, (uint32_t)max(0, min(kv_end - kv0, ROWS)) * row_bytes);
 #pragma unroll
-        for (int i = 0; i < ROWS / (4 * CP_ROWS); ++i) {
-          uint32_t o = cp_off;
-          if (i) asm volatile("" : "+v"(o));     // formed here, not kept in a register of its own through the loop
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(dst + (4 * i + wave) * CP_ROWS * Tile<D>::LD), 16,
-                                                   (int)(o + (uint32_t)(4 * i * CP_ROWS) * row_bytes), 0, 0, 0);
+      for (int i = 0; i < ROWS / (4 * CP_ROWS); ++i) {
+        uint32_t o = cp_off;
+        if (i) asm volatile("" : "+v"(o));     // formed here, not kept in a register of its own through the loop
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(dst + (4 * i + wave) * CP_ROWS * Tile<D>::LD), 16,
+                                                 (int)(o + (uint32_t)(4 * i * CP_ROWS) * row_bytes), 0, 0, 0);
+      }
+    };
+    copy(a.k, 0, sK0);       // a barrier stands between the last reads of the buffers and this
+    const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
+    bf16x8 qf[2][KEPT];
+    auto parked = [&](int m, int i) { return reinterpret_cast<bf16x8*>(sPark + 4096 * (m * (KH - KEPT) + i - KEPT) + 1024 * wave + 16 * here()); };
+    {
+      const int ln = here();
+      const uint32_t off = (uint32_t)(32 * wave + (ln & 31)) * row_bytes + (uint32_t)(16 * (ln >> 5));
+      const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) qf[m][i] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * (m * KH + i)));
+#pragma unroll
+        for (int i = KEPT; i < KH; ++i) *parked(m, i) = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * (m * KH + i)));
+      }
+    }
+    f32x16 o[2][DB];
+    DiffSoftmax st[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[m][db] = zero16();
+    wait_async_loads();
+    lds_barrier();
+    copy(a.v, 0, sV0);
+    copy(a.k, 1, sK1);
+
+    bf16x8 ak[KH];
+    auto keys = [&](const __bf16* tK, int kb, int m, int i) __attribute__((always_inline)) { ak[i] = k_rows.get(tK, kb, m * KH + i); };
+    // One slot: the scores sn of map NEXT (QK: its keys in `ak`), the probabilities pn of scores s against map NOW's reference (PR), the
+    // product of map NEXT's probabilities pb with the values tV (PV).  Groups of a product each, fences between them, so that the order
+    // below is the order issued; `behind(i)` goes into the groups of the second product.
+    auto slot = [&](auto qk_tag, auto pr_tag, auto pv_tag, auto next_tag, const f32x16& s, f32x16& sn, const bf16x8 (&pb)[2], bf16x8 (&pn)[2],
+                    const __bf16* tV, int vb, float& sum, auto behind) __attribute__((always_inline)) {
+      constexpr bool QK = decltype(qk_tag)::value, PR = decltype(pr_tag)::value, PV = decltype(pv_tag)::value;
+      constexpr int NEXT = decltype(next_tag)::value, NOW = 1 - NEXT;
+      constexpr int GROUPS = (QK ? KH : 0) + (PV ? 2 * DB : 0), PER = PR ? (16 + GROUPS - 1) / GROUPS : 0;
+      const float mc = st[NOW].mc;
+      float p[16];
+      int r = 0;
+      auto form = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          if (r < 16) {
+            p[r] = fast_exp2(__builtin_fmaf(s[r], c, -mc));
+            sum += p[r];
+            pn[r >> 3][r & 7] = (__bf16)p[r];
+          }
+          ++r;
         }
       };
-      copy(a.k, 0, sK0);       // a barrier stands between the last reads of the buffers and this
-      const uint32_t rows_bytes = (uint32_t)min(L - q0, C::BM) * row_bytes;
-      bf16x8 qf[2][KEPT];
-      auto parked = [&](int m, int i) { return reinterpret_cast<bf16x8*>(sPark + 4096 * (m * (KH - KEPT) + i - KEPT) + 1024 * wave + 16 * here()); };
-      {
-        const int ln = here();
-        const uint32_t off = (uint32_t)(32 * wave + (ln & 31)) * row_bytes + (uint32_t)(16 * (ln >> 5));
-        const auto rq = make_rsrc(a.q + seq_at + (size_t)q0 * row_stride, rows_bytes);
+      bf16x8 vt[2 * DB];
+      auto value = [&](int j) __attribute__((always_inline)) { vt[j] = v_cols.get(tV, vb, 16 * (j / DB), j % DB); };
+      sum = 0.f;
+      if constexpr (PV && !QK) { value(0); value(1); KNAP_SCHED_FENCE(); }
+      if constexpr (QK) {
+        bf16x8 last[KH];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-#pragma unroll
-          for (int i = 0; i < KEPT; ++i) qf[m][i] = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * (m * KH + i)));
-#pragma unroll
-          for (int i = KEPT; i < KH; ++i) *parked(m, i) = __builtin_bit_cast(bf16x8, buffer_load16(rq, off + 32u * (m * KH + i)));
+        for (int i = 0; i < KH; ++i) {
+          sn = mfma32(ak[i], i < KEPT ? qf[NEXT][i < KEPT ? i : 0] : last[i], i == 0 ? zero16() : sn);
+          if (i + 2 >= KEPT && i + 2 < KH) last[i + 2] = *parked(NEXT, i + 2);
+          if (PV && i >= KH - 2) value(i - (KH - 2));
+          form();
+          KNAP_SCHED_FENCE();
         }
       }
-      f32x16 o[2][DB];
-      DiffSoftmax st[2];
+      if constexpr (PV) {
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+        for (int j = 0; j < 2 * DB; ++j) {
+          o[NEXT][j % DB] = mfma32(vt[j], pb[j / DB], o[NEXT][j % DB]);
+          if (j + 2 < 2 * DB) value(j + 2);
+          behind(j);
+          form();
+          KNAP_SCHED_FENCE();
+        }
+      }
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    constexpr std::integral_constant<int, 0> map0{};
+    constexpr std::integral_constant<int, 1> map1{};
+    f32x16 s0, s1;            // scores of the maps
+    bf16x8 pb0[2], pb1[2];    // their probabilities
+    auto nothing = [](int) {};
+    const bool masked = CAUSAL || (n_own == n_half && kv_end % ROWS != 0);
+    auto mask = [&](f32x16& s, int h) __attribute__((always_inline)) {
+      if (masked && h == n_own - 1) {
+        const int ln = here();
+        mask_half(s, (CAUSAL ? q0 + 32 * wave + (ln & 31) + 1 : L) - h * ROWS, ln >> 5);
+      }
+      KNAP_SCHED_FENCE();
+    };
+    if (n_own > 0) {
+      float sum;
+      {
+        const int kb = k_rows.fresh();
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[m][db] = zero16();
+        for (int i = 0; i < KH; ++i) keys(sK0, kb, 0, i);
+#pragma unroll
+        for (int i = 0; i < KH; ++i) s0 = mfma32(ak[i], i < KEPT ? qf[0][i < KEPT ? i : 0] : *parked(0, i), i == 0 ? zero16() : s0);
+#pragma unroll
+        for (int i = 0; i < KH; ++i) keys(sK0, kb, 1, i);
+      }
+      mask(s0, 0);
+      slot(yes, yes, no, map1, s0, s1, pb1, pb0, sV0, 0, sum, nothing);
+      st[0].template settle<DB>(s0, c, sum, pb0, o[0]);
+      mask(s1, 0);
+    }
+    // the second map of half h and the first of half h + 1 go through the softmax
+    auto turn = [&](int h, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) __attribute__((always_inline)) {
       wait_async_loads();
       lds_barrier();
-      copy(a.v, 0, sV0);
-      copy(a.k, 1, sK1);
-
-      bf16x8 ak[KH];
-      auto keys = [&](const __bf16* tK, int kb, int m, int i) __attribute__((always_inline)) { ak[i] = k_rows.get(tK, kb, m * KH + i); };
-      // One slot: the scores sn of map NEXT (QK: its keys in `ak`), the probabilities pn of scores s against map NOW's reference (PR), the
-      // product of map NEXT's probabilities pb with the values tV (PV).  Groups of a product each, fences between them, so that the order
-      // below is the order issued; `behind(i)` goes into the groups of the second product.
-      auto slot = [&](auto qk_tag, auto pr_tag, auto pv_tag, auto next_tag, const f32x16& s, f32x16& sn, const bf16x8 (&pb)[2], bf16x8 (&pn)[2],
-                      const __bf16* tV, int vb, float& sum, auto behind) __attribute__((always_inline)) {
-        constexpr bool QK = decltype(qk_tag)::value, PR = decltype(pr_tag)::value, PV = decltype(pv_tag)::value;
-        constexpr int NEXT = decltype(next_tag)::value, NOW = 1 - NEXT;
-        constexpr int GROUPS = (QK ? KH : 0) + (PV ? 2 * DB : 0), PER = PR ? (16 + GROUPS - 1) / GROUPS : 0;
-        const float mc = st[NOW].mc;
-        float p[16];
-        int r = 0;
-        auto form = [&]() __attribute__((always_inline)) {
+      const int kb = k_rows.fresh(), vb = v_cols.fresh();
 #pragma unroll
-          for (int e = 0; e < PER; ++e) {
-            if (r < 16) {
-              p[r] = fast_exp2(__builtin_fmaf(s[r], c, -mc));
-              sum += p[r];
-              pn[r >> 3][r & 7] = (__bf16)p[r];
-            }
-            ++r;
-          }
-        };
-        bf16x8 vt[2 * DB];
-        auto value = [&](int j) __attribute__((always_inline)) { vt[j] = v_cols.get(tV, vb, 16 * (j / DB), j % DB); };
-        sum = 0.f;
-        if constexpr (PV && !QK) { value(0); value(1); KNAP_SCHED_FENCE(); }
-        if constexpr (QK) {
-          bf16x8 last[KH];
-#pragma unroll
-          for (int i = 0; i < KH; ++i) {
-            sn = mfma32(ak[i], i < KEPT ? qf[NEXT][i < KEPT ? i : 0] : last[i], i == 0 ? zero16() : sn);
-            if (i + 2 >= KEPT && i + 2 < KH) last[i + 2] = *parked(NEXT, i + 2);
-            if (PV && i >= KH - 2) value(i - (KH - 2));
-            form();
-            KNAP_SCHED_FENCE();
-          }
-        }
-        if constexpr (PV) {
-#pragma unroll
-          for (int j = 0; j < 2 * DB; ++j) {
-            o[NEXT][j % DB] = mfma32(vt[j], pb[j / DB], o[NEXT][j % DB]);
-            if (j + 2 < 2 * DB) value(j + 2);
-            behind(j);
-            form();
-            KNAP_SCHED_FENCE();
-          }
-        }
-      };
-      constexpr std::true_type yes{};
-      constexpr std::false_type no{};
-      constexpr std::integral_constant<int, 0> map0{};
-      constexpr std::integral_constant<int, 1> map1{};
-      f32x16 s0, s1;            // scores of the maps
-      bf16x8 pb0[2], pb1[2];    // their probabilities
-      auto nothing = [](int) {};
-      const bool masked = CAUSAL || (n_own == n_half && kv_end % ROWS != 0);
-      auto mask = [&](f32x16& s, int h) __attribute__((always_inline)) {
-        if (masked && h == n_own - 1) {
-          const int ln = here();
-          mask_half(s, (CAUSAL ? q0 + 32 * wave + (ln & 31) + 1 : L) - h * ROWS, ln >> 5);
-        }
-        KNAP_SCHED_FENCE();
-      };
-      if (n_own > 0) {
-        float sum;
-        {
-          const int kb = k_rows.fresh();
-#pragma unroll
-          for (int i = 0; i < KH; ++i) keys(sK0, kb, 0, i);
-#pragma unroll
-          for (int i = 0; i < KH; ++i) s0 = mfma32(ak[i], i < KEPT ? qf[0][i < KEPT ? i : 0] : *parked(0, i), i == 0 ? zero16() : s0);
-#pragma unroll
-          for (int i = 0; i < KH; ++i) keys(sK0, kb, 1, i);
-        }
-        mask(s0, 0);
-        slot(yes, yes, no, map1, s0, s1, pb1, pb0, sV0, 0, sum, nothing);
-        st[0].template settle<DB>(s0, c, sum, pb0, o[0]);
-        mask(s1, 0);
-      }
-      // the second map of half h and the first of half h + 1 go through the softmax
-      auto turn = [&](int h, const __bf16* tK, const __bf16* tV, __bf16* nK, __bf16* nV) __attribute__((always_inline)) {
-        wait_async_loads();
-        lds_barrier();
-        const int kb = k_rows.fresh(), vb = v_cols.fresh();
-#pragma unroll
-        for (int i = 0; i < KH; ++i) keys(tK, kb, 0, i);
-        copy(a.k, h + 2, nK);
-        copy(a.v, h + 1, nV);
-        float sum;
-        slot(yes, yes, yes, map0, s1, s0, pb0, pb1, tV, vb, sum, [&](int j) __attribute__((always_inline)) { if (j >= 2 * DB - KH) keys(tK, kb, 1, j - (2 * DB - KH)); });
-        st[1].template settle<DB>(s1, c, sum, pb1, o[1]);
-        mask(s0, h + 1);
-        slot(yes, yes, yes, map1, s0, s1, pb1, pb0, tV, vb, sum, nothing);
-        st[0].template settle<DB>(s0, c, sum, pb0, o[0]);
-        mask(s1, h + 1);
-      };
-      int h = 0;
-      for (; h < n_own - 1; h += 2) {
-        turn(h, sK1, sV0, sK0, sV1);
-        if (h + 2 < n_own) turn(h + 1, sK0, sV1, sK1, sV0);
-      }
-      h = max(n_own - 1, 0);
-      // the last half's second map, and its products; then, and for waves without rows from the start, the others' turns: copies alone
+      for (int i = 0; i < KH; ++i) keys(tK, kb, 0, i);
+      copy(a.k, h + 2, nK);
+      copy(a.v, h + 1, nV);
+      float sum;
+      slot(yes, yes, yes, map0, s1, s0, pb0, pb1, tV, vb, sum, [&](int j) __attribute__((always_inline)) { if (j >= 2 * DB - KH) keys(tK, kb, 1, j - (2 * DB - KH)); });
+      st[1].template settle<DB>(s1, c, sum, pb1, o[1]);
+      mask(s0, h + 1);
+      slot(yes, yes, yes, map1, s0, s1, pb1, pb0, tV, vb, sum, nothing);
+      st[0].template settle<DB>(s0, c, sum, pb0, o[0]);
+      mask(s1, h + 1);
+    };
+    int h = 0;
+    for (; h < n_own - 1; h += 2) {
+      turn(h, sK1, sV0, sK0, sV1);
+      if (h + 2 < n_own) turn(h + 1, sK0, sV1, sK1, sV0);
+    }
+    h = max(n_own - 1, 0);
+    // the last half's second map, and its products; then, and for waves without rows from the start, the others' turns: copies alone
+    wait_async_loads();
+    lds_barrier();
+    if (h + 1 < n_half) {
+      copy(a.k, h + 2, (h & 1) ? sK1 : sK0);
+      copy(a.v, h + 1, (h & 1) ? sV0 : sV1);
+    }
+    if (n_own > 0) {
+      const __bf16* tV = (h & 1) ? sV1 : sV0;
+      const int vb = v_cols.fresh();
+      float sum;
+      slot(no, yes, yes, map0, s1, s0, pb0, pb1, tV, vb, sum, nothing);
+      st[1].template settle<DB>(s1, c, sum, pb1, o[1]);
+      slot(no, no, yes, map1, s0, s1, pb1, pb0, tV, vb, sum, nothing);
+    }
+    for (++h; h < n_half; ++h) {
       wait_async_loads();
       lds_barrier();
       if (h + 1 < n_half) {
         copy(a.k, h + 2, (h & 1) ? sK1 : sK0);
         copy(a.v, h + 1, (h & 1) ? sV0 : sV1);
       }
-      if (n_own > 0) {
-        const __bf16* tV = (h & 1) ? sV1 : sV0;
-        const int vb = v_cols.fresh();
-        float sum;
-        slot(no, yes, yes, map0, s1, s0, pb0, pb1, tV, vb, sum, nothing);
-        st[1].template settle<DB>(s1, c, sum, pb1, o[1]);
-        slot(no, no, yes, map1, s0, s1, pb1, pb0, tV, vb, sum, nothing);
-      }
-      for (++h; h < n_half; ++h) {
-        wait_async_loads();
-        lds_barrier();
-        if (h + 1 < n_half) {
-          copy(a.k, h + 2, (h & 1) ? sK1 : sK0);
-          copy(a.v, h + 1, (h & 1) ? sV0 : sV1);
-        }
-      }
-      if (queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
-
-      const int ln = here();
-      const uint32_t off = (uint32_t)(32 * wave + (ln & 31)) * row_bytes + (uint32_t)(16 * (ln >> 5));
-      float inv[2];
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const float l = st[m].l + xor32(st[m].l);
-        inv[m] = 1.0f / l;
-        const auto rl = make_rsrc(a.lse + ((size_t)m * H + head) * T + it.row0 + q0, (uint32_t)min(L - q0, C::BM) * 4u);
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, st[m].m_ref * a.scale + __logf(l)), rl,
-                                              ln < 32 ? (32 * wave + ln) * 4 : 4 * C::BM, 0, 0);
-      }
-      const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        f32x16 x;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = o[0][db][r] * inv[0] - lambda * (o[1][db][r] * inv[1]);
-        store_block(ro, off + 64u * db, x, 1.0f);
-      }
-      if (a.out2) {
-        const auto r2 = make_rsrc(a.out2 + seq_at + (size_t)q0 * row_stride, rows_bytes);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) store_block(r2, off + 64u * db, o[1][db], inv[1]);
-      }
-      lds_barrier();        // nobody reads a tile any longer
     }
+    if (queue.draws && tid == 0) next_ticket = atomicAdd(queue.ctr, 1u);
+
+    const int ln = here();
+    const uint32_t off = (uint32_t)(32 * wave + (ln & 31)) * row_bytes + (uint32_t)(16 * (ln >> 5));
+    float inv[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float l = st[m].l + xor32(st[m].l);
+      inv[m] = 1.0f / l;
+      const auto rl = make_rsrc(a.lse + ((size_t)m * H + head) * T + it.row0 + q0, (uint32_t)min(L - q0, C::BM) * 4u);
+      __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, st[m].m_ref * a.scale + __logf(l)), rl,
+                                            ln < 32 ? (32 * wave + ln) * 4 : 4 * C::BM, 0, 0);
+    }
+    const auto ro = make_rsrc(a.out + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      f32x16 x;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = o[0][db][r] * inv[0] - lambda * (o[1][db][r] * inv[1]);
+      store_block(ro, off + 64u * db, x, 1.0f);
+    }
+    if (a.out2) {
+      const auto r2 = make_rsrc(a.out2 + seq_at + (size_t)q0 * row_stride, rows_bytes);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store_block(r2, off + 64u * db, o[1][db], inv[1]);
+    }
+    lds_barrier();        // nobody reads a tile any longer
     if (!queue.draws) return;
     if (tid == 0) s_ticket = drawn_ticket(queue, next_ticket);
     lds_barrier();
@@ -298,7 +289,7 @@ template <int D>
 static hipError_t launch_diff_fwd_t(const DiffFwdArgs& a, bool causal, int cus, hipStream_t stream) {
   const size_t dyn = (size_t)(2 * a.n_seq + 1) * sizeof(int);
   auto* kernel = causal ? diff_fwd_kernel<D, true> : diff_fwd_kernel<D, false>;
-  hipLaunchKernelGGL(kernel, dim3(2 * cus), dim3(kThreads), dyn, stream, a);
+  hipLaunchKernelGGL(kernel, dim3(diff_workgroups(D) * cus), dim3(kThreads), dyn, stream, a);
   return hipGetLastError();
 }
 
