@@ -120,7 +120,7 @@ def _check(code: int, where: str) -> None:
 
 def _ptr(t) -> int:
     """Device (or host) address of a tensor; None -> NULL."""
-    return 0 if t is None else int(t.data_ptr())
+    return 0 if t is None else t.data_ptr()
 
 
 # The current stream's handle without a Stream object around it, which costs more than the rest of a call's marshalling: 2.8 us
@@ -455,28 +455,29 @@ def _rows(where: str, name: str, t, shape, dtype=None) -> int:
     return t.stride(0)
 
 
-def _vector(where: str, name: str, t, n: int, dtype=None) -> None:
-    if t is None:
-        return
-    if t.numel() != n or not t.is_contiguous() or (t.dtype not in _KNAP_TYPES if dtype is None else t.dtype is not dtype):
+def _vector(where: str, name: str, t, n: int, dtype) -> int:
+    """The address of a vector of n values, checked."""
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         _refuse(where, f"{name} is a contiguous vector of {n} values of its type")
+    return t.data_ptr()
 
 
 def knap_layer_norm_fwd(x, weight, bias, eps: float, y, mean=None, rstd=None, stream=None, check: bool = True) -> int:
     """y = (x - mean) rstd weight + bias of every row of x (rows, width); weight and bias (of one type) may be None."""
     where = "knap_layer_norm_fwd"
     _here(where, x, weight, bias, y, mean, rstd)
-    shape = x.shape
+    shape, types, f32 = x.shape, _KNAP_TYPES, torch.float32
     xs, ys = _rows(where, "x", x, shape), _rows(where, "y", y, shape)
     rows, width = shape
-    _vector(where, "weight", weight, width)
-    _vector(where, "bias", bias, width, None if weight is None else weight.dtype)
-    _vector(where, "mean", mean, rows, torch.float32)
-    _vector(where, "rstd", rstd, rows, torch.float32)
-    w = weight if weight is not None else bias
-    rc = lib.knap_layer_norm_fwd(_ptr(x), _KNAP_TYPES[x.dtype], xs, rows, width, _ptr(weight), _ptr(bias),
-                                 KNAP_F32 if w is None else _KNAP_TYPES[w.dtype], eps, _ptr(y), _KNAP_TYPES[y.dtype], ys, _ptr(mean),
-                                 _ptr(rstd), _stream_handle(stream))
+    w_type = f32 if weight is None and bias is None else (bias if weight is None else weight).dtype
+    if w_type not in types:
+        _refuse(where, "the type of weight and bias")
+    w_at = 0 if weight is None else _vector(where, "weight", weight, width, w_type)
+    b_at = 0 if bias is None else _vector(where, "bias", bias, width, w_type)
+    mean_at = 0 if mean is None else _vector(where, "mean", mean, rows, f32)
+    rstd_at = 0 if rstd is None else _vector(where, "rstd", rstd, rows, f32)
+    rc = lib.knap_layer_norm_fwd(x.data_ptr(), types[x.dtype], xs, rows, width, w_at, b_at, types[w_type], eps, y.data_ptr(), types[y.dtype], ys,
+                                 mean_at, rstd_at, _stream_handle(stream))
     if check:
         _check(rc, where)
     return rc
@@ -491,17 +492,21 @@ def knap_layer_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace
     """dx (of x's type), dweight and dbias (fp32, or None) of knap_layer_norm_fwd, whose mean and rstd it takes."""
     where = "knap_layer_norm_bwd"
     _here(where, x, weight, mean, rstd, dy, dx, dweight, dbias, workspace)
-    shape = x.shape
+    shape, types, f32 = x.shape, _KNAP_TYPES, torch.float32
     xs, dys, dxs = _rows(where, "x", x, shape), _rows(where, "dy", dy, shape), _rows(where, "dx", dx, shape, x.dtype)
     rows, width = shape
-    _vector(where, "weight", weight, width)
-    for name, t, n in (("mean", mean, rows), ("rstd", rstd, rows), ("dweight", dweight, width), ("dbias", dbias, width)):
-        _vector(where, name, t, n, torch.float32)
+    w_type = f32 if weight is None else weight.dtype
+    if w_type not in types:
+        _refuse(where, "the type of weight")
+    w_at = 0 if weight is None else _vector(where, "weight", weight, width, w_type)
+    dw_at = 0 if dweight is None else _vector(where, "dweight", dweight, width, f32)
+    db_at = 0 if dbias is None else _vector(where, "dbias", dbias, width, f32)
+    mean_at = 0 if mean is None else _vector(where, "mean", mean, rows, f32)
+    rstd_at = 0 if rstd is None else _vector(where, "rstd", rstd, rows, f32)
     if workspace_bytes is None:
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib.knap_layer_norm_bwd(_ptr(x), _KNAP_TYPES[x.dtype], xs, rows, width, _ptr(weight),
-                                 KNAP_F32 if weight is None else _KNAP_TYPES[weight.dtype], _ptr(mean), _ptr(rstd), _ptr(dy),
-                                 _KNAP_TYPES[dy.dtype], dys, _ptr(dx), dxs, _ptr(dweight), _ptr(dbias), _ptr(workspace), workspace_bytes,
+    rc = lib.knap_layer_norm_bwd(x.data_ptr(), types[x.dtype], xs, rows, width, w_at, types[w_type], mean_at, rstd_at, dy.data_ptr(), types[dy.dtype],
+                                 dys, dx.data_ptr(), dxs, dw_at, db_at, 0 if workspace is None else workspace.data_ptr(), workspace_bytes,
                                  _stream_handle(stream))
     if check:
         _check(rc, where)
