@@ -12,6 +12,11 @@
 //   diff_dkdv_kernel    dK, dV; behind its items dlambda, one workgroup a head, in a fixed order
 // Probabilities are carried times 2^15 (the log-sums are stored that much smaller), which fp16 holds with 11 bits down to 2^-29: so
 // that the waves that form dK get them from the waves that form dV with no rounding worth counting.  The results' factors take it out.
+//
+// What bounds them: vector arithmetic beside the matrix units (7.8 vector instructions a matrix one; these busy 42 % of the time in dQ, 51 % in
+// dK/dV).  Measured, dQ and dK/dV, us (TFLOP/s of their 6 and 8 L^2 d): 16384, 3 x 128, 750 (820) and 960 (860, on 192 of 256 CUs); 17 of
+// 328 .. 4533 under the mask, 6 x 128, 258 (790) and 361 (750), 24 x 128, 1018 (800) and 1427 (760); 16384, 12 x 64, 1520 (810) and 2966 (560: a
+// step's vector work is that of d = 128 for half the matrix work, at two waves a SIMD); 37 .. 311, 2 x 64, 13 and 17.
 #include "knap_attn_dkdv.h"
 #include "knap_attn_dq.h"
 #include "knap_diff.h"
