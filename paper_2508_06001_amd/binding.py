@@ -313,7 +313,9 @@ def _diff_tensors(where: str, cu_seqlens, n_seq, bf16, f32) -> None:
 def _diff_fwd(fn, where: str, q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse, stream, check) -> int:
     _here(where, q, k, v, cu_seqlens, lam, out, out2, lse)
     n = q.numel()
-    _diff_tensors(where, cu_seqlens, n_seq, ((q, n), (k, n), (v, n), (out, n), (out2, n)), ((lam, H), (lse, 0)))
+    # the kernel writes 2 H T log-sums, T = cu_seqlens[n_seq], which the host cannot see: room for all rows, or the shape that a padded bag's has
+    room = 0 if lse is not None and lse.dim() == 3 and lse.shape[0] == 2 and lse.shape[1] == H else 2 * H * q.shape[0]
+    _diff_tensors(where, cu_seqlens, n_seq, ((q, n), (k, n), (v, n), (out, n), (out2, n)), ((lam, H), (lse, room)))
     rc = fn(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), n_seq, H, d, scale, _ptr(lam), _ptr(out), _ptr(out2), _ptr(lse), _stream_handle(stream))
     if check:
         _check(rc, where)
@@ -322,7 +324,8 @@ def _diff_fwd(fn, where: str, q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out,
 
 def knap_varlen_diff_attn_fwd(q, k, v, cu_seqlens, n_seq: int, H: int, d: int, scale: float, lam, out, out2, lse, stream=None,
                               check: bool = True) -> int:
-    """Enqueue the forward of differential attention.  q, k, v, out, out2 (or None): bf16 (T, H, d); lam: fp32 (H,); lse: fp32 (2, H, T)."""
+    """Enqueue the forward of differential attention.  q, k, v, out, out2 (or None): bf16 (T, H, d); lam: fp32 (H,); lse: fp32 (2, H, T), where
+    the tensors may have more rows than T = cu_seqlens[n_seq] (a padded bag), or any contiguous fp32 tensor of 2 H values a row."""
     return _diff_fwd(lib.knap_varlen_diff_attn_fwd, "knap_varlen_diff_attn_fwd", q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse,
                      stream, check)
 
