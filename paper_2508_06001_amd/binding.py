@@ -299,23 +299,31 @@ _KNAP_TYPES = {torch.bfloat16: KNAP_BF16, torch.float32: KNAP_F32}
 
 # --------------------------------------------------------------------------- differential attention
 
-def _diff_tensors(where: str, cu_seqlens, n_seq, bf16, f32) -> None:
+def _diff_tensors(where: str, cu_seqlens, n_seq, H, d, rows, f32) -> int:
+    """How many rows the tensors have, q first among them, checked; f32: vectors and the least that each holds."""
     if cu_seqlens is not None and (cu_seqlens.dtype is not torch.int32 or cu_seqlens.numel() <= n_seq or not cu_seqlens.is_contiguous()):
         _refuse(where, "cu_seqlens is a contiguous int32 tensor of n_seq + 1 entries")
-    for t, shape in bf16:
-        if t is not None and (t.dtype is not torch.bfloat16 or t.numel() != shape or not t.is_contiguous()):
+    shape = () if rows[0] is None else rows[0].shape
+    T, bf16 = shape[0] if shape else -1, torch.bfloat16
+    shapes = ((T, H, d), (T, H * d))
+    if shape not in shapes:
+        _refuse(where, "q is a (T, H, d) tensor")
+    for t in rows:
+        if t is not None and (t.dtype is not bf16 or not t.is_contiguous() or (t.shape != shape and t.shape not in shapes)):
             _refuse(where, "q, k, v, the outputs and their gradients are contiguous bf16 (T, H, d) tensors")
     for t, n in f32:
         if t is not None and (t.dtype is not torch.float32 or t.numel() < n or not t.is_contiguous()):
             _refuse(where, "lambda and dlambda are contiguous fp32 (H,) tensors, lse is an fp32 (2, H, T) one")
+    return T
 
 
 def _diff_fwd(fn, where: str, q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse, stream, check) -> int:
     _here(where, q, k, v, cu_seqlens, lam, out, out2, lse)
-    n = q.numel()
-    # the kernel writes 2 H T log-sums, T = cu_seqlens[n_seq], which the host cannot see: room for all rows, or the shape that a padded bag's has
-    room = 0 if lse is not None and lse.dim() == 3 and lse.shape[0] == 2 and lse.shape[1] == H else 2 * H * q.shape[0]
-    _diff_tensors(where, cu_seqlens, n_seq, ((q, n), (k, n), (v, n), (out, n), (out2, n)), ((lam, H), (lse, room)))
+    T = _diff_tensors(where, cu_seqlens, n_seq, H, d, (q, k, v, out, out2), ((lam, H), (lse, 0)))
+    # the kernel writes 2 H log-sums for each token of the bag, whose number the host cannot see: room for all rows, or the shape that a
+    # padded bag's has
+    if lse is not None and lse.numel() < 2 * H * T and (lse.dim() != 3 or lse.shape[0] != 2 or lse.shape[1] != H):
+        _refuse(where, "lse is an fp32 (2, H, T) tensor")
     rc = fn(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), n_seq, H, d, scale, _ptr(lam), _ptr(out), _ptr(out2), _ptr(lse), _stream_handle(stream))
     if check:
         _check(rc, where)
@@ -344,10 +352,8 @@ def knap_varlen_diff_attn_bwd_workspace_bytes(total_tokens: int, n_seq: int, H: 
 def _diff_bwd(fn, where: str, q, k, v, cu_seqlens, n_seq, H, d, scale, lam, out, out2, lse, dout, dq, dk, dv, dlam, total_tokens, workspace,
               workspace_bytes, stream, check) -> int:
     _here(where, q, k, v, cu_seqlens, lam, out, out2, lse, dout, dq, dk, dv, dlam, workspace)
-    n = q.numel()
-    _diff_tensors(where, cu_seqlens, n_seq, [(t, n) for t in (q, k, v, out, out2, dout, dq, dk, dv)],
-                  ((lam, H), (dlam, H), (lse, 2 * H * total_tokens)))
-    if total_tokens * H * d > n:
+    T = _diff_tensors(where, cu_seqlens, n_seq, H, d, (q, k, v, out, out2, dout, dq, dk, dv), ((lam, H), (dlam, H), (lse, 2 * H * total_tokens)))
+    if total_tokens > T:
         _refuse(where, "total_tokens is more than the tensors hold")
     if workspace_bytes is None:
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()

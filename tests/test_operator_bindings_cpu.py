@@ -46,3 +46,21 @@ def test_log_sums_of_differential_attention_have_room(calls, fn, backward):
         with pytest.raises(K.KnapError):
             fn(**{**diff_args(rows, backward), "lse": lse})
     assert len(calls) == 4
+
+
+@pytest.mark.parametrize("fn,backward", DIFF)
+def test_rows_of_differential_attention_are_of_h_heads_of_d(calls, fn, backward):
+    """The kernels go by H and d: tensors of other heads, of another d, of another order or with fewer rows are refused."""
+    fn(**diff_args(backward=backward))
+    flat = diff_args(backward=backward)
+    fn(**{n: t.view(T, H * d) if torch.is_tensor(t) and t.dim() == 3 and t.dtype is torch.bfloat16 else t for n, t in flat.items()})
+    assert len(calls) == 2
+    wrong = [dict(H=3), dict(H=1), dict(d=128), dict(H=1, d=128), dict(H=4, d=32), dict(H=2 * H, lam=torch.zeros((2 * H,))), dict(q=None)]
+    names = ["k", "v", "out", "out2"] + (["dout", "dq", "dk", "dv"] if backward else [])
+    for n in names:
+        wrong += [{n: torch.zeros((T - 1, H, d), dtype=torch.bfloat16)}, {n: torch.zeros((H, T, d), dtype=torch.bfloat16)},
+                  {n: torch.zeros((T, d, H), dtype=torch.bfloat16)}]
+    for w in wrong:
+        with pytest.raises(K.KnapError):
+            fn(**{**diff_args(backward=backward), **w})
+    assert len(calls) == 2
