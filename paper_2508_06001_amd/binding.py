@@ -407,8 +407,9 @@ def _rope(fn, where: str, q, k, rot, layout, freq, factor, q_out, k_out, positio
         _refuse(where, "freq is a contiguous float64 tensor of rot / 2 entries")
     n_axes, pairs, n_seq, pos_at, cu_at = 0, None, 0, 0, 0
     if positions is not None:
-        n_axes = 1 if positions.dim() == 1 else positions.shape[-1]
-        if positions.dtype is not torch.int32 or positions.numel() != T * n_axes or positions.shape[0] != T or not positions.is_contiguous():
+        n_axes = 1 if positions.dim() == 1 else positions.shape[-1] if positions.dim() else 0
+        # (none: no address, which the library takes for no positions given)
+        if n_axes < 1 or positions.dtype is not torch.int32 or positions.numel() != T * n_axes or positions.shape[0] != T or not positions.is_contiguous():
             _refuse(where, "positions is a contiguous int32 (tokens,) or (tokens, axes) tensor")
         pos_at = positions.data_ptr()
         if axis_pairs:

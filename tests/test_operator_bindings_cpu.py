@@ -64,3 +64,20 @@ def test_rows_of_differential_attention_are_of_h_heads_of_d(calls, fn, backward)
         with pytest.raises(K.KnapError):
             fn(**{**diff_args(backward=backward), **w})
     assert len(calls) == 2
+
+
+@pytest.mark.parametrize("fn", [K.knap_rope_fwd, K.knap_rope_bwd])
+def test_rotary_positions_have_an_axis(calls, fn):
+    """A tensor of positions without an axis has no address, which the library takes for none given: nothing would be turned."""
+    x = torch.zeros((T, H, d), dtype=torch.bfloat16)
+    call = lambda pos, **kw: fn(x, None, d, K.KNAP_ROPE_HALF, torch.ones((d // 2,), dtype=torch.float64), 1.0, torch.empty_like(x), None,  # noqa: E731
+                                positions=pos, stream=0, **kw)
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    call(ints(T))
+    call(ints(T, 1))
+    call(ints(T, 2), axis_pairs=[16, 16])
+    assert len(calls) == 3
+    for wrong in (ints(T, 0), ints(), ints(T, 2, 0)):
+        with pytest.raises(K.KnapError):
+            call(wrong)
+    assert len(calls) == 3
