@@ -89,7 +89,7 @@ struct RopeArgs {
   const double* freq;
   float factor, sign;      // sign: of the sine
   bool copies;             // columns from rot on go to another tensor
-  int tokens_per_group;    // set by the launch
+  int tokens_per_group, first_group;    // set by the launch
 };
 hipError_t launch_rope(RopeArgs a, bool half, bool aligned, int cus, hipStream_t stream);
 

@@ -20,6 +20,9 @@ namespace {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeMaxTokens = 8;        // of a workgroup
+// workgroups of a launch.  A grid's threads are counted in 32 bits: one of 2^32 and more is taken modulo 2^32, with no error
+constexpr int64_t kRopeMostGroups = ((int64_t)1 << 24) - 1;
+static_assert(kRopeMostGroups * kRopeThreads < (int64_t)1 << 32, "");
 
 // number of boundaries of the bag in front of token t, as the first row of its sequence: the largest boundary not behind t; -1 for
 // rows at or behind the last boundary, which belong to no sequence.  By one wave.
@@ -73,7 +76,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
   extern __shared__ float2 s_trig[];                 // (tokens, pairs)
   __shared__ int s_first[kRopeMaxTokens];
   const int tid = threadIdx.x, pairs = a.rot / 2;
-  const int t0 = (int)blockIdx.x * a.tokens_per_group;
+  const int t0 = (a.first_group + (int)blockIdx.x) * a.tokens_per_group;
   const int n_tok = min(a.tokens_per_group, a.T - t0);
   const uint32_t heads = (uint32_t)(a.H + a.Hk);
 
@@ -203,14 +206,20 @@ hipError_t launch_rope(RopeArgs a, bool half, bool aligned, int cus, hipStream_t
   const int64_t per_tok = (int64_t)(a.H + a.Hk) * (form == kPairs ? a.d : units);
   // tokens of a workgroup: enough units that its threads have three or four each, but not so many that the CUs run out of workgroups
   int tokens = (int)std::max<int64_t>(1, std::min<int64_t>(kRopeMaxTokens, 4 * kRopeThreads / per_tok));
-  while (tokens > 1 && (a.T + tokens - 1) / tokens < 4 * cus) tokens /= 2;
+  while (tokens > 1 && ((int64_t)a.T + tokens - 1) / tokens < 4 * cus) tokens /= 2;
   a.tokens_per_group = tokens;
   size_t lds = (size_t)tokens * (a.rot / 2) * sizeof(float2);
   if (form == kStaged) lds = (lds + 15) / 16 * 16 + kStageColumns * sizeof(__bf16);
   auto* kernel = half ? (form == kUnits ? rope_kernel<true, kUnits> : form == kStaged ? rope_kernel<true, kStaged> : rope_kernel<true, kPairs>)
                       : (form == kUnits ? rope_kernel<false, kUnits> : form == kStaged ? rope_kernel<false, kStaged> : rope_kernel<false, kPairs>);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((a.T + (int64_t)tokens - 1) / tokens)), dim3(kRopeThreads), lds, stream, a);
-  return hipGetLastError();
+  const int64_t groups = ((int64_t)a.T + tokens - 1) / tokens;
+  for (int64_t first = 0; first < groups; first += kRopeMostGroups) {
+    a.first_group = (int)first;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(groups - first, kRopeMostGroups)), dim3(kRopeThreads), lds, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace knap

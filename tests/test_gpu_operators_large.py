@@ -101,3 +101,35 @@ def test_layer_norm(width):
     # sums of n terms (the other rows add zeros) in any order: n 2^-24 of the sum of their magnitudes, and xh off by 2^-20
     for got, terms in ((dw, e * xh), (db, e)):
         assert np.all(np.abs(f64(got) - terms.sum(0)) <= (n * 2.0 ** -24 + 2.0 ** -18) * np.abs(terms).sum(0) + 1e-6)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,d,rot,odd,given", [((1 << 27) + 11, 8, 8, False, False), ((1 << 24) + 5, 520, 2, True, True)])
+def test_rotary_positions_of_more_tokens_than_one_grid_takes(tokens, d, rot, odd, given):
+    """Eight tokens a workgroup, and one (rows on 2 bytes): more workgroups of 256 threads than 2^32 threads make.  In place, every row;
+    the bar is that of test_gpu_rope.py."""
+    import torch
+    import paper_2508_06001_amd as K
+    say(f"[gpu] large rope tokens={tokens} d={d} rot={rot} odd={odd} given={given}")
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    pad = 1 if odd else 0
+    flat = torch.full((tokens * d + pad,), 3.0, dtype=torch.bfloat16, device="cuda")
+    x = flat[pad:].view(tokens, 1, d)
+    head = torch.randn((tokens, rot), generator=g, dtype=torch.bfloat16, device="cuda")
+    x[:, 0, :rot] = head
+    pos = torch.randint(0, 1 << 30, (tokens,), generator=g, dtype=torch.int32, device="cuda") if given else None
+    freq, factor = K.knap_rope_frequencies(rot)
+    rope = K.RotaryPositions(rot, K.KNAP_ROPE_INTERLEAVED, freq, factor, positions=pos, cu_seqlens=None if given else [0, tokens])
+    rope.forward(x, None, x, None)
+    torch.cuda.synchronize()
+    f = torch.tensor(freq, dtype=torch.float64, device="cuda")
+    for i in range(0, tokens, 1 << 24):
+        rows = slice(i, min(tokens, i + (1 << 24)))
+        p = (pos[rows] if given else torch.arange(rows.start, rows.stop, device="cuda")).double()
+        ang = p[:, None] * f
+        a, b = head[rows, 0::2].double(), head[rows, 1::2].double()
+        near = (a.abs() + b.abs()) * (1e-6 + ang * 2.0 ** -51)
+        got = x[rows, 0, :rot].double()
+        for y, ref in ((got[:, 0::2], a * ang.cos() - b * ang.sin()), (got[:, 1::2], a * ang.sin() + b * ang.cos())):
+            assert bool(((y - ref).abs() <= near + 2.0 ** -8 * (ref.abs() + near)).all()), i
+    assert bool((x[:, 0, rot:] == 3.0).all())
