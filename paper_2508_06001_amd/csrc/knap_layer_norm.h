@@ -8,6 +8,7 @@
 
 #include "knap_device.h"
 #include "knap_kernels.h"
+#include "knap_row_span.h"
 
 #include <type_traits>
 
@@ -64,25 +65,21 @@ struct RowRaw {
 template <class C, class T>
 struct RowPlace {
   __amdgpu_buffer_rsrc_t r;
-  uint32_t off, end;      // byte offsets of the row and behind it
-  __device__ __forceinline__ RowPlace(const T* base, int64_t stride, int64_t row0, int group, int64_t rows, int width) {
+  RowSpan span;
+  static constexpr uint32_t SIZE = sizeof(T);
+  __device__ __forceinline__ RowPlace(const T* base, int64_t stride, int64_t row0, int group, int64_t rows, int width)
+      : span(C::LANES >= 64 ? 0 : group, C::LANES >= 64 ? 1 : min((int64_t)C::GROUPS, rows - row0), stride, width, SIZE) {
     if constexpr (C::LANES >= 64) {
       const int64_t row = row0 + __builtin_amdgcn_readfirstlane(group);
-      r = make_rsrc(base + row * stride, row < rows ? (uint32_t)width * (uint32_t)sizeof(T) : 0u);
-      off = 0;
-      end = (uint32_t)width * (uint32_t)sizeof(T);
-    } else {              // the rows of all groups, at most 2^22 columns apart, or the form is not taken: offsets of 16 of them in 32 bits
-      const int64_t left = min((int64_t)C::GROUPS, rows - row0);
-      r = make_rsrc(base + row0 * stride, left > 0 ? (uint32_t)((left - 1) * stride + width) * (uint32_t)sizeof(T) : 0u);
-      off = (uint32_t)group * (uint32_t)stride * (uint32_t)sizeof(T);
-      end = group < left ? off + (uint32_t)width * (uint32_t)sizeof(T) : 0u;
+      r = make_rsrc(base + row * stride, row < rows ? (uint32_t)width * SIZE : 0u);
+    } else {              // the rows of all groups, at most 2^22 columns apart, or the form is not taken
+      r = make_rsrc(base + row0 * stride, RowSpan::bytes(min((int64_t)C::GROUPS, rows - row0), stride, width, SIZE));
     }
   }
   // the byte offset of column c, or one behind everything for columns that the row does not have
   __device__ __forceinline__ int at(int c) const {
-    const uint32_t o = off + (uint32_t)c * (uint32_t)sizeof(T);
-    if constexpr (C::LANES >= 64) return (int)o;
-    else return o < end ? (int)o : 0x7ffffff0;
+    if constexpr (C::LANES >= 64) return c * (int)SIZE;
+    else return span.at((uint32_t)c * SIZE);
   }
 };
 
