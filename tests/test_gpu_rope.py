@@ -315,3 +315,60 @@ def test_the_binding_refuses_what_the_library_cannot_see():
                            (x, torch.empty_like(x), dict(positions=pos.view(4, 1, 1).expand(4, 1, 2).contiguous()))):
         with pytest.raises(K.KnapError):
             K.knap_rope_fwd(q, None, q_out=q_out, k_out=None, **{**ok, **more})
+
+
+def transposed(x, y, g, r, factor):
+    """Rows in which <R x, g> = <x, R^T g> holds for y = R x and r = R^T g, each rounded to bf16.  A rounding moves a term by at most 2^-8 of it;
+    taken as independent, of either sign, a sum of such terms leaves six times the root of their squares' sum with a probability of
+    2 exp(-18).  Before the rounding a pair is off by 10^-6 of its two values (the head of this file), which the last term bounds for all."""
+    a, b = y * g, x * r
+    bar = 6 * 2.0 ** -8 * np.sqrt((a * a).sum(-1) + (b * b).sum(-1)) + 4e-6 * abs(factor) * np.sqrt((x * x).sum(-1) * (g * g).sum(-1))
+    return np.abs(a.sum(-1) - b.sum(-1)) <= bar
+
+
+FACTOR = 1.25
+
+
+def wrong_backwards(x, g, pos, freq, rot, half):
+    """Gradients as backwards would give them that are not the transpose."""
+    turned = lambda sign, f=FACTOR: rope_ref(g, pos, freq, f, rot, half, sign)[0]  # noqa: E731
+    rng = np.random.default_rng(12)
+    return {"the forward's sign": turned(1.0), "not turned": g, "the factor alone": FACTOR * g, "without the factor": turned(-1.0, 1.0),
+            "factor's inverse": turned(-1.0, 1.0 / FACTOR), "the other layout": rope_ref(g, pos, freq, FACTOR, rot, not half, -1.0)[0],
+            "one position on": rope_ref(g, pos + 1, freq, FACTOR, rot, half, -1.0)[0], "nothing": 0 * g, "noise": rng.standard_normal(g.shape)}
+
+
+@pytest.mark.parametrize("half", [True, False])
+def test_what_the_transpose_check_catches(half):
+    """The formula, rounded, passes in every row; a backward that is anything else fails in some."""
+    import torch
+    rng = np.random.default_rng(5)
+    bf16 = lambda t: f64(torch.from_numpy(np.ascontiguousarray(t)).bfloat16())  # noqa: E731
+    T, H, d, rot = 200, 4, 64, 48
+    x, g = bf16(rng.standard_normal((T, H, d))), bf16(rng.standard_normal((T, H, d)))
+    pos = np.repeat(np.concatenate([np.arange(77), np.arange(123)])[:, None], rot // 2, 1)
+    freq = 10000.0 ** (-2.0 * np.arange(rot // 2) / rot)
+    y = bf16(rope_ref(x, pos, freq, FACTOR, rot, half)[0])
+    assert transposed(x, y, g, bf16(rope_ref(g, pos, freq, FACTOR, rot, half, -1.0)[0]), FACTOR).all()
+    for name, r in wrong_backwards(x, g, pos, freq, rot, half).items():
+        caught = 1.0 - transposed(x, y, g, bf16(r), FACTOR).mean()
+        assert caught > 0.2, (name, caught)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("T,H,Hk,d,rot,given", [(200, 4, 4, 128, 128, False), (200, 4, 2, 64, 48, False), (131, 3, 1, 64, 20, True), (97, 2, 2, 10, 6, True)])
+def test_backward_is_the_transpose_in_every_row(T, H, Hk, d, rot, given, half):
+    import torch
+    import paper_2508_06001_amd as K
+    say(f"[gpu] rope transpose T={T} H={H}/{Hk} d={d} rot={rot} given={given} half={half}")
+    g = torch.Generator(device="cuda").manual_seed(T + rot)
+    q, k, gq, gk = (torch.randn((T, h, d), generator=g, device="cuda").bfloat16() for h in (H, Hk, H, Hk))
+    at = dict(positions=torch.randint(0, 5000, (T,), generator=g, device="cuda", dtype=torch.int32)) if given else dict(cu_seqlens=[0, 77, 77, T])
+    rope = K.RotaryPositions(rot, K.KNAP_ROPE_HALF if half else K.KNAP_ROPE_INTERLEAVED, K.knap_rope_frequencies(rot)[0], FACTOR, **at)
+    q_out, k_out, rq, rk = (torch.empty_like(t) for t in (q, k, q, k))
+    rope.forward(q, k, q_out, k_out)
+    rope.backward(gq, gk, rq, rk)
+    torch.cuda.synchronize()
+    for x, y, e, r in ((q, q_out, gq, rq), (k, k_out, gk, rk)):
+        assert transposed(f64(x), f64(y), f64(e), f64(r), FACTOR).all()
