@@ -79,7 +79,8 @@ extern "C" {
  * take 12288 sets in rotation: calls
  * from several threads and on several streams may overlap freely as long as no
  * eager forward call on a device runs beside one that came 4096 or more such
- * calls later.  Results of calls that break this are undefined, those of calls
+ * calls later.  Calls of differential attention, its backward too, count as
+ * forward calls here: they take sets of the same rotation.  Results of calls that break this are undefined, those of calls
  * 12288 later are not: every 4096th call clears the sets of the 4096 to 8191
  * after it (a small launch of its own).
  * A launch recorded under stream capture takes one of 4096 other sets
@@ -184,6 +185,8 @@ int knap_varlen_attn_causal_bwd(const void* q, const void* k, const void* v,
  *   out2     bf16 (T, H, d): O_2, which the backward takes; NULL in the forward where no backward
  *            follows.
  *   lse      fp32 (2, H, T): the log-sums of map 1, then of map 2.
+ *   dq, dk, dv: a probability of less than 2^-40 counts as zero in dk and, where it is the first map's, in dv (the kernel
+ *            hands them on in 16 bits, times 2^15, of which 11 are right down to 2^-29): a key that no query pays more has dk = 0.
  *   dlambda  fp32[H] = -sum over rows of dout . O_2, summed in 32 bits over the probabilities
  *            as they are, in a fixed order; zeros where total_tokens is 0 and n_seq is not.  Not
  *            the array of lambda.
@@ -275,7 +278,7 @@ int knap_ulysses_scatter_chunks(const void* z, const int32_t* row_map, int64_t t
  * gradients back through it: the same call with -sin.
  *
  * q (tokens, H, d) -> q_out, k (tokens, H_k, d) -> k_out, bf16, d fastest; both in one
- * launch.  H_k = 0: q alone (k and k_out are not looked at).  strides: NULL for
+ * launch (from 2^24 tokens on in several, each of its share of the tokens).  H_k = 0: q alone (k and k_out are not looked at).  strides: NULL for
  * contiguous tensors, else a HOST array of eight strides in elements: of a token and
  * of a head in q, k, q_out, k_out.  Strides of inputs are 0 or larger; rows of an
  * output must not overlap (either the heads of a token lie between two tokens, or the
