@@ -14,9 +14,12 @@
 // that the waves that form dK get them from the waves that form dV with no rounding worth counting.  The results' factors take it out.
 //
 // What bounds them: vector arithmetic beside the matrix units (7.8 vector instructions a matrix one; these busy 42 % of the time in dQ, 51 % in
-// dK/dV).  Measured, dQ and dK/dV, us (TFLOP/s of their 6 and 8 L^2 d): 16384, 3 x 128, 750 (820) and 960 (860, on 192 of 256 CUs); 17 of
-// 328 .. 4533 under the mask, 6 x 128, 258 (790) and 361 (750), 24 x 128, 1018 (800) and 1427 (760); 16384, 12 x 64, 1520 (810) and 2966 (560: a
-// step's vector work is that of d = 128 for half the matrix work, at two waves a SIMD); 37 .. 311, 2 x 64, 13 and 17.
+// dK/dV).  Measured at a settled clock (the first passes of a run take 5 to 20 % longer), dQ and dK/dV, us (TFLOP/s of their 6 and 8 L^2 d):
+// 16384, 3 x 128, 710 (870) and 883 (930, on 192 of 256 CUs); 17 of 328 .. 4533 under the mask, 6 x 128, 250 (810) and 359 (750), 24 x 128, 1029 (790)
+// and 1444 (750); 16384, 12 x 64, 1529 (810) and 3076 (540: a step's vector work is that of d = 128 for half the matrix work, at two waves a
+// SIMD); 37 .. 311, 2 x 64, 14 and 17.
+// No register is spilled in the loops over tiles: what the compiler puts aside (three values in the dK/dV kernel of four pairs, one in dQ at
+// d = 128) it stores and reloads once an item, the ticket among it, or once a launch.
 #include "knap_attn_dkdv.h"
 #include "knap_attn_dq.h"
 #include "knap_diff.h"

@@ -8,9 +8,9 @@
 // in all, where four calls of plain attention (two maps, two halves of the values) would take 8.
 //
 // What bounds it: two exponentials a score pair where plain attention has one, beside 24 matrix instructions a half of 32 keys and wave;
-// 7.4 vector instructions a matrix one, the matrix units busy 57 % of the time.  Measured, us (TFLOP/s): 4173 and 4096, 24 x 128, 620 (1010); 17 of
-// 328 .. 4533 under the mask, 6 x 128, 227 (890), 24 x 128, 870 (930); 16384, 3 x 128, 653 (950, on the 75 % of the workgroups that have an
-// item); 37 .. 311, 2 x 64, 11.
+// 7.4 vector instructions a matrix one, the matrix units busy 57 % of the time.  Measured at a settled clock (the first passes of a run take
+// 5 to 20 % longer), us (TFLOP/s): 4173 and 4096, 24 x 128, 622 (1010); 17 of 328 .. 4533 under the mask, 6 x 128, 219 (920), 24 x 128, 876 (920);
+// 16384, 3 x 128, 653 (950, on the 75 % of the workgroups that have an item); 16384, 12 x 64, 1309 (940); 37 .. 311, 2 x 64, 11.
 // Under the mask items are single query tiles, those with most keys first, drawn one by one (pairs of a long and a short tile in even shares, as
 // plain attention has them, us: 17 of 328 .. 4533, 6 x 128, 255 -> 231; 4 of 4096 200 -> 170; 32 of 200, 6 x 128, 28 -> 19; 8000, 12 x 64, 260 -> 203;
 // the longest items alone decide for 16384, 3 x 128, 433 -> 473).  Parts of 64 queries for few items, as plain attention has them, cost more

