@@ -187,6 +187,9 @@ int knap_varlen_attn_causal_bwd(const void* q, const void* k, const void* v,
  *   lse      fp32 (2, H, T): the log-sums of map 1, then of map 2.
  *   dq, dk, dv: a probability of less than 2^-40 counts as zero in dk and, where it is the first map's, in dv (the kernel
  *            hands them on in 16 bits, times 2^15, of which 11 are right down to 2^-29): a key that no query pays more has dk = 0.
+ *            The first map's row sums dout . O_1 are formed from out and lambda out2, each rounded to bf16: errors of that map's dq and
+ *            dk grow with |lambda|.  Where |scale q . k| passes 2^21, the rounding of a log-sum alone may move a probability
+ *            to more than two, which 16 bits do not hold: dk and dv may then not be finite.
  *   dlambda  fp32[H] = -sum over rows of dout . O_2, summed in 32 bits over the probabilities
  *            as they are, in a fixed order; zeros where total_tokens is 0 and n_seq is not.  Not
  *            the array of lambda.
