@@ -385,6 +385,105 @@ int knap_layer_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t row
                         void* workspace, size_t workspace_bytes, void* stream);
 size_t knap_layer_norm_bwd_workspace_bytes(int64_t rows, int width);
 
+/* ------------------------------------------------------------------------
+ * The norms on both sides of a branch (attention, feed-forward), its gate and
+ * residual scale, and the modulation in front of the next branch, in one pass
+ * over the rows of a packed bag.  With gate, scale and shift of the row's sequence:
+ *     fh = N_post(f),  x' = x + alpha gate (fh w_post),  xh = N(x'),
+ *     y = xh w (1 + scale) + shift
+ * post_norm and norm, each one of
+ *     KNAP_NORM_NONE   fh = f; as norm: there is no y (a block's last residual)
+ *     KNAP_NORM_RMS    v rstd, rstd = 1 / sqrt(mean(v^2) + eps)
+ *     KNAP_NORM_LAYER  (v - mean) rstd, rstd = 1 / sqrt(var + eps)
+ * f NULL: there is no branch (a block's first norm), x' = x, and x_out, gate, post_weight
+ * and post_norm are not given.  backward, from dx_out (the gradient that x' has from elsewhere,
+ * NULL for none) and dy (NULL where norm is none):
+ *     g = dy (1 + scale) w,  X = dx_out + rstd (g - [mean g] - xh mean(g xh)),  dx = X,
+ *     e = alpha gate w_post X,  df = rstd_post (e - [mean e] - fh mean(e fh))   ([]: layer norm;
+ *     df = e without a post norm)
+ *     dshift = sum dy,  dscale = w sum dy xh,  dgate = alpha w_post sum X fh    (rows of a sequence)
+ *     dweight = sum (1 + scale) dy xh,  dpost_weight = alpha sum gate X fh      (all rows)
+ *
+ * x, x_out, dx_out, dx (rows, width): x_type, KNAP_BF16 or KNAP_F32.  f, y, df, dy (rows, width):
+ * branch_type, the same or KNAP_BF16.  Columns are contiguous; strides count elements from a row to the
+ * next, >= width (not looked at for a single row, nor for tensors that are not given).
+ * cu_seqlens: device int32[n_seq + 1] as for attention; rows from cu_seqlens[n_seq] on (a padded
+ * bag) are left as they were.  NULL: one sequence of all rows (n_seq = 1).
+ * gate, scale, shift (n_seq, width): mod_type; gate_stride of gate, mod_stride of scale and shift
+ * count elements from a sequence to the next, >= 0 (chunks of one projection's (n_seq, 6 width)
+ * result as they lie).  NULL for ones, zeros, zeros.  weight, post_weight: `width` values of w_type, NULL for ones.
+ * x' is normed as it is before its rounding to x_type, and the backward forms it again from x and f.
+ * Sums and statistics are 32-bit.  stats: fp32 (4, rows): mean and rstd of x', then of f; rows of it whose
+ * norm there is not are not touched; NULL in the forward where no backward follows, in the backward where there are no norms.
+ * dgate, dscale, dshift: fp32 (n_seq, width), strides dgate_stride and dmod_stride >= width;
+ * dweight, dpost_weight: fp32[width].  Any of them, dx and df may be NULL: not wanted.  The sums are
+ * fully overwritten (zeros for a sequence without rows) and added up in a fixed order: the same call on
+ * the same device gives the same bits.  workspace: knap_residual_norm_bwd_workspace_bytes(rows, width, n_seq)
+ * bytes, 256-byte aligned, needed where one of the sums is wanted; one for each call that may run at the same time.
+ * x_out may be x and dx may be dx_out (in place, same stride; the backward takes x as it was); otherwise
+ * outputs must not alias inputs or each other.  Pointers need the alignment of their type only; 16 bytes, strides and
+ * widths that are multiples of 8 give the fast form.
+ *
+ * Supported: 1 <= width <= KNAP_LAYER_NORM_MAX_WIDTH, 0 <= rows < 2^31, n_seq <= KNAP_MAX_SEQS, eps finite and >= 0
+ * (a row of zeros, in a layer norm a constant one, with eps = 0 gives NaN), alpha finite.  Values that are not finite stay in their row
+ * but for the sums.  rows = 0 enqueues nothing in the forward and zeros in the sums in the backward.  As for the
+ * forward of attention, the first call of the library on a device must not be captured.
+ * ------------------------------------------------------------------------ */
+#define KNAP_NORM_NONE  0
+#define KNAP_NORM_RMS   1
+#define KNAP_NORM_LAYER 2
+
+int knap_residual_norm_fwd(const void* x, int x_type, int64_t x_stride, int64_t rows, int width,
+                           const void* f, int branch_type, int64_t f_stride,
+                           const int32_t* cu_seqlens, int n_seq,
+                           const void* gate, int64_t gate_stride,
+                           const void* scale, const void* shift, int64_t mod_stride, int mod_type,
+                           const void* post_weight, const void* weight, int w_type,
+                           int post_norm, int norm, float alpha, float eps,
+                           void* x_out, int64_t x_out_stride, void* y, int64_t y_stride,
+                           float* stats, void* stream);
+int knap_residual_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t rows, int width,
+                           const void* f, int branch_type, int64_t f_stride,
+                           const int32_t* cu_seqlens, int n_seq,
+                           const void* gate, int64_t gate_stride, const void* scale, int64_t mod_stride, int mod_type,
+                           const void* post_weight, const void* weight, int w_type,
+                           int post_norm, int norm, float alpha, const float* stats,
+                           const void* dx_out, int64_t dx_out_stride, const void* dy, int64_t dy_stride,
+                           void* dx, int64_t dx_stride, void* df, int64_t df_stride,
+                           float* dgate, int64_t dgate_stride, float* dscale, float* dshift, int64_t dmod_stride,
+                           float* dweight, float* dpost_weight,
+                           void* workspace, size_t workspace_bytes, void* stream);
+size_t knap_residual_norm_bwd_workspace_bytes(int64_t rows, int width, int n_seq);
+
+/* ------------------------------------------------------------------------
+ * The global norm of a list of gradients, and clipping by it: the end of a training step.
+ *     sum_sq = sum over all tensors of g^2,  norm = sqrt(sum_sq),
+ *     c = min(1, max_norm / (norm + eps)),  out = c g
+ * Two calls, so that ranks that hold parts of the gradients can add up their sum_sq (an
+ * all-reduce of one double) between them.
+ *
+ * grads, out: HOST arrays of n device pointers, numel and types HOST arrays of n (KNAP_BF16 or KNAP_F32); all are read
+ * before the call returns.  A tensor is numel contiguous values, aligned to its type; 16 bytes give the fast form.  numel
+ * may be 0 (the pointer is not looked at then).  out[i] has the type of grads[i] and may be grads[i] itself (in place, which
+ * writes nothing where c is 1); otherwise a part of out that overlaps another one or a gradient is refused, and with it a
+ * list that has a tensor twice, which would be scaled twice.
+ * sum_sq: device double, the sum in 64 bits in a fixed order, so that the same call gives the same bits; it does not
+ * overflow for any finite gradients.  workspace: knap_grad_sum_squares_workspace_bytes(n) bytes, 256-byte aligned, one for each
+ * call that may run at the same time.
+ * norm (device fp32, or NULL) is written by knap_grad_clip (infinity where 32 bits do not hold it; c is right there too).  A sum_sq that is not finite gives what the formula says:
+ * infinity c = 0, NaN NaN everywhere; a caller that wants to skip such a step looks at norm.
+ * c is formed in 64 bits and rounded to 32, products in 32, rounded once to their type.
+ *
+ * Supported: 0 <= n, 0 <= numel, numel of a tensor < 2^40, max_norm > 0 (infinity: never clips) and eps >= 0, finite.  n = 0: sum_sq = 0.
+ * Captured calls keep the pointers of the lists.  As for the forward of attention, the first call of the library on a
+ * device must not be captured.
+ * ------------------------------------------------------------------------ */
+int knap_grad_sum_squares(const void* const* grads, const int64_t* numel, const int* types, int n,
+                          double* sum_sq, void* workspace, size_t workspace_bytes, void* stream);
+size_t knap_grad_sum_squares_workspace_bytes(int n);
+int knap_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n,
+                   const double* sum_sq, float max_norm, float eps, float* norm, void* stream);
+
 /* Message for a KNAP_ERR_* code (static string, never NULL). */
 const char* knap_strerror(int code);
 

@@ -36,6 +36,9 @@ KNAP_ROPE_PARTS = 3
 KNAP_BF16 = 0
 KNAP_F32 = 1
 KNAP_LAYER_NORM_MAX_WIDTH = 16384
+KNAP_NORM_NONE = 0
+KNAP_NORM_RMS = 1
+KNAP_NORM_LAYER = 2
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -78,6 +81,14 @@ _SIGNATURES = {
     "knap_layer_norm_fwd": (_i, [_vp, _i, _i64, _i64, _i, _vp, _vp, _i, _f, _vp, _i, _i64, _vp, _vp, _vp]),
     "knap_layer_norm_bwd": (_i, [_vp, _i, _i64, _i64, _i, _vp, _i, _vp, _vp, _vp, _i, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
     "knap_layer_norm_bwd_workspace_bytes": (_sz, [_i64, _i]),
+    "knap_residual_norm_fwd": (_i, [_vp, _i, _i64, _i64, _i, _vp, _i, _i64, _vp, _i, _vp, _i64, _vp, _vp, _i64, _i, _vp, _vp, _i, _i, _i, _f, _f,
+                                    _vp, _i64, _vp, _i64, _vp, _vp]),
+    "knap_residual_norm_bwd": (_i, [_vp, _i, _i64, _i64, _i, _vp, _i, _i64, _vp, _i, _vp, _i64, _vp, _i64, _i, _vp, _vp, _i, _i, _i, _f, _vp,
+                                    _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "knap_residual_norm_bwd_workspace_bytes": (_sz, [_i64, _i, _i]),
+    "knap_grad_sum_squares": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _sz, _vp]),
+    "knap_grad_sum_squares_workspace_bytes": (_sz, [_i]),
+    "knap_grad_clip": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _f, _f, _vp, _vp]),
     "knap_strerror": (C.c_char_p, [_i]),
     "knap_last_hip_error": (_i, []),
     "knap_launch_workgroups": (_i, [_i]),
@@ -518,6 +529,197 @@ def knap_layer_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace
     rc = lib.knap_layer_norm_bwd(x.data_ptr(), types[x.dtype], xs, rows, width, w_at, types[w_type], mean_at, rstd_at, dy.data_ptr(), types[dy.dtype],
                                  dys, dx.data_ptr(), dxs, dw_at, db_at, 0 if workspace is None else workspace.data_ptr(), workspace_bytes,
                                  _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+# --------------------------------------------------------------------------- residual norm
+
+def _modulation(where: str, name: str, t, n_seq: int, width: int, dtype) -> int:
+    """The row stride of an (n_seq, width) tensor of `dtype` with contiguous rows, checked."""
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != n_seq or t.shape[1] != width:
+        _refuse(where, f"{name} is an (n_seq, width) tensor of its type")
+    if width > 1 and t.stride(1) != 1:
+        _refuse(where, f"the rows of {name} are contiguous")
+    return t.stride(0)
+
+
+class _Residual:
+    """What both directions hand over of x, f, the vectors and the weights, checked."""
+
+    def __init__(self, where: str, x, f, branch_type, cu_seqlens, gate, scale, shift, weight, post_weight):
+        types, f32 = _KNAP_TYPES, torch.float32
+        shape = x.shape
+        self.xs = _rows(where, "x", x, shape)
+        self.rows, self.width = rows, width = shape
+        self.shape = shape
+        if branch_type not in types:
+            _refuse(where, "the type of the branch")
+        self.fs = 0 if f is None else _rows(where, "f", f, shape, branch_type)
+        self.f_at = 0 if f is None else f.data_ptr()
+        self.n_seq, self.cu_at = 1, 0
+        if cu_seqlens is not None:
+            if cu_seqlens.dtype is not torch.int32 or not cu_seqlens.is_contiguous() or cu_seqlens.numel() < 1:
+                _refuse(where, "cu_seqlens is a contiguous int32 tensor of n_seq + 1 entries")
+            self.n_seq, self.cu_at = cu_seqlens.numel() - 1, cu_seqlens.data_ptr()
+        n = self.n_seq
+        given = gate if gate is not None else scale if scale is not None else shift
+        mod = f32 if given is None else given.dtype
+        if mod not in types:
+            _refuse(where, "the type of gate, scale and shift")
+        self.gs = 0 if gate is None else _modulation(where, "gate", gate, n, width, mod)
+        self.ms = 0
+        for name, t in (("scale", scale), ("shift", shift)):
+            if t is not None:
+                ms = _modulation(where, name, t, n, width, mod)
+                if n > 1 and scale is not None and t is shift and ms != self.ms:
+                    _refuse(where, "scale and shift have one stride")
+                self.ms = ms
+        self.gate_at, self.scale_at, self.shift_at = _ptr(gate), _ptr(scale), _ptr(shift)
+        wt = f32 if weight is None and post_weight is None else (post_weight if weight is None else weight).dtype
+        if wt not in types:
+            _refuse(where, "the type of weight and post_weight")
+        self.w_at = 0 if weight is None else _vector(where, "weight", weight, width, wt)
+        self.wp_at = 0 if post_weight is None else _vector(where, "post_weight", post_weight, width, wt)
+        self.xt, self.bt, self.mt, self.wt = types[x.dtype], types[branch_type], types[mod], types[wt]
+
+
+def knap_residual_norm_fwd(x, f, x_out, y, norm: int = KNAP_NORM_LAYER, post_norm: int = KNAP_NORM_NONE, weight=None, post_weight=None, gate=None,
+                           scale=None, shift=None, cu_seqlens=None, alpha: float = 1.0, eps: float = 1e-6, stats=None, stream=None,
+                           check: bool = True) -> int:
+    """x_out = x + alpha gate N_post(f) post_weight,  y = N(x_out) weight (1 + scale) + shift over the rows of a packed bag.  x, x_out: (rows,
+    width) of one type; f (None: no branch, no x_out) and y (None: norm is KNAP_NORM_NONE) of the same or bf16; gate, scale, shift:
+    (n_seq, width) or None; weights: (width,) or None; stats: fp32 (4, rows) for a backward."""
+    where = "knap_residual_norm_fwd"
+    _here(where, x, f, x_out, y, weight, post_weight, gate, scale, shift, cu_seqlens, stats)
+    r = _Residual(where, x, f, (y if f is None else f).dtype if f is not None or y is not None else x.dtype, cu_seqlens, gate, scale, shift, weight,
+                  post_weight)
+    xos = 0 if x_out is None else _rows(where, "x_out", x_out, r.shape, x.dtype)
+    ys = 0 if y is None else _rows(where, "y", y, r.shape, y.dtype if f is None else f.dtype)
+    if stats is not None:
+        _vector(where, "stats", stats, 4 * r.rows, torch.float32)
+    rc = lib.knap_residual_norm_fwd(x.data_ptr(), r.xt, r.xs, r.rows, r.width, r.f_at, r.bt, r.fs, r.cu_at, r.n_seq, r.gate_at, r.gs, r.scale_at,
+                                    r.shift_at, r.ms, r.mt, r.wp_at, r.w_at, r.wt, post_norm, norm, alpha, eps, _ptr(x_out), xos, _ptr(y), ys,
+                                    _ptr(stats), _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+def knap_residual_norm_bwd_workspace_bytes(rows: int, width: int, n_seq: int) -> int:
+    return int(lib.knap_residual_norm_bwd_workspace_bytes(rows, width, n_seq))
+
+
+def knap_residual_norm_bwd(x, f, stats, dx_out, dy, dx, df, norm: int = KNAP_NORM_LAYER, post_norm: int = KNAP_NORM_NONE, weight=None,
+                           post_weight=None, gate=None, scale=None, cu_seqlens=None, alpha: float = 1.0, dgate=None, dscale=None, dshift=None,
+                           dweight=None, dpost_weight=None, workspace=None, workspace_bytes: Optional[int] = None, stream=None,
+                           check: bool = True) -> int:
+    """Gradients of knap_residual_norm_fwd, whose x, f and stats it takes: dx of x's type, df of f's, dgate, dscale and dshift fp32 (n_seq, width),
+    dweight and dpost_weight fp32 (width,); each of them, and dx_out, may be None."""
+    where = "knap_residual_norm_bwd"
+    _here(where, x, f, stats, dx_out, dy, dx, df, weight, post_weight, gate, scale, cu_seqlens, dgate, dscale, dshift, dweight, dpost_weight, workspace)
+    f32 = torch.float32
+    r = _Residual(where, x, f, (dy if f is None else f).dtype if f is not None or dy is not None else x.dtype, cu_seqlens, gate, scale, None, weight,
+                  post_weight)
+    if stats is not None:
+        _vector(where, "stats", stats, 4 * r.rows, f32)
+    xt, bt = x.dtype, f.dtype if f is not None else None if dy is None else dy.dtype
+    dxos = 0 if dx_out is None else _rows(where, "dx_out", dx_out, r.shape, xt)
+    dys = 0 if dy is None else _rows(where, "dy", dy, r.shape, bt)
+    dxs = 0 if dx is None else _rows(where, "dx", dx, r.shape, xt)
+    dfs = 0 if df is None else _rows(where, "df", df, r.shape, bt)
+    dgs = 0 if dgate is None else _modulation(where, "dgate", dgate, r.n_seq, r.width, f32)
+    dms = 0 if dscale is None else _modulation(where, "dscale", dscale, r.n_seq, r.width, f32)
+    if dshift is not None:
+        ms = _modulation(where, "dshift", dshift, r.n_seq, r.width, f32)
+        if dscale is not None and r.n_seq > 1 and ms != dms:
+            _refuse(where, "dscale and dshift have one stride")
+        dms = ms
+    dw_at = 0 if dweight is None else _vector(where, "dweight", dweight, r.width, f32)
+    dwp_at = 0 if dpost_weight is None else _vector(where, "dpost_weight", dpost_weight, r.width, f32)
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib.knap_residual_norm_bwd(x.data_ptr(), r.xt, r.xs, r.rows, r.width, r.f_at, r.bt, r.fs, r.cu_at, r.n_seq, r.gate_at, r.gs, r.scale_at, r.ms,
+                                    r.mt, r.wp_at, r.w_at, r.wt, post_norm, norm, alpha, _ptr(stats), _ptr(dx_out), dxos, _ptr(dy), dys, _ptr(dx),
+                                    dxs, _ptr(df), dfs, _ptr(dgate), dgs, _ptr(dscale), _ptr(dshift), dms, dw_at, dwp_at, _ptr(workspace),
+                                    workspace_bytes, _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+# --------------------------------------------------------------------------- gradient norm and clipping
+
+class GradList:
+    """The HOST arrays that knap_grad_sum_squares and knap_grad_clip take of a list of gradients (contiguous bf16 or fp32 tensors, all on one
+    device) and, for clipping, of where each goes (None: in place).  Keeps the tensors."""
+
+    def __init__(self, grads, out=None):
+        where = "GradList"
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        n = self.n = len(self.grads)
+        if len(self.out) != n:
+            _refuse(where, "as many outputs as gradients")
+        self.device = self.grads[0].get_device() if n else None
+        for g, o in zip(self.grads, self.out):
+            if g.dtype not in _KNAP_TYPES or o.dtype is not g.dtype or o.numel() != g.numel():
+                _refuse(where, "gradients are bf16 or fp32 tensors, an output is of its gradient's type and size")
+            if not g.is_contiguous() or not o.is_contiguous():
+                _refuse(where, "gradients and outputs are contiguous")
+            if g.get_device() != self.device or o.get_device() != self.device:
+                _refuse(where, "tensors on several devices")
+        self.grads_at = (C.c_void_p * max(1, n))(*[g.data_ptr() for g in self.grads])
+        self.out_at = (C.c_void_p * max(1, n))(*[o.data_ptr() for o in self.out])
+        self.numel = (C.c_int64 * max(1, n))(*[g.numel() for g in self.grads])
+        self.types = (C.c_int * max(1, n))(*[_KNAP_TYPES[g.dtype] for g in self.grads])
+
+    def on(self, where: str) -> None:
+        dev = _current_device() if _current_device is not None else torch.cuda.current_device()
+        if self.device is not None and self.device != dev:
+            _refuse(where, f"gradients on device {self.device} while device {dev} is current")
+
+
+def _one(where: str, name: str, t, dtype) -> int:
+    if t.dtype is not dtype or t.numel() < 1:
+        _refuse(where, f"the type of {name}")
+    return t.data_ptr()
+
+
+def knap_grad_sum_squares_workspace_bytes(n: int) -> int:
+    return int(lib.knap_grad_sum_squares_workspace_bytes(n))
+
+
+def knap_grad_sum_squares(grads, sum_sq, workspace, workspace_bytes: Optional[int] = None, stream=None, check: bool = True) -> int:
+    """sum_sq (a float64 CUDA tensor of one value) = sum of g^2 over all gradients: a GradList, or tensors."""
+    where = "knap_grad_sum_squares"
+    if not isinstance(grads, GradList):
+        grads = GradList(grads)
+    grads.on(where)
+    _here(where, sum_sq, workspace)
+    at = _one(where, "sum_sq", sum_sq, torch.float64)
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib.knap_grad_sum_squares(grads.grads_at, grads.numel, grads.types, grads.n, at, _ptr(workspace), workspace_bytes, _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+def knap_grad_clip(grads, sum_sq, max_norm: float, eps: float = 1e-6, norm=None, out=None, stream=None, check: bool = True) -> int:
+    """out = min(1, max_norm / (sqrt(sum_sq) + eps)) grads, in place where `out` is None; grads: a GradList (which has its outputs), or tensors.
+    norm: an fp32 CUDA tensor of one value, or None."""
+    where = "knap_grad_clip"
+    if not isinstance(grads, GradList):
+        grads = GradList(grads, out)
+    elif out is not None:
+        _refuse(where, "a GradList has its outputs")
+    grads.on(where)
+    _here(where, sum_sq, norm)
+    at = _one(where, "sum_sq", sum_sq, torch.float64)
+    norm_at = 0 if norm is None else _one(where, "norm", norm, torch.float32)
+    rc = lib.knap_grad_clip(grads.grads_at, grads.out_at, grads.numel, grads.types, grads.n, at, max_norm, eps, norm_at, _stream_handle(stream))
     if check:
         _check(rc, where)
     return rc

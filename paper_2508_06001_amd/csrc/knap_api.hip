@@ -125,6 +125,17 @@ int bwd_impl(const void* q, const void* k, const void* v, const int32_t* cu_seql
 
 }  // namespace
 
+int knap::device_cus() {
+  DeviceInfo* di = device_info();
+  return di ? di->cus : 0;
+}
+
+int knap::launch_status(hipError_t e) {
+  if (e == hipSuccess) return KNAP_OK;
+  g_last_hip_error = static_cast<int>(e);
+  return KNAP_ERR_LAUNCH_FAILED;
+}
+
 extern "C" {
 
 int knap_varlen_attn_fwd(const void* q, const void* k, const void* v,

@@ -1,0 +1,307 @@
+// C-ABI entry points of the operators between the attention calls of a block and behind its backward: argument checks and launches.
+// Nothing here allocates device memory, frees or synchronises.
+#include "knapattn.h"
+#include "knap_kernels.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdlib>
+
+namespace {
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline size_t size_of(int type) { return type == KNAP_BF16 ? 2 : 4; }
+inline bool type_ok(int type) { return type == KNAP_BF16 || type == KNAP_F32; }
+inline bool finite_f(float x) { return x > -3.0e38f && x < 3.0e38f; }
+
+// a tensor of rows that is given, and whether 16-byte accesses reach every row of it (rows further apart than 2^22 columns take the other
+// form, whose offsets count one row alone)
+struct Rows {
+  bool ok = true, wide = true;
+  int64_t rows;
+  int width;
+  void add(const void* p, int type, int64_t stride) {
+    if (!p) return;
+    if (rows == 1) stride = width;
+    ok = ok && aligned(p, size_of(type)) && stride >= width && stride <= ((int64_t)1 << 30);
+    wide = wide && aligned(p, 16) && (rows == 1 || (stride % 8 == 0 && stride <= (1 << 22)));
+  }
+};
+
+// what both directions of the residual norm check alike
+int check_residual(const void* x, int x_type, int64_t rows, int width, const void* f, int branch_type, const int32_t* cu, int n_seq,
+                   const void* gate, int64_t gate_stride, const void* scale, const void* shift, int64_t mod_stride, int mod_type,
+                   const void* post_weight, const void* weight, int w_type, int post_norm, int norm, float alpha) {
+  if (!type_ok(x_type) || !type_ok(branch_type) || !type_ok(mod_type) || !type_ok(w_type) || (x_type == KNAP_BF16 && branch_type == KNAP_F32)) return KNAP_ERR_INVALID_ARG;
+  if (rows < 0 || rows > INT32_MAX || width < 1 || width > KNAP_LAYER_NORM_MAX_WIDTH || n_seq < 0) return KNAP_ERR_INVALID_ARG;
+  if (n_seq > KNAP_MAX_SEQS) return KNAP_ERR_TOO_MANY_SEQS;
+  if (!cu && n_seq != 1) return KNAP_ERR_INVALID_ARG;
+  if (post_norm < KNAP_NORM_NONE || post_norm > KNAP_NORM_LAYER || norm < KNAP_NORM_NONE || norm > KNAP_NORM_LAYER || !finite_f(alpha)) return KNAP_ERR_INVALID_ARG;
+  const bool branch = f || rows == 0;      // no rows: no tensors either
+  if (!branch && (gate || post_weight || post_norm != KNAP_NORM_NONE || norm == KNAP_NORM_NONE)) return KNAP_ERR_INVALID_ARG;
+  if (norm == KNAP_NORM_NONE && (weight || scale || shift)) return KNAP_ERR_INVALID_ARG;
+  if (n_seq > 1 && ((gate && (gate_stride < 0 || gate_stride > ((int64_t)1 << 40))) || ((scale || shift) && (mod_stride < 0 || mod_stride > ((int64_t)1 << 40)))))
+    return KNAP_ERR_INVALID_ARG;
+  if (!aligned(cu, 4) || !aligned(gate, size_of(mod_type)) || !aligned(scale, size_of(mod_type)) || !aligned(shift, size_of(mod_type)) ||
+      !aligned(weight, size_of(w_type)) || !aligned(post_weight, size_of(w_type)))
+    return KNAP_ERR_INVALID_ARG;
+  if (rows > 0 && !x) return KNAP_ERR_INVALID_ARG;
+  return KNAP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+// ---------------------------------------------------------------------------
+// Residual norm
+// ---------------------------------------------------------------------------
+
+int knap_residual_norm_fwd(const void* x, int x_type, int64_t x_stride, int64_t rows, int width, const void* f, int branch_type, int64_t f_stride,
+                           const int32_t* cu_seqlens, int n_seq, const void* gate, int64_t gate_stride, const void* scale, const void* shift,
+                           int64_t mod_stride, int mod_type, const void* post_weight, const void* weight, int w_type, int post_norm, int norm,
+                           float alpha, float eps, void* x_out, int64_t x_out_stride, void* y, int64_t y_stride, float* stats, void* stream) {
+  const int rc = check_residual(x, x_type, rows, width, f, branch_type, cu_seqlens, n_seq, gate, gate_stride, scale, shift, mod_stride, mod_type,
+                                post_weight, weight, w_type, post_norm, norm, alpha);
+  if (rc != KNAP_OK) return rc;
+  if (!(eps >= 0.f) || !finite_f(eps)) return KNAP_ERR_INVALID_ARG;
+  if (rows == 0 || n_seq == 0) return KNAP_OK;
+  if (!!f != !!x_out || (norm != KNAP_NORM_NONE) != !!y || !aligned(stats, 4)) return KNAP_ERR_INVALID_ARG;
+  Rows t;
+  t.rows = rows; t.width = width;
+  t.add(x, x_type, x_stride);
+  t.add(f, branch_type, f_stride);
+  t.add(x_out, x_type, x_out_stride);
+  t.add(y, branch_type, y_stride);
+  if (!t.ok || x == y || f == x || (f && (f == x_out || f == y)) || (y && y == x_out)) return KNAP_ERR_INVALID_ARG;
+  if (x == x_out && rows > 1 && x_stride != x_out_stride) return KNAP_ERR_INVALID_ARG;
+  knap::ResidualArgs a{};
+  a.x = x; a.f = f; a.gate = gate; a.scale = scale; a.shift = shift; a.weight = weight; a.post_weight = post_weight;
+  a.cu = cu_seqlens; a.n_seq = n_seq;
+  a.x_out = x_out; a.y = y; a.stats = stats;
+  a.x_stride = rows == 1 ? width : x_stride; a.f_stride = rows == 1 ? width : f_stride;
+  a.x_out_stride = rows == 1 ? width : x_out_stride; a.y_stride = rows == 1 ? width : y_stride;
+  a.gate_stride = n_seq == 1 ? 0 : gate_stride; a.mod_stride = n_seq == 1 ? 0 : mod_stride;
+  a.rows = rows; a.width = width; a.alpha = alpha; a.eps = eps; a.norm = norm; a.post_norm = post_norm;
+  a.w_bf16 = w_type == KNAP_BF16; a.mod_bf16 = mod_type == KNAP_BF16;
+  const int cus = knap::device_cus();
+  if (!cus) return KNAP_ERR_LAUNCH_FAILED;
+  return knap::launch_status(knap::launch_residual_norm_fwd(a, x_type == KNAP_BF16, branch_type == KNAP_BF16, width % 8 == 0 && t.wide, cus,
+                                                            static_cast<hipStream_t>(stream)));
+}
+
+size_t knap_residual_norm_bwd_workspace_bytes(int64_t rows, int width, int n_seq) {
+  if (rows <= 0 || width <= 0 || n_seq <= 0) return 0;
+  const size_t groups = (size_t)std::min<int64_t>(rows, knap::kResidualMaxGroups);
+  return round_up(((groups + n_seq) * 3 + groups * 2) * (size_t)width * sizeof(float), 256);
+}
+
+int knap_residual_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t rows, int width, const void* f, int branch_type, int64_t f_stride,
+                           const int32_t* cu_seqlens, int n_seq, const void* gate, int64_t gate_stride, const void* scale, int64_t mod_stride,
+                           int mod_type, const void* post_weight, const void* weight, int w_type, int post_norm, int norm, float alpha,
+                           const float* stats, const void* dx_out, int64_t dx_out_stride, const void* dy, int64_t dy_stride, void* dx,
+                           int64_t dx_stride, void* df, int64_t df_stride, float* dgate, int64_t dgate_stride, float* dscale, float* dshift,
+                           int64_t dmod_stride, float* dweight, float* dpost_weight, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_residual(x, x_type, rows, width, f, branch_type, cu_seqlens, n_seq, gate, gate_stride, scale, nullptr, mod_stride, mod_type,
+                                post_weight, weight, w_type, post_norm, norm, alpha);
+  if (rc != KNAP_OK) return rc;
+  const bool none = rows == 0 || n_seq == 0;
+  const bool sums = dgate || dscale || dshift || dweight || dpost_weight;
+  float* const outs[5] = {dgate, dscale, dshift, dweight, dpost_weight};
+  for (int i = 0; i < 5; ++i) {
+    if (!aligned(outs[i], 4)) return KNAP_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j]) return KNAP_ERR_INVALID_ARG;
+  }
+  if (n_seq > 1 && ((dgate && dgate_stride < width) || ((dscale || dshift) && dmod_stride < width))) return KNAP_ERR_INVALID_ARG;
+  knap::ResidualArgs a{};
+  a.cu = cu_seqlens; a.n_seq = n_seq;
+  a.rows = none ? 0 : rows; a.width = width; a.alpha = alpha; a.norm = norm; a.post_norm = post_norm;
+  a.w_bf16 = w_type == KNAP_BF16; a.mod_bf16 = mod_type == KNAP_BF16;
+  a.gate = gate; a.scale = scale; a.weight = weight; a.post_weight = post_weight;
+  a.gate_stride = n_seq == 1 ? 0 : gate_stride; a.mod_stride = n_seq == 1 ? 0 : mod_stride;
+  a.dgate = dgate; a.dscale = dscale; a.dshift = dshift; a.dweight = dweight; a.dpost_weight = dpost_weight;
+  a.dgate_stride = n_seq == 1 ? 0 : dgate_stride; a.dmod_stride = n_seq == 1 ? 0 : dmod_stride;
+  Rows t;
+  t.rows = rows; t.width = width;
+  if (!none) {
+    const bool normed = norm != KNAP_NORM_NONE;
+    if (normed != !!dy || (df && !f) || (!f && (dgate || dpost_weight)) || (!normed && (dscale || dshift || dweight))) return KNAP_ERR_INVALID_ARG;
+    if ((normed || post_norm != KNAP_NORM_NONE) && (!stats || !aligned(stats, 4))) return KNAP_ERR_INVALID_ARG;
+    t.add(x, x_type, x_stride);
+    t.add(f, branch_type, f_stride);
+    t.add(dx_out, x_type, dx_out_stride);
+    t.add(dy, branch_type, dy_stride);
+    t.add(dx, x_type, dx_stride);
+    t.add(df, branch_type, df_stride);
+    if (!t.ok || f == x) return KNAP_ERR_INVALID_ARG;
+    if (dx && (dx == x || dx == f || dx == dy || dx == df || (dx == dx_out && rows > 1 && dx_stride != dx_out_stride))) return KNAP_ERR_INVALID_ARG;
+    if (df && (df == x || df == f || df == dy || df == dx_out)) return KNAP_ERR_INVALID_ARG;
+    if (sums) {
+      if (!workspace || !aligned(workspace, 256)) return KNAP_ERR_INVALID_ARG;
+      if (workspace_bytes < knap_residual_norm_bwd_workspace_bytes(rows, width, n_seq)) return KNAP_ERR_WORKSPACE_TOO_SMALL;
+      const size_t groups = (size_t)std::min<int64_t>(rows, knap::kResidualMaxGroups);
+      a.partial = static_cast<float*>(workspace);
+      a.totals = dweight || dpost_weight ? a.partial + (groups + n_seq) * 3 * (size_t)width : nullptr;
+    }
+    a.x = x; a.f = f; a.dx_out = dx_out; a.dy = dy; a.dx = dx; a.df = df;
+    a.stats = const_cast<float*>(stats);
+    a.x_stride = rows == 1 ? width : x_stride; a.f_stride = rows == 1 ? width : f_stride;
+    a.dx_out_stride = rows == 1 ? width : dx_out_stride; a.dy_stride = rows == 1 ? width : dy_stride;
+    a.dx_stride = rows == 1 ? width : dx_stride; a.df_stride = rows == 1 ? width : df_stride;
+  }
+  if (none && !sums) return KNAP_OK;
+  const int cus = knap::device_cus();
+  if (!cus) return KNAP_ERR_LAUNCH_FAILED;
+  return knap::launch_status(knap::launch_residual_norm_bwd(a, x_type == KNAP_BF16, branch_type == KNAP_BF16, width % 8 == 0 && t.wide, cus,
+                                                            static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// Gradient norm and clipping
+// ---------------------------------------------------------------------------
+
+}  // extern "C"
+
+namespace {
+
+constexpr int64_t kGradMost = (int64_t)1 << 40;      // elements of a tensor
+
+int check_grads(const void* const* grads, const int64_t* numel, const int* types, int n) {
+  if (n < 0 || (n > 0 && (!grads || !numel || !types))) return KNAP_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i) {
+    if (!type_ok(types[i]) || numel[i] < 0 || numel[i] >= kGradMost) return KNAP_ERR_INVALID_ARG;
+    if (numel[i] > 0 && (!grads[i] || !aligned(grads[i], size_of(types[i])))) return KNAP_ERR_INVALID_ARG;
+  }
+  return KNAP_OK;
+}
+
+// Whether every part of `out` is apart from the others and from all gradients but its own.  In ascending order, as tensors of one
+// allocation mostly are, one walk does; else an array of their order is sorted.
+int grads_apart(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n) {
+  struct Span { uintptr_t from, to; int i; };
+  constexpr int kOnStack = 512;
+  Span some[kOnStack], *spans = some;
+  if (n > kOnStack) {
+    spans = static_cast<Span*>(malloc((size_t)n * sizeof(Span)));
+    if (!spans) return KNAP_ERR_CAPACITY;
+  }
+  int m = 0;
+  bool in_place = true, sorted = true;
+  for (int i = 0; i < n; ++i) {
+    if (numel[i] == 0) continue;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(out[i]);
+    spans[m] = {at, at + (size_t)numel[i] * size_of(types[i]), i};
+    sorted = sorted && (m == 0 || spans[m - 1].from <= at);
+    in_place = in_place && grads[i] == out[i];
+    ++m;
+  }
+  if (!sorted) std::sort(spans, spans + m, [](const Span& a, const Span& b) { return a.from < b.from; });
+  bool ok = true;
+  for (int k = 1; k < m && ok; ++k) ok = spans[k - 1].to <= spans[k].from;
+  if (ok && !in_place)
+    for (int i = 0; i < n && ok; ++i) {
+      if (numel[i] == 0) continue;
+      const uintptr_t from = reinterpret_cast<uintptr_t>(grads[i]), to = from + (size_t)numel[i] * size_of(types[i]);
+      // the parts of `out` do not overlap, so that their ends ascend too: the first that ends behind `from`
+      const Span* s = std::upper_bound(spans, spans + m, from, [](uintptr_t v, const Span& x) { return v < x.to; });
+      for (; s < spans + m && s->from < to && ok; ++s) ok = s->i == i && s->from == from;
+    }
+  if (spans != some) free(spans);
+  return ok ? KNAP_OK : KNAP_ERR_INVALID_ARG;
+}
+
+// Fills tables with the tensors that hold anything, as many as a launch takes, and hands each to f; stops at a status that is not hipSuccess.
+template <class F>
+hipError_t for_tables(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n, F f) {
+  knap::GradTable t;
+  t.n = 0;
+  uint32_t chunks = 0;
+  auto hand = [&]() {
+    t.first[t.n] = chunks;
+    const hipError_t e = t.n ? f(t, chunks) : hipSuccess;
+    t.n = 0;
+    chunks = 0;
+    return e;
+  };
+  for (int i = 0; i < n; ++i) {
+    if (numel[i] == 0) continue;
+    const uint32_t mine = (uint32_t)((numel[i] + knap::kGradChunk - 1) / knap::kGradChunk);      // below 2^27
+    if (t.n == knap::kGradTensors || chunks > (1u << 30)) {
+      const hipError_t e = hand();
+      if (e != hipSuccess) return e;
+    }
+    t.from[t.n] = grads[i];
+    t.to[t.n] = out ? out[i] : nullptr;
+    t.numel[t.n] = numel[i];
+    t.bf16[t.n] = types[i] == KNAP_BF16;
+    t.first[t.n] = chunks;
+    ++t.n;
+    chunks += mine;
+  }
+  return hand();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t knap_grad_sum_squares_workspace_bytes(int n) {
+  if (n <= 0) return 0;
+  const size_t launches = ((size_t)n + knap::kGradTensors - 1) / knap::kGradTensors + 1;
+  return round_up(launches * knap::kGradGroups * sizeof(double), 256);
+}
+
+int knap_grad_sum_squares(const void* const* grads, const int64_t* numel, const int* types, int n, double* sum_sq, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  const int rc = check_grads(grads, numel, types, n);
+  if (rc != KNAP_OK) return rc;
+  if (!sum_sq || !aligned(sum_sq, 8)) return KNAP_ERR_INVALID_ARG;
+  if (n > 0 && (!workspace || !aligned(workspace, 256))) return KNAP_ERR_INVALID_ARG;
+  if (workspace_bytes < knap_grad_sum_squares_workspace_bytes(n)) return KNAP_ERR_WORKSPACE_TOO_SMALL;
+  const int cus = knap::device_cus();
+  if (!cus) return KNAP_ERR_LAUNCH_FAILED;
+  double* partial = static_cast<double*>(workspace);
+  int filled = 0;
+  const size_t room = workspace_bytes / sizeof(double);
+  hipError_t e = for_tables(grads, nullptr, numel, types, n, [&](const knap::GradTable& t, uint32_t chunks) {
+    const int groups = (int)std::min<uint32_t>(chunks, std::min(4 * cus, knap::kGradGroups));
+    if ((size_t)filled + groups > room) return hipErrorInvalidValue;
+    const hipError_t err = knap::launch_grad_squares(t, partial + filled, groups, static_cast<hipStream_t>(stream));
+    filled += groups;
+    return err;
+  });
+  if (e == hipSuccess) e = knap::launch_grad_join(partial, filled, sum_sq, static_cast<hipStream_t>(stream));
+  return knap::launch_status(e);
+}
+
+int knap_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n, const double* sum_sq, float max_norm,
+                   float eps, float* norm, void* stream) {
+  const int rc = check_grads(grads, numel, types, n);
+  if (rc != KNAP_OK) return rc;
+  if (!sum_sq || !aligned(sum_sq, 8) || !aligned(norm, 4) || !(max_norm > 0.f) || !(eps >= 0.f) || !finite_f(eps) || (n > 0 && !out)) return KNAP_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i)
+    if (numel[i] > 0 && (!out[i] || !aligned(out[i], size_of(types[i])))) return KNAP_ERR_INVALID_ARG;
+  const int apart = grads_apart(grads, out, numel, types, n);
+  if (apart != KNAP_OK) return apart;
+  const int cus = knap::device_cus();
+  if (!cus) return KNAP_ERR_LAUNCH_FAILED;
+  bool first = true;
+  hipError_t e = for_tables(grads, out, numel, types, n, [&](const knap::GradTable& t, uint32_t chunks) {
+    const int groups = (int)std::min<uint32_t>(chunks, (uint32_t)(8 * cus));
+    const hipError_t err = knap::launch_grad_clip(t, sum_sq, max_norm, eps, first ? norm : nullptr, groups, static_cast<hipStream_t>(stream));
+    first = false;
+    return err;
+  });
+  if (e == hipSuccess && first && norm) {      // no elements at all: the norm alone
+    knap::GradTable none;
+    none.n = 0;
+    none.first[0] = 0;
+    e = knap::launch_grad_clip(none, sum_sq, max_norm, eps, norm, 1, static_cast<hipStream_t>(stream));
+  }
+  return knap::launch_status(e);
+}
+
+}  // extern "C"

@@ -108,6 +108,47 @@ hipError_t launch_layer_norm_fwd(const NormArgs& a, bool x_bf16, bool y_bf16, bo
 hipError_t launch_layer_norm_bwd(const NormArgs& a, float* dw, float* db, bool x_bf16, bool y_bf16, bool wide, int cus, hipStream_t stream);
 hipError_t launch_layer_norm_zero(float* dw, float* db, int width, hipStream_t stream);
 
+// Residual norm; pointers that are not wanted, and tensors that there are none of, are nullptr
+struct ResidualArgs {
+  const void *x, *f, *gate, *scale, *shift, *weight, *post_weight, *dx_out, *dy;
+  const int32_t* cu;      // or nullptr: one sequence of all rows
+  int n_seq;
+  void *x_out, *y, *dx, *df;
+  float *stats;           // (4, rows): mean and rstd of x', mean and rstd of f
+  float *dgate, *dscale, *dshift, *dweight, *dpost_weight;
+  float *partial, *totals;      // (workgroups + n_seq, 3, width), (workgroups, 2, width)
+  int64_t x_stride, f_stride, x_out_stride, y_stride, dx_out_stride, dy_stride, dx_stride, df_stride;
+  int64_t gate_stride, mod_stride, dgate_stride, dmod_stride;
+  int64_t rows;
+  int width, chunk;       // chunk: rows of a workgroup, set by the launch
+  float alpha, eps;
+  int norm, post_norm;
+  bool w_bf16, mod_bf16;
+};
+constexpr int kResidualMaxGroups = 512;      // workgroups of a backward
+hipError_t launch_residual_norm_fwd(const ResidualArgs& a, bool x_bf16, bool b_bf16, bool wide, int cus, hipStream_t stream);
+hipError_t launch_residual_norm_bwd(const ResidualArgs& a, bool x_bf16, bool b_bf16, bool wide, int cus, hipStream_t stream);
+
+// Gradient norm and clipping.  A launch takes up to kGradTensors tensors; workgroups find theirs by the chunks of kGradChunk elements in
+// front of it.
+constexpr int kGradTensors = 112, kGradGroups = 1024, kGradChunk = 8192;
+struct GradTable {
+  const void* from[kGradTensors];
+  void* to[kGradTensors];              // of clipping
+  int64_t numel[kGradTensors];
+  uint32_t first[kGradTensors + 1];    // chunks in front of a tensor; [n]: of all
+  uint8_t bf16[kGradTensors];
+  int n;
+};
+hipError_t launch_grad_squares(const GradTable& t, double* partial, int groups, hipStream_t stream);
+hipError_t launch_grad_join(const double* partial, int n, double* sum, hipStream_t stream);
+hipError_t launch_grad_clip(const GradTable& t, const double* sum, float max_norm, float eps, float* norm, int groups, hipStream_t stream);
+
+// for entry points in other files than knap_api.hip: compute units of the current device, 0 where they could not be looked up (as for the
+// forward of attention, the first call on a device asks the runtime), and the status of a launch, which is kept for knap_last_hip_error
+int device_cus();
+int launch_status(hipError_t e);
+
 // resident workgroups per compute unit of the persistent kernels
 int fwd_workgroups_per_cu(int d);
 int bwd_dq_workgroups_per_cu(int d);

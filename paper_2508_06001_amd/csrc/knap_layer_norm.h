@@ -18,7 +18,7 @@ template <int LANES_, int UNITS_, int ROWS_, bool WIDE_>
 struct NormCfg {
   static constexpr int LANES = LANES_, UNITS = UNITS_, ROWS = ROWS_;
   static constexpr bool WIDE = WIDE_;
-  static constexpr int THREADS = LANES > 256 ? LANES : 256;
+  static constexpr int THREADS = LANES > 64 ? LANES : 256;
   static constexpr int GROUPS = THREADS / LANES;          // rows side by side
   static constexpr int COLS = 8 * UNITS;                  // of a thread
   static constexpr int PASS = GROUPS * ROWS;              // rows of a workgroup at a time

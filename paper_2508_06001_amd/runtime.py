@@ -75,6 +75,82 @@ class LayerNorm:
         return self.dx, self.dweight, self.dbias
 
 
+class ResidualNorm:
+    """Buffers + calls of the norms around a branch (knap_residual_norm_fwd) over the rows of a packed bag: `post_norm` with `post_weight` behind
+    the branch, the residual scale `alpha`, `norm` with `weight` in front of the next branch.  `cu_seqlens` None: one sequence of all rows.
+    `branch=False`: a block's first norm, without a residual.  Gradients of the vectors are in `dgate`, `dscale` and `dshift`, those of the
+    weights in `dweight` and `dpost_weight`."""
+
+    def __init__(self, rows: int, width: int, cu_seqlens=None, norm: int = B.KNAP_NORM_LAYER, weight=None, post_norm: int = B.KNAP_NORM_NONE,
+                 post_weight=None, alpha: float = 1.0, eps: float = 1e-6, x_type=torch.bfloat16, branch_type=torch.bfloat16, branch: bool = True,
+                 train: bool = True, device="cuda"):
+        self.rows, self.width, self.alpha, self.eps = int(rows), int(width), float(alpha), float(eps)
+        self.norm, self.weight, self.post_norm, self.post_weight = norm, weight, post_norm, post_weight
+        self.cu = None if cu_seqlens is None else torch.as_tensor(cu_seqlens, dtype=torch.int32).to(device)
+        self.n_seq = 1 if self.cu is None else self.cu.numel() - 1
+        self.branch = bool(branch)
+        normed = norm != B.KNAP_NORM_NONE
+
+        def new(there, dtype, *shape):
+            return torch.empty(shape or (self.rows, self.width), dtype=dtype, device=device) if there else None
+
+        f32 = torch.float32
+        self.x_out, self.y = new(branch, x_type), new(normed, branch_type)
+        self.stats = new(train, f32, 4, self.rows)
+        self.dx, self.df = new(train, x_type), new(train and branch, branch_type)
+        vectors = (self.n_seq, self.width)
+        self._dgate = new(train and branch, f32, *vectors)
+        self._dscale, self._dshift = new(train and normed, f32, *vectors), new(train and normed, f32, *vectors)
+        self.dgate = self.dscale = self.dshift = None
+        self.dweight, self.dpost_weight = new(train and weight is not None, f32, self.width), new(train and post_weight is not None, f32, self.width)
+        self.workspace = None
+        if train:
+            nbytes = B.knap_residual_norm_bwd_workspace_bytes(self.rows, self.width, self.n_seq)
+            self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+    def forward(self, x, f=None, gate=None, scale=None, shift=None, stream=None):
+        """x_out (x itself without a branch) and y (None without a norm)."""
+        B.knap_residual_norm_fwd(x, f, self.x_out, self.y, self.norm, self.post_norm, self.weight, self.post_weight, gate, scale, shift, self.cu,
+                                 self.alpha, self.eps, self.stats, stream)
+        return (self.x_out if self.branch else x), self.y
+
+    def backward(self, x, f, dx_out, dy, gate=None, scale=None, shift=None, stream=None):
+        """dx and df (None without a branch); x, f, gate and scale as the forward had them.  dgate is formed where a gate is given, dscale where
+        a scale is, dshift where a scale or a shift is."""
+        self.dgate = self._dgate if gate is not None else None
+        self.dscale = self._dscale if scale is not None else None
+        self.dshift = self._dshift if scale is not None or shift is not None else None
+        B.knap_residual_norm_bwd(x, f, self.stats, dx_out, dy, self.dx, self.df, self.norm, self.post_norm, self.weight, self.post_weight, gate, scale,
+                                 self.cu, self.alpha, self.dgate, self.dscale, self.dshift, self.dweight, self.dpost_weight, self.workspace, None,
+                                 stream)
+        return self.dx, self.df
+
+
+class GradientClip:
+    """Buffers + calls of the global norm of a fixed list of gradients and clipping by it, in place or into `out`.  Ranks that hold parts of the
+    gradients call sum_squares, add up `sum_sq` (an all-reduce of one float64) and call scale; clip does both on one GPU."""
+
+    def __init__(self, grads, max_norm: float, eps: float = 1e-6, out=None, device="cuda"):
+        self.list = B.GradList(grads, out)
+        self.max_norm, self.eps = float(max_norm), float(eps)
+        self.sum_sq = torch.zeros((), dtype=torch.float64, device=device)
+        self.norm = torch.zeros((), dtype=torch.float32, device=device)
+        self.workspace = torch.empty(max(B.knap_grad_sum_squares_workspace_bytes(self.list.n), 256), dtype=torch.uint8, device=device)
+
+    def sum_squares(self, stream=None):
+        B.knap_grad_sum_squares(self.list, self.sum_sq, self.workspace, None, stream)
+        return self.sum_sq
+
+    def scale(self, stream=None):
+        B.knap_grad_clip(self.list, self.sum_sq, self.max_norm, self.eps, self.norm, None, stream)
+        return self.norm
+
+    def clip(self, stream=None):
+        """The norm as it was before."""
+        self.sum_squares(stream)
+        return self.scale(stream)
+
+
 class VarlenAttention:
     """Buffers + calls for one packed bag: T tokens, H heads, head dim d; `causal` selects the
     causal pair of entry points; `rope`, a RotaryPositions, turns q and k in front of the attention
