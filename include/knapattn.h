@@ -456,6 +456,47 @@ int knap_residual_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t 
 size_t knap_residual_norm_bwd_workspace_bytes(int64_t rows, int width, int n_seq);
 
 /* ------------------------------------------------------------------------
+ * Gated feed-forward block, the other branch of a transformer block, forward and backward:
+ *     a = x Wg^T,  b = x Wu^T,  h = act(a) b,  y = h Wd^T
+ *     dh = dy Wd,  da = dh b act'(a),  db = dh act(a),
+ *     dx = da Wg + db Wu,  dWg = da^T x,  dWu = db^T x,  dWd = dy^T h
+ * act: KNAP_SILU a / (1 + exp(-a)), KNAP_GELU_TANH a / (1 + exp(-2 u)) with u = sqrt(2 / pi) (a + 0.044715 a^3),
+ * which is 0.5 a (1 + tanh u).
+ *
+ * All tensors are bf16.  x, y, dy, dx (tokens, width): columns contiguous, strides in elements from a row to the next, multiples of
+ * 8, >= width (not looked at for a single row).  w_gate, w_up (hidden, width), w_down (width, hidden), their gradients, and gate, up, h
+ * (tokens, hidden): contiguous.  gate and up, a and b, are what a backward takes; both NULL in the
+ * forward where none follows.  h is always written (the forward's second product reads it).
+ * Products are added up in 32 bits.  a, b, h, da and db are rounded to bf16: h, da and db, formed in 32 bits, because they are the next
+ * product's operand, a and b for the backward alone (h is formed from them as they were).
+ * Backward: dx and each of dw_gate, dw_up and dw_down may be NULL: not wanted.  Outputs are fully overwritten, must not alias inputs or each
+ * other, and have the same bits every time for the same call.  workspace: device scratch of at least
+ * knap_gated_ffn_fwd_workspace_bytes / _bwd_workspace_bytes(tokens, width, hidden) bytes, 256-byte aligned (NULL where that is 0): parts of
+ * sums over k and, backward, da and db; its contents on entry are ignored; one for each call that may run at the same time.
+ *
+ * Supported: width and hidden multiples of 8, 8 <= width, hidden <= KNAP_FFN_MAX_WIDTH, strides <= 2^20, 0 <= tokens <= 2^26; pointers aligned to 16 bytes.
+ * tokens = 0 enqueues nothing in the forward and zeros in the weights' gradients in the backward.  Rows are
+ * independent of each other: a value that is not finite stays in its row of y and dx.  As for the forward of attention, the first call of
+ * the library on a device must not be captured.
+ * ------------------------------------------------------------------------ */
+#define KNAP_SILU      0
+#define KNAP_GELU_TANH 1
+#define KNAP_FFN_MAX_WIDTH 65536
+
+int knap_gated_ffn_fwd(const void* x, int64_t x_stride, int64_t tokens, int width, int hidden,
+                       const void* w_gate, const void* w_up, const void* w_down, int act,
+                       void* gate, void* up, void* h, void* y, int64_t y_stride,
+                       void* workspace, size_t workspace_bytes, void* stream);
+size_t knap_gated_ffn_fwd_workspace_bytes(int64_t tokens, int width, int hidden);
+int knap_gated_ffn_bwd(const void* x, int64_t x_stride, int64_t tokens, int width, int hidden,
+                       const void* w_gate, const void* w_up, const void* w_down, int act,
+                       const void* gate, const void* up, const void* h,
+                       const void* dy, int64_t dy_stride, void* dx, int64_t dx_stride,
+                       void* dw_gate, void* dw_up, void* dw_down,
+                       void* workspace, size_t workspace_bytes, void* stream);
+size_t knap_gated_ffn_bwd_workspace_bytes(int64_t tokens, int width, int hidden);
+
+/* ------------------------------------------------------------------------
  * The global norm of a list of gradients, and clipping by it: the end of a training step.
  *     sum_sq = sum over all tensors of g^2,  norm = sqrt(sum_sq),
  *     c = min(1, max_norm / (norm + eps)),  out = c g

@@ -36,6 +36,9 @@ KNAP_ROPE_PARTS = 3
 KNAP_BF16 = 0
 KNAP_F32 = 1
 KNAP_LAYER_NORM_MAX_WIDTH = 16384
+KNAP_SILU = 0
+KNAP_GELU_TANH = 1
+KNAP_FFN_MAX_WIDTH = 65536
 KNAP_NORM_NONE = 0
 KNAP_NORM_RMS = 1
 KNAP_NORM_LAYER = 2
@@ -86,6 +89,10 @@ _SIGNATURES = {
     "knap_residual_norm_bwd": (_i, [_vp, _i, _i64, _i64, _i, _vp, _i, _i64, _vp, _i, _vp, _i64, _vp, _i64, _i, _vp, _vp, _i, _i, _i, _f, _vp,
                                     _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
     "knap_residual_norm_bwd_workspace_bytes": (_sz, [_i64, _i, _i]),
+    "knap_gated_ffn_fwd": (_i, [_vp, _i64, _i64, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "knap_gated_ffn_fwd_workspace_bytes": (_sz, [_i64, _i, _i]),
+    "knap_gated_ffn_bwd": (_i, [_vp, _i64, _i64, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "knap_gated_ffn_bwd_workspace_bytes": (_sz, [_i64, _i, _i]),
     "knap_grad_sum_squares": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _sz, _vp]),
     "knap_grad_sum_squares_workspace_bytes": (_sz, [_i]),
     "knap_grad_clip": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _f, _f, _vp, _vp]),
@@ -644,6 +651,76 @@ def knap_residual_norm_bwd(x, f, stats, dx_out, dy, dx, df, norm: int = KNAP_NOR
                                     r.mt, r.wp_at, r.w_at, r.wt, post_norm, norm, alpha, _ptr(stats), _ptr(dx_out), dxos, _ptr(dy), dys, _ptr(dx),
                                     dxs, _ptr(df), dfs, _ptr(dgate), dgs, _ptr(dscale), _ptr(dshift), dms, dw_at, dwp_at, _ptr(workspace),
                                     workspace_bytes, _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+# --------------------------------------------------------------------------- gated feed-forward
+
+def _ffn_rows(where: str, name: str, t, shape) -> int:
+    if t.dtype is not torch.bfloat16 or t.shape != shape or len(shape) != 2:
+        _refuse(where, f"{name} is a bf16 (tokens, width) tensor")
+    if t.is_contiguous():
+        return shape[1]
+    if t.stride(1) != 1:
+        _refuse(where, f"the rows of {name} are contiguous")
+    return t.stride(0)
+
+
+def _ffn_dense(where: str, *tensors) -> None:
+    for t, rows, cols in tensors:
+        if t is not None and (t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or not t.is_contiguous()):
+            _refuse(where, "weights (hidden, width), (hidden, width) and (width, hidden), their gradients, and gate, up and h (tokens, hidden) are "
+                           "contiguous bf16 tensors")
+
+
+def knap_gated_ffn_fwd_workspace_bytes(tokens: int, width: int, hidden: int) -> int:
+    return int(lib.knap_gated_ffn_fwd_workspace_bytes(tokens, width, hidden))
+
+
+def knap_gated_ffn_bwd_workspace_bytes(tokens: int, width: int, hidden: int) -> int:
+    return int(lib.knap_gated_ffn_bwd_workspace_bytes(tokens, width, hidden))
+
+
+def knap_gated_ffn_fwd(x, w_gate, w_up, w_down, act: int, gate, up, h, y, workspace, workspace_bytes: Optional[int] = None, stream=None,
+                       check: bool = True) -> int:
+    """y = (act(x w_gate^T) (x w_up^T)) w_down^T.  x, y: bf16 (tokens, width); w_gate, w_up: (hidden, width); w_down: (width, hidden); h and, for a
+    backward (else None), gate and up: (tokens, hidden)."""
+    where = "knap_gated_ffn_fwd"
+    _here(where, x, w_gate, w_up, w_down, gate, up, h, y, workspace)
+    shape = x.shape
+    xs, ys = _ffn_rows(where, "x", x, shape), _ffn_rows(where, "y", y, shape)
+    tokens, width = shape
+    hidden = w_gate.shape[0]
+    _ffn_dense(where, (w_gate, hidden, width), (w_up, hidden, width), (w_down, width, hidden), (gate, tokens, hidden), (up, tokens, hidden),
+               (h, tokens, hidden))
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib.knap_gated_ffn_fwd(x.data_ptr(), xs, tokens, width, hidden, w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), act, _ptr(gate), _ptr(up),
+                                _ptr(h), y.data_ptr(), ys, _ptr(workspace), workspace_bytes, _stream_handle(stream))
+    if check:
+        _check(rc, where)
+    return rc
+
+
+def knap_gated_ffn_bwd(x, w_gate, w_up, w_down, act: int, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, workspace,
+                       workspace_bytes: Optional[int] = None, stream=None, check: bool = True) -> int:
+    """Gradients of knap_gated_ffn_fwd, whose gate, up and h it takes; dx, dw_gate, dw_up and dw_down may be None."""
+    where = "knap_gated_ffn_bwd"
+    _here(where, x, w_gate, w_up, w_down, gate, up, h, dy, dx, dw_gate, dw_up, dw_down, workspace)
+    shape = x.shape
+    xs, dys = _ffn_rows(where, "x", x, shape), _ffn_rows(where, "dy", dy, shape)
+    dxs = 0 if dx is None else _ffn_rows(where, "dx", dx, shape)
+    tokens, width = shape
+    hidden = w_gate.shape[0]
+    _ffn_dense(where, (w_gate, hidden, width), (w_up, hidden, width), (w_down, width, hidden), (gate, tokens, hidden), (up, tokens, hidden),
+               (h, tokens, hidden), (dw_gate, hidden, width), (dw_up, hidden, width), (dw_down, width, hidden))
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib.knap_gated_ffn_bwd(x.data_ptr(), xs, tokens, width, hidden, w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), act, _ptr(gate), _ptr(up),
+                                _ptr(h), dy.data_ptr(), dys, _ptr(dx), dxs, _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace),
+                                workspace_bytes, _stream_handle(stream))
     if check:
         _check(rc, where)
     return rc

@@ -160,6 +160,109 @@ int knap_residual_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t 
 }
 
 // ---------------------------------------------------------------------------
+// Gated feed-forward
+// ---------------------------------------------------------------------------
+
+}  // extern "C"
+
+namespace {
+
+constexpr int64_t kFfnMostTokens = (int64_t)1 << 26;
+
+int check_ffn(int64_t tokens, int width, int hidden, const void* w_gate, const void* w_up, const void* w_down, int act) {
+  if (tokens < 0 || tokens > kFfnMostTokens || width < 8 || width > KNAP_FFN_MAX_WIDTH || width % 8 || hidden < 8 || hidden > KNAP_FFN_MAX_WIDTH || hidden % 8)
+    return KNAP_ERR_INVALID_ARG;
+  if (act != KNAP_SILU && act != KNAP_GELU_TANH) return KNAP_ERR_INVALID_ARG;
+  if (tokens > 0 && (!w_gate || !w_up || !w_down || !aligned(w_gate, 16) || !aligned(w_up, 16) || !aligned(w_down, 16))) return KNAP_ERR_INVALID_ARG;
+  return KNAP_OK;
+}
+bool ffn_rows(const void* p, int64_t stride, int64_t rows, int width) {
+  return p && aligned(p, 16) && (rows == 1 || (stride >= width && stride % 8 == 0 && stride <= (1 << 20)));
+}
+size_t ffn_hidden_bytes(int64_t tokens, int hidden) { return round_up((size_t)tokens * hidden * 2, 256); }
+
+}  // namespace
+
+extern "C" {
+
+size_t knap_gated_ffn_fwd_workspace_bytes(int64_t tokens, int width, int hidden) {
+  if (tokens <= 0 || tokens > kFfnMostTokens || width <= 0 || hidden <= 0 || width > KNAP_FFN_MAX_WIDTH || hidden > KNAP_FFN_MAX_WIDTH) return 0;
+  return round_up(knap::ffn_partial_bytes(tokens, width, hidden, false), 256);
+}
+
+size_t knap_gated_ffn_bwd_workspace_bytes(int64_t tokens, int width, int hidden) {
+  if (tokens <= 0 || tokens > kFfnMostTokens || width <= 0 || hidden <= 0 || width > KNAP_FFN_MAX_WIDTH || hidden > KNAP_FFN_MAX_WIDTH) return 0;
+  return 2 * ffn_hidden_bytes(tokens, hidden) + round_up(knap::ffn_partial_bytes(tokens, width, hidden, true), 256);
+}
+
+int knap_gated_ffn_fwd(const void* x, int64_t x_stride, int64_t tokens, int width, int hidden, const void* w_gate, const void* w_up, const void* w_down,
+                       int act, void* gate, void* up, void* h, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_ffn(tokens, width, hidden, w_gate, w_up, w_down, act);
+  if (rc != KNAP_OK) return rc;
+  if (tokens == 0) return KNAP_OK;
+  if (!ffn_rows(x, x_stride, tokens, width) || !ffn_rows(y, y_stride, tokens, width) || !h || !aligned(h, 16) || !gate != !up || !aligned(gate, 16) ||
+      !aligned(up, 16))
+    return KNAP_ERR_INVALID_ARG;
+  if (x == y || x == h || y == h || (gate && (gate == up || gate == h || up == h || gate == x || up == x || gate == y || up == y))) return KNAP_ERR_INVALID_ARG;
+  const size_t need = knap_gated_ffn_fwd_workspace_bytes(tokens, width, hidden);
+  if ((need && !workspace) || !aligned(workspace, 256)) return KNAP_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return KNAP_ERR_WORKSPACE_TOO_SMALL;
+  knap::FfnArgs a{};
+  a.x = static_cast<const __bf16*>(x);
+  a.w_gate = static_cast<const __bf16*>(w_gate); a.w_up = static_cast<const __bf16*>(w_up); a.w_down = static_cast<const __bf16*>(w_down);
+  a.x_stride = tokens == 1 ? width : x_stride; a.y_stride = tokens == 1 ? width : y_stride;
+  a.tokens = (int)tokens; a.width = width; a.hidden = hidden; a.gelu = act == KNAP_GELU_TANH;
+  a.gate = static_cast<__bf16*>(gate); a.up = static_cast<__bf16*>(up); a.h = static_cast<__bf16*>(h); a.y = static_cast<__bf16*>(y);
+  a.partial = static_cast<float*>(workspace);
+  if (!knap::device_cus()) return KNAP_ERR_LAUNCH_FAILED;
+  return knap::launch_status(knap::launch_ffn_fwd(a, static_cast<hipStream_t>(stream)));
+}
+
+int knap_gated_ffn_bwd(const void* x, int64_t x_stride, int64_t tokens, int width, int hidden, const void* w_gate, const void* w_up, const void* w_down,
+                       int act, const void* gate, const void* up, const void* h, const void* dy, int64_t dy_stride, void* dx, int64_t dx_stride,
+                       void* dw_gate, void* dw_up, void* dw_down, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_ffn(tokens, width, hidden, w_gate, w_up, w_down, act);
+  if (rc != KNAP_OK) return rc;
+  void* const outs[4] = {dx, dw_gate, dw_up, dw_down};
+  const void* const ins[6] = {x, gate, up, h, dy, workspace};
+  for (int i = 0; i < 4; ++i) {
+    if (!aligned(outs[i], 16)) return KNAP_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j]) return KNAP_ERR_INVALID_ARG;
+    for (const void* in : ins)
+      if (outs[i] && tokens > 0 && outs[i] == in) return KNAP_ERR_INVALID_ARG;
+    if (outs[i] && tokens > 0 && (outs[i] == w_gate || outs[i] == w_up || outs[i] == w_down)) return KNAP_ERR_INVALID_ARG;
+  }
+  if (tokens > 0) {
+    if (!ffn_rows(x, x_stride, tokens, width) || !ffn_rows(dy, dy_stride, tokens, width) || (dx && !ffn_rows(dx, dx_stride, tokens, width)))
+      return KNAP_ERR_INVALID_ARG;
+    if (!gate || !up || !h || !aligned(gate, 16) || !aligned(up, 16) || !aligned(h, 16)) return KNAP_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256)) return KNAP_ERR_INVALID_ARG;
+    if (workspace_bytes < knap_gated_ffn_bwd_workspace_bytes(tokens, width, hidden)) return KNAP_ERR_WORKSPACE_TOO_SMALL;
+  } else if (!dw_gate && !dw_up && !dw_down) {
+    return KNAP_OK;
+  }
+  knap::FfnArgs a{};
+  a.x = static_cast<const __bf16*>(x); a.dy = static_cast<const __bf16*>(dy);
+  a.w_gate = static_cast<const __bf16*>(w_gate); a.w_up = static_cast<const __bf16*>(w_up); a.w_down = static_cast<const __bf16*>(w_down);
+  a.x_stride = tokens == 1 ? width : x_stride; a.dy_stride = tokens == 1 ? width : dy_stride; a.dx_stride = tokens == 1 ? width : dx_stride;
+  a.tokens = (int)tokens; a.width = width; a.hidden = hidden; a.gelu = act == KNAP_GELU_TANH;
+  a.gate = const_cast<__bf16*>(static_cast<const __bf16*>(gate)); a.up = const_cast<__bf16*>(static_cast<const __bf16*>(up));
+  a.h = const_cast<__bf16*>(static_cast<const __bf16*>(h));
+  a.dx = static_cast<__bf16*>(dx);
+  a.dw_gate = static_cast<__bf16*>(dw_gate); a.dw_up = static_cast<__bf16*>(dw_up); a.dw_down = static_cast<__bf16*>(dw_down);
+  if (tokens > 0) {
+    char* ws = static_cast<char*>(workspace);
+    const size_t each = ffn_hidden_bytes(tokens, hidden);
+    a.dgate = reinterpret_cast<__bf16*>(ws);
+    a.dup = reinterpret_cast<__bf16*>(ws + each);
+    a.partial = reinterpret_cast<float*>(ws + 2 * each);
+  }
+  if (!knap::device_cus()) return KNAP_ERR_LAUNCH_FAILED;
+  return knap::launch_status(knap::launch_ffn_bwd(a, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
 // Gradient norm and clipping
 // ---------------------------------------------------------------------------
 

@@ -1,0 +1,306 @@
+// Gated feed-forward block, forward and backward, of T tokens (rows of x), D columns and F hidden ones:
+//   a = x Wg^T,  b = x Wu^T,  h = act(a) b,  y = h Wd^T
+//   dh = dy Wd,  da = dh b act'(a),  db = dh act(a),  dx = da Wg + db Wu,  dWg = da^T x,  dWu = db^T x,  dWd = dy^T h
+// act(a) = a s with s the logistic function of a (SiLU) or of 2 sqrt(2 / pi) (a + 0.044715 a^3) (GELU in its tanh form).
+// Five launches of the product of knap_gemm.h.  a and b are formed side by side, blocks of 32 columns of either in turn, so that a wave has both of
+// an element and act(a) b is its epilogue; da and db are the epilogue of dh, which never reaches memory; dx adds up two products over k.
+// a, b, h, da and db are rounded to 16 bits (h and da, db from 32-bit values): they are what the matrix cores multiply next.
+#include "knap_gemm.h"
+
+#include <algorithm>
+
+namespace knap {
+
+enum Epilogue { kStore, kActForward, kActBackward };
+
+// s(a) of the activation and, for its slope, the derivative of its argument
+__device__ __forceinline__ float logistic(float u) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(-kLog2e * u)); }
+__device__ __forceinline__ void activation(float a, bool gelu, float& s, float& du) {
+  if (gelu) {
+    // beyond 16 the logistic function is 0 or 1 in 32 bits, and a squared may overflow
+    const float c = __builtin_fminf(__builtin_fmaxf(a, -16.f), 16.f);
+    constexpr float k = 1.5957691216057308f;      // 2 sqrt(2 / pi)
+    s = logistic(k * __builtin_fmaf(0.044715f * c, c * c, c));
+    du = k * __builtin_fmaf(3.f * 0.044715f * c, c, 1.f);
+  } else {
+    s = logistic(a);
+    du = 1.f;
+  }
+}
+
+template <class C, int EP>
+__device__ __forceinline__ void finish_block(const GemmLaunch& g, const GemmProblem& p, int m0, int n0, int i, int j, const f32x16& x, const f32x16& x2) {
+  if constexpr (EP == kStore) {
+    const BlockPlace<C> at(m0, n0, i, j);
+    const TileRows c(p.c, p.ldc, p.M, p.N, m0, C::BM);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) c.store(at.m, at.n + 16 * u, pack_unit(x, u));
+  } else if constexpr (EP == kActForward) {      // x, x2: a and b of block j / 2 of the tile's hidden columns
+    const BlockPlace<C> pair(m0, 0, i, j);
+    const int m = pair.m, wn_first = pair.n - 8 * ((threadIdx.x & 63) >> 5);
+    const int n = n0 + wn_first / 2 + 8 * ((threadIdx.x & 63) >> 5);
+    f32x16 h;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float s, du;
+      activation(x[r], g.gelu, s, du);
+      h[r] = x[r] * s * x2[r];
+    }
+    const TileRows c(g.h, p.N, p.M, p.N, m0, C::BM);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) c.store(m, n + 16 * u, pack_unit(h, u));
+    if (g.gate) {
+      const TileRows ga(g.gate, p.N, p.M, p.N, m0, C::BM), up(g.up, p.N, p.M, p.N, m0, C::BM);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        ga.store(m, n + 16 * u, pack_unit(x, u));
+        up.store(m, n + 16 * u, pack_unit(x2, u));
+      }
+    }
+  } else {
+    const BlockPlace<C> at(m0, n0, i, j);
+    const TileRows gi(g.gate_in, p.N, p.M, p.N, m0, C::BM), ui(g.up_in, p.N, p.M, p.N, m0, C::BM);
+    const TileRows go(g.gate, p.N, p.M, p.N, m0, C::BM), uo(g.up, p.N, p.M, p.N, m0, C::BM);
+    f32x16 da, db;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float a[8], b[8];
+      open_unit(gi.load(at.m, at.n + 16 * u), a);
+      open_unit(ui.load(at.m, at.n + 16 * u), b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float s, du;
+        activation(a[e], g.gelu, s, du);
+        const float dh = x[8 * u + e];
+        da[8 * u + e] = dh * b[e] * __builtin_fmaf(a[e] * du, s * (1.f - s), s);
+        db[8 * u + e] = dh * a[e] * s;
+      }
+      go.store(at.m, at.n + 16 * u, pack_unit(da, u));
+      uo.store(at.m, at.n + 16 * u, pack_unit(db, u));
+    }
+  }
+}
+
+// which product a tile is of, and where it lies
+template <class C, bool PAIRED>
+__device__ __forceinline__ int locate(const GemmLaunch& g, int tile, int& m0, int& n0) {
+  const int q = tile >= g.first[1] ? (tile >= g.first[2] ? 2 : 1) : 0;
+  int tm, tn;
+  tile_place(tile - g.first[q], g.p[q].tiles_m, g.p[q].tiles_n, tm, tn);
+  m0 = tm * C::BM;
+  n0 = tn * (PAIRED ? C::BN / 2 : C::BN);
+  return q;
+}
+
+template <class C, bool A_ROWK, bool B_ROWK, int EP>
+__global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C::WAVES / 2) void gemm_kernel(GemmLaunch g) {
+  __shared__ __align__(1024) __bf16 lds[2 * C::STAGE];
+  constexpr bool PAIRED = EP == kActForward;
+  int tile, part = 0, parts = 1;
+  if ((int)blockIdx.x < g.whole) tile = xcd_order(blockIdx.x, g.whole);
+  else {
+    const int r = (int)blockIdx.x - g.whole;
+    tile = g.whole + r / g.splits;
+    part = r % g.splits;
+    parts = g.splits;
+  }
+  int m0, n0;
+  const int q = locate<C, PAIRED>(g, tile, m0, n0);
+  const GemmProblem& p = g.p[q];
+  const int steps = (p.K + kGemmK - 1) / kGemmK * p.segments;
+  f32x16 acc[C::TM][C::TN];
+  gemm_tile<C, A_ROWK, B_ROWK, PAIRED>(p, m0, n0, (int)((int64_t)steps * part / parts), (int)((int64_t)steps * (part + 1) / parts), lds, acc);
+  if (parts > 1) {
+    f32x4* to = reinterpret_cast<f32x4*>(g.partial) + (size_t)((int)blockIdx.x - g.whole) * (C::BM * C::BN / 4) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          to[((i * C::TN + j) * 4 + k) * C::THREADS] = f32x4{acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+    for (int j = 0; j < C::TN; j += PAIRED ? 2 : 1) finish_block<C, EP>(g, p, m0, n0, i, j, acc[i][j], acc[i][PAIRED ? j + 1 : j]);
+}
+
+// Adds up the parts of a tile's block (blockIdx.y; of a pair of blocks) in their order and finishes it
+template <class C, int EP>
+__global__ __launch_bounds__(C::THREADS) void gemm_join_kernel(GemmLaunch g) {
+  constexpr bool PAIRED = EP == kActForward;
+  constexpr int STEP = PAIRED ? 2 : 1;
+  int m0, n0;
+  const int q = locate<C, PAIRED>(g, g.whole + (int)blockIdx.x, m0, n0);
+  const int i = (int)blockIdx.y / (C::TN / STEP), j = (int)blockIdx.y % (C::TN / STEP) * STEP;
+  f32x16 x[STEP];
+  for (int e = 0; e < STEP; ++e) x[e] = zero16();
+  for (int z = 0; z < g.splits; ++z) {
+    const f32x4* from = reinterpret_cast<const f32x4*>(g.partial) + ((size_t)blockIdx.x * g.splits + z) * (C::BM * C::BN / 4) + threadIdx.x;
+#pragma unroll
+    for (int e = 0; e < STEP; ++e)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const f32x4 v = from[((i * C::TN + j + e) * 4 + k) * C::THREADS];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) x[e][4 * k + w] += v[w];
+      }
+  }
+  // the block's place is a constant of the epilogue's accesses only by its row and column
+#pragma unroll
+  for (int ii = 0; ii < C::TM; ++ii)
+#pragma unroll
+    for (int jj = 0; jj < C::TN; jj += STEP)
+      if (ii == i && jj == j) finish_block<C, EP>(g, g.p[q], m0, n0, ii, jj, x[0], x[STEP - 1]);
+}
+
+using Large = GemmCfg<256, 256, 2, 4>;
+using Small = GemmCfg<128, 128, 2, 2>;
+
+// ---------------------------------------------------------------------------
+// Plans
+// ---------------------------------------------------------------------------
+constexpr int kGemmCus = 256;
+
+// Tiles of the products in `g`, what of them goes in parts, and the bytes that the parts take
+template <class C>
+size_t plan(GemmLaunch& g, bool paired) {
+  int tiles = 0, steps = 1 << 30;
+  for (int q = 0; q < 3; ++q) {
+    g.first[q] = q < g.n ? tiles : INT32_MAX;
+    if (q >= g.n) continue;
+    GemmProblem& p = g.p[q];
+    const int bn = paired ? C::BN / 2 : C::BN;
+    p.tiles_m = (p.M + C::BM - 1) / C::BM;
+    p.tiles_n = (p.N + bn - 1) / bn;
+    tiles += p.tiles_m * p.tiles_n;
+    steps = std::min(steps, (p.K + kGemmK - 1) / kGemmK * p.segments);
+  }
+  const int slots = kGemmCus * (C::LDS_BYTES > 81920 ? 1 : 2);
+  const int rest = tiles % slots;
+  g.splits = rest ? std::min(slots / rest, std::max(1, steps / 4)) : 1;
+  g.whole = g.splits > 1 ? tiles - rest : tiles;
+  g.tail = tiles - g.whole;
+  return (size_t)g.tail * g.splits * C::BM * C::BN * sizeof(float);
+}
+
+template <class C, bool A_ROWK, bool B_ROWK, int EP>
+hipError_t launch_gemm(const GemmLaunch& g, hipStream_t stream) {
+  constexpr int BLOCKS = C::TM * C::TN / (EP == kActForward ? 2 : 1);
+  if (g.whole + (int64_t)g.tail * g.splits > 1 << 22) return hipErrorInvalidValue;      // 2^38 results, more than the card holds
+  hipLaunchKernelGGL((gemm_kernel<C, A_ROWK, B_ROWK, EP>), dim3(g.whole + g.tail * g.splits), dim3(C::THREADS), 0, stream, g);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || g.tail == 0) return e;
+  hipLaunchKernelGGL((gemm_join_kernel<C, EP>), dim3(g.tail, BLOCKS), dim3(C::THREADS), 0, stream, g);
+  return hipGetLastError();
+}
+
+// Tiles of 256 x 256 where they fill the card more than once, else of 128 x 128
+static bool large(const GemmLaunch& g, bool paired) {
+  int64_t tiles = 0;
+  for (int q = 0; q < g.n; ++q) tiles += (int64_t)((g.p[q].M + 255) / 256) * ((g.p[q].N + (paired ? 127 : 255)) / (paired ? 128 : 256));
+  return tiles >= kGemmCus;
+}
+
+template <bool A_ROWK, bool B_ROWK, int EP>
+size_t bytes_of(GemmLaunch g) {
+  return large(g, EP == kActForward) ? plan<Large>(g, EP == kActForward) : plan<Small>(g, EP == kActForward);
+}
+template <bool A_ROWK, bool B_ROWK, int EP>
+hipError_t run(GemmLaunch g, hipStream_t stream) {
+  if (large(g, EP == kActForward)) {
+    plan<Large>(g, EP == kActForward);
+    return launch_gemm<Large, A_ROWK, B_ROWK, EP>(g, stream);
+  }
+  plan<Small>(g, EP == kActForward);
+  return launch_gemm<Small, A_ROWK, B_ROWK, EP>(g, stream);
+}
+
+static GemmProblem product(const __bf16* a, int64_t lda, const __bf16* b, int64_t ldb, __bf16* c, int64_t ldc, int M, int N, int K) {
+  GemmProblem p{};
+  p.a[0] = p.a[1] = a;
+  p.b[0] = p.b[1] = b;
+  p.c = c;
+  p.lda = lda; p.ldb = ldb; p.ldc = ldc;
+  p.M = M; p.N = N; p.K = K;
+  p.segments = 1;
+  return p;
+}
+
+static GemmLaunch up_products(const FfnArgs& a) {
+  GemmLaunch g{};
+  g.n = 1;
+  g.p[0] = product(a.x, a.x_stride, a.w_gate, a.width, nullptr, 0, a.tokens, a.hidden, a.width);
+  g.p[0].b[1] = a.w_up;
+  g.gate = a.gate; g.up = a.up; g.h = a.h;
+  g.gelu = a.gelu;
+  g.partial = a.partial;
+  return g;
+}
+static GemmLaunch down_product(const FfnArgs& a) {
+  GemmLaunch g{};
+  g.n = 1;
+  g.p[0] = product(a.h, a.hidden, a.w_down, a.hidden, a.y, a.y_stride, a.tokens, a.width, a.hidden);
+  g.partial = a.partial;
+  return g;
+}
+static GemmLaunch hidden_gradients(const FfnArgs& a) {
+  GemmLaunch g{};
+  g.n = 1;
+  g.p[0] = product(a.dy, a.dy_stride, a.w_down, a.hidden, nullptr, 0, a.tokens, a.hidden, a.width);
+  g.gate_in = a.gate; g.up_in = a.up;
+  g.gate = a.dgate; g.up = a.dup;
+  g.gelu = a.gelu;
+  g.partial = a.partial;
+  return g;
+}
+static GemmLaunch input_gradient(const FfnArgs& a) {
+  GemmLaunch g{};
+  g.n = 1;
+  g.p[0] = product(a.dgate, a.hidden, a.w_gate, a.width, a.dx, a.dx_stride, a.tokens, a.width, a.hidden);
+  g.p[0].a[1] = a.dup;
+  g.p[0].b[1] = a.w_up;
+  g.p[0].segments = 2;
+  g.partial = a.partial;
+  return g;
+}
+static GemmLaunch weight_gradients(const FfnArgs& a) {
+  GemmLaunch g{};
+  if (a.dw_gate) g.p[g.n++] = product(a.dgate, a.hidden, a.x, a.x_stride, a.dw_gate, a.width, a.hidden, a.width, a.tokens);
+  if (a.dw_up) g.p[g.n++] = product(a.dup, a.hidden, a.x, a.x_stride, a.dw_up, a.width, a.hidden, a.width, a.tokens);
+  if (a.dw_down) g.p[g.n++] = product(a.dy, a.dy_stride, a.h, a.hidden, a.dw_down, a.hidden, a.width, a.hidden, a.tokens);
+  g.partial = a.partial;
+  return g;
+}
+
+size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward) {
+  FfnArgs a{};
+  a.tokens = (int)tokens; a.width = width; a.hidden = hidden;
+  if (!backward) return std::max(bytes_of<true, true, kActForward>(up_products(a)), bytes_of<true, true, kStore>(down_product(a)));
+  size_t most = std::max(bytes_of<true, false, kActBackward>(hidden_gradients(a)), bytes_of<true, false, kStore>(input_gradient(a)));
+  for (int wanted = 1; wanted < 8; ++wanted) {      // whichever gradients of weights a call asks for
+    static __bf16 none;
+    a.dw_gate = wanted & 1 ? &none : nullptr;
+    a.dw_up = wanted & 2 ? &none : nullptr;
+    a.dw_down = wanted & 4 ? &none : nullptr;
+    most = std::max(most, bytes_of<false, false, kStore>(weight_gradients(a)));
+  }
+  return most;
+}
+
+hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t stream) {
+  const hipError_t e = run<true, true, kActForward>(up_products(a), stream);
+  return e != hipSuccess ? e : run<true, true, kStore>(down_product(a), stream);
+}
+
+hipError_t launch_ffn_bwd(const FfnArgs& a, hipStream_t stream) {
+  hipError_t e = hipSuccess;
+  if (a.tokens > 0 && (a.dx || a.dw_gate || a.dw_up)) e = run<true, false, kActBackward>(hidden_gradients(a), stream);
+  if (e == hipSuccess && a.tokens > 0 && a.dx) e = run<true, false, kStore>(input_gradient(a), stream);
+  if (e == hipSuccess && (a.dw_gate || a.dw_up || a.dw_down)) e = run<false, false, kStore>(weight_gradients(a), stream);
+  return e;
+}
+
+}  // namespace knap

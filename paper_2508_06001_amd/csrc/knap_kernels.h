@@ -144,6 +144,39 @@ hipError_t launch_grad_squares(const GradTable& t, double* partial, int groups, 
 hipError_t launch_grad_join(const double* partial, int n, double* sum, hipStream_t stream);
 hipError_t launch_grad_clip(const GradTable& t, const double* sum, float max_norm, float eps, float* norm, int groups, hipStream_t stream);
 
+// Matrix products of the gated feed-forward block (knap_gemm.h).  One product of a launch:
+struct GemmProblem {
+  const __bf16 *a[2], *b[2];      // of the segments of k; a pair of products: b of the first and of the second
+  __bf16* c;
+  int64_t lda, ldb, ldc;
+  int M, N, K;
+  int segments;                   // 1 or 2 products of K each, added up
+  int tiles_m, tiles_n;
+};
+struct GemmLaunch {
+  GemmProblem p[3];
+  int first[3];             // tiles in front of a product's
+  int n;                    // products
+  int whole, tail, splits;  // tiles that a workgroup forms alone; the others, in `splits` parts of their steps
+  float* partial;           // of the parts
+  // epilogues: activations' inputs and outputs, (tokens, hidden)
+  const __bf16 *gate_in, *up_in;
+  __bf16 *gate, *up, *h;
+  bool gelu;
+};
+struct FfnArgs {
+  const __bf16 *x, *w_gate, *w_up, *w_down, *dy;
+  int64_t x_stride, y_stride, dy_stride, dx_stride;
+  int tokens, width, hidden;
+  bool gelu;
+  __bf16 *gate, *up, *h, *y;      // gate, up (forward): or nullptr
+  __bf16 *dgate, *dup, *dx, *dw_gate, *dw_up, *dw_down;
+  float* partial;
+};
+size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward);
+hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t stream);
+hipError_t launch_ffn_bwd(const FfnArgs& a, hipStream_t stream);
+
 // for entry points in other files than knap_api.hip: compute units of the current device, 0 where they could not be looked up (as for the
 // forward of attention, the first call on a device asks the runtime), and the status of a launch, which is kept for knap_last_hip_error
 int device_cus();

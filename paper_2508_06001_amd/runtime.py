@@ -126,6 +126,35 @@ class ResidualNorm:
         return self.dx, self.df
 
 
+class GatedFeedForward:
+    """Buffers + calls of the gated feed-forward block of (tokens, width) rows: y = (act(x w_gate^T) (x w_up^T)) w_down^T."""
+
+    def __init__(self, tokens: int, width: int, hidden: int, w_gate, w_up, w_down, act: int = B.KNAP_SILU, train: bool = True, device="cuda"):
+        self.tokens, self.width, self.hidden, self.act = int(tokens), int(width), int(hidden), act
+        self.w_gate, self.w_up, self.w_down = w_gate, w_up, w_down
+
+        def new(*shape):
+            return torch.empty(shape, dtype=torch.bfloat16, device=device)
+
+        self.y, self.h = new(self.tokens, self.width), new(self.tokens, self.hidden)
+        self.gate = self.up = self.dx = self.dw_gate = self.dw_up = self.dw_down = None
+        nbytes = B.knap_gated_ffn_fwd_workspace_bytes(self.tokens, self.width, self.hidden)
+        if train:
+            self.gate, self.up, self.dx = new(self.tokens, self.hidden), new(self.tokens, self.hidden), new(self.tokens, self.width)
+            self.dw_gate, self.dw_up, self.dw_down = new(self.hidden, self.width), new(self.hidden, self.width), new(self.width, self.hidden)
+            nbytes = max(nbytes, B.knap_gated_ffn_bwd_workspace_bytes(self.tokens, self.width, self.hidden))
+        self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+    def forward(self, x, stream=None):
+        B.knap_gated_ffn_fwd(x, self.w_gate, self.w_up, self.w_down, self.act, self.gate, self.up, self.h, self.y, self.workspace, None, stream)
+        return self.y
+
+    def backward(self, x, dy, stream=None):
+        B.knap_gated_ffn_bwd(x, self.w_gate, self.w_up, self.w_down, self.act, self.gate, self.up, self.h, dy, self.dx, self.dw_gate, self.dw_up,
+                             self.dw_down, self.workspace, None, stream)
+        return self.dx, self.dw_gate, self.dw_up, self.dw_down
+
+
 class GradientClip:
     """Buffers + calls of the global norm of a fixed list of gradients and clipping by it, in place or into `out`.  Ranks that hold parts of the
     gradients call sum_squares, add up `sum_sq` (an all-reduce of one float64) and call scale; clip does both on one GPU."""
