@@ -28,6 +28,15 @@ __device__ __forceinline__ void activation(float a, bool gelu, float& s, float& 
   }
 }
 
+// da and db of an element
+__device__ __forceinline__ void hidden_gradient(float dh, float a, float b, bool gelu, float& da, float& db) {
+  float s, du;
+  activation(a, gelu, s, du);
+  da = dh * b * __builtin_fmaf(a * du, s * (1.f - s), s);
+  db = dh * a * s;
+}
+
+// The epilogue of one block, from its registers (of tiles whose parts were added up)
 template <class C, int EP>
 __device__ __forceinline__ void finish_block(const GemmLaunch& g, const GemmProblem& p, int m0, int n0, int i, int j, const f32x16& x, const f32x16& x2) {
   if constexpr (EP == kStore) {
@@ -69,15 +78,122 @@ __device__ __forceinline__ void finish_block(const GemmLaunch& g, const GemmProb
       open_unit(ui.load(at.m, at.n + 16 * u), b);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float s, du;
-        activation(a[e], g.gelu, s, du);
-        const float dh = x[8 * u + e];
-        da[8 * u + e] = dh * b[e] * __builtin_fmaf(a[e] * du, s * (1.f - s), s);
-        db[8 * u + e] = dh * a[e] * s;
+        float ga, gb;
+        hidden_gradient(x[8 * u + e], a[e], b[e], g.gelu, ga, gb);
+        da[8 * u + e] = ga;
+        db[8 * u + e] = gb;
       }
       go.store(at.m, at.n + 16 * u, pack_unit(da, u));
       uo.store(at.m, at.n + 16 * u, pack_unit(db, u));
     }
+  }
+}
+
+// The epilogue of a whole tile.  A wave's rows of results lie across its lanes' registers, so that stores from there would write 32 bytes of 32 rows
+// each; they go through its own part of the buffers in LDS, 32 rows at a time, and out in rows, past the caches: what is written there would only
+// push out what the other workgroups multiply (256 x 256 tiles, us, from registers, through LDS, and past the caches as well: 32768 x 8192 x 1536
+// 809, 741, 640; 8192^3 858, 811, 756).
+constexpr int kPast = 2;      // the non-temporal bit of a buffer access
+template <class C, int EP>
+__device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProblem& p, int m0, int n0, const f32x16 (&acc)[C::TM][C::TN],
+                                            const GemmBuffers& lds) {
+  static_assert(C::WAVES == 4 && C::BUFFERS == 2 && C::STAGE >= 4 * 32 * 32 * C::TN, "a wave has half of a buffer");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / C::WN, wn = wave % C::WN;
+  // (of the LDS address space, which a choice between two arrays otherwise loses)
+  using LdsFloat = __attribute__((address_space(3))) float;
+  using LdsFloat4 = __attribute__((address_space(3))) f32x4;
+  LdsFloat* const part0 = (LdsFloat*)lds.b0;
+  LdsFloat* const part1 = (LdsFloat*)lds.b1;
+  LdsFloat* mine = (wave & 1 ? part1 : part0) + (wave >> 1) * (C::STAGE / 4);
+  constexpr int COLS = 32 * C::TN, UNITS = COLS / 8;      // of a wave's rows
+  constexpr int OUT = EP == kActForward ? COLS / 2 : COLS, OUT_UNITS = OUT / 8;      // of an output
+  const int n_first = n0 + wn * OUT;
+  auto place = [&](int row, int unit) { return mine + row * COLS + (unit ^ (row & (UNITS - 1))) * 8; };
+  auto settle = [&]() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    KNAP_SCHED_FENCE();
+  };
+  auto fetch = [&](int row, int unit, float (&v)[8]) {
+    const f32x4 x = *(const LdsFloat4*)place(row, unit), y = *(const LdsFloat4*)(place(row, unit) + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = x[e]; v[4 + e] = y[e]; }
+  };
+  auto put = [&](const TileRows& to, int at, const float (&v)[8]) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, pack8(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7])), to.r, at, 0, kPast);
+  };
+  const TileRows out0(EP == kStore ? p.c : g.gate, EP == kStore ? p.ldc : p.N, g.gate || EP == kStore ? p.M : 0, p.N, m0, C::BM);
+  const TileRows out1(EP == kStore ? nullptr : g.up, p.N, EP != kStore && g.up ? p.M : 0, p.N, m0, C::BM);
+  const TileRows in0(EP == kActForward ? g.h : g.gate_in, p.N, p.M, p.N, m0, C::BM), in1(g.up_in, p.N, p.M, p.N, m0, C::BM);
+  constexpr int TURNS = 32 * OUT_UNITS / 64;
+  // a and b of 32 rows, asked for while the 32 before them are worked on
+  constexpr bool INPUTS = EP == kActBackward;
+  u32x4 a_ahead[INPUTS ? TURNS : 1], b_ahead[INPUTS ? TURNS : 1];
+  auto ask = [&](int i) {
+    if constexpr (INPUTS) {
+#pragma unroll
+      for (int q = 0; q < TURNS; ++q) {
+        const int row = (q * 64 + lane) / OUT_UNITS, unit = (q * 64 + lane) % OUT_UNITS;
+        const int at = in0.at(m0 + (wm * C::TM + i) * 32 + row, n_first + 8 * unit);
+        a_ahead[q] = __builtin_amdgcn_raw_buffer_load_b128(in0.r, at, 0, kPast);
+        b_ahead[q] = __builtin_amdgcn_raw_buffer_load_b128(in1.r, at, 0, kPast);
+      }
+    }
+  };
+  ask(0);
+#pragma unroll
+  for (int i = 0; i < C::TM; ++i) {
+    u32x4 a_now[INPUTS ? TURNS : 1], b_now[INPUTS ? TURNS : 1];
+    if constexpr (INPUTS) {
+#pragma unroll
+      for (int q = 0; q < TURNS; ++q) { a_now[q] = a_ahead[q]; b_now[q] = b_ahead[q]; }
+      if (i + 1 < C::TM) ask(i + 1);
+    }
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)      // columns 8 q + 4 (lane / 32) .. + 3 of the block
+        *(LdsFloat4*)(place(lane & 31, 4 * j + q) + 4 * (lane >> 5)) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    settle();
+#pragma unroll
+    for (int q = 0; q < TURNS; ++q) {
+      const int row = (q * 64 + lane) / OUT_UNITS, unit = (q * 64 + lane) % OUT_UNITS;
+      const int at = out0.at(m0 + (wm * C::TM + i) * 32 + row, n_first + 8 * unit);
+      float x[8];
+      if constexpr (EP == kStore) {
+        fetch(row, unit, x);
+        put(out0, at, x);
+      } else if constexpr (EP == kActForward) {
+        float b[8], h[8];
+        const int from = (unit >> 2) * 8 + (unit & 3);      // a's block of 32 columns, b's behind it
+        fetch(row, from, x);
+        fetch(row, from + 4, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float s, du;
+          activation(x[e], g.gelu, s, du);
+          h[e] = x[e] * s * b[e];
+        }
+        const int place_h = in0.at(m0 + (wm * C::TM + i) * 32 + row, n_first + 8 * unit);
+        put(in0, place_h, h);
+        put(out0, at, x);
+        put(out1, at, b);
+      } else {
+        const u32x4 av = a_now[q], bv = b_now[q];
+        fetch(row, unit, x);
+        float da[8], db[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float a = __builtin_bit_cast(float, (e & 1) ? av[e >> 1] & 0xffff0000u : av[e >> 1] << 16);
+          const float b = __builtin_bit_cast(float, (e & 1) ? bv[e >> 1] & 0xffff0000u : bv[e >> 1] << 16);
+          hidden_gradient(x[e], a, b, g.gelu, da[e], db[e]);
+        }
+        put(out0, at, da);
+        put(out1, at, db);
+      }
+    }
+    settle();
   }
 }
 
@@ -94,8 +210,8 @@ __device__ __forceinline__ int locate(const GemmLaunch& g, int tile, int& m0, in
 
 template <class C, bool A_ROWK, bool B_ROWK, int EP>
 __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C::WAVES / 2) void gemm_kernel(GemmLaunch g) {
-  __shared__ __align__(1024) __bf16 lds[2 * C::STAGE];
-  constexpr bool PAIRED = EP == kActForward;
+  __shared__ __align__(1024) __bf16 b0[C::STAGE], b1[C::STAGE];
+  constexpr bool PAIRED = EP == kActForward, TWO = EP == kStore && A_ROWK && !B_ROWK;      // dx alone adds up two products
   int tile, part = 0, parts = 1;
   if ((int)blockIdx.x < g.whole) tile = xcd_order(blockIdx.x, g.whole);
   else {
@@ -107,9 +223,9 @@ __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C
   int m0, n0;
   const int q = locate<C, PAIRED>(g, tile, m0, n0);
   const GemmProblem& p = g.p[q];
-  const int steps = (p.K + kGemmK - 1) / kGemmK * p.segments;
+  const int stages = (p.K + C::KS - 1) / C::KS * p.segments;
   f32x16 acc[C::TM][C::TN];
-  gemm_tile<C, A_ROWK, B_ROWK, PAIRED>(p, m0, n0, (int)((int64_t)steps * part / parts), (int)((int64_t)steps * (part + 1) / parts), lds, acc);
+  gemm_tile<C, A_ROWK, B_ROWK, PAIRED, TWO>(p, m0, n0, (int)((int64_t)stages * part / parts), (int)((int64_t)stages * (part + 1) / parts), GemmBuffers{b0, b1}, acc);
   if (parts > 1) {
     f32x4* to = reinterpret_cast<f32x4*>(g.partial) + (size_t)((int)blockIdx.x - g.whole) * (C::BM * C::BN / 4) + threadIdx.x;
 #pragma unroll
@@ -121,10 +237,7 @@ __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C
           to[((i * C::TN + j) * 4 + k) * C::THREADS] = f32x4{acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
     return;
   }
-#pragma unroll
-  for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-    for (int j = 0; j < C::TN; j += PAIRED ? 2 : 1) finish_block<C, EP>(g, p, m0, n0, i, j, acc[i][j], acc[i][PAIRED ? j + 1 : j]);
+  finish_tile<C, EP>(g, p, m0, n0, acc, GemmBuffers{b0, b1});
 }
 
 // Adds up the parts of a tile's block (blockIdx.y; of a pair of blocks) in their order and finishes it
@@ -156,7 +269,7 @@ __global__ __launch_bounds__(C::THREADS) void gemm_join_kernel(GemmLaunch g) {
       if (ii == i && jj == j) finish_block<C, EP>(g, g.p[q], m0, n0, ii, jj, x[0], x[STEP - 1]);
 }
 
-using Large = GemmCfg<256, 256, 2, 4>;
+using Large = GemmCfg<256, 256, 2, 2>;
 using Small = GemmCfg<128, 128, 2, 2>;
 
 // ---------------------------------------------------------------------------
@@ -167,7 +280,7 @@ constexpr int kGemmCus = 256;
 // Tiles of the products in `g`, what of them goes in parts, and the bytes that the parts take
 template <class C>
 size_t plan(GemmLaunch& g, bool paired) {
-  int tiles = 0, steps = 1 << 30;
+  int tiles = 0, stages = 1 << 30;
   for (int q = 0; q < 3; ++q) {
     g.first[q] = q < g.n ? tiles : INT32_MAX;
     if (q >= g.n) continue;
@@ -176,11 +289,11 @@ size_t plan(GemmLaunch& g, bool paired) {
     p.tiles_m = (p.M + C::BM - 1) / C::BM;
     p.tiles_n = (p.N + bn - 1) / bn;
     tiles += p.tiles_m * p.tiles_n;
-    steps = std::min(steps, (p.K + kGemmK - 1) / kGemmK * p.segments);
+    stages = std::min(stages, (p.K + C::KS - 1) / C::KS * p.segments);
   }
   const int slots = kGemmCus * (C::LDS_BYTES > 81920 ? 1 : 2);
   const int rest = tiles % slots;
-  g.splits = rest ? std::min(slots / rest, std::max(1, steps / 4)) : 1;
+  g.splits = rest ? std::min(slots / rest, std::max(1, stages / 4)) : 1;
   g.whole = g.splits > 1 ? tiles - rest : tiles;
   g.tail = tiles - g.whole;
   return (size_t)g.tail * g.splits * C::BM * C::BN * sizeof(float);

@@ -2,11 +2,12 @@
 // An operand either lies with k along its rows (ROWK: element (r, k) at r ld + k) or with k down its rows (element (r, k) at k ld + r), so that
 // all products of the block take their tensors as they are: nothing is transposed in memory.
 //
-// A workgroup of WM x WN waves forms a tile of BM x BN, a wave TM x TN blocks of 32 x 32.  Steps of 64 k's go through two buffers in LDS,
-// filled past the registers by asynchronous copies in the swizzled layouts of knap_device.h: [rows][64] for ROWK, read 16 bytes a lane, and
-// [64][128] for the other, read transposed.  A wave reads the fragments of the next 16 k's while it multiplies these; at a step's last 16 it
-// first meets the others (whose reads of this step are behind them, so that its buffer is free for the step after next), and goes on with products of
-// fragments that it has: the matrix cores wait at no barrier for memory.
+// A workgroup of WM x WN waves forms a tile of BM x BN, a wave TM x TN blocks of 32 x 32.  Stages of 32 k's go through a ring of four buffers in LDS,
+// filled past the registers by asynchronous copies three stages ahead: [rows][32] for ROWK, read 16 bytes a lane, and [32][128] for the other, read
+// transposed, both in layouts that neither way of reading meets a bank twice in.  A wave reads the fragments of the next 16 k's while it multiplies
+// these; in the middle of a stage it meets the others, whose reads of the stage before are behind them (so that its buffer is free) and whose copies of
+// the next one have arrived, and goes on with products of fragments that it has: the matrix cores wait at no barrier for memory.  The buffers are
+// arrays of their own, and the ring is unrolled: of one array the compiler would wait for every copy under way in front of each transposed read.
 //
 // Rows and k's that a tensor does not have are zeros: the descriptors end behind its last row; k's behind a row's end, which memory
 // holds something else at, are asked for behind the descriptor.  Columns behind the last one of a tensor with k down its rows are whatever the next row
@@ -16,36 +17,47 @@
 #include "knap_device.h"
 #include "knap_kernels.h"
 
+#include <type_traits>
+
 namespace knap {
 
-constexpr int kGemmK = 64;               // k's of a step
 constexpr int kGemmNowhere = 0x7fffffe0;  // a byte offset behind every descriptor
 
 template <int BM_, int BN_, int WM_, int WN_>
 struct GemmCfg {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int KS = 64, BUFFERS = 2;              // k's of a stage, buffers of the ring
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-  static constexpr int STAGE = (BM + BN) * kGemmK;      // elements
-  static constexpr int LDS_BYTES = 2 * STAGE * 2;
+  static constexpr int STAGE = (BM + BN) * KS;      // elements
+  static constexpr int LDS_BYTES = BUFFERS * STAGE * 2;
 };
+struct GemmBuffers { __bf16 *b0, *b1; };
+template <int B>
+__device__ __forceinline__ __bf16* buffer_of(const GemmBuffers& s) {
+  if constexpr (B == 0) return s.b0;
+  else return s.b1;
+}
 
-// Copies of R rows (columns) of an operand for one step: instruction i of a wave fills 1 KB.
-// ROWK: 8 rows of 128 bytes each; else 4 rows of 256 bytes in one of the R / 128 blocks of [64][128].
-template <int R, bool ROWK, int WAVES>
+// Copies of R rows (columns) of an operand for one stage of KS k's: instruction i of a wave fills 1 KB.
+// ROWK: whole rows of 64 or 128 bytes.  Unit c (16 bytes) of row r lies at c ^ ((r / 4) % 4) or c ^ ((r / 2) % 8): 16 rows put one unit in 16 places
+// of a 256-byte line.  else: 4 rows of 256 bytes in one of the R / 128 blocks of [KS][128], a Tile<128>.
+template <int R, bool ROWK, int WAVES, int KS>
 struct OperandLoader {
-  static constexpr int COUNT = R / 8 / WAVES;
-  static_assert(R % (8 * WAVES) == 0 && (ROWK || R % 128 == 0), "whole instructions for every wave");
-  // the row (of the R, or of the 64 k's) and the 16-byte unit within it that this lane brings in instruction i
+  static constexpr int UNITS = KS / 8, ROWS = 64 / UNITS;      // units of a row, rows of an instruction (ROWK)
+  static constexpr int COUNT = R / ROWS / WAVES;
+  static_assert(R % (ROWS * WAVES) == 0 && (ROWK || R % 128 == 0), "whole instructions for every wave");
+  // the row (of the R, or of the KS k's) and the 16-byte unit within it that this lane brings in instruction i
   static __device__ __forceinline__ int row(int i, int wave, int lane) {
     const int q = i * WAVES + wave;
-    return ROWK ? 8 * q + (lane >> 3) : 4 * (q & 15) + (lane >> 4);
+    return ROWK ? ROWS * q + lane / UNITS : 4 * (q & (KS / 4 - 1)) + (lane >> 4);
   }
   static __device__ __forceinline__ int unit(int i, int wave, int lane) {
     const int r = row(i, wave, lane);
-    return ROWK ? (lane & 7) ^ ((r >> 1) & 7) : (lane & 15) ^ (4 * (r & 3) + ((r >> 2) & 3));
+    if constexpr (ROWK) return KS == 32 ? (lane & 3) ^ ((r >> 2) & 3) : (lane & 7) ^ ((r >> 1) & 7);
+    else return (lane & 15) ^ (4 * (r & 3) + ((r >> 2) & 3));
   }
-  static __device__ __forceinline__ int block(int i, int wave) { return ROWK ? 0 : (i * WAVES + wave) >> 4; }
+  static __device__ __forceinline__ int block(int i, int wave) { return ROWK ? 0 : (i * WAVES + wave) / (KS / 4); }
   // LDS element that the instruction starts at
   static __device__ __forceinline__ int place(int i, int wave) { return (i * WAVES + wave) * 512; }
 };
@@ -55,11 +67,12 @@ __device__ __forceinline__ void copy_1k(__bf16* to, __amdgpu_buffer_rsrc_t r, in
 }
 
 // Reads of MFMA operands: k's 16 kk + 8 (lane / 32) + 0..7 of row 32 block + lane % 32.
-template <bool ROWK>
+template <bool ROWK, int KS>
 struct FragmentReader {
   int base;      // bytes
   __device__ __forceinline__ void init(int lane) {
-    if constexpr (ROWK) base = 2 * Tile<64>::off(lane & 31, 8 * (lane >> 5));
+    if constexpr (ROWK && KS == 32) base = (lane & 31) * 64 + ((lane >> 5) ^ ((lane >> 2) & 3)) * 16;
+    else if constexpr (ROWK) base = (lane & 31) * 128 + ((lane >> 5) ^ ((lane >> 1) & 7)) * 16;
     else {
       const int i = lane & 15;
       base = 2 * Tile<128>::off(8 * (lane >> 5) + (i >> 2), ((lane >> 4) & 1) * 16 + 4 * (i & 3));
@@ -67,24 +80,59 @@ struct FragmentReader {
   }
   __device__ __forceinline__ bf16x8 get(const __bf16* tile, int block, int kk) const {
     const char* p = reinterpret_cast<const char*>(tile);
-    if constexpr (ROWK) return *reinterpret_cast<const bf16x8*>(p + block * 4096 + (base ^ (32 * kk)));
+    if constexpr (ROWK) return *reinterpret_cast<const bf16x8*>(p + block * 64 * KS + (base ^ (32 * kk)));
     else {      // four rows further down the swizzle flips the unit's lowest bit
-      const char* q = p + (block >> 2) * 16384 + kk * 4096;
+      const char* q = p + (block >> 2) * 256 * KS + kk * 4096;
       return join(lds_read_tr(reinterpret_cast<const __bf16*>(q + (base ^ (64 * (block & 3))))),
                   lds_read_tr(reinterpret_cast<const __bf16*>(q + 1024 + (base ^ (64 * (block & 3) + 16)))));
     }
   }
 };
 
-// The accumulators of one tile (m0, n0), steps [s0, s1) of all segments.
-template <class C, bool A_ROWK, bool B_ROWK, bool PAIRED>
-__device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, int s0, int s1, __bf16* lds, f32x16 (&acc)[C::TM][C::TN]) {
-  using LA = OperandLoader<C::BM, A_ROWK, C::WAVES>;
-  using LB = OperandLoader<C::BN, B_ROWK, C::WAVES>;
+// What the copies of an operand take, stage after stage: the descriptor of this one's k's.
+template <bool ROWK, int KS>
+struct OperandStream {
+  uint64_t base, step;      // of the stage's first k; bytes to the next
+  uint32_t bytes;           // of the descriptor where all k's are there
+  uint32_t ld2;             // bytes of a row
+  // rows [first, first + tile) of `limit`, from k0 on
+  __device__ __forceinline__ void aim(const __bf16* p, int64_t ld, int first, int limit, int tile, int k0) {
+    ld2 = (uint32_t)ld * 2u;
+    if constexpr (ROWK) {
+      base = reinterpret_cast<uint64_t>(p + (int64_t)first * ld + k0);
+      step = 2 * KS;
+      bytes = (uint32_t)(min(tile, limit - first) - 1) * ld2;      // up to the last row; its k's are added below
+    } else {
+      base = reinterpret_cast<uint64_t>(p + (int64_t)k0 * ld + first);
+      step = (uint64_t)ld2 * KS;
+      bytes = (uint32_t)(limit - first) * 2u;                      // of the last row of the stage; the others are added below
+    }
+  }
+  // `left` k's from here on, none where that is 0 or less
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(int left) const {
+    const uint32_t n = (uint32_t)min(left, KS);
+    const uint32_t all = ROWK ? bytes + 2 * n : (n - 1) * ld2 + bytes;
+    return make_rsrc(reinterpret_cast<const void*>(base), left > 0 ? all : 0u);
+  }
+};
+
+// The accumulators of one tile (m0, n0), stages [s0, s1) of all segments.
+// PAIRED: b of even and of odd blocks of 32 columns are two matrices; TWO: there are two segments.
+template <class C, bool A_ROWK, bool B_ROWK, bool PAIRED, bool TWO>
+__device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, int s0, int s1, const GemmBuffers& lds, f32x16 (&acc)[C::TM][C::TN]) {
+  using LA = OperandLoader<C::BM, A_ROWK, C::WAVES, C::KS>;
+  using LB = OperandLoader<C::BN, B_ROWK, C::WAVES, C::KS>;
+  constexpr int L = LA::COUNT + LB::COUNT, SUB = C::KS / 16;      // copies of a stage, its steps of 16 k's
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
-  const int per = (p.K + kGemmK - 1) / kGemmK;      // steps of a segment
-  // byte offsets of this lane's 16 bytes from the step's base, and the k that they start at (ROWK)
+  const int per = (p.K + C::KS - 1) / C::KS;      // stages of a segment
+#pragma unroll
+  for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) acc[i][j] = zero16();
+  if (s0 >= s1) return;
+
+  // byte offsets of this lane's 16 bytes from the stage's base
   int off_a[LA::COUNT], off_b[LB::COUNT];
 #pragma unroll
   for (int i = 0; i < LA::COUNT; ++i)
@@ -95,81 +143,142 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
     if constexpr (PAIRED) r = (r >> 6) * 32 + (r & 31);      // which of the two matrices follows from the instruction
     off_b[i] = r * (int)p.ldb * 2 + LB::block(i, wave) * 256 + LB::unit(i, wave, lane) * 16;
   }
-  auto copy = [&](int s, int buffer) {
-    const int seg = s >= per ? 1 : 0, k0 = (s - seg * per) * kGemmK;
-    const bool tail = k0 + kGemmK > p.K;
-    __bf16* to_a = lds + buffer * C::STAGE;
-    __bf16* to_b = to_a + C::BM * kGemmK;
-    auto whole = [&](const __bf16* base, int64_t ld, bool rowk, int first, int limit, int tile) {
-      if (rowk) {
-        const int64_t rows = min(tile, limit - first);
-        return make_rsrc(base + (int64_t)first * ld + k0, rows > 0 ? (uint32_t)((rows * ld - k0) * 2) : 0u);
-      }
-      const int64_t rows = min(kGemmK, p.K - k0);
-      return make_rsrc(base + (int64_t)k0 * ld + first, (uint32_t)(((rows - 1) * ld + limit - first) * 2));
-    };
-    const __amdgpu_buffer_rsrc_t ra = whole(p.a[seg], p.lda, A_ROWK, m0, p.M, C::BM);
-#pragma unroll
-    for (int i = 0; i < LA::COUNT; ++i) {
-      int o = off_a[i];
-      if constexpr (A_ROWK) o = tail && k0 + 8 * LA::unit(i, wave, lane) >= p.K ? kGemmNowhere : o;
-      copy_1k(to_a + LA::place(i, wave), ra, o);
-    }
-    const __amdgpu_buffer_rsrc_t rb0 = whole(p.b[PAIRED ? 0 : seg], p.ldb, B_ROWK, n0, p.N, PAIRED ? C::BN / 2 : C::BN);
-    __amdgpu_buffer_rsrc_t rb1 = rb0;
-    if constexpr (PAIRED) rb1 = whole(p.b[1], p.ldb, B_ROWK, n0, p.N, C::BN / 2);
-#pragma unroll
-    for (int i = 0; i < LB::COUNT; ++i) {
-      int o = off_b[i];
-      if constexpr (B_ROWK) o = tail && k0 + 8 * LB::unit(i, wave, lane) >= p.K ? kGemmNowhere : o;
-      const bool odd = PAIRED && (LB::row(i, wave, 0) & 32);
-      copy_1k(to_b + LB::place(i, wave), odd ? rb1 : rb0, o);
+  // the stage that is copied next
+  OperandStream<A_ROWK, C::KS> sa;
+  OperandStream<B_ROWK, C::KS> sb, sb2;
+  int at = s0, left;
+  auto enter = [&](int seg, int k0) {
+    sa.aim(p.a[seg], p.lda, m0, p.M, C::BM, k0);
+    sb.aim(p.b[PAIRED ? 0 : seg], p.ldb, n0, p.N, PAIRED ? C::BN / 2 : C::BN, k0);
+    if constexpr (PAIRED) sb2.aim(p.b[1], p.ldb, n0, p.N, C::BN / 2, k0);
+    left = p.K - k0;
+  };
+  const int seg = TWO && s0 >= per ? 1 : 0;
+  enter(seg, (s0 - seg * per) * C::KS);
+  auto advance = [&]() {
+    ++at;
+    sa.base += sa.step;
+    sb.base += sb.step;
+    if constexpr (PAIRED) sb2.base += sb2.step;
+    left -= C::KS;
+    if constexpr (TWO) {
+      if (at == per) enter(1, 0);
     }
   };
-  FragmentReader<A_ROWK> ra;
-  FragmentReader<B_ROWK> rb;
+  // its descriptors; of a stage that there is not they are empty, and its buffer gets zeros, so that waits count alike
+  __amdgpu_buffer_rsrc_t da, db, db2;
+  int k;
+  auto prepare = [&]() {
+    k = at < s1 ? left : 0;
+    da = sa.descriptor(k);
+    db = sb.descriptor(k);
+    if constexpr (PAIRED) db2 = sb2.descriptor(k);
+  };
+  // copies [from, to) of the L
+  auto copy = [&](__bf16* buffer, int from, int to) {
+#pragma unroll
+    for (int q = 0; q < L; ++q) {
+      if (q < from || q >= to) continue;
+      if (q < LA::COUNT) {
+        int o = off_a[q];
+        if constexpr (A_ROWK) o = 8 * LA::unit(q, wave, lane) >= k ? kGemmNowhere : o;
+        copy_1k(buffer + LA::place(q, wave), da, o);
+      } else {
+        const int i = q - LA::COUNT;
+        int o = off_b[i];
+        if constexpr (B_ROWK) o = 8 * LB::unit(i, wave, lane) >= k ? kGemmNowhere : o;
+        const bool odd = PAIRED && (LB::row(i, wave, 0) & 32);
+        copy_1k(buffer + C::BM * C::KS + LB::place(i, wave), odd ? db2 : db, o);
+      }
+    }
+  };
+  FragmentReader<A_ROWK, C::KS> ra;
+  FragmentReader<B_ROWK, C::KS> rb;
   ra.init(lane);
   rb.init(lane);
   bf16x8 fa[2][C::TM], fb[2][C::TN];
-  auto read = [&](int buffer, int kk, int set) {
-    const __bf16* ta = lds + buffer * C::STAGE;
-    const __bf16* tb = ta + C::BM * kGemmK;
+  auto read = [&](const __bf16* buffer, int kk) {      // into the set of kk's parity
 #pragma unroll
-    for (int i = 0; i < C::TM; ++i) fa[set][i] = ra.get(ta, wm * C::TM + i, kk);
+    for (int j = 0; j < C::TN; ++j) fb[kk & 1][j] = rb.get(buffer + C::BM * C::KS, wn * C::TN + j, kk);
 #pragma unroll
-    for (int j = 0; j < C::TN; ++j) fb[set][j] = rb.get(tb, wn * C::TN + j, kk);
+    for (int i = 0; i < C::TM; ++i) fa[kk & 1][i] = ra.get(buffer, wm * C::TM + i, kk);
   };
+  // the first fragments of the next stage stay where they are read, although the loop may end before their use: the compiler would read them behind
+  // the branch, in front of the products that need them
+  auto hold = [&]() {
 #pragma unroll
-  for (int i = 0; i < C::TM; ++i)
+    for (int i = 0; i < C::TM; ++i) asm volatile("" : "+v"(fa[0][i]));
 #pragma unroll
-    for (int j = 0; j < C::TN; ++j) acc[i][j] = zero16();
-  if (s0 >= s1) return;
-  copy(s0, 0);
-  if (s0 + 1 < s1) {
-    copy(s0 + 1, 1);
-    wait_vm<LA::COUNT + LB::COUNT>();
-  } else {
-    wait_vm<0>();
-  }
-  lds_barrier();
-  read(0, 0, 0);
-  int buffer = 0;
-  for (int s = s0; s < s1; ++s, buffer ^= 1) {
+    for (int j = 0; j < C::TN; ++j) asm volatile("" : "+v"(fb[0][j]));
+  };
+  auto multiply = [&](int kk) {
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      if (kk < 3) read(buffer, kk + 1, (kk + 1) & 1);
-      else if (s + 1 < s1) {
-        wait_vm<0>();
-        lds_barrier();
-        if (s + 2 < s1) copy(s + 2, buffer);
-        read(buffer ^ 1, 0, 0);
-      }
+    for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-      for (int j = 0; j < C::TN; ++j)
+      for (int j = 0; j < C::TN; ++j) acc[i][j] = mfma32(fb[kk & 1][j], fa[kk & 1][i], acc[i][j]);
+  };
+  // the order of 16 k's: reads of the next fragments and copies spread over the products
+  auto order = [&](auto copies) {      // at most so many of those
+    constexpr int MF = C::TM * C::TN, READS = C::TM * (A_ROWK ? 1 : 2) + C::TN * (B_ROWK ? 1 : 2), EACH = (READS + MF - 1) / MF;
+    constexpr int N = decltype(copies)::value, EVERY = N ? MF / N : MF + 1;
 #pragma unroll
-        for (int i = 0; i < C::TM; ++i) acc[i][j] = mfma32(fb[kk & 1][j], fa[kk & 1][i], acc[i][j]);
+    for (int q = 0; q < MF; ++q) {
+      KNAP_SGB(KNAP_SG_MFMA, 1);
+      if (q * EACH < READS) KNAP_SGB(KNAP_SG_DS_READ, EACH);
+      if (N && q % EVERY == 0 && q / EVERY < N) KNAP_SGB(KNAP_SG_VMEM_READ, 1);
     }
+    KNAP_SCHED_FENCE();
+  };
+  // the copies of a stage go out in shares, the first once its buffer is free: behind the barrier in front of the last 16 k's of the stage that
+  // lies there; the others with the first 16 k's (of 64: and the second) of the next one
+  constexpr int SHARES = SUB == 2 ? 2 : 3;
+  auto share = [](int i) { return L * i / SHARES; };
+  prepare();
+  copy(buffer_of<0>(lds), 0, L);
+  advance();
+  prepare();
+  copy(buffer_of<1>(lds), 0, L);
+  advance();
+  prepare();
+  wait_vm<(C::BUFFERS - 1) * L>();
+  lds_barrier();
+  read(buffer_of<0>(lds), 0);
+  KNAP_SCHED_FENCE();
+  // `behind`: there is a stage in front of this one, whose buffer is being filled
+  auto stage = [&](auto which, auto behind) {
+    constexpr int B = decltype(which)::value, N = C::BUFFERS;
+    constexpr bool FILL = decltype(behind)::value;
+#pragma unroll
+    for (int kk = 0; kk < SUB; ++kk) {
+      if (kk < SUB - 1) {
+        if (FILL && kk + 1 < SHARES) copy(buffer_of<(B + N - 1) % N>(lds), share(kk + 1), share(kk + 2));
+        read(buffer_of<B>(lds), kk + 1);
+        multiply(kk);
+      } else {
+        wait_vm<(N - 2) * L>();
+        lds_barrier();
+        KNAP_SCHED_FENCE();
+        copy(buffer_of<B>(lds), 0, share(1));
+        read(buffer_of<(B + 1) % N>(lds), 0);
+        multiply(kk);
+      }
+      order(std::integral_constant<int, (L + SHARES - 1) / SHARES>{});
+      if (kk == SUB - 1) hold();
+      if (FILL && kk + 2 == SHARES) {      // behind the last share: the descriptors of the next stage, beside the products that copy nothing
+        advance();
+        prepare();
+      }
+    }
+  };
+  int s = s0;
+  stage(std::integral_constant<int, 0>{}, std::false_type{});
+  while (true) {
+    if (++s >= s1) break;
+    stage(std::integral_constant<int, 1>{}, std::true_type{});
+    if (++s >= s1) break;
+    stage(std::integral_constant<int, 0>{}, std::true_type{});
   }
+  wait_vm<0>();
   lds_barrier();      // the buffers are free
 }
 
