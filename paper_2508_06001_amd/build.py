@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(HERE, "libknapattn.so")
 
 HIP_SOURCES = ["knap_attn_fwd.hip", "knap_attn_fwd_full.hip", "knap_attn_bwd.hip", "knap_attn_bwd_causal.hip",
                "knap_attn_bwd_small.hip", "knap_diff_fwd.hip", "knap_diff_bwd.hip", "knap_ulysses.hip", "knap_rope.hip", "knap_layer_norm_fwd.hip",
-               "knap_layer_norm_bwd.hip", "knap_residual_norm_fwd.hip", "knap_residual_norm_bwd.hip", "knap_grad_clip.hip", "knap_ffn.hip", "knap_api.hip",
+               "knap_layer_norm_bwd.hip", "knap_residual_norm_fwd.hip", "knap_residual_norm_bwd.hip", "knap_grad_clip.hip", "knap_ffn.hip", "knap_ffn_few.hip", "knap_api.hip",
                "knap_block_api.hip"]
 C_SOURCES = ["knap_host.c"]
 

@@ -391,6 +391,7 @@ static GemmLaunch weight_gradients(const FfnArgs& a) {
 size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward) {
   FfnArgs a{};
   a.tokens = (int)tokens; a.width = width; a.hidden = hidden;
+  if (!backward && tokens <= kFfnFew) return 0;
   if (!backward) return std::max(bytes_of<true, true, kActForward>(up_products(a)), bytes_of<true, true, kStore>(down_product(a)));
   size_t most = std::max(bytes_of<true, false, kActBackward>(hidden_gradients(a)), bytes_of<true, false, kStore>(input_gradient(a)));
   for (int wanted = 1; wanted < 8; ++wanted) {      // whichever gradients of weights a call asks for
@@ -404,6 +405,7 @@ size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward) {
 }
 
 hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t stream) {
+  if (a.tokens <= kFfnFew) return launch_ffn_few(a, stream);
   const hipError_t e = run<true, true, kActForward>(up_products(a), stream);
   return e != hipSuccess ? e : run<true, true, kStore>(down_product(a), stream);
 }

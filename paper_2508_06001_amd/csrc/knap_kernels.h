@@ -174,6 +174,8 @@ struct FfnArgs {
   float* partial;
 };
 size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward);
+constexpr int kFfnFew = 64;      // tokens up to which the forward takes the form of knap_ffn_few.hip
+hipError_t launch_ffn_few(const FfnArgs& a, hipStream_t stream);
 hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t stream);
 hipError_t launch_ffn_bwd(const FfnArgs& a, hipStream_t stream);
 
