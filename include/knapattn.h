@@ -503,27 +503,38 @@ size_t knap_gated_ffn_bwd_workspace_bytes(int64_t tokens, int width, int hidden)
  * Two calls, so that ranks that hold parts of the gradients can add up their sum_sq (an
  * all-reduce of one double) between them.
  *
- * grads, out: HOST arrays of n device pointers, numel and types HOST arrays of n (KNAP_BF16 or KNAP_F32); all are read
- * before the call returns.  A tensor is numel contiguous values, aligned to its type; 16 bytes give the fast form.  numel
- * may be 0 (the pointer is not looked at then).  out[i] has the type of grads[i] and may be grads[i] itself (in place, which
- * writes nothing where c is 1); otherwise a part of out that overlaps another one or a gradient is refused, and with it a
- * list that has a tensor twice, which would be scaled twice.
+ * Plan.  Which tensors, and where each goes, is laid down once: knap_grad_plan fills a HOST array of
+ * knap_grad_plan_bytes(numel, n) bytes, 8-byte aligned, which the caller copies to the device and keeps as long as the tensors
+ * stay where they are; the two calls take the device copy, `plan` (8-byte aligned), and its size.  It holds a record for every
+ * KNAP_GRAD_CHUNK elements of a tensor, so that a launch covers any number of tensors, and no call looks a list through.
+ *   grads, out: HOST arrays of n device pointers, numel and types HOST arrays of n (KNAP_BF16 or KNAP_F32).  A tensor is numel
+ *   contiguous values, aligned to its type; 16 bytes give the fast form.  numel may be 0 (the pointers are not looked at
+ *   then).  out[i] has the type of grads[i] and may be grads[i] itself (in place, which writes nothing where c is 1);
+ *   otherwise a part of out that overlaps another one or a gradient is refused, and with it a list that has a tensor twice,
+ *   which would be scaled twice.
+ * The device copy is not validated: another one than knap_grad_plan made is a caller error with undefined results.
+ *
  * sum_sq: device double, the sum in 64 bits in a fixed order, so that the same call gives the same bits; it does not
- * overflow for any finite gradients.  workspace: knap_grad_sum_squares_workspace_bytes(n) bytes, 256-byte aligned, one for each
+ * overflow for any finite gradients.  workspace: KNAP_GRAD_WORKSPACE_BYTES bytes, 256-byte aligned, one for each
  * call that may run at the same time.
- * norm (device fp32, or NULL) is written by knap_grad_clip (infinity where 32 bits do not hold it; c is right there too).  A sum_sq that is not finite gives what the formula says:
- * infinity c = 0, NaN NaN everywhere; a caller that wants to skip such a step looks at norm.
+ * norm (device fp32, or NULL) is written by knap_grad_clip (infinity where 32 bits do not hold it; c is right there too).  A sum_sq
+ * that is not finite gives what the formula says: infinity c = 0, NaN NaN everywhere; a caller that wants to skip such a step looks at norm.
  * c is formed in 64 bits and rounded to 32, products in 32, rounded once to their type.
  *
- * Supported: 0 <= n, 0 <= numel, numel of a tensor < 2^40, max_norm > 0 (infinity: never clips) and eps >= 0, finite.  n = 0: sum_sq = 0.
- * Captured calls keep the pointers of the lists.  As for the forward of attention, the first call of the library on a
- * device must not be captured.
+ * Supported: 0 <= n, 0 <= numel, numel of a tensor < 2^40, max_norm > 0 (infinity: never clips) and eps >= 0, finite.  An empty
+ * plan (plan_bytes = 0, plan NULL): sum_sq = 0.  Captured calls keep the pointer of the plan and read it at every replay.  As for the
+ * forward of attention, the first call of the library on a device must not be captured (knap_grad_plan uses no device).
  * ------------------------------------------------------------------------ */
-int knap_grad_sum_squares(const void* const* grads, const int64_t* numel, const int* types, int n,
-                          double* sum_sq, void* workspace, size_t workspace_bytes, void* stream);
-size_t knap_grad_sum_squares_workspace_bytes(int n);
-int knap_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n,
-                   const double* sum_sq, float max_norm, float eps, float* norm, void* stream);
+#define KNAP_GRAD_CHUNK           8192
+#define KNAP_GRAD_WORKSPACE_BYTES 8192
+
+size_t knap_grad_plan_bytes(const int64_t* numel, int n);
+int knap_grad_plan(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n,
+                   void* plan, size_t plan_bytes);
+int knap_grad_sum_squares(const void* plan, size_t plan_bytes, double* sum_sq,
+                          void* workspace, size_t workspace_bytes, void* stream);
+int knap_grad_clip(const void* plan, size_t plan_bytes, const double* sum_sq, float max_norm, float eps,
+                   float* norm, void* stream);
 
 /* Message for a KNAP_ERR_* code (static string, never NULL). */
 const char* knap_strerror(int code);

@@ -39,6 +39,8 @@ KNAP_LAYER_NORM_MAX_WIDTH = 16384
 KNAP_SILU = 0
 KNAP_GELU_TANH = 1
 KNAP_FFN_MAX_WIDTH = 65536
+KNAP_GRAD_CHUNK = 8192
+KNAP_GRAD_WORKSPACE_BYTES = 8192
 KNAP_NORM_NONE = 0
 KNAP_NORM_RMS = 1
 KNAP_NORM_LAYER = 2
@@ -93,9 +95,10 @@ _SIGNATURES = {
     "knap_gated_ffn_fwd_workspace_bytes": (_sz, [_i64, _i, _i]),
     "knap_gated_ffn_bwd": (_i, [_vp, _i64, _i64, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _sz, _vp]),
     "knap_gated_ffn_bwd_workspace_bytes": (_sz, [_i64, _i, _i]),
-    "knap_grad_sum_squares": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _sz, _vp]),
-    "knap_grad_sum_squares_workspace_bytes": (_sz, [_i]),
-    "knap_grad_clip": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _f, _f, _vp, _vp]),
+    "knap_grad_plan_bytes": (_sz, [_vp, _i]),
+    "knap_grad_plan": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _sz]),
+    "knap_grad_sum_squares": (_i, [_vp, _sz, _vp, _vp, _sz, _vp]),
+    "knap_grad_clip": (_i, [_vp, _sz, _vp, _f, _f, _vp, _vp]),
     "knap_strerror": (C.c_char_p, [_i]),
     "knap_last_hip_error": (_i, []),
     "knap_launch_workgroups": (_i, [_i]),
@@ -545,51 +548,56 @@ def knap_layer_norm_bwd(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace
 
 def _modulation(where: str, name: str, t, n_seq: int, width: int, dtype) -> int:
     """The row stride of an (n_seq, width) tensor of `dtype` with contiguous rows, checked."""
-    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != n_seq or t.shape[1] != width:
+    if t.dtype is not dtype or t.shape != (n_seq, width):
         _refuse(where, f"{name} is an (n_seq, width) tensor of its type")
-    if width > 1 and t.stride(1) != 1:
+    stride = t.stride()
+    if width > 1 and stride[1] != 1:
         _refuse(where, f"the rows of {name} are contiguous")
-    return t.stride(0)
+    return stride[0]
 
 
-class _Residual:
-    """What both directions hand over of x, f, the vectors and the weights, checked."""
-
-    def __init__(self, where: str, x, f, branch_type, cu_seqlens, gate, scale, shift, weight, post_weight):
-        types, f32 = _KNAP_TYPES, torch.float32
-        shape = x.shape
-        self.xs = _rows(where, "x", x, shape)
-        self.rows, self.width = rows, width = shape
-        self.shape = shape
-        if branch_type not in types:
-            _refuse(where, "the type of the branch")
-        self.fs = 0 if f is None else _rows(where, "f", f, shape, branch_type)
-        self.f_at = 0 if f is None else f.data_ptr()
-        self.n_seq, self.cu_at = 1, 0
-        if cu_seqlens is not None:
-            if cu_seqlens.dtype is not torch.int32 or not cu_seqlens.is_contiguous() or cu_seqlens.numel() < 1:
-                _refuse(where, "cu_seqlens is a contiguous int32 tensor of n_seq + 1 entries")
-            self.n_seq, self.cu_at = cu_seqlens.numel() - 1, cu_seqlens.data_ptr()
-        n = self.n_seq
-        given = gate if gate is not None else scale if scale is not None else shift
-        mod = f32 if given is None else given.dtype
-        if mod not in types:
-            _refuse(where, "the type of gate, scale and shift")
-        self.gs = 0 if gate is None else _modulation(where, "gate", gate, n, width, mod)
-        self.ms = 0
-        for name, t in (("scale", scale), ("shift", shift)):
-            if t is not None:
-                ms = _modulation(where, name, t, n, width, mod)
-                if n > 1 and scale is not None and t is shift and ms != self.ms:
-                    _refuse(where, "scale and shift have one stride")
-                self.ms = ms
-        self.gate_at, self.scale_at, self.shift_at = _ptr(gate), _ptr(scale), _ptr(shift)
-        wt = f32 if weight is None and post_weight is None else (post_weight if weight is None else weight).dtype
-        if wt not in types:
-            _refuse(where, "the type of weight and post_weight")
-        self.w_at = 0 if weight is None else _vector(where, "weight", weight, width, wt)
-        self.wp_at = 0 if post_weight is None else _vector(where, "post_weight", post_weight, width, wt)
-        self.xt, self.bt, self.mt, self.wt = types[x.dtype], types[branch_type], types[mod], types[wt]
+def _residual(where: str, x, f, branch_type, cu_seqlens, gate, scale, shift, weight, post_weight) -> tuple:
+    """What both directions hand over of x, f, the vectors and the weights, checked: the arguments up to gate_stride, then the rest of them."""
+    # the host's time bounds the smallest calls: each property is asked for once
+    types, f32 = _KNAP_TYPES, torch.float32
+    shape = x.shape
+    xs = _rows(where, "x", x, shape)
+    rows, width = shape
+    if branch_type not in types:
+        _refuse(where, "the type of the branch")
+    fs = f_at = cu_at = gs = ms = gate_at = scale_at = shift_at = w_at = wp_at = 0
+    if f is not None:
+        fs, f_at = _rows(where, "f", f, shape, branch_type), f.data_ptr()
+    n = 1
+    if cu_seqlens is not None:
+        n, cu_at = cu_seqlens.numel() - 1, cu_seqlens.data_ptr()
+        if n < 0 or cu_seqlens.dtype is not torch.int32 or not cu_seqlens.is_contiguous():
+            _refuse(where, "cu_seqlens is a contiguous int32 tensor of n_seq + 1 entries")
+    mod = f32
+    if gate is not None:
+        mod = gate.dtype
+        gs, gate_at = _modulation(where, "gate", gate, n, width, mod), gate.data_ptr()
+    elif scale is not None or shift is not None:
+        mod = (shift if scale is None else scale).dtype
+    if scale is not None:
+        ms, scale_at = _modulation(where, "scale", scale, n, width, mod), scale.data_ptr()
+    if shift is not None:
+        stride, shift_at = _modulation(where, "shift", shift, n, width, mod), shift.data_ptr()
+        if scale is not None and n > 1 and stride != ms:
+            _refuse(where, "scale and shift have one stride")
+        ms = stride
+    wt = f32
+    if weight is not None:
+        wt = weight.dtype
+        w_at = _vector(where, "weight", weight, width, wt)
+    elif post_weight is not None:
+        wt = post_weight.dtype
+    if post_weight is not None:
+        wp_at = _vector(where, "post_weight", post_weight, width, wt)
+    if mod not in types or wt not in types:
+        _refuse(where, "the type of gate, scale and shift, or of the weights")
+    return (x.data_ptr(), types[x.dtype], xs, rows, width, f_at, types[branch_type], fs, cu_at, n, gate_at, gs), scale_at, shift_at, ms, types[mod], (
+        wp_at, w_at, types[wt])
 
 
 def knap_residual_norm_fwd(x, f, x_out, y, norm: int = KNAP_NORM_LAYER, post_norm: int = KNAP_NORM_NONE, weight=None, post_weight=None, gate=None,
@@ -600,15 +608,18 @@ def knap_residual_norm_fwd(x, f, x_out, y, norm: int = KNAP_NORM_LAYER, post_nor
     (n_seq, width) or None; weights: (width,) or None; stats: fp32 (4, rows) for a backward."""
     where = "knap_residual_norm_fwd"
     _here(where, x, f, x_out, y, weight, post_weight, gate, scale, shift, cu_seqlens, stats)
-    r = _Residual(where, x, f, (y if f is None else f).dtype if f is not None or y is not None else x.dtype, cu_seqlens, gate, scale, shift, weight,
-                  post_weight)
-    xos = 0 if x_out is None else _rows(where, "x_out", x_out, r.shape, x.dtype)
-    ys = 0 if y is None else _rows(where, "y", y, r.shape, y.dtype if f is None else f.dtype)
+    bt = f.dtype if f is not None else x.dtype if y is None else y.dtype
+    first, scale_at, shift_at, ms, mt, weights = _residual(where, x, f, bt, cu_seqlens, gate, scale, shift, weight, post_weight)
+    shape = x.shape
+    xos = xo_at = ys = y_at = stats_at = 0
+    if x_out is not None:
+        xos, xo_at = _rows(where, "x_out", x_out, shape, x.dtype), x_out.data_ptr()
+    if y is not None:
+        ys, y_at = _rows(where, "y", y, shape, bt), y.data_ptr()
     if stats is not None:
-        _vector(where, "stats", stats, 4 * r.rows, torch.float32)
-    rc = lib.knap_residual_norm_fwd(x.data_ptr(), r.xt, r.xs, r.rows, r.width, r.f_at, r.bt, r.fs, r.cu_at, r.n_seq, r.gate_at, r.gs, r.scale_at,
-                                    r.shift_at, r.ms, r.mt, r.wp_at, r.w_at, r.wt, post_norm, norm, alpha, eps, _ptr(x_out), xos, _ptr(y), ys,
-                                    _ptr(stats), _stream_handle(stream))
+        stats_at = _vector(where, "stats", stats, 4 * shape[0], torch.float32)
+    rc = lib.knap_residual_norm_fwd(*first, scale_at, shift_at, ms, mt, *weights, post_norm, norm, alpha, eps, xo_at, xos, y_at, ys, stats_at,
+                                    _stream_handle(stream))
     if check:
         _check(rc, where)
     return rc
@@ -626,29 +637,28 @@ def knap_residual_norm_bwd(x, f, stats, dx_out, dy, dx, df, norm: int = KNAP_NOR
     dweight and dpost_weight fp32 (width,); each of them, and dx_out, may be None."""
     where = "knap_residual_norm_bwd"
     _here(where, x, f, stats, dx_out, dy, dx, df, weight, post_weight, gate, scale, cu_seqlens, dgate, dscale, dshift, dweight, dpost_weight, workspace)
-    f32 = torch.float32
-    r = _Residual(where, x, f, (dy if f is None else f).dtype if f is not None or dy is not None else x.dtype, cu_seqlens, gate, scale, None, weight,
-                  post_weight)
-    if stats is not None:
-        _vector(where, "stats", stats, 4 * r.rows, f32)
-    xt, bt = x.dtype, f.dtype if f is not None else None if dy is None else dy.dtype
-    dxos = 0 if dx_out is None else _rows(where, "dx_out", dx_out, r.shape, xt)
-    dys = 0 if dy is None else _rows(where, "dy", dy, r.shape, bt)
-    dxs = 0 if dx is None else _rows(where, "dx", dx, r.shape, xt)
-    dfs = 0 if df is None else _rows(where, "df", df, r.shape, bt)
-    dgs = 0 if dgate is None else _modulation(where, "dgate", dgate, r.n_seq, r.width, f32)
-    dms = 0 if dscale is None else _modulation(where, "dscale", dscale, r.n_seq, r.width, f32)
+    f32, xt = torch.float32, x.dtype
+    bt = f.dtype if f is not None else xt if dy is None else dy.dtype
+    first, scale_at, _, ms, mt, weights = _residual(where, x, f, bt, cu_seqlens, gate, scale, None, weight, post_weight)
+    shape, n = x.shape, first[9]
+    width = shape[1]
+    stats_at = 0 if stats is None else _vector(where, "stats", stats, 4 * shape[0], f32)
+    dxos = 0 if dx_out is None else _rows(where, "dx_out", dx_out, shape, xt)
+    dys = 0 if dy is None else _rows(where, "dy", dy, shape, bt)
+    dxs = 0 if dx is None else _rows(where, "dx", dx, shape, xt)
+    dfs = 0 if df is None else _rows(where, "df", df, shape, bt)
+    dgs = 0 if dgate is None else _modulation(where, "dgate", dgate, n, width, f32)
+    dms = 0 if dscale is None else _modulation(where, "dscale", dscale, n, width, f32)
     if dshift is not None:
-        ms = _modulation(where, "dshift", dshift, r.n_seq, r.width, f32)
-        if dscale is not None and r.n_seq > 1 and ms != dms:
+        stride = _modulation(where, "dshift", dshift, n, width, f32)
+        if dscale is not None and n > 1 and stride != dms:
             _refuse(where, "dscale and dshift have one stride")
-        dms = ms
-    dw_at = 0 if dweight is None else _vector(where, "dweight", dweight, r.width, f32)
-    dwp_at = 0 if dpost_weight is None else _vector(where, "dpost_weight", dpost_weight, r.width, f32)
+        dms = stride
+    dw_at = 0 if dweight is None else _vector(where, "dweight", dweight, width, f32)
+    dwp_at = 0 if dpost_weight is None else _vector(where, "dpost_weight", dpost_weight, width, f32)
     if workspace_bytes is None:
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib.knap_residual_norm_bwd(x.data_ptr(), r.xt, r.xs, r.rows, r.width, r.f_at, r.bt, r.fs, r.cu_at, r.n_seq, r.gate_at, r.gs, r.scale_at, r.ms,
-                                    r.mt, r.wp_at, r.w_at, r.wt, post_norm, norm, alpha, _ptr(stats), _ptr(dx_out), dxos, _ptr(dy), dys, _ptr(dx),
+    rc = lib.knap_residual_norm_bwd(*first, scale_at, ms, mt, *weights, post_norm, norm, alpha, stats_at, _ptr(dx_out), dxos, _ptr(dy), dys, _ptr(dx),
                                     dxs, _ptr(df), dfs, _ptr(dgate), dgs, _ptr(dscale), _ptr(dshift), dms, dw_at, dwp_at, _ptr(workspace),
                                     workspace_bytes, _stream_handle(stream))
     if check:
@@ -728,75 +738,65 @@ def knap_gated_ffn_bwd(x, w_gate, w_up, w_down, act: int, gate, up, h, dy, dx, d
 
 # --------------------------------------------------------------------------- gradient norm and clipping
 
-class GradList:
-    """The HOST arrays that knap_grad_sum_squares and knap_grad_clip take of a list of gradients (contiguous bf16 or fp32 tensors, all on one
-    device) and, for clipping, of where each goes (None: in place).  Keeps the tensors."""
+def knap_grad_plan(grads, out=None):
+    """The plan of a list of gradients (contiguous bf16 or fp32 CUDA tensors, all on one device) and of where each goes when it is clipped (None:
+    in place): a uint8 tensor on their device, for knap_grad_sum_squares and knap_grad_clip.  It stands for the tensors as long as they stay
+    where they are; the caller keeps them."""
+    where = "knap_grad_plan"
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    n = len(grads)
+    if len(out) != n:
+        _refuse(where, "as many outputs as gradients")
+    device = grads[0].device if n else None
+    for g, o in zip(grads, out):
+        if g.dtype not in _KNAP_TYPES or o.dtype is not g.dtype or o.numel() != g.numel():
+            _refuse(where, "gradients are bf16 or fp32 tensors, an output is of its gradient's type and size")
+        if not g.is_contiguous() or not o.is_contiguous():
+            _refuse(where, "gradients and outputs are contiguous")
+        if g.device != device or o.device != device:
+            _refuse(where, "tensors on several devices")
+    grads_at, out_at = ((C.c_void_p * max(1, n))(*[t.data_ptr() for t in ts]) for ts in (grads, out))
+    numel = (C.c_int64 * max(1, n))(*[g.numel() for g in grads])
+    types = (C.c_int * max(1, n))(*[_KNAP_TYPES[g.dtype] for g in grads])
+    nbytes = int(lib.knap_grad_plan_bytes(numel, n))
+    host = torch.empty((nbytes,), dtype=torch.uint8)
+    _check(lib.knap_grad_plan(grads_at, out_at, numel, types, n, host.data_ptr(), nbytes), where)
+    return host.to(device if n else "cuda")
 
-    def __init__(self, grads, out=None):
-        where = "GradList"
-        self.grads = list(grads)
-        self.out = self.grads if out is None else list(out)
-        n = self.n = len(self.grads)
-        if len(self.out) != n:
-            _refuse(where, "as many outputs as gradients")
-        self.device = self.grads[0].get_device() if n else None
-        for g, o in zip(self.grads, self.out):
-            if g.dtype not in _KNAP_TYPES or o.dtype is not g.dtype or o.numel() != g.numel():
-                _refuse(where, "gradients are bf16 or fp32 tensors, an output is of its gradient's type and size")
-            if not g.is_contiguous() or not o.is_contiguous():
-                _refuse(where, "gradients and outputs are contiguous")
-            if g.get_device() != self.device or o.get_device() != self.device:
-                _refuse(where, "tensors on several devices")
-        self.grads_at = (C.c_void_p * max(1, n))(*[g.data_ptr() for g in self.grads])
-        self.out_at = (C.c_void_p * max(1, n))(*[o.data_ptr() for o in self.out])
-        self.numel = (C.c_int64 * max(1, n))(*[g.numel() for g in self.grads])
-        self.types = (C.c_int * max(1, n))(*[_KNAP_TYPES[g.dtype] for g in self.grads])
 
-    def on(self, where: str) -> None:
-        dev = _current_device() if _current_device is not None else torch.cuda.current_device()
-        if self.device is not None and self.device != dev:
-            _refuse(where, f"gradients on device {self.device} while device {dev} is current")
+def _plan(where: str, plan) -> int:
+    if plan.dtype is not torch.uint8 or not plan.is_contiguous():
+        _refuse(where, "plan is the tensor that knap_grad_plan made")
+    return plan.numel()
 
 
 def _one(where: str, name: str, t, dtype) -> int:
-    if t.dtype is not dtype or t.numel() < 1:
-        _refuse(where, f"the type of {name}")
+    if t.dtype is not dtype or t.numel() != 1:
+        _refuse(where, f"{name} is a tensor of one value of its type")
     return t.data_ptr()
 
 
-def knap_grad_sum_squares_workspace_bytes(n: int) -> int:
-    return int(lib.knap_grad_sum_squares_workspace_bytes(n))
-
-
-def knap_grad_sum_squares(grads, sum_sq, workspace, workspace_bytes: Optional[int] = None, stream=None, check: bool = True) -> int:
-    """sum_sq (a float64 CUDA tensor of one value) = sum of g^2 over all gradients: a GradList, or tensors."""
+def knap_grad_sum_squares(plan, sum_sq, workspace, workspace_bytes: Optional[int] = None, stream=None, check: bool = True) -> int:
+    """sum_sq (a float64 CUDA tensor of one value) = sum of g^2 over all gradients of the plan."""
     where = "knap_grad_sum_squares"
-    if not isinstance(grads, GradList):
-        grads = GradList(grads)
-    grads.on(where)
-    _here(where, sum_sq, workspace)
-    at = _one(where, "sum_sq", sum_sq, torch.float64)
+    _here(where, plan, sum_sq, workspace)
     if workspace_bytes is None:
         workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib.knap_grad_sum_squares(grads.grads_at, grads.numel, grads.types, grads.n, at, _ptr(workspace), workspace_bytes, _stream_handle(stream))
+    rc = lib.knap_grad_sum_squares(plan.data_ptr(), _plan(where, plan), _one(where, "sum_sq", sum_sq, torch.float64), _ptr(workspace), workspace_bytes,
+                                   _stream_handle(stream))
     if check:
         _check(rc, where)
     return rc
 
 
-def knap_grad_clip(grads, sum_sq, max_norm: float, eps: float = 1e-6, norm=None, out=None, stream=None, check: bool = True) -> int:
-    """out = min(1, max_norm / (sqrt(sum_sq) + eps)) grads, in place where `out` is None; grads: a GradList (which has its outputs), or tensors.
-    norm: an fp32 CUDA tensor of one value, or None."""
+def knap_grad_clip(plan, sum_sq, max_norm: float, eps: float = 1e-6, norm=None, stream=None, check: bool = True) -> int:
+    """Every gradient of the plan times min(1, max_norm / (sqrt(sum_sq) + eps)), to where the plan says.  norm: an fp32 CUDA tensor of one value,
+    or None."""
     where = "knap_grad_clip"
-    if not isinstance(grads, GradList):
-        grads = GradList(grads, out)
-    elif out is not None:
-        _refuse(where, "a GradList has its outputs")
-    grads.on(where)
-    _here(where, sum_sq, norm)
-    at = _one(where, "sum_sq", sum_sq, torch.float64)
-    norm_at = 0 if norm is None else _one(where, "norm", norm, torch.float32)
-    rc = lib.knap_grad_clip(grads.grads_at, grads.out_at, grads.numel, grads.types, grads.n, at, max_norm, eps, norm_at, _stream_handle(stream))
+    _here(where, plan, sum_sq, norm)
+    rc = lib.knap_grad_clip(plan.data_ptr(), _plan(where, plan), _one(where, "sum_sq", sum_sq, torch.float64), max_norm, eps,
+                            0 if norm is None else _one(where, "norm", norm, torch.float32), _stream_handle(stream))
     if check:
         _check(rc, where)
     return rc

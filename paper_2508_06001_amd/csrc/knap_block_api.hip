@@ -272,15 +272,6 @@ namespace {
 
 constexpr int64_t kGradMost = (int64_t)1 << 40;      // elements of a tensor
 
-int check_grads(const void* const* grads, const int64_t* numel, const int* types, int n) {
-  if (n < 0 || (n > 0 && (!grads || !numel || !types))) return KNAP_ERR_INVALID_ARG;
-  for (int i = 0; i < n; ++i) {
-    if (!type_ok(types[i]) || numel[i] < 0 || numel[i] >= kGradMost) return KNAP_ERR_INVALID_ARG;
-    if (numel[i] > 0 && (!grads[i] || !aligned(grads[i], size_of(types[i])))) return KNAP_ERR_INVALID_ARG;
-  }
-  return KNAP_OK;
-}
-
 // Whether every part of `out` is apart from the others and from all gradients but its own.  In ascending order, as tensors of one
 // allocation mostly are, one walk does; else an array of their order is sorted.
 int grads_apart(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n) {
@@ -316,95 +307,60 @@ int grads_apart(const void* const* grads, void* const* out, const int64_t* numel
   return ok ? KNAP_OK : KNAP_ERR_INVALID_ARG;
 }
 
-// Fills tables with the tensors that hold anything, as many as a launch takes, and hands each to f; stops at a status that is not hipSuccess.
-template <class F>
-hipError_t for_tables(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n, F f) {
-  knap::GradTable t;
-  t.n = 0;
-  uint32_t chunks = 0;
-  auto hand = [&]() {
-    t.first[t.n] = chunks;
-    const hipError_t e = t.n ? f(t, chunks) : hipSuccess;
-    t.n = 0;
-    chunks = 0;
-    return e;
-  };
-  for (int i = 0; i < n; ++i) {
-    if (numel[i] == 0) continue;
-    const uint32_t mine = (uint32_t)((numel[i] + knap::kGradChunk - 1) / knap::kGradChunk);      // below 2^27
-    if (t.n == knap::kGradTensors || chunks > (1u << 30)) {
-      const hipError_t e = hand();
-      if (e != hipSuccess) return e;
-    }
-    t.from[t.n] = grads[i];
-    t.to[t.n] = out ? out[i] : nullptr;
-    t.numel[t.n] = numel[i];
-    t.bf16[t.n] = types[i] == KNAP_BF16;
-    t.first[t.n] = chunks;
-    ++t.n;
-    chunks += mine;
-  }
-  return hand();
-}
-
 }  // namespace
 
 extern "C" {
 
-size_t knap_grad_sum_squares_workspace_bytes(int n) {
-  if (n <= 0) return 0;
-  const size_t launches = ((size_t)n + knap::kGradTensors - 1) / knap::kGradTensors + 1;
-  return round_up(launches * knap::kGradGroups * sizeof(double), 256);
+size_t knap_grad_plan_bytes(const int64_t* numel, int n) {
+  size_t chunks = 0;
+  for (int i = 0; numel && i < n; ++i)
+    if (numel[i] > 0 && numel[i] < kGradMost) chunks += (size_t)((numel[i] + KNAP_GRAD_CHUNK - 1) / KNAP_GRAD_CHUNK);
+  return chunks * sizeof(knap::GradChunk);
 }
 
-int knap_grad_sum_squares(const void* const* grads, const int64_t* numel, const int* types, int n, double* sum_sq, void* workspace,
-                          size_t workspace_bytes, void* stream) {
-  const int rc = check_grads(grads, numel, types, n);
-  if (rc != KNAP_OK) return rc;
-  if (!sum_sq || !aligned(sum_sq, 8)) return KNAP_ERR_INVALID_ARG;
-  if (n > 0 && (!workspace || !aligned(workspace, 256))) return KNAP_ERR_INVALID_ARG;
-  if (workspace_bytes < knap_grad_sum_squares_workspace_bytes(n)) return KNAP_ERR_WORKSPACE_TOO_SMALL;
-  const int cus = knap::device_cus();
-  if (!cus) return KNAP_ERR_LAUNCH_FAILED;
-  double* partial = static_cast<double*>(workspace);
-  int filled = 0;
-  const size_t room = workspace_bytes / sizeof(double);
-  hipError_t e = for_tables(grads, nullptr, numel, types, n, [&](const knap::GradTable& t, uint32_t chunks) {
-    const int groups = (int)std::min<uint32_t>(chunks, std::min(4 * cus, knap::kGradGroups));
-    if ((size_t)filled + groups > room) return hipErrorInvalidValue;
-    const hipError_t err = knap::launch_grad_squares(t, partial + filled, groups, static_cast<hipStream_t>(stream));
-    filled += groups;
-    return err;
-  });
-  if (e == hipSuccess) e = knap::launch_grad_join(partial, filled, sum_sq, static_cast<hipStream_t>(stream));
-  return knap::launch_status(e);
-}
-
-int knap_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n, const double* sum_sq, float max_norm,
-                   float eps, float* norm, void* stream) {
-  const int rc = check_grads(grads, numel, types, n);
-  if (rc != KNAP_OK) return rc;
-  if (!sum_sq || !aligned(sum_sq, 8) || !aligned(norm, 4) || !(max_norm > 0.f) || !(eps >= 0.f) || !finite_f(eps) || (n > 0 && !out)) return KNAP_ERR_INVALID_ARG;
-  for (int i = 0; i < n; ++i)
-    if (numel[i] > 0 && (!out[i] || !aligned(out[i], size_of(types[i])))) return KNAP_ERR_INVALID_ARG;
+int knap_grad_plan(const void* const* grads, void* const* out, const int64_t* numel, const int* types, int n, void* plan, size_t plan_bytes) {
+  if (n < 0 || (n > 0 && (!grads || !out || !numel || !types))) return KNAP_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i) {
+    if (!type_ok(types[i]) || numel[i] < 0 || numel[i] >= kGradMost) return KNAP_ERR_INVALID_ARG;
+    if (numel[i] > 0 && (!grads[i] || !out[i] || !aligned(grads[i], size_of(types[i])) || !aligned(out[i], size_of(types[i])))) return KNAP_ERR_INVALID_ARG;
+  }
   const int apart = grads_apart(grads, out, numel, types, n);
   if (apart != KNAP_OK) return apart;
+  const size_t need = knap_grad_plan_bytes(numel, n);
+  if (need == 0) return KNAP_OK;
+  if (!plan || !aligned(plan, 8)) return KNAP_ERR_INVALID_ARG;
+  if (plan_bytes < need) return KNAP_ERR_CAPACITY;
+  knap::GradChunk* to = static_cast<knap::GradChunk*>(plan);
+  for (int i = 0; i < n; ++i)
+    for (int64_t at = 0; at < numel[i]; at += KNAP_GRAD_CHUNK) {
+      const size_t bytes = (size_t)at * size_of(types[i]);
+      *to++ = knap::GradChunk{static_cast<const char*>(grads[i]) + bytes, static_cast<char*>(out[i]) + bytes,
+                              (int32_t)std::min<int64_t>(KNAP_GRAD_CHUNK, numel[i] - at), types[i] == KNAP_BF16};
+    }
+  return KNAP_OK;
+}
+
+static bool plan_ok(const void* plan, size_t plan_bytes) {
+  return plan_bytes % sizeof(knap::GradChunk) == 0 && (plan_bytes == 0 || (plan && aligned(plan, 8)));
+}
+
+int knap_grad_sum_squares(const void* plan, size_t plan_bytes, double* sum_sq, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!plan_ok(plan, plan_bytes) || !sum_sq || !aligned(sum_sq, 8) || !workspace || !aligned(workspace, 256)) return KNAP_ERR_INVALID_ARG;
+  if (workspace_bytes < KNAP_GRAD_WORKSPACE_BYTES) return KNAP_ERR_WORKSPACE_TOO_SMALL;
   const int cus = knap::device_cus();
   if (!cus) return KNAP_ERR_LAUNCH_FAILED;
-  bool first = true;
-  hipError_t e = for_tables(grads, out, numel, types, n, [&](const knap::GradTable& t, uint32_t chunks) {
-    const int groups = (int)std::min<uint32_t>(chunks, (uint32_t)(8 * cus));
-    const hipError_t err = knap::launch_grad_clip(t, sum_sq, max_norm, eps, first ? norm : nullptr, groups, static_cast<hipStream_t>(stream));
-    first = false;
-    return err;
-  });
-  if (e == hipSuccess && first && norm) {      // no elements at all: the norm alone
-    knap::GradTable none;
-    none.n = 0;
-    none.first[0] = 0;
-    e = knap::launch_grad_clip(none, sum_sq, max_norm, eps, norm, 1, static_cast<hipStream_t>(stream));
-  }
-  return knap::launch_status(e);
+  return knap::launch_status(knap::launch_grad_squares(static_cast<const knap::GradChunk*>(plan), (int64_t)(plan_bytes / sizeof(knap::GradChunk)),
+                                                       static_cast<double*>(workspace), sum_sq, cus, static_cast<hipStream_t>(stream)));
+}
+
+int knap_grad_clip(const void* plan, size_t plan_bytes, const double* sum_sq, float max_norm, float eps, float* norm, void* stream) {
+  if (!plan_ok(plan, plan_bytes) || !sum_sq || !aligned(sum_sq, 8) || !aligned(norm, 4) || !(max_norm > 0.f) || !(eps >= 0.f) || !finite_f(eps))
+    return KNAP_ERR_INVALID_ARG;
+  if (plan_bytes == 0 && !norm) return KNAP_OK;
+  const int cus = knap::device_cus();
+  if (!cus) return KNAP_ERR_LAUNCH_FAILED;
+  return knap::launch_status(knap::launch_grad_clip(static_cast<const knap::GradChunk*>(plan), (int64_t)(plan_bytes / sizeof(knap::GradChunk)), sum_sq,
+                                                    max_norm, eps, norm, cus, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

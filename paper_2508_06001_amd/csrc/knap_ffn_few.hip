@@ -4,6 +4,10 @@
 //                              D: registers r are rows 4 (lane / 16) + r of column lane % 16
 // A workgroup forms 16 results (rows of the weights) of all tokens, 16 tokens a block of columns; its waves share the k's in runs of 32 STEPS, so that a row's
 // bytes are asked for in whole lines, with the next run's loads under way, and add up their sums in LDS in a fixed order.
+// Bound by HBM; what more tokens add is x and h, which every workgroup reads from L2.  Waves and steps as measured on weights that are in no cache, us (the
+// second product behind the +; 4 waves of 2 steps and 8 of 4 as they are here, against 8 and 16 waves of 4): one token 2048 x 5504 12.9 + 8.2 (15.2 + 8.7),
+// 4096 x 10944 35.6 + 15.0 (36.1 + 15.8; 5.0 and 6.0 TB/s); 24 tokens 47.5 + 29.2 (52.1 + 30.2).  32 rows of the weights a workgroup read x half as often, but
+// are fewer workgroups: 24 tokens 60 + 47.
 #include "knap_device.h"
 #include "knap_kernels.h"
 
@@ -28,9 +32,9 @@ __device__ __forceinline__ float gated(float a, float b, bool gelu) {
   return a * __builtin_amdgcn_rcpf(1.f + fast_exp2(-kLog2e * u)) * b;
 }
 
-template <int BLOCKS, bool PAIR, int WAVES>
+template <int BLOCKS, bool PAIR, int WAVES, int STEPS>
 __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(FewArgs a) {
-  constexpr int STEPS = BLOCKS > 2 ? 2 : 4, MATS = PAIR ? 2 : 1, RUN = 32 * STEPS;
+  constexpr int MATS = PAIR ? 2 : 1, RUN = 32 * STEPS;
   constexpr int kNowhere = 0x7fffffe0;      // a byte offset behind every descriptor
   __shared__ f32x4 s_sum[WAVES][MATS * BLOCKS][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -111,15 +115,14 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(FewArgs a) {
   }
 }
 
-template <bool PAIR, int WAVES>
+template <bool PAIR, int WAVES, int STEPS>
 static hipError_t launch_few(const FewArgs& a, hipStream_t stream) {
   const dim3 grid((a.N + 15) / 16), block(64 * WAVES);
-  if (a.tokens <= 16) hipLaunchKernelGGL((ffn_few_kernel<1, PAIR, WAVES>), grid, block, 0, stream, a);
-  else if (a.tokens <= 32) hipLaunchKernelGGL((ffn_few_kernel<2, PAIR, WAVES>), grid, block, 0, stream, a);
-  else if (a.tokens <= 48) hipLaunchKernelGGL((ffn_few_kernel<3, PAIR, WAVES>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((ffn_few_kernel<4, PAIR, WAVES>), grid, block, 0, stream, a);
+  if (a.tokens <= 16) hipLaunchKernelGGL((ffn_few_kernel<1, PAIR, WAVES, STEPS>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((ffn_few_kernel<2, PAIR, WAVES, STEPS>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
+static_assert(kFfnFew == 32, "one block of 16 tokens, or two");
 
 hipError_t launch_ffn_few(const FfnArgs& f, hipStream_t stream) {
   FewArgs a{};
@@ -127,12 +130,12 @@ hipError_t launch_ffn_few(const FfnArgs& f, hipStream_t stream) {
   a.tokens = f.tokens; a.N = f.hidden; a.K = f.width;
   a.out = f.h; a.out_stride = f.hidden; a.gate = f.gate; a.up = f.up;
   a.gelu = f.gelu;
-  const hipError_t e = launch_few<true, 8>(a, stream);
+  const hipError_t e = launch_few<true, 4, 2>(a, stream);
   if (e != hipSuccess) return e;
   a.w0 = f.w_down; a.w1 = nullptr; a.x = f.h; a.x_stride = f.hidden;
   a.N = f.width; a.K = f.hidden;
   a.out = f.y; a.out_stride = f.y_stride; a.gate = a.up = nullptr;
-  return launch_few<false, 16>(a, stream);
+  return launch_few<false, 8, 4>(a, stream);
 }
 
 }  // namespace knap

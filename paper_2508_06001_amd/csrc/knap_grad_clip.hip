@@ -1,25 +1,16 @@
 // Global norm of many gradients and clipping by it:
 //   S = sum g^2 over all tensors,  c = min(1, max_norm / (sqrt(S) + eps)),  out = c g.
-// Bound by HBM: every gradient is read once for S and once more for the product, which is written once.  A launch takes a table of tensors
-// in its arguments, so that nothing is copied to the device before it; its workgroups take chunks of kGradChunk elements in turn and look
-// up whose they are.  Squares and sums are in 64 bits (of which the card does as many as of 32): no gradient that is finite overflows or
-// vanishes in them, and the norm is right to its last bit in 32.  Every workgroup leaves one sum, which a second launch adds up in a fixed order.
+// Bound by HBM: every gradient is read once for S and once more for the product, which is written once.  Workgroups take chunks of a plan
+// in turn, whose records say where they lie.  Squares and sums are in 64 bits (of which the card does as many as of 32): no gradient that is finite
+// overflows or vanishes in them, and the norm is right to its last bit in 32.  Every workgroup leaves one sum, which a second launch adds up in a fixed order.
 #include "knap_device.h"
 #include "knap_kernels.h"
+
+#include <algorithm>
 
 namespace knap {
 
 constexpr int kGradThreads = 256;
-
-// the tensor that chunk c belongs to
-__device__ __forceinline__ int tensor_of(const GradTable& t, uint32_t c) {
-  int lo = 0, hi = t.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.first[mid] <= c) lo = mid; else hi = mid - 1;
-  }
-  return lo;
-}
 
 // 16 bytes as floats
 template <class T> struct Unit;
@@ -54,7 +45,7 @@ template <> struct Unit<float> {
 template <class T>
 __device__ __forceinline__ double chunk_squares(const T* p, int count) {
   using U = Unit<T>;
-  constexpr int TURNS = kGradChunk / (U::N * kGradThreads);
+  constexpr int TURNS = KNAP_GRAD_CHUNK / (U::N * kGradThreads);
   double s0 = 0.0, s1 = 0.0;
   if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, (uint32_t)count / U::N * 16u);
@@ -96,16 +87,15 @@ __device__ __forceinline__ double group_sum(double x, double* s_part) {
   return x;
 }
 
-__global__ __launch_bounds__(kGradThreads) void grad_squares_kernel(GradTable t, double* partial) {
+__global__ __launch_bounds__(kGradThreads) void grad_squares_kernel(const GradChunk* __restrict__ plan, int64_t chunks, double* __restrict__ partial) {
   __shared__ double s_part[kGradThreads / 64];
   double sum = 0.0;
-  const uint32_t chunks = t.first[t.n];
-  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const int i = tensor_of(t, c);
-    const int64_t start = (int64_t)(c - t.first[i]) * kGradChunk;
-    const int count = (int)min((int64_t)kGradChunk, t.numel[i] - start);
-    if (t.bf16[i]) sum += chunk_squares(static_cast<const __bf16*>(t.from[i]) + start, count);
-    else sum += chunk_squares(static_cast<const float*>(t.from[i]) + start, count);
+  GradChunk next = plan[blockIdx.x];
+  for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    const GradChunk k = next;
+    if (c + gridDim.x < chunks) next = plan[c + gridDim.x];
+    if (k.bf16) sum += chunk_squares(static_cast<const __bf16*>(k.from), k.count);
+    else sum += chunk_squares(static_cast<const float*>(k.from), k.count);
   }
   sum = group_sum(sum, s_part);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
@@ -123,7 +113,7 @@ __global__ __launch_bounds__(1024) void grad_join_kernel(const double* __restric
 template <class T>
 __device__ __forceinline__ void chunk_scale(const T* p, T* q, int count, float c) {
   using U = Unit<T>;
-  constexpr int TURNS = kGradChunk / (U::N * kGradThreads);
+  constexpr int TURNS = KNAP_GRAD_CHUNK / (U::N * kGradThreads);
   if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15) == 0) {
     const uint32_t bytes = (uint32_t)count / U::N * 16u;
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, bytes), w = make_rsrc(q, bytes);
@@ -145,33 +135,38 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* q, int count, float c
   }
 }
 
-__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(GradTable t, const double* __restrict__ sum, float max_norm, float eps, float* norm) {
+__global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(const GradChunk* __restrict__ plan, int64_t chunks, const double* __restrict__ sum,
+                                                                 float max_norm, float eps, float* norm) {
   const double length = sqrt(*sum);
   const double q = (double)max_norm / (length + (double)eps);
   // a NaN stays one; no limit clips nothing, whatever the norm
   const float c = q >= 1.0 || max_norm > 3.4028234e38f ? 1.f : (float)q;
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)length;
-  const uint32_t chunks = t.first[t.n];
-  for (uint32_t k = blockIdx.x; k < chunks; k += gridDim.x) {
-    const int i = tensor_of(t, k);
-    if (c == 1.f && t.from[i] == t.to[i]) continue;
-    const int64_t start = (int64_t)(k - t.first[i]) * kGradChunk;
-    const int count = (int)min((int64_t)kGradChunk, t.numel[i] - start);
-    if (t.bf16[i]) chunk_scale(static_cast<const __bf16*>(t.from[i]) + start, static_cast<__bf16*>(t.to[i]) + start, count, c);
-    else chunk_scale(static_cast<const float*>(t.from[i]) + start, static_cast<float*>(t.to[i]) + start, count, c);
+  if (blockIdx.x >= chunks) return;
+  GradChunk next = plan[blockIdx.x];
+  for (int64_t i = blockIdx.x; i < chunks; i += gridDim.x) {
+    const GradChunk k = next;
+    if (i + gridDim.x < chunks) next = plan[i + gridDim.x];
+    if (c == 1.f && k.from == k.to) continue;
+    if (k.bf16) chunk_scale(static_cast<const __bf16*>(k.from), static_cast<__bf16*>(k.to), k.count, c);
+    else chunk_scale(static_cast<const float*>(k.from), static_cast<float*>(k.to), k.count, c);
   }
 }
 
-hipError_t launch_grad_squares(const GradTable& t, double* partial, int groups, hipStream_t stream) {
-  hipLaunchKernelGGL(grad_squares_kernel, dim3(groups), dim3(kGradThreads), 0, stream, t, partial);
+hipError_t launch_grad_squares(const GradChunk* plan, int64_t chunks, double* partial, double* sum, int cus, hipStream_t stream) {
+  const int groups = (int)std::min<int64_t>(chunks, std::min(4 * cus, kGradGroups));
+  if (groups > 0) {
+    hipLaunchKernelGGL(grad_squares_kernel, dim3(groups), dim3(kGradThreads), 0, stream, plan, chunks, partial);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(grad_join_kernel, dim3(1), dim3(1024), 0, stream, partial, groups, sum);
   return hipGetLastError();
 }
-hipError_t launch_grad_join(const double* partial, int n, double* sum, hipStream_t stream) {
-  hipLaunchKernelGGL(grad_join_kernel, dim3(1), dim3(1024), 0, stream, partial, n, sum);
-  return hipGetLastError();
-}
-hipError_t launch_grad_clip(const GradTable& t, const double* sum, float max_norm, float eps, float* norm, int groups, hipStream_t stream) {
-  hipLaunchKernelGGL(grad_clip_kernel, dim3(groups), dim3(kGradThreads), 0, stream, t, sum, max_norm, eps, norm);
+
+hipError_t launch_grad_clip(const GradChunk* plan, int64_t chunks, const double* sum, float max_norm, float eps, float* norm, int cus, hipStream_t stream) {
+  const int groups = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, 8 * cus));
+  hipLaunchKernelGGL(grad_clip_kernel, dim3(groups), dim3(kGradThreads), 0, stream, plan, chunks, sum, max_norm, eps, norm);
   return hipGetLastError();
 }
 

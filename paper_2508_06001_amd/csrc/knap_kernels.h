@@ -129,20 +129,17 @@ constexpr int kResidualMaxGroups = 512;      // workgroups of a backward
 hipError_t launch_residual_norm_fwd(const ResidualArgs& a, bool x_bf16, bool b_bf16, bool wide, int cus, hipStream_t stream);
 hipError_t launch_residual_norm_bwd(const ResidualArgs& a, bool x_bf16, bool b_bf16, bool wide, int cus, hipStream_t stream);
 
-// Gradient norm and clipping.  A launch takes up to kGradTensors tensors; workgroups find theirs by the chunks of kGradChunk elements in
-// front of it.
-constexpr int kGradTensors = 112, kGradGroups = 1024, kGradChunk = 8192;
-struct GradTable {
-  const void* from[kGradTensors];
-  void* to[kGradTensors];              // of clipping
-  int64_t numel[kGradTensors];
-  uint32_t first[kGradTensors + 1];    // chunks in front of a tensor; [n]: of all
-  uint8_t bf16[kGradTensors];
-  int n;
+// Gradient norm and clipping: a record of the plan stands for up to KNAP_GRAD_CHUNK elements of one tensor
+struct GradChunk {
+  const void* from;
+  void* to;
+  int32_t count;
+  int32_t bf16;
 };
-hipError_t launch_grad_squares(const GradTable& t, double* partial, int groups, hipStream_t stream);
-hipError_t launch_grad_join(const double* partial, int n, double* sum, hipStream_t stream);
-hipError_t launch_grad_clip(const GradTable& t, const double* sum, float max_norm, float eps, float* norm, int groups, hipStream_t stream);
+constexpr int kGradGroups = 1024;      // most workgroups of a sum, one double each
+static_assert(KNAP_GRAD_WORKSPACE_BYTES == kGradGroups * sizeof(double), "a double a workgroup");
+hipError_t launch_grad_squares(const GradChunk* plan, int64_t chunks, double* partial, double* sum, int cus, hipStream_t stream);
+hipError_t launch_grad_clip(const GradChunk* plan, int64_t chunks, const double* sum, float max_norm, float eps, float* norm, int cus, hipStream_t stream);
 
 // Matrix products of the gated feed-forward block (knap_gemm.h).  One product of a launch:
 struct GemmProblem {
@@ -174,7 +171,7 @@ struct FfnArgs {
   float* partial;
 };
 size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward);
-constexpr int kFfnFew = 64;      // tokens up to which the forward takes the form of knap_ffn_few.hip
+constexpr int kFfnFew = 32;      // tokens up to which the forward takes the form of knap_ffn_few.hip
 hipError_t launch_ffn_few(const FfnArgs& a, hipStream_t stream);
 hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t stream);
 hipError_t launch_ffn_bwd(const FfnArgs& a, hipStream_t stream);

@@ -159,19 +159,22 @@ class GradientClip:
     """Buffers + calls of the global norm of a fixed list of gradients and clipping by it, in place or into `out`.  Ranks that hold parts of the
     gradients call sum_squares, add up `sum_sq` (an all-reduce of one float64) and call scale; clip does both on one GPU."""
 
-    def __init__(self, grads, max_norm: float, eps: float = 1e-6, out=None, device="cuda"):
-        self.list = B.GradList(grads, out)
+    def __init__(self, grads, max_norm: float, eps: float = 1e-6, out=None):
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        self.plan = B.knap_grad_plan(self.grads, self.out)
         self.max_norm, self.eps = float(max_norm), float(eps)
+        device = self.plan.device
         self.sum_sq = torch.zeros((), dtype=torch.float64, device=device)
         self.norm = torch.zeros((), dtype=torch.float32, device=device)
-        self.workspace = torch.empty(max(B.knap_grad_sum_squares_workspace_bytes(self.list.n), 256), dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(B.KNAP_GRAD_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
     def sum_squares(self, stream=None):
-        B.knap_grad_sum_squares(self.list, self.sum_sq, self.workspace, None, stream)
+        B.knap_grad_sum_squares(self.plan, self.sum_sq, self.workspace, B.KNAP_GRAD_WORKSPACE_BYTES, stream)
         return self.sum_sq
 
     def scale(self, stream=None):
-        B.knap_grad_clip(self.list, self.sum_sq, self.max_norm, self.eps, self.norm, None, stream)
+        B.knap_grad_clip(self.plan, self.sum_sq, self.max_norm, self.eps, self.norm, stream)
         return self.norm
 
     def clip(self, stream=None):

@@ -171,36 +171,68 @@ def arrays(at, numel, types):
 
 
 def test_bad_arguments_are_refused_without_touching_a_gpu():
+    import ctypes as C
     import paper_2508_06001_amd as K
     bad = K.KNAP_ERR_INVALID_ARG
+    room = (C.c_uint64 * 3000)()
 
-    def squares(at=(256, 512), numel=(8, 8), types=(0, 1), n=2, s=256, ws=256, size=1 << 20):
-        return K.lib.knap_grad_sum_squares(*arrays(at, numel, types), n, s, ws, size, 0)
-
-    def scale(at=(4096, 8192), out=(16384, 32768), numel=(8, 8), types=(0, 1), n=2, s=256, top=1.0, eps=0.0, norm=256):
+    def plan(at=(4096, 8192), out=(16384, 32768), numel=(8, 8), types=(0, 1), n=2, to=room, size=None):
         a, m, t = arrays(at, numel, types)
-        o = arrays(out, numel, types)[0]
-        return K.lib.knap_grad_clip(a, o, m, t, n, s, top, eps, norm, 0)
+        return K.lib.knap_grad_plan(a, arrays(out, numel, types)[0], m, t, n, C.cast(to, C.c_void_p) if to is not None else 0,
+                                    C.sizeof(room) if size is None else size)
 
-    for wrong in (dict(n=-1), dict(at=(0, 512)), dict(at=(257, 512)), dict(at=(256, 514)), dict(numel=(-1, 8)), dict(numel=(1 << 40, 8)), dict(types=(2, 0)),
-                  dict(types=(0, -1)), dict(s=0), dict(s=260), dict(ws=0), dict(ws=128)):
-        assert squares(**wrong) == bad, wrong
-    need = K.knap_grad_sum_squares_workspace_bytes(2)
-    assert need > 0 and squares(size=need - 1) == K.KNAP_ERR_WORKSPACE_TOO_SMALL and K.knap_grad_sum_squares_workspace_bytes(0) == 0
-    assert K.lib.knap_grad_sum_squares(0, 0, 0, 1, 256, 256, 1 << 20, 0) == bad
-    nan, inf = float("nan"), float("inf")
-    for wrong in (dict(n=-1), dict(at=(0, 512)), dict(out=(0, 512)), dict(out=(16385, 32768)), dict(s=0), dict(s=4), dict(top=0.0), dict(top=-1.0), dict(top=nan),
-                  dict(eps=-1.0), dict(eps=nan), dict(eps=inf), dict(norm=2),
+    assert plan() == K.KNAP_OK and plan(at=(4096, 0), out=(0, 0), numel=(0, 0)) == K.KNAP_OK and plan(n=0, to=None) == K.KNAP_OK
+    assert plan(at=(4096, 8192), out=(4096, 8192)) == K.KNAP_OK and plan(at=(4096, 4096), types=(1, 1)) == K.KNAP_OK      # read twice: as it says
+    for wrong in (dict(n=-1), dict(at=(0, 8192)), dict(at=(4097, 8192)), dict(at=(4096, 8194)), dict(out=(0, 32768)), dict(out=(16385, 32768)),
+                  dict(numel=(-1, 8)), dict(numel=(1 << 40, 8)), dict(types=(2, 0)), dict(types=(0, -1)), dict(to=None),
                   dict(at=(4096, 4096), out=(4096, 4096), types=(1, 1)),            # a tensor twice
                   dict(out=(16384, 16392)), dict(out=(16392, 16384)),               # parts of out that overlap
                   dict(out=(4096, 8176)), dict(out=(8192, 4096)), dict(out=(4104, 32768)), dict(out=(16384, 4096))):      # and that overlap a gradient
-        assert scale(**wrong) == bad, wrong
+        assert plan(**wrong) == bad, wrong
+    assert plan(size=47) == K.KNAP_ERR_CAPACITY
     many = 600           # more than the space on the stack holds: in order, in reverse order, one of them twice
     up = [4096 + 64 * i for i in range(many)]
     again = up[:-1] + [up[3]]
-    assert scale(at=again, out=again, numel=[8] * many, types=[1] * many, n=many) == bad
+    assert plan(at=again, out=again, numel=[8] * many, types=[1] * many, n=many) == bad
     shifted = [a + 16 for a in up[::-1]]
-    assert scale(at=up[::-1], out=shifted, numel=[8] * many, types=[1] * many, n=many) == bad
+    assert plan(at=up[::-1], out=shifted, numel=[8] * many, types=[1] * many, n=many) == bad
+    assert plan(at=up[::-1], out=up[::-1], numel=[8] * many, types=[1] * many, n=many) == K.KNAP_OK
+    assert K.lib.knap_grad_plan_bytes(0, 5) == 0
+    squares = lambda p=256, size=48, s=256, ws=256, n=8192: K.lib.knap_grad_sum_squares(p, size, s, ws, n, 0)  # noqa: E731
+    scale = lambda p=256, size=48, s=256, top=1.0, eps=0.0, norm=256: K.lib.knap_grad_clip(p, size, s, top, eps, norm, 0)  # noqa: E731
+    for wrong in (dict(p=0), dict(p=260), dict(size=47), dict(s=0), dict(s=260), dict(ws=0), dict(ws=128)):
+        assert squares(**wrong) == bad, wrong
+    assert squares(n=K.KNAP_GRAD_WORKSPACE_BYTES - 1) == K.KNAP_ERR_WORKSPACE_TOO_SMALL
+    nan, inf = float("nan"), float("inf")
+    for wrong in (dict(p=0), dict(p=4), dict(size=100), dict(s=0), dict(s=4), dict(top=0.0), dict(top=-1.0), dict(top=nan), dict(eps=-1.0), dict(eps=nan),
+                  dict(eps=inf), dict(norm=2)):
+        assert scale(**wrong) == bad, wrong
+    assert scale(p=0, size=0, norm=0) == K.KNAP_OK
+
+
+def test_a_plan_covers_every_element_once():
+    """Walks through the records as the kernels do."""
+    import ctypes as C
+    import paper_2508_06001_amd as K
+    numel = [1, 0, 8191, 8192, 8193, 5, 3 * 8192 + 17]
+    types = [0, 1, 1, 0, 1, 0, 1]
+    at = [1 << 20, 0, 2 << 20, 3 << 20, 4 << 20, 5 << 20, 6 << 20]
+    to = [a + (64 << 20) for a in at]
+    a, m, t = arrays(at, numel, types)
+    size = K.lib.knap_grad_plan_bytes(m, len(numel))
+    buf = (C.c_uint8 * size)()
+    assert K.lib.knap_grad_plan(a, arrays(to, numel, types)[0], m, t, len(numel), C.cast(buf, C.c_void_p), size) == K.KNAP_OK
+    records = np.frombuffer(bytes(buf), dtype=[("from", "<u8"), ("to", "<u8"), ("count", "<i4"), ("bf16", "<i4")])
+    i = 0
+    for n, ty, g, o in zip(numel, types, at, to):
+        done, width = 0, 2 if ty == 0 else 4
+        while done < n:
+            r = records[i]
+            i += 1
+            assert r["from"] == g + done * width and r["to"] == o + done * width and r["bf16"] == (ty == 0) and 0 < r["count"] <= K.KNAP_GRAD_CHUNK
+            done += int(r["count"])
+        assert done == n
+    assert i == len(records)
 
 
 @pytest.mark.gpu
@@ -209,14 +241,17 @@ def test_the_binding_refuses_what_the_library_cannot_see():
     import paper_2508_06001_amd as K
     g = torch.zeros((8, 8), device="cuda")
     s, ws = torch.zeros((), dtype=torch.float64, device="cuda"), torch.empty((1 << 16,), dtype=torch.uint8, device="cuda")
-    K.knap_grad_sum_squares([g], s, ws)
-    K.knap_grad_clip([g], s, 1.0)
-    for grads, out in (([g.half()], None), ([g.t()[:, :4]], None), ([g], []), ([g], [g.bfloat16()]), ([g], [g[:4]]), ([g.cpu(), g], None)):
+    plan = K.knap_grad_plan([g])
+    K.knap_grad_sum_squares(plan, s, ws)
+    K.knap_grad_clip(plan, s, 1.0)
+    for grads, out in (([g.half()], None), ([g.t()[:, :4]], None), ([g], []), ([g], [g.bfloat16()]), ([g], [g[:4]]), ([g.cpu(), g], None), ([g, g], None),
+                       ([g, g[:4]], None)):
         with pytest.raises(K.KnapError):
-            K.GradList(grads, out)
-    for args in (([g], s.float(), ws), ([g], s, None), ([g], s, ws[:64]), ([g], s.cpu(), ws), ([g.cpu()], s, ws)):
+            K.knap_grad_plan(grads, out)
+    for args in ((plan, s.float(), ws), (plan, s, None), (plan, s, ws[:64]), (plan, s.cpu(), ws), (plan.cpu(), s, ws), (plan.view(torch.int32), s, ws),
+                 (plan[:23], s, ws), (plan, s.new_zeros(2), ws)):
         with pytest.raises(K.KnapError):
             K.knap_grad_sum_squares(*args)
-    for args, kw in ((([g, g], s, 1.0), {}), (([g], s, 0.0), {}), (([g], s, 1.0), dict(norm=s)), ((K.GradList([g]), s, 1.0), dict(out=[g]))):
+    for args, kw in (((plan, s, 0.0), {}), ((plan, s, 1.0), dict(norm=s)), ((plan.cpu(), s, 1.0), {}), ((plan, s.float(), 1.0), {})):
         with pytest.raises(K.KnapError):
             K.knap_grad_clip(*args, **kw)
