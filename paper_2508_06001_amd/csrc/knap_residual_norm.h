@@ -64,24 +64,27 @@ __device__ __forceinline__ void load_scale(const ResidualArgs& a, int seq, int g
   for (int i = 0; i < C::COLS; ++i) sw[i] = norm_has<C>(g, i, a.width) ? (1.f + sw[i]) * w[i] : 0.f;
 }
 
-// Which form a width takes: up to 16 columns of a thread, so that the vectors of a sequence and its sums fit the registers beside the rows;
-// a thread of the widest has 32.
+// Which form a width takes: 8 columns of a thread, or 16, so that the vectors of a sequence and its sums fit the registers beside the rows; two rows
+// at a time where that leaves registers (single columns, which take a register each: 8191 rows of 1003 in 32 bits, one and two rows, forward 28 and 35 us).
 template <bool WIDE, class F>
 hipError_t residual_form(int width, F f) {
   if constexpr (WIDE) {
     if (width <= 128) return f(NormCfg<16, 1, 2, WIDE>{});
     if (width <= 256) return f(NormCfg<32, 1, 2, WIDE>{});
   }
-  if (width <= 512) return f(NormCfg<64, 1, 2, WIDE>{});
+  if (width <= 512) return f(NormCfg<64, 1, WIDE ? 2 : 1, WIDE>{});
   if constexpr (WIDE) {
     if (width <= 1024) return f(NormCfg<64, 2, 1, WIDE>{});
     if (width <= 1536) return f(NormCfg<192, 1, 2, WIDE>{});
   }
-  if (width <= 2048) return f(NormCfg<256, 1, 2, WIDE>{});
-  if (width <= 4096) return f(NormCfg<256, 2, 1, WIDE>{});
-  if (width <= 8192) return f(NormCfg<512, 2, 1, WIDE>{});
-  return f(NormCfg<512, 4, 1, WIDE>{});
+  if (width <= 2048) return f(NormCfg<256, 1, WIDE ? 2 : 1, WIDE>{});
+  if (width <= 4096) return f(NormCfg<512, 1, 1, WIDE>{});
+  if (width <= 8192) return f(NormCfg<1024, 1, 1, WIDE>{});
+  return f(NormCfg<1024, 2, 1, WIDE>{});
 }
+// whether the next rows' loads are under way while these are worked on: where there are registers for both
+template <class C, class TX>
+constexpr bool residual_ahead() { return C::LANES < 1024 && (C::UNITS == 1 || sizeof(TX) == 2); }
 
 // Rows of a workgroup where `most` of them share `rows`: whole passes, but where there are few rows
 inline int residual_chunk(int64_t rows, int64_t most, int pass) {

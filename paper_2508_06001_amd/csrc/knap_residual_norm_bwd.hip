@@ -13,15 +13,15 @@
 
 namespace knap {
 
-template <class C, class TX, class TB>
-__global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual_norm_bwd_kernel(ResidualArgs a) {
-  __shared__ float s_sum[2][2 * C::ROWS * 8];
+template <class C, class TX, class TB, bool POST>
+__global__ __launch_bounds__(C::THREADS, C::THREADS > 512 ? 4 : 2) void residual_norm_bwd_kernel(ResidualArgs a) {
+  __shared__ float s_sum[2][2 * C::ROWS * C::THREADS / 64];
   __shared__ float s_cols[C::GROUPS > 1 ? C::THREADS * C::COLS : 1];
-  constexpr bool AHEAD = C::COLS * sizeof(TX) <= 32;
+  constexpr bool AHEAD = residual_ahead<C, TX>();
   const int g = threadIdx.x % C::LANES, group = threadIdx.x / C::LANES;
   const int width = a.width;
   const float n = (float)width;
-  const bool layer = a.norm == KNAP_NORM_LAYER, post_layer = a.post_norm == KNAP_NORM_LAYER, post = a.post_norm != KNAP_NORM_NONE;
+  const bool layer = a.norm == KNAP_NORM_LAYER, post_layer = a.post_norm == KNAP_NORM_LAYER;
   const TX* x_base = static_cast<const TX*>(a.x);
   const TB* f_base = static_cast<const TB*>(a.f);
   const TX* dxo_base = static_cast<const TX*>(a.dx_out);
@@ -45,8 +45,8 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual
       const bool there = row < c.end;
       raw_stats[k][0] = there && dy_base ? a.stats[row] : 0.f;
       raw_stats[k][1] = there && dy_base ? a.stats[a.rows + row] : 0.f;
-      raw_stats[k][2] = there && post ? a.stats[2 * a.rows + row] : 0.f;
-      raw_stats[k][3] = post ? (there ? a.stats[3 * a.rows + row] : 0.f) : 1.f;
+      raw_stats[k][2] = there && POST ? a.stats[2 * a.rows + row] : 0.f;
+      raw_stats[k][3] = POST ? (there ? a.stats[3 * a.rows + row] : 0.f) : 1.f;
     }
   };
   if (AHEAD && at.row < at.limit) load(at);
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual
     total[0] = first_sum ? tb : total[0] + tb;
     total[width] = first_sum ? tc : total[width] + tc;
   };
-  auto flush = [&]() {
+  auto flush = [&](int g) {
     if (!a.partial) return;
     if constexpr (C::GROUPS == 1) {
 #pragma unroll
@@ -105,16 +105,21 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual
     }
     first_sum = false;
   };
-  while (at.row < at.limit) {
-    if (!AHEAD) load(at);
-    if (at.seq != seq) {
-      if (seq >= 0) flush();
+  while (true) {
+    const bool done = at.row >= at.limit;
+    if (done || at.seq != seq) {
+      // what is done once a sequence forms its addresses here: outside of the loop they would take the registers of the rows
+      int own = g;
+      asm volatile("" : "+v"(own));
+      if (seq >= 0) flush(own);
+      if (done) return;
       seq = at.seq;
-      load_gate<C>(a, seq, g, gz);
-      load_scale<C>(a, seq, g, sw);
+      load_gate<C>(a, seq, own, gz);
+      load_scale<C>(a, seq, own, sw);
 #pragma unroll
       for (int i = 0; i < C::COLS; ++i) sa[i] = sb[i] = sc[i] = 0.f;
     }
+    if (!AHEAD) load(at);
     // x' in place of x, the normed f
     float x[C::ROWS][C::COLS], f[C::ROWS][C::COLS], mean[C::ROWS], rstd[C::ROWS], rp[C::ROWS];
     RowRaw<C, TX> dxo[C::ROWS];
@@ -129,7 +134,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual
       dy[k] = raw_dy[k];
 #pragma unroll
       for (int i = 0; i < C::COLS; ++i) {
-        f[k][i] = (raw_f[k].get(i) - raw_stats[k][2]) * rp[k];
+        f[k][i] = POST ? (raw_f[k].get(i) - raw_stats[k][2]) * rp[k] : raw_f[k].get(i);
         x[k][i] = __builtin_fmaf(f[k][i], gz[i], raw_x[k].get(i));
       }
     }
@@ -164,29 +169,30 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual
         const float X = __builtin_fmaf(rstd[k], __builtin_fmaf(dy[k].get(i), sw[i], -m1) - x[k][i] * m2, dxo[k].get(i));
         x[k][i] = X;                                  // X from here on
         sc[i] = __builtin_fmaf(X, f[k][i], sc[i]);
-        const float e = X * gz[i];
-        s1 += e;
-        s2 = __builtin_fmaf(e, f[k][i], s2);
+        if constexpr (POST) {
+          const float e = X * gz[i];
+          s1 += e;
+          s2 = __builtin_fmaf(e, f[k][i], s2);
+        }
       }
       sums[2 * k] = s1;
       sums[2 * k + 1] = s2;
       if (dx_base) store_row<C, TX>(RowPlace<C, TX>(dx_base, a.dx_stride, (int64_t)now.row + k * C::GROUPS, group, now.end, width), g, x[k]);
     }
     if (!df_base) continue;
-    if (post) {
+    if constexpr (POST) {
       row_sums<C>(sums, s_sum[turn]);
       turn ^= 1;
     }
 #pragma unroll
     for (int k = 0; k < C::ROWS; ++k) {
-      const float m1 = post_layer ? sums[2 * k] / n : 0.f, m2 = post ? sums[2 * k + 1] / n : 0.f;
+      const float m1 = post_layer ? sums[2 * k] / n : 0.f, m2 = sums[2 * k + 1] / n;
       float df[C::COLS];
 #pragma unroll
-      for (int i = 0; i < C::COLS; ++i) df[i] = rp[k] * (__builtin_fmaf(x[k][i], gz[i], -m1) - f[k][i] * m2);
+      for (int i = 0; i < C::COLS; ++i) df[i] = POST ? rp[k] * (__builtin_fmaf(x[k][i], gz[i], -m1) - f[k][i] * m2) : x[k][i] * gz[i];
       store_row<C, TB>(RowPlace<C, TB>(df_base, a.df_stride, (int64_t)now.row + k * C::GROUPS, group, now.end, width), g, df);
     }
   }
-  if (seq >= 0) flush();
 }
 
 // Adds up what the workgroups left.  blockIdx.y: a sequence, or n_seq for the sums over all of them; COLS columns of the three (two) sums
@@ -236,9 +242,10 @@ static hipError_t launch_sums(const ResidualArgs& a, int groups, hipStream_t str
   const bool each = a.dshift || a.dscale || a.dgate, whole = a.dweight || a.dpost_weight;
   if (!each && !whole) return hipSuccess;
   const int cols = 3 * a.width;
-  // the rows of a sequence's sums are `groups` at most and few where there are many sequences: threads side by side accordingly
-  if (groups > 16 * a.n_seq) hipLaunchKernelGGL((residual_norm_sum_kernel<16, 64>), dim3((cols + 15) / 16, a.n_seq + 1), dim3(1024), 0, stream, a, cols);
-  else hipLaunchKernelGGL((residual_norm_sum_kernel<64, 8>), dim3((cols + 63) / 64, a.n_seq + 1), dim3(512), 0, stream, a, cols);
+  const dim3 grid((cols + 63) / 64, a.n_seq + (whole ? 1 : 0));
+  // a sequence's rows of sums are `groups` / n_seq on the average: threads side by side accordingly
+  if (groups > 32 * a.n_seq) hipLaunchKernelGGL((residual_norm_sum_kernel<64, 16>), grid, dim3(1024), 0, stream, a, cols);
+  else hipLaunchKernelGGL((residual_norm_sum_kernel<64, 4>), grid, dim3(256), 0, stream, a, cols);
   return hipGetLastError();
 }
 
@@ -249,7 +256,7 @@ static hipError_t launch_bwd_t(ResidualArgs a, int cus, hipStream_t stream) {
     a.chunk = residual_chunk(a.rows, std::min(2 * cus, kResidualMaxGroups), C::PASS);
     const int groups = (int)((a.rows + a.chunk - 1) / a.chunk);
     if (groups > 0) {
-      hipLaunchKernelGGL((residual_norm_bwd_kernel<C, TX, TB>), dim3(groups), dim3(C::THREADS), 0, stream, a);
+      hipLaunchKernelGGL((a.post_norm == KNAP_NORM_NONE ? residual_norm_bwd_kernel<C, TX, TB, false> : residual_norm_bwd_kernel<C, TX, TB, true>), dim3(groups), dim3(C::THREADS), 0, stream, a);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }

@@ -10,7 +10,7 @@ namespace knap {
 
 // mean (layer norm alone) and rstd of ROWS rows that the threads hold
 template <class C>
-__device__ __forceinline__ void row_stats(const float (&x)[C::ROWS][C::COLS], bool layer, int g, int width, float eps, float (*s_sum)[C::ROWS * 8],
+__device__ __forceinline__ void row_stats(const float (&x)[C::ROWS][C::COLS], bool layer, int g, int width, float eps, float (*s_sum)[C::ROWS * C::THREADS / 64],
                                           int& turn, float (&mean)[C::ROWS], float (&rstd)[C::ROWS]) {
   const float n = (float)width;
   float sum[C::ROWS];
@@ -44,10 +44,10 @@ __device__ __forceinline__ void row_stats(const float (&x)[C::ROWS][C::COLS], bo
   for (int k = 0; k < C::ROWS; ++k) rstd[k] = 1.0f / sqrtf(sum[k] / n + eps);
 }
 
-template <class C, class TX, class TB>
-__global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual_norm_fwd_kernel(ResidualArgs a) {
-  __shared__ float s_sum[2][C::ROWS * 8];
-  constexpr bool AHEAD = C::COLS <= 16;      // the next rows' loads under way while these are worked on
+template <class C, class TX, class TB, bool POST>
+__global__ __launch_bounds__(C::THREADS, C::THREADS > 512 ? 4 : 2) void residual_norm_fwd_kernel(ResidualArgs a) {
+  __shared__ float s_sum[2][C::ROWS * C::THREADS / 64];
+  constexpr bool AHEAD = residual_ahead<C, TX>();
   const int g = threadIdx.x % C::LANES, group = threadIdx.x / C::LANES;
   const int width = a.width;
   const TX* x_base = static_cast<const TX*>(a.x);
@@ -73,11 +73,13 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual
     if (!AHEAD) load(at);
     if (at.seq != seq) {
       seq = at.seq;
-      if (f_base) load_gate<C>(a, seq, g, gz);
+      int own = g;      // addresses that are formed here and not outside of the loop, where they would take registers
+      asm volatile("" : "+v"(own));
+      if (f_base) load_gate<C>(a, seq, own, gz);
       if (y_base) {
-        load_scale<C>(a, seq, g, sw);
+        load_scale<C>(a, seq, own, sw);
         const char* shift = a.shift ? static_cast<const char*>(a.shift) + (int64_t)seq * a.mod_stride * (a.mod_bf16 ? 2 : 4) : nullptr;
-        load_weight<C>(shift, a.mod_bf16, 0.f, g, width, sh);
+        load_weight<C>(shift, a.mod_bf16, 0.f, own, width, sh);
       }
     }
     float x[C::ROWS][C::COLS], f[C::ROWS][C::COLS];
@@ -93,7 +95,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS > 256 ? 1 : 2) void residual
     if (AHEAD && at.row < at.limit) load(at);
     float mean[C::ROWS], rstd[C::ROWS];
     if (f_base) {
-      if (a.post_norm != KNAP_NORM_NONE) {
+      if constexpr (POST) {
         row_stats<C>(f, a.post_norm == KNAP_NORM_LAYER, g, width, a.eps, s_sum, turn, mean, rstd);
 #pragma unroll
         for (int k = 0; k < C::ROWS; ++k) {
@@ -135,7 +137,7 @@ static hipError_t launch_fwd_t(ResidualArgs a, int cus, hipStream_t stream) {
   return residual_form<WIDE>(a.width, [&](auto cfg) {
     using C = decltype(cfg);
     a.chunk = residual_chunk(a.rows, 4 * cus, C::PASS);
-    hipLaunchKernelGGL((residual_norm_fwd_kernel<C, TX, TB>), dim3((unsigned)((a.rows + a.chunk - 1) / a.chunk)), dim3(C::THREADS), 0, stream, a);
+    hipLaunchKernelGGL((a.post_norm == KNAP_NORM_NONE ? residual_norm_fwd_kernel<C, TX, TB, false> : residual_norm_fwd_kernel<C, TX, TB, true>), dim3((unsigned)((a.rows + a.chunk - 1) / a.chunk)), dim3(C::THREADS), 0, stream, a);
     return hipGetLastError();
   });
 }
