@@ -97,7 +97,7 @@ constexpr int kPast = 2;      // the non-temporal bit of a buffer access
 template <class C, int EP>
 __device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProblem& p, int m0, int n0, const f32x16 (&acc)[C::TM][C::TN],
                                             const GemmBuffers& lds) {
-  static_assert(C::WAVES == 4 && C::BUFFERS == 2 && C::STAGE >= 4 * 32 * 32 * C::TN, "a wave has half of a buffer");
+  static_assert(C::WAVES == 4 && C::STAGE >= 4 * 32 * 32 * C::TN, "a wave has half of a buffer");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
   // (of the LDS address space, which a choice between two arrays otherwise loses)
@@ -210,7 +210,7 @@ __device__ __forceinline__ int locate(const GemmLaunch& g, int tile, int& m0, in
 
 template <class C, bool A_ROWK, bool B_ROWK, int EP>
 __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C::WAVES / 2) void gemm_kernel(GemmLaunch g) {
-  __shared__ __align__(1024) __bf16 b0[C::STAGE], b1[C::STAGE];
+  __shared__ __align__(1024) __bf16 b0[C::STAGE], b1[C::STAGE], b2[C::BUFFERS == 4 ? C::STAGE : 8], b3[C::BUFFERS == 4 ? C::STAGE : 8];
   constexpr bool PAIRED = EP == kActForward, TWO = EP == kStore && A_ROWK && !B_ROWK;      // dx alone adds up two products
   int tile, part = 0, parts = 1;
   if ((int)blockIdx.x < g.whole) tile = xcd_order(blockIdx.x, g.whole);
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C
   const GemmProblem& p = g.p[q];
   const int stages = (p.K + C::KS - 1) / C::KS * p.segments;
   f32x16 acc[C::TM][C::TN];
-  gemm_tile<C, A_ROWK, B_ROWK, PAIRED, TWO>(p, m0, n0, (int)((int64_t)stages * part / parts), (int)((int64_t)stages * (part + 1) / parts), GemmBuffers{b0, b1}, acc);
+  gemm_tile<C, A_ROWK, B_ROWK, PAIRED, TWO>(p, m0, n0, (int)((int64_t)stages * part / parts), (int)((int64_t)stages * (part + 1) / parts), GemmBuffers{b0, b1, b2, b3}, acc);
   if (parts > 1) {
     f32x4* to = reinterpret_cast<f32x4*>(g.partial) + (size_t)((int)blockIdx.x - g.whole) * (C::BM * C::BN / 4) + threadIdx.x;
 #pragma unroll
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C
           to[((i * C::TN + j) * 4 + k) * C::THREADS] = f32x4{acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
     return;
   }
-  finish_tile<C, EP>(g, p, m0, n0, acc, GemmBuffers{b0, b1});
+  finish_tile<C, EP>(g, p, m0, n0, acc, GemmBuffers{b0, b1, b2, b3});
 }
 
 // Adds up the parts of a tile's block (blockIdx.y; of a pair of blocks) in their order and finishes it
@@ -269,17 +269,36 @@ __global__ __launch_bounds__(C::THREADS) void gemm_join_kernel(GemmLaunch g) {
       if (ii == i && jj == j) finish_block<C, EP>(g, g.p[q], m0, n0, ii, jj, x[0], x[STEP - 1]);
 }
 
-using Large = GemmCfg<256, 256, 2, 2>;
-using Small = GemmCfg<128, 128, 2, 2>;
+// Forms.  Large: the fewest bytes of LDS and L2 a product; Small: two workgroups a CU; Deep: one, whose copies run four stages ahead, for calls with so
+// few tiles that a stage waits for memory (613 tokens, 1000 x 2664, dx without parts: 48 us, Small 70; 4173 tokens, 2048 x 5504, up: Large 167, Small 205,
+// Deep 237).
+// Large reads its fragments two steps ahead, but for a and b together (4173 tokens, 2048 x 5504, us, two and one: up 181 and 167; 31464 tokens,
+// 1536 x 4096: dx 643 and 709, down 299 and 307, up 706 and 691).
+template <int EP>
+using Large = GemmCfg<256, 256, 2, 2, 2, EP == kActForward ? 1 : 2>;
+using Small = GemmCfg<128, 128, 2, 2, 2, 1>;
+using Deep = GemmCfg<128, 128, 2, 2, 4, 1>;
 
 // ---------------------------------------------------------------------------
 // Plans
 // ---------------------------------------------------------------------------
 constexpr int kGemmCus = 256;
 
-// Tiles of the products in `g`, what of them goes in parts, and the bytes that the parts take
+// What a form costs, in us, as measured: a stage of a round of workgroups with `fill` of the card's places taken, and what a part adds that is written
+// and read again.
+struct FormCost {
+  int places;                   // workgroups at one time
+  float stage, more, part;      // a stage takes stage + more * fill
+};
+template <class C> constexpr FormCost form_cost() { return {kGemmCus, 1.15f, 0.55f, 0.105f}; }      // Large
+template <> constexpr FormCost form_cost<Small>() { return {2 * kGemmCus, 0.62f, 0.43f, 0.026f}; }
+template <> constexpr FormCost form_cost<Deep>() { return {kGemmCus, 0.38f, 0.22f, 0.026f}; }
+constexpr float kJoin = 4.f;      // the launch that adds up parts
+
+// Lays down the tiles of the products in `g` in form C, and how many parts the tiles of the last round go in (which is not full: more of them take less
+// time and more bytes); returns the estimated time.
 template <class C>
-size_t plan(GemmLaunch& g, bool paired) {
+float plan(GemmLaunch& g, bool paired) {
   int tiles = 0, stages = 1 << 30;
   for (int q = 0; q < 3; ++q) {
     g.first[q] = q < g.n ? tiles : INT32_MAX;
@@ -291,18 +310,42 @@ size_t plan(GemmLaunch& g, bool paired) {
     tiles += p.tiles_m * p.tiles_n;
     stages = std::min(stages, (p.K + C::KS - 1) / C::KS * p.segments);
   }
-  const int slots = kGemmCus * (C::LDS_BYTES > 81920 ? 1 : 2);
-  const int rest = tiles % slots;
-  g.splits = rest ? std::min(slots / rest, std::max(1, stages / 4)) : 1;
+  constexpr FormCost f = form_cost<C>();
+  const int rest = tiles % f.places;
+  float last = 0.f;
+  g.splits = 1;
+  if (rest) {
+    auto round = [&](int parts) { return (float)stages / (float)parts * (f.stage + f.more * (float)(rest * parts) / (float)f.places); };
+    last = round(1);
+    const int most = std::min(f.places / rest, stages / 4);
+    for (int parts = 2; parts <= most; ++parts) {
+      const float t = round(parts) + kJoin + f.part * (float)(rest * parts);
+      if (t < last) { last = t; g.splits = parts; }
+    }
+  }
   g.whole = g.splits > 1 ? tiles - rest : tiles;
   g.tail = tiles - g.whole;
-  return (size_t)g.tail * g.splits * C::BM * C::BN * sizeof(float);
+  return (float)(tiles / f.places) * (float)stages * (f.stage + f.more) + last;
+}
+
+template <class C>
+size_t parts_bytes(const GemmLaunch& g) { return (size_t)g.tail * g.splits * C::BM * C::BN * sizeof(float); }
+
+// calls f(form, launch) with the form of the least estimated time
+template <int EP, class F>
+auto with_form(const GemmLaunch& g, F f) {
+  constexpr bool paired = EP == kActForward;
+  GemmLaunch large = g, small = g, deep = g;
+  const float tl = plan<Large<EP>>(large, paired), ts = plan<Small>(small, paired), td = plan<Deep>(deep, paired);
+  if (tl <= ts && tl <= td) return f(Large<EP>{}, large);
+  if (ts <= td) return f(Small{}, small);
+  return f(Deep{}, deep);
 }
 
 template <class C, bool A_ROWK, bool B_ROWK, int EP>
 hipError_t launch_gemm(const GemmLaunch& g, hipStream_t stream) {
   constexpr int BLOCKS = C::TM * C::TN / (EP == kActForward ? 2 : 1);
-  if (g.whole + (int64_t)g.tail * g.splits > 1 << 22) return hipErrorInvalidValue;      // 2^38 results, more than the card holds
+  if (g.whole + (int64_t)g.tail * g.splits > 1 << 22) return hipErrorInvalidValue;      // 2^36 results, which the card does not hold
   hipLaunchKernelGGL((gemm_kernel<C, A_ROWK, B_ROWK, EP>), dim3(g.whole + g.tail * g.splits), dim3(C::THREADS), 0, stream, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.tail == 0) return e;
@@ -310,25 +353,13 @@ hipError_t launch_gemm(const GemmLaunch& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Tiles of 256 x 256 where they fill the card more than once, else of 128 x 128
-static bool large(const GemmLaunch& g, bool paired) {
-  int64_t tiles = 0;
-  for (int q = 0; q < g.n; ++q) tiles += (int64_t)((g.p[q].M + 255) / 256) * ((g.p[q].N + (paired ? 127 : 255)) / (paired ? 128 : 256));
-  return tiles >= kGemmCus;
-}
-
-template <bool A_ROWK, bool B_ROWK, int EP>
-size_t bytes_of(GemmLaunch g) {
-  return large(g, EP == kActForward) ? plan<Large>(g, EP == kActForward) : plan<Small>(g, EP == kActForward);
+template <int EP>
+size_t bytes_of(const GemmLaunch& g) {
+  return with_form<EP>(g, [](auto form, const GemmLaunch& planned) { return parts_bytes<decltype(form)>(planned); });
 }
 template <bool A_ROWK, bool B_ROWK, int EP>
-hipError_t run(GemmLaunch g, hipStream_t stream) {
-  if (large(g, EP == kActForward)) {
-    plan<Large>(g, EP == kActForward);
-    return launch_gemm<Large, A_ROWK, B_ROWK, EP>(g, stream);
-  }
-  plan<Small>(g, EP == kActForward);
-  return launch_gemm<Small, A_ROWK, B_ROWK, EP>(g, stream);
+hipError_t run(const GemmLaunch& g, hipStream_t stream) {
+  return with_form<EP>(g, [&](auto form, const GemmLaunch& planned) { return launch_gemm<decltype(form), A_ROWK, B_ROWK, EP>(planned, stream); });
 }
 
 static GemmProblem product(const __bf16* a, int64_t lda, const __bf16* b, int64_t ldb, __bf16* c, int64_t ldc, int M, int N, int K) {
@@ -391,21 +422,21 @@ static GemmLaunch weight_gradients(const FfnArgs& a) {
 size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward) {
   FfnArgs a{};
   a.tokens = (int)tokens; a.width = width; a.hidden = hidden;
-  if (!backward && tokens <= kFfnFew) return 0;
-  if (!backward) return std::max(bytes_of<true, true, kActForward>(up_products(a)), bytes_of<true, true, kStore>(down_product(a)));
-  size_t most = std::max(bytes_of<true, false, kActBackward>(hidden_gradients(a)), bytes_of<true, false, kStore>(input_gradient(a)));
+  if (!backward && ffn_few(tokens, width, hidden)) return 0;
+  if (!backward) return std::max(bytes_of<kActForward>(up_products(a)), bytes_of<kStore>(down_product(a)));
+  size_t most = std::max(bytes_of<kActBackward>(hidden_gradients(a)), bytes_of<kStore>(input_gradient(a)));
   for (int wanted = 1; wanted < 8; ++wanted) {      // whichever gradients of weights a call asks for
     static __bf16 none;
     a.dw_gate = wanted & 1 ? &none : nullptr;
     a.dw_up = wanted & 2 ? &none : nullptr;
     a.dw_down = wanted & 4 ? &none : nullptr;
-    most = std::max(most, bytes_of<false, false, kStore>(weight_gradients(a)));
+    most = std::max(most, bytes_of<kStore>(weight_gradients(a)));
   }
   return most;
 }
 
 hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t stream) {
-  if (a.tokens <= kFfnFew) return launch_ffn_few(a, stream);
+  if (ffn_few(a.tokens, a.width, a.hidden)) return launch_ffn_few(a, stream);
   const hipError_t e = run<true, true, kActForward>(up_products(a), stream);
   return e != hipSuccess ? e : run<true, true, kStore>(down_product(a), stream);
 }

@@ -1,4 +1,4 @@
-// Gated feed-forward block, forward, of few tokens (the next ones of some sequences): both products of knap_ffn.hip where the weights' bytes are all
+// Gated feed-forward block, forward, of few tokens (the next ones of some sequences, at most 32): both products of knap_ffn.hip where the weights' bytes are all
 // that counts.  Every weight is read once, straight into registers; x, h and the sums stay in the caches.
 //   v_mfma_f32_16x16x32_bf16   A: lane holds row lane % 16, k's 8 (lane / 16) .. + 7, B: column lane % 16, the same k's,
 //                              D: registers r are rows 4 (lane / 16) + r of column lane % 16
@@ -122,7 +122,6 @@ static hipError_t launch_few(const FewArgs& a, hipStream_t stream) {
   else hipLaunchKernelGGL((ffn_few_kernel<2, PAIR, WAVES, STEPS>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
-static_assert(kFfnFew == 32, "one block of 16 tokens, or two");
 
 hipError_t launch_ffn_few(const FfnArgs& f, hipStream_t stream) {
   FewArgs a{};

@@ -23,20 +23,23 @@ namespace knap {
 
 constexpr int kGemmNowhere = 0x7fffffe0;  // a byte offset behind every descriptor
 
-template <int BM_, int BN_, int WM_, int WN_>
+template <int BM_, int BN_, int WM_, int WN_, int BUFFERS_, int AHEAD_>
 struct GemmCfg {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
-  static constexpr int KS = 64, BUFFERS = 2;              // k's of a stage, buffers of the ring
+  static constexpr int KS = 64, BUFFERS = BUFFERS_;       // k's of a stage, buffers of the ring (2 or 4)
+  static constexpr int AHEAD = AHEAD_;                    // steps of 16 k's that fragments are read ahead of their products (1 or 2)
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   static constexpr int STAGE = (BM + BN) * KS;      // elements
   static constexpr int LDS_BYTES = BUFFERS * STAGE * 2;
 };
-struct GemmBuffers { __bf16 *b0, *b1; };
+struct GemmBuffers { __bf16 *b0, *b1, *b2, *b3; };
 template <int B>
 __device__ __forceinline__ __bf16* buffer_of(const GemmBuffers& s) {
   if constexpr (B == 0) return s.b0;
-  else return s.b1;
+  else if constexpr (B == 1) return s.b1;
+  else if constexpr (B == 2) return s.b2;
+  else return s.b3;
 }
 
 // Copies of R rows (columns) of an operand for one stage of KS k's: instruction i of a wave fills 1 KB.
@@ -196,26 +199,30 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
   FragmentReader<B_ROWK, C::KS> rb;
   ra.init(lane);
   rb.init(lane);
-  bf16x8 fa[2][C::TM], fb[2][C::TN];
-  auto read = [&](const __bf16* buffer, int kk) {      // into the set of kk's parity
+  constexpr int SETS = 2 * C::AHEAD;
+  bf16x8 fa[SETS][C::TM], fb[SETS][C::TN];
+  auto read = [&](const __bf16* buffer, int kk) {
 #pragma unroll
-    for (int j = 0; j < C::TN; ++j) fb[kk & 1][j] = rb.get(buffer + C::BM * C::KS, wn * C::TN + j, kk);
+    for (int j = 0; j < C::TN; ++j) fb[kk % SETS][j] = rb.get(buffer + C::BM * C::KS, wn * C::TN + j, kk);
 #pragma unroll
-    for (int i = 0; i < C::TM; ++i) fa[kk & 1][i] = ra.get(buffer, wm * C::TM + i, kk);
+    for (int i = 0; i < C::TM; ++i) fa[kk % SETS][i] = ra.get(buffer, wm * C::TM + i, kk);
   };
   // the first fragments of the next stage stay where they are read, although the loop may end before their use: the compiler would read them behind
   // the branch, in front of the products that need them
   auto hold = [&]() {
 #pragma unroll
-    for (int i = 0; i < C::TM; ++i) asm volatile("" : "+v"(fa[0][i]));
+    for (int kk = 0; kk < C::AHEAD; ++kk) {
 #pragma unroll
-    for (int j = 0; j < C::TN; ++j) asm volatile("" : "+v"(fb[0][j]));
+      for (int i = 0; i < C::TM; ++i) asm volatile("" : "+v"(fa[kk][i]));
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) asm volatile("" : "+v"(fb[kk][j]));
+    }
   };
   auto multiply = [&](int kk) {
 #pragma unroll
     for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-      for (int j = 0; j < C::TN; ++j) acc[i][j] = mfma32(fb[kk & 1][j], fa[kk & 1][i], acc[i][j]);
+      for (int j = 0; j < C::TN; ++j) acc[i][j] = mfma32(fb[kk % SETS][j], fa[kk % SETS][i], acc[i][j]);
   };
   // the order of 16 k's: reads of the next fragments and copies spread over the products
   auto order = [&](auto copies) {      // at most so many of those
@@ -229,9 +236,9 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
     }
     KNAP_SCHED_FENCE();
   };
-  // the copies of a stage go out in shares, the first once its buffer is free: behind the barrier in front of the last 16 k's of the stage that
-  // lies there; the others with the first 16 k's (of 64: and the second) of the next one
-  constexpr int SHARES = SUB == 2 ? 2 : 3;
+  // the copies of a stage go out in shares beside three steps' products, from the step in front of which its buffer becomes free: behind the barrier
+  // of the stage that lies there
+  constexpr int SHARES = 3, MEET = SUB - C::AHEAD;      // MEET: the step that the waves meet in front of
   auto share = [](int i) { return L * i / SHARES; };
   prepare();
   copy(buffer_of<0>(lds), 0, L);
@@ -240,9 +247,18 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
   copy(buffer_of<1>(lds), 0, L);
   advance();
   prepare();
+  if constexpr (C::BUFFERS == 4) {
+    copy(buffer_of<2>(lds), 0, L);
+    advance();
+    prepare();
+    copy(buffer_of<3>(lds), 0, L);
+    advance();
+    prepare();
+  }
   wait_vm<(C::BUFFERS - 1) * L>();
   lds_barrier();
-  read(buffer_of<0>(lds), 0);
+#pragma unroll
+  for (int kk = 0; kk < C::AHEAD; ++kk) read(buffer_of<0>(lds), kk);
   KNAP_SCHED_FENCE();
   // `behind`: there is a stage in front of this one, whose buffer is being filled
   auto stage = [&](auto which, auto behind) {
@@ -250,31 +266,39 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
     constexpr bool FILL = decltype(behind)::value;
 #pragma unroll
     for (int kk = 0; kk < SUB; ++kk) {
-      if (kk < SUB - 1) {
-        if (FILL && kk + 1 < SHARES) copy(buffer_of<(B + N - 1) % N>(lds), share(kk + 1), share(kk + 2));
-        read(buffer_of<B>(lds), kk + 1);
-        multiply(kk);
-      } else {
+      if (kk == MEET) {
         wait_vm<(N - 2) * L>();
         lds_barrier();
         KNAP_SCHED_FENCE();
-        copy(buffer_of<B>(lds), 0, share(1));
-        read(buffer_of<(B + 1) % N>(lds), 0);
-        multiply(kk);
       }
+      const int i = kk >= MEET ? kk - MEET : kk + C::AHEAD;      // the share that goes out here
+      const bool fill = i < SHARES && (kk >= MEET || FILL);
+      if (fill) {
+        if (kk >= MEET) copy(buffer_of<B>(lds), share(i), share(i + 1));
+        else copy(buffer_of<(B + N - 1) % N>(lds), share(i), share(i + 1));
+      }
+      if (kk < MEET) read(buffer_of<B>(lds), kk + C::AHEAD);
+      else read(buffer_of<(B + 1) % N>(lds), kk - MEET);
+      multiply(kk);
       order(std::integral_constant<int, (L + SHARES - 1) / SHARES>{});
-      if (kk == SUB - 1) hold();
-      if (FILL && kk + 2 == SHARES) {      // behind the last share: the descriptors of the next stage, beside the products that copy nothing
+      if (fill && i == SHARES - 1) {      // the descriptors of the next stage, beside the products that copy nothing
         advance();
         prepare();
       }
     }
+    hold();
   };
   int s = s0;
   stage(std::integral_constant<int, 0>{}, std::false_type{});
   while (true) {
     if (++s >= s1) break;
     stage(std::integral_constant<int, 1>{}, std::true_type{});
+    if constexpr (C::BUFFERS == 4) {
+      if (++s >= s1) break;
+      stage(std::integral_constant<int, 2>{}, std::true_type{});
+      if (++s >= s1) break;
+      stage(std::integral_constant<int, 3>{}, std::true_type{});
+    }
     if (++s >= s1) break;
     stage(std::integral_constant<int, 0>{}, std::true_type{});
   }

@@ -125,7 +125,7 @@ struct ResidualArgs {
   int norm, post_norm;
   bool w_bf16, mod_bf16;
 };
-constexpr int kResidualMaxGroups = 512;      // workgroups of a backward
+constexpr int kResidualMaxGroups = 768;      // workgroups of a backward
 hipError_t launch_residual_norm_fwd(const ResidualArgs& a, bool x_bf16, bool b_bf16, bool wide, int cus, hipStream_t stream);
 hipError_t launch_residual_norm_bwd(const ResidualArgs& a, bool x_bf16, bool b_bf16, bool wide, int cus, hipStream_t stream);
 
@@ -171,7 +171,10 @@ struct FfnArgs {
   float* partial;
 };
 size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward);
-constexpr int kFfnFew = 32;      // tokens up to which the forward takes the form of knap_ffn_few.hip
+// Whether a forward takes the form of knap_ffn_few.hip: up to 16 tokens, and up to 32 of smaller weights, whose tiles are too few for the card; larger
+// ones are the faster in tiles, which read the second 16 tokens less often (24 tokens, us, this form and tiles: 768 x 2048 12 and 21, 2048 x 5504 30 and 33,
+// 4096 x 10944 72 and 67).
+inline bool ffn_few(int64_t tokens, int64_t width, int64_t hidden) { return tokens <= 16 || (tokens <= 32 && width * hidden <= 16000000); }
 hipError_t launch_ffn_few(const FfnArgs& a, hipStream_t stream);
 hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t stream);
 hipError_t launch_ffn_bwd(const FfnArgs& a, hipStream_t stream);

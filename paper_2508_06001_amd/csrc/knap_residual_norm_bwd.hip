@@ -253,7 +253,9 @@ template <class TX, class TB, bool WIDE>
 static hipError_t launch_bwd_t(ResidualArgs a, int cus, hipStream_t stream) {
   return residual_form<WIDE>(a.width, [&](auto cfg) {
     using C = decltype(cfg);
-    a.chunk = residual_chunk(a.rows, std::min(2 * cus, kResidualMaxGroups), C::PASS);
+    // workgroups a CU: more leave more sums to add up (31464 rows of 1536 in 16 bits, two and three a CU: 132 and 140 us), which rows of 32 bits
+    // make up for (24576 of 2048: 225 and 209; 8191 of 1003: 56 and 50)
+    a.chunk = residual_chunk(a.rows, std::min((sizeof(TX) == 4 ? 3 : 2) * cus, kResidualMaxGroups), C::PASS);
     const int groups = (int)((a.rows + a.chunk - 1) / a.chunk);
     if (groups > 0) {
       hipLaunchKernelGGL((a.post_norm == KNAP_NORM_NONE ? residual_norm_bwd_kernel<C, TX, TB, false> : residual_norm_bwd_kernel<C, TX, TB, true>), dim3(groups), dim3(C::THREADS), 0, stream, a);
