@@ -223,7 +223,7 @@ __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C
   int m0, n0;
   const int q = locate<C, PAIRED>(g, tile, m0, n0);
   const GemmProblem& p = g.p[q];
-  const int stages = (p.K + C::KS - 1) / C::KS * p.segments;
+  const int stages = (p.K + kGemmK - 1) / kGemmK * p.segments;
   f32x16 acc[C::TM][C::TN];
   gemm_tile<C, A_ROWK, B_ROWK, PAIRED, TWO>(p, m0, n0, (int)((int64_t)stages * part / parts), (int)((int64_t)stages * (part + 1) / parts), GemmBuffers{b0, b1, b2, b3}, acc);
   if (parts > 1) {
@@ -308,7 +308,7 @@ float plan(GemmLaunch& g, bool paired) {
     p.tiles_m = (p.M + C::BM - 1) / C::BM;
     p.tiles_n = (p.N + bn - 1) / bn;
     tiles += p.tiles_m * p.tiles_n;
-    stages = std::min(stages, (p.K + C::KS - 1) / C::KS * p.segments);
+    stages = std::min(stages, (p.K + kGemmK - 1) / kGemmK * p.segments);
   }
   constexpr FormCost f = form_cost<C>();
   const int rest = tiles % f.places;
@@ -425,11 +425,11 @@ size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward) {
   if (!backward && ffn_few(tokens, width, hidden)) return 0;
   if (!backward) return std::max(bytes_of<kActForward>(up_products(a)), bytes_of<kStore>(down_product(a)));
   size_t most = std::max(bytes_of<kActBackward>(hidden_gradients(a)), bytes_of<kStore>(input_gradient(a)));
-  for (int wanted = 1; wanted < 8; ++wanted) {      // whichever gradients of weights a call asks for
-    static __bf16 none;
-    a.dw_gate = wanted & 1 ? &none : nullptr;
-    a.dw_up = wanted & 2 ? &none : nullptr;
-    a.dw_down = wanted & 4 ? &none : nullptr;
+  __bf16* const some = reinterpret_cast<__bf16*>(16);      // asked for, not looked at
+  for (int wanted = 1; wanted < 8; ++wanted) {             // whichever gradients of weights a call wants
+    a.dw_gate = wanted & 1 ? some : nullptr;
+    a.dw_up = wanted & 2 ? some : nullptr;
+    a.dw_down = wanted & 4 ? some : nullptr;
     most = std::max(most, bytes_of<kStore>(weight_gradients(a)));
   }
   return most;

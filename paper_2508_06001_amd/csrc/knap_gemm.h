@@ -2,12 +2,17 @@
 // An operand either lies with k along its rows (ROWK: element (r, k) at r ld + k) or with k down its rows (element (r, k) at k ld + r), so that
 // all products of the block take their tensors as they are: nothing is transposed in memory.
 //
-// A workgroup of WM x WN waves forms a tile of BM x BN, a wave TM x TN blocks of 32 x 32.  Stages of 32 k's go through a ring of four buffers in LDS,
-// filled past the registers by asynchronous copies three stages ahead: [rows][32] for ROWK, read 16 bytes a lane, and [32][128] for the other, read
-// transposed, both in layouts that neither way of reading meets a bank twice in.  A wave reads the fragments of the next 16 k's while it multiplies
-// these; in the middle of a stage it meets the others, whose reads of the stage before are behind them (so that its buffer is free) and whose copies of
-// the next one have arrived, and goes on with products of fragments that it has: the matrix cores wait at no barrier for memory.  The buffers are
-// arrays of their own, and the ring is unrolled: of one array the compiler would wait for every copy under way in front of each transposed read.
+// A workgroup of WM x WN waves forms a tile of BM x BN, a wave TM x TN blocks of 32 x 32.  Stages of 64 k's go through a ring of two or four buffers in
+// LDS, filled past the registers by asynchronous copies: [rows][64] for ROWK, whose rows are whole lines of 128 bytes, read 16 bytes a lane, and [64][128]
+// for the other, read transposed, both in layouts that neither way of reading meets a bank twice in.  A wave reads fragments one or two steps of 16 k's
+// ahead of their products.  Once a stage's last fragments are asked for, it meets the others: their reads of this buffer are behind them, so that it is
+// free for the stage BUFFERS further on, and their copies of the next stage have arrived; and goes on with products of fragments that it has.  The matrix
+// cores wait at no barrier for memory.  Waves of 128 x 128 read half as much from LDS as those of 128 x 64 would, two of which share a SIMD (8192^3, us: 823
+// and 892, before what the epilogue saves).  The buffers are arrays of their own, and the ring is unrolled: of one array the compiler would wait for every
+// copy under way in front of each transposed read (8192^3 with k down the rows of b: 1607 us so, 800 as it is).
+//
+// Bound by the matrix cores at the clock that the card holds under them: 32768 x 1536 x 4096 takes 310 us (1.33 PFLOP/s; 64 steps of 2.3 to 2.6 thousand
+// clocks, of which 2048 are products, at 1.7 GHz).
 //
 // Rows and k's that a tensor does not have are zeros: the descriptors end behind its last row; k's behind a row's end, which memory
 // holds something else at, are asked for behind the descriptor.  Columns behind the last one of a tensor with k down its rows are whatever the next row
@@ -21,16 +26,17 @@
 
 namespace knap {
 
+constexpr int kGemmK = 64;                // k's of a stage
 constexpr int kGemmNowhere = 0x7fffffe0;  // a byte offset behind every descriptor
 
 template <int BM_, int BN_, int WM_, int WN_, int BUFFERS_, int AHEAD_>
 struct GemmCfg {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
-  static constexpr int KS = 64, BUFFERS = BUFFERS_;       // k's of a stage, buffers of the ring (2 or 4)
+  static constexpr int BUFFERS = BUFFERS_;                // of the ring, 2 or 4
   static constexpr int AHEAD = AHEAD_;                    // steps of 16 k's that fragments are read ahead of their products (1 or 2)
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-  static constexpr int STAGE = (BM + BN) * KS;      // elements
+  static constexpr int STAGE = (BM + BN) * kGemmK;      // elements
   static constexpr int LDS_BYTES = BUFFERS * STAGE * 2;
 };
 struct GemmBuffers { __bf16 *b0, *b1, *b2, *b3; };
@@ -42,25 +48,23 @@ __device__ __forceinline__ __bf16* buffer_of(const GemmBuffers& s) {
   else return s.b3;
 }
 
-// Copies of R rows (columns) of an operand for one stage of KS k's: instruction i of a wave fills 1 KB.
-// ROWK: whole rows of 64 or 128 bytes.  Unit c (16 bytes) of row r lies at c ^ ((r / 4) % 4) or c ^ ((r / 2) % 8): 16 rows put one unit in 16 places
-// of a 256-byte line.  else: 4 rows of 256 bytes in one of the R / 128 blocks of [KS][128], a Tile<128>.
-template <int R, bool ROWK, int WAVES, int KS>
+// Copies of R rows (columns) of an operand for one stage: instruction i of a wave fills 1 KB.
+// ROWK: 8 rows of 128 bytes.  Unit c (16 bytes) of row r lies at c ^ ((r / 2) % 8): 16 rows put one unit in 16 places of a 256-byte line.
+// else: 4 rows of 256 bytes in one of the R / 128 blocks of [64][128], a Tile<128>.
+template <int R, bool ROWK, int WAVES>
 struct OperandLoader {
-  static constexpr int UNITS = KS / 8, ROWS = 64 / UNITS;      // units of a row, rows of an instruction (ROWK)
-  static constexpr int COUNT = R / ROWS / WAVES;
-  static_assert(R % (ROWS * WAVES) == 0 && (ROWK || R % 128 == 0), "whole instructions for every wave");
-  // the row (of the R, or of the KS k's) and the 16-byte unit within it that this lane brings in instruction i
+  static constexpr int COUNT = R / 8 / WAVES;
+  static_assert(R % (8 * WAVES) == 0 && (ROWK || R % 128 == 0), "whole instructions for every wave");
+  // the row (of the R, or of the 64 k's) and the 16-byte unit within it that this lane brings in instruction i
   static __device__ __forceinline__ int row(int i, int wave, int lane) {
     const int q = i * WAVES + wave;
-    return ROWK ? ROWS * q + lane / UNITS : 4 * (q & (KS / 4 - 1)) + (lane >> 4);
+    return ROWK ? 8 * q + (lane >> 3) : 4 * (q & 15) + (lane >> 4);
   }
   static __device__ __forceinline__ int unit(int i, int wave, int lane) {
     const int r = row(i, wave, lane);
-    if constexpr (ROWK) return KS == 32 ? (lane & 3) ^ ((r >> 2) & 3) : (lane & 7) ^ ((r >> 1) & 7);
-    else return (lane & 15) ^ (4 * (r & 3) + ((r >> 2) & 3));
+    return ROWK ? (lane & 7) ^ ((r >> 1) & 7) : (lane & 15) ^ (4 * (r & 3) + ((r >> 2) & 3));
   }
-  static __device__ __forceinline__ int block(int i, int wave) { return ROWK ? 0 : (i * WAVES + wave) / (KS / 4); }
+  static __device__ __forceinline__ int block(int i, int wave) { return ROWK ? 0 : (i * WAVES + wave) >> 4; }
   // LDS element that the instruction starts at
   static __device__ __forceinline__ int place(int i, int wave) { return (i * WAVES + wave) * 512; }
 };
@@ -70,12 +74,11 @@ __device__ __forceinline__ void copy_1k(__bf16* to, __amdgpu_buffer_rsrc_t r, in
 }
 
 // Reads of MFMA operands: k's 16 kk + 8 (lane / 32) + 0..7 of row 32 block + lane % 32.
-template <bool ROWK, int KS>
+template <bool ROWK>
 struct FragmentReader {
   int base;      // bytes
   __device__ __forceinline__ void init(int lane) {
-    if constexpr (ROWK && KS == 32) base = (lane & 31) * 64 + ((lane >> 5) ^ ((lane >> 2) & 3)) * 16;
-    else if constexpr (ROWK) base = (lane & 31) * 128 + ((lane >> 5) ^ ((lane >> 1) & 7)) * 16;
+    if constexpr (ROWK) base = 2 * Tile<64>::off(lane & 31, 8 * (lane >> 5));
     else {
       const int i = lane & 15;
       base = 2 * Tile<128>::off(8 * (lane >> 5) + (i >> 2), ((lane >> 4) & 1) * 16 + 4 * (i & 3));
@@ -83,9 +86,9 @@ struct FragmentReader {
   }
   __device__ __forceinline__ bf16x8 get(const __bf16* tile, int block, int kk) const {
     const char* p = reinterpret_cast<const char*>(tile);
-    if constexpr (ROWK) return *reinterpret_cast<const bf16x8*>(p + block * 64 * KS + (base ^ (32 * kk)));
+    if constexpr (ROWK) return *reinterpret_cast<const bf16x8*>(p + block * 4096 + (base ^ (32 * kk)));
     else {      // four rows further down the swizzle flips the unit's lowest bit
-      const char* q = p + (block >> 2) * 256 * KS + kk * 4096;
+      const char* q = p + (block >> 2) * 16384 + kk * 4096;
       return join(lds_read_tr(reinterpret_cast<const __bf16*>(q + (base ^ (64 * (block & 3))))),
                   lds_read_tr(reinterpret_cast<const __bf16*>(q + 1024 + (base ^ (64 * (block & 3) + 16)))));
     }
@@ -93,27 +96,27 @@ struct FragmentReader {
 };
 
 // What the copies of an operand take, stage after stage: the descriptor of this one's k's.
-template <bool ROWK, int KS>
+template <bool ROWK>
 struct OperandStream {
   uint64_t base, step;      // of the stage's first k; bytes to the next
-  uint32_t bytes;           // of the descriptor where all k's are there
+  uint32_t bytes;           // of the descriptor, but for those that the number of k's decides
   uint32_t ld2;             // bytes of a row
   // rows [first, first + tile) of `limit`, from k0 on
   __device__ __forceinline__ void aim(const __bf16* p, int64_t ld, int first, int limit, int tile, int k0) {
     ld2 = (uint32_t)ld * 2u;
     if constexpr (ROWK) {
       base = reinterpret_cast<uint64_t>(p + (int64_t)first * ld + k0);
-      step = 2 * KS;
+      step = 2 * kGemmK;
       bytes = (uint32_t)(min(tile, limit - first) - 1) * ld2;      // up to the last row; its k's are added below
     } else {
       base = reinterpret_cast<uint64_t>(p + (int64_t)k0 * ld + first);
-      step = (uint64_t)ld2 * KS;
+      step = (uint64_t)ld2 * kGemmK;
       bytes = (uint32_t)(limit - first) * 2u;                      // of the last row of the stage; the others are added below
     }
   }
   // `left` k's from here on, none where that is 0 or less
   __device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(int left) const {
-    const uint32_t n = (uint32_t)min(left, KS);
+    const uint32_t n = (uint32_t)min(left, kGemmK);
     const uint32_t all = ROWK ? bytes + 2 * n : (n - 1) * ld2 + bytes;
     return make_rsrc(reinterpret_cast<const void*>(base), left > 0 ? all : 0u);
   }
@@ -123,12 +126,12 @@ struct OperandStream {
 // PAIRED: b of even and of odd blocks of 32 columns are two matrices; TWO: there are two segments.
 template <class C, bool A_ROWK, bool B_ROWK, bool PAIRED, bool TWO>
 __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, int s0, int s1, const GemmBuffers& lds, f32x16 (&acc)[C::TM][C::TN]) {
-  using LA = OperandLoader<C::BM, A_ROWK, C::WAVES, C::KS>;
-  using LB = OperandLoader<C::BN, B_ROWK, C::WAVES, C::KS>;
-  constexpr int L = LA::COUNT + LB::COUNT, SUB = C::KS / 16;      // copies of a stage, its steps of 16 k's
+  using LA = OperandLoader<C::BM, A_ROWK, C::WAVES>;
+  using LB = OperandLoader<C::BN, B_ROWK, C::WAVES>;
+  constexpr int L = LA::COUNT + LB::COUNT, SUB = kGemmK / 16;      // copies of a stage, its steps of 16 k's
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
-  const int per = (p.K + C::KS - 1) / C::KS;      // stages of a segment
+  const int per = (p.K + kGemmK - 1) / kGemmK;      // stages of a segment
 #pragma unroll
   for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -147,8 +150,8 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
     off_b[i] = r * (int)p.ldb * 2 + LB::block(i, wave) * 256 + LB::unit(i, wave, lane) * 16;
   }
   // the stage that is copied next
-  OperandStream<A_ROWK, C::KS> sa;
-  OperandStream<B_ROWK, C::KS> sb, sb2;
+  OperandStream<A_ROWK> sa;
+  OperandStream<B_ROWK> sb, sb2;
   int at = s0, left;
   auto enter = [&](int seg, int k0) {
     sa.aim(p.a[seg], p.lda, m0, p.M, C::BM, k0);
@@ -157,13 +160,13 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
     left = p.K - k0;
   };
   const int seg = TWO && s0 >= per ? 1 : 0;
-  enter(seg, (s0 - seg * per) * C::KS);
+  enter(seg, (s0 - seg * per) * kGemmK);
   auto advance = [&]() {
     ++at;
     sa.base += sa.step;
     sb.base += sb.step;
     if constexpr (PAIRED) sb2.base += sb2.step;
-    left -= C::KS;
+    left -= kGemmK;
     if constexpr (TWO) {
       if (at == per) enter(1, 0);
     }
@@ -191,19 +194,19 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
         int o = off_b[i];
         if constexpr (B_ROWK) o = 8 * LB::unit(i, wave, lane) >= k ? kGemmNowhere : o;
         const bool odd = PAIRED && (LB::row(i, wave, 0) & 32);
-        copy_1k(buffer + C::BM * C::KS + LB::place(i, wave), odd ? db2 : db, o);
+        copy_1k(buffer + C::BM * kGemmK + LB::place(i, wave), odd ? db2 : db, o);
       }
     }
   };
-  FragmentReader<A_ROWK, C::KS> ra;
-  FragmentReader<B_ROWK, C::KS> rb;
+  FragmentReader<A_ROWK> ra;
+  FragmentReader<B_ROWK> rb;
   ra.init(lane);
   rb.init(lane);
   constexpr int SETS = 2 * C::AHEAD;
   bf16x8 fa[SETS][C::TM], fb[SETS][C::TN];
   auto read = [&](const __bf16* buffer, int kk) {
 #pragma unroll
-    for (int j = 0; j < C::TN; ++j) fb[kk % SETS][j] = rb.get(buffer + C::BM * C::KS, wn * C::TN + j, kk);
+    for (int j = 0; j < C::TN; ++j) fb[kk % SETS][j] = rb.get(buffer + C::BM * kGemmK, wn * C::TN + j, kk);
 #pragma unroll
     for (int i = 0; i < C::TM; ++i) fa[kk % SETS][i] = ra.get(buffer, wm * C::TM + i, kk);
   };

@@ -240,7 +240,7 @@ __global__ __launch_bounds__(COLS * SLICES) void residual_norm_sum_kernel(Residu
 static hipError_t launch_sums(const ResidualArgs& a, int groups, hipStream_t stream) {
   // columns of the three sums of a sequence, or of the two over all of them, that anyone wants
   const bool each = a.dshift || a.dscale || a.dgate, whole = a.dweight || a.dpost_weight;
-  if (!each && !whole) return hipSuccess;
+  if ((!each || a.n_seq == 0) && !whole) return hipSuccess;
   const int cols = 3 * a.width;
   const dim3 grid((cols + 63) / 64, a.n_seq + (whole ? 1 : 0));
   // a sequence's rows of sums are `groups` / n_seq on the average: threads side by side accordingly

@@ -252,6 +252,26 @@ def test_in_place_no_rows_and_a_gate_for_all():
 
 
 @pytest.mark.gpu
+def test_a_bag_of_no_sequences():
+    """Rows, all of them padding: nothing is written but the sums over all rows, which are zeros; sums of no sequence need no launch."""
+    import torch
+    import paper_2508_06001_amd as K
+    cu = torch.zeros((1,), dtype=torch.int32, device="cuda")
+    x, y = torch.ones((5, 64), device="cuda"), torch.full((5, 64), 7.0, device="cuda")
+    grad = torch.full((64,), 7.0, device="cuda")
+    K.knap_residual_norm_fwd(x, None, None, y, cu_seqlens=cu)
+    at = {n: t.data_ptr() for n, t in (("x", x), ("dy", y), ("dx", y), ("cu", cu), ("stats", y), ("g", grad))}
+    args = dict(BWD, x=at["x"], xt=1, bt=1, xs=64, rows=5, f=0, fs=0, cu=at["cu"], n=0, gate=0, scale=0, wp=0, w=0, post=0, norm=2, stats=at["stats"], dxo=0,
+                dy=at["x"], dx=at["dx"], df=0, dgate=0, dscale=at["g"], dshift=0, dw=0, dwp=0, ws=0, nbytes=0)
+    assert K.lib.knap_residual_norm_bwd(*args.values(), 0) == K.KNAP_OK
+    torch.cuda.synchronize()
+    assert bool((y == 7.0).all()) and bool((grad == 7.0).all())
+    assert K.lib.knap_residual_norm_bwd(*dict(args, dscale=0, dw=at["g"]).values(), 0) == K.KNAP_OK
+    torch.cuda.synchronize()
+    assert bool((y == 7.0).all()) and not bool(grad.any())
+
+
+@pytest.mark.gpu
 def test_a_bad_row_stays_in_its_row():
     import torch
     for width, post in ((128, R.NONE), (1536, R.RMS), (1001, R.LAYER)):
