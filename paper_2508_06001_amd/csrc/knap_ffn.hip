@@ -39,9 +39,10 @@ __device__ __forceinline__ void hidden_gradient(float dh, float a, float b, bool
 // The epilogue of one block, from its registers (of tiles whose parts were added up)
 template <class C, int EP>
 __device__ __forceinline__ void finish_block(const GemmLaunch& g, const GemmProblem& p, int m0, int n0, int i, int j, const f32x16& x, const f32x16& x2) {
+  const int columns = min(p.N, n0 + p.step);
   if constexpr (EP == kStore) {
     const BlockPlace<C> at(m0, n0, i, j);
-    const TileRows c(p.c, p.ldc, p.M, p.N, m0, C::BM);
+    const TileRows c(p.c, p.ldc, p.M, columns, m0, C::BM);
 #pragma unroll
     for (int u = 0; u < 2; ++u) c.store(at.m, at.n + 16 * u, pack_unit(x, u));
   } else if constexpr (EP == kActForward) {      // x, x2: a and b of block j / 2 of the tile's hidden columns
@@ -55,11 +56,11 @@ __device__ __forceinline__ void finish_block(const GemmLaunch& g, const GemmProb
       activation(x[r], g.gelu, s, du);
       h[r] = x[r] * s * x2[r];
     }
-    const TileRows c(g.h, p.N, p.M, p.N, m0, C::BM);
+    const TileRows c(g.h, p.N, p.M, columns, m0, C::BM);
 #pragma unroll
     for (int u = 0; u < 2; ++u) c.store(m, n + 16 * u, pack_unit(h, u));
     if (g.gate) {
-      const TileRows ga(g.gate, p.N, p.M, p.N, m0, C::BM), up(g.up, p.N, p.M, p.N, m0, C::BM);
+      const TileRows ga(g.gate, p.N, p.M, columns, m0, C::BM), up(g.up, p.N, p.M, columns, m0, C::BM);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         ga.store(m, n + 16 * u, pack_unit(x, u));
@@ -68,8 +69,8 @@ __device__ __forceinline__ void finish_block(const GemmLaunch& g, const GemmProb
     }
   } else {
     const BlockPlace<C> at(m0, n0, i, j);
-    const TileRows gi(g.gate_in, p.N, p.M, p.N, m0, C::BM), ui(g.up_in, p.N, p.M, p.N, m0, C::BM);
-    const TileRows go(g.gate, p.N, p.M, p.N, m0, C::BM), uo(g.up, p.N, p.M, p.N, m0, C::BM);
+    const TileRows gi(g.gate_in, p.N, p.M, columns, m0, C::BM), ui(g.up_in, p.N, p.M, columns, m0, C::BM);
+    const TileRows go(g.gate, p.N, p.M, columns, m0, C::BM), uo(g.up, p.N, p.M, columns, m0, C::BM);
     f32x16 da, db;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -97,7 +98,7 @@ constexpr int kPast = 2;      // the non-temporal bit of a buffer access
 template <class C, int EP>
 __device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProblem& p, int m0, int n0, const f32x16 (&acc)[C::TM][C::TN],
                                             const GemmBuffers& lds) {
-  static_assert(C::WAVES == 4 && C::STAGE >= 4 * 32 * 32 * C::TN, "a wave has half of a buffer");
+  static_assert((C::WAVES == 4 || C::WAVES <= 2) && C::STAGE >= C::WAVES * 32 * 32 * C::TN, "a wave has half of a buffer, one of two a whole one");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WN, wn = wave % C::WN;
   // (of the LDS address space, which a choice between two arrays otherwise loses)
@@ -122,9 +123,10 @@ __device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProbl
   auto put = [&](const TileRows& to, int at, const float (&v)[8]) {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, pack8(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7])), to.r, at, 0, kPast);
   };
-  const TileRows out0(EP == kStore ? p.c : g.gate, EP == kStore ? p.ldc : p.N, g.gate || EP == kStore ? p.M : 0, p.N, m0, C::BM);
-  const TileRows out1(EP == kStore ? nullptr : g.up, p.N, EP != kStore && g.up ? p.M : 0, p.N, m0, C::BM);
-  const TileRows in0(EP == kActForward ? g.h : g.gate_in, p.N, p.M, p.N, m0, C::BM), in1(g.up_in, p.N, p.M, p.N, m0, C::BM);
+  const int columns = min(p.N, n0 + p.step);
+  const TileRows out0(EP == kStore ? p.c : g.gate, EP == kStore ? p.ldc : p.N, g.gate || EP == kStore ? p.M : 0, columns, m0, C::BM);
+  const TileRows out1(EP == kStore ? nullptr : g.up, p.N, EP != kStore && g.up ? p.M : 0, columns, m0, C::BM);
+  const TileRows in0(EP == kActForward ? g.h : g.gate_in, p.N, p.M, columns, m0, C::BM), in1(g.up_in, p.N, p.M, columns, m0, C::BM);
   constexpr int TURNS = 32 * OUT_UNITS / 64;
   // a and b of 32 rows, asked for while the 32 before them are worked on
   constexpr bool INPUTS = EP == kActBackward;
@@ -198,19 +200,20 @@ __device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProbl
 }
 
 // which product a tile is of, and where it lies
-template <class C, bool PAIRED>
+template <class C>
 __device__ __forceinline__ int locate(const GemmLaunch& g, int tile, int& m0, int& n0) {
   const int q = tile >= g.first[1] ? (tile >= g.first[2] ? 2 : 1) : 0;
   int tm, tn;
   tile_place(tile - g.first[q], g.p[q].tiles_m, g.p[q].tiles_n, tm, tn);
   m0 = tm * C::BM;
-  n0 = tn * (PAIRED ? C::BN / 2 : C::BN);
+  n0 = tn * g.p[q].step;
   return q;
 }
 
 template <class C, bool A_ROWK, bool B_ROWK, int EP>
-__global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C::WAVES / 2) void gemm_kernel(GemmLaunch g) {
-  __shared__ __align__(1024) __bf16 b0[C::STAGE], b1[C::STAGE], b2[C::BUFFERS == 4 ? C::STAGE : 8], b3[C::BUFFERS == 4 ? C::STAGE : 8];
+__global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 || C::WAVES == 1 ? (C::WAVES + 3) / 4 : C::WAVES / 2) void gemm_kernel(GemmLaunch g) {
+  __shared__ __align__(1024) __bf16 b0[C::STAGE], b1[C::STAGE], b2[C::BUFFERS > 2 ? C::STAGE : 8], b3[C::BUFFERS > 3 ? C::STAGE : 8],
+      b4[C::BUFFERS > 4 ? C::STAGE : 8], b5[C::BUFFERS > 5 ? C::STAGE : 8];
   constexpr bool PAIRED = EP == kActForward, TWO = EP == kStore && A_ROWK && !B_ROWK;      // dx alone adds up two products
   int tile, part = 0, parts = 1;
   if ((int)blockIdx.x < g.whole) tile = xcd_order(blockIdx.x, g.whole);
@@ -221,11 +224,11 @@ __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C
     parts = g.splits;
   }
   int m0, n0;
-  const int q = locate<C, PAIRED>(g, tile, m0, n0);
+  const int q = locate<C>(g, tile, m0, n0);
   const GemmProblem& p = g.p[q];
   const int stages = (p.K + kGemmK - 1) / kGemmK * p.segments;
   f32x16 acc[C::TM][C::TN];
-  gemm_tile<C, A_ROWK, B_ROWK, PAIRED, TWO>(p, m0, n0, (int)((int64_t)stages * part / parts), (int)((int64_t)stages * (part + 1) / parts), GemmBuffers{b0, b1, b2, b3}, acc);
+  gemm_tile<C, A_ROWK, B_ROWK, PAIRED, TWO>(p, m0, n0, (int)((int64_t)stages * part / parts), (int)((int64_t)stages * (part + 1) / parts), GemmBuffers{b0, b1, b2, b3, b4, b5}, acc);
   if (parts > 1) {
     f32x4* to = reinterpret_cast<f32x4*>(g.partial) + (size_t)((int)blockIdx.x - g.whole) * (C::BM * C::BN / 4) + threadIdx.x;
 #pragma unroll
@@ -237,7 +240,7 @@ __global__ __launch_bounds__(C::THREADS, C::LDS_BYTES > 81920 ? C::WAVES / 4 : C
           to[((i * C::TN + j) * 4 + k) * C::THREADS] = f32x4{acc[i][j][4 * k], acc[i][j][4 * k + 1], acc[i][j][4 * k + 2], acc[i][j][4 * k + 3]};
     return;
   }
-  finish_tile<C, EP>(g, p, m0, n0, acc, GemmBuffers{b0, b1, b2, b3});
+  finish_tile<C, EP>(g, p, m0, n0, acc, GemmBuffers{b0, b1, b2, b3, b4, b5});
 }
 
 // Adds up the parts of a tile's block (blockIdx.y; of a pair of blocks) in their order and finishes it
@@ -246,7 +249,7 @@ __global__ __launch_bounds__(C::THREADS) void gemm_join_kernel(GemmLaunch g) {
   constexpr bool PAIRED = EP == kActForward;
   constexpr int STEP = PAIRED ? 2 : 1;
   int m0, n0;
-  const int q = locate<C, PAIRED>(g, g.whole + (int)blockIdx.x, m0, n0);
+  const int q = locate<C>(g, g.whole + (int)blockIdx.x, m0, n0);
   const int i = (int)blockIdx.y / (C::TN / STEP), j = (int)blockIdx.y % (C::TN / STEP) * STEP;
   f32x16 x[STEP];
   for (int e = 0; e < STEP; ++e) x[e] = zero16();
@@ -279,6 +282,14 @@ using Large = GemmCfg<256, 256, 2, 2, 2, EP == kActForward ? 1 : 2>;
 using Small = GemmCfg<128, 128, 2, 2, 2, 1>;
 using Deep = GemmCfg<128, 128, 2, 2, 4, 1>;
 
+// Forms of a row of tiles, for a forward of up to 32 and of up to 64 tokens, bound by the weights' bytes: two workgroups a CU, rings so deep that both have 80 KB
+// on the way, and tiles of as many columns, up to 64, as spread them evenly over the CUs.  us of a forward on weights that are in no cache, these forms and
+// those above (where the weights lie in memory makes 3 % between two runs): 4096 x 10944, 24 tokens 70 and 79, 48 tokens 73 and 81; 4096 x 16384, 24 tokens 103
+// and 110, 48 tokens 104 and 112; 2048 x 5504, 32 tokens 34 and 38, 48 tokens 33 and 41; 768 x 2048, 48 tokens 20 and 23.  128 columns and one workgroup a CU:
+// 24 tokens 4096 x 10944 65 to 68, 4096 x 16384 108 to 112, 2048 x 5504 35; 48 tokens 71, 109, 38.
+using Few32 = GemmCfg<32, 64, 1, 1, 6, 1>;
+using Few64 = GemmCfg<64, 64, 2, 1, 5, 1>;
+
 // ---------------------------------------------------------------------------
 // Plans
 // ---------------------------------------------------------------------------
@@ -307,6 +318,7 @@ float plan(GemmLaunch& g, bool paired) {
     const int bn = paired ? C::BN / 2 : C::BN;
     p.tiles_m = (p.M + C::BM - 1) / C::BM;
     p.tiles_n = (p.N + bn - 1) / bn;
+    p.step = bn;
     tiles += p.tiles_m * p.tiles_n;
     stages = std::min(stages, (p.K + kGemmK - 1) / kGemmK * p.segments);
   }
@@ -328,13 +340,56 @@ float plan(GemmLaunch& g, bool paired) {
   return (float)(tiles / f.places) * (float)stages * (f.stage + f.more) + last;
 }
 
+// The same for one product of one row of tiles in a form for few tokens: how many columns a tile has, and how many parts it goes in.
+template <class C>
+void plan_few(GemmLaunch& g, bool paired) {
+  // us: a launch's start, a stage at least, a row of 128 bytes that a CU reads, a part that is written and read again
+  constexpr float kStart = 3.f, kStage = 0.35f, kRow = 0.0046f, kPart = 0.5f * C::BM * C::BN * 1e-6f;
+  static_assert(C::LDS_BYTES <= 81920, "two workgroups a CU");
+  constexpr int PLACES = 2;      // of a CU
+  GemmProblem& p = g.p[0];
+  const int mats = paired ? 2 : 1, stages = (p.K + kGemmK - 1) / kGemmK;
+  float best = 1e30f;
+  for (int step = 8; step <= C::BN / mats && step < p.N + 8; step += 8) {
+    const int tiles = (p.N + step - 1) / step;
+    const float row = kRow * (float)(mats * step + p.M);
+    for (int parts = 1; parts == 1 || (tiles * parts <= PLACES * kGemmCus && parts <= stages / 4); ++parts) {
+      const int each = (tiles * parts + kGemmCus - 1) / kGemmCus;      // workgroups of a CU
+      const float rounds = (float)((each + PLACES - 1) / PLACES);
+      float t = rounds * kStart + (float)stages / (float)parts * std::max(rounds * kStage, (float)each * row);
+      if (parts > 1) t += kJoin + kPart * (float)(tiles * parts);
+      if (t >= best) continue;
+      best = t;
+      p.step = step;
+      p.tiles_n = tiles;
+      g.splits = parts;
+    }
+  }
+  p.tiles_m = 1;
+  g.first[0] = 0;
+  g.first[1] = g.first[2] = INT32_MAX;
+  g.whole = g.splits > 1 ? 0 : p.tiles_n;
+  g.tail = p.tiles_n - g.whole;
+}
+
 template <class C>
 size_t parts_bytes(const GemmLaunch& g) { return (size_t)g.tail * g.splits * C::BM * C::BN * sizeof(float); }
 
-// calls f(form, launch) with the form of the least estimated time
-template <int EP, class F>
+// calls f(form, launch) with the form of the least estimated time.  ROWS: both operands have k along their rows, as in a forward
+template <int EP, bool ROWS, class F>
 auto with_form(const GemmLaunch& g, F f) {
   constexpr bool paired = EP == kActForward;
+  if constexpr (ROWS) {
+    GemmLaunch few = g;
+    if (g.p[0].M <= 32) {
+      plan_few<Few32>(few, paired);
+      return f(Few32{}, few);
+    }
+    if (g.p[0].M <= 64) {
+      plan_few<Few64>(few, paired);
+      return f(Few64{}, few);
+    }
+  }
   GemmLaunch large = g, small = g, deep = g;
   const float tl = plan<Large<EP>>(large, paired), ts = plan<Small>(small, paired), td = plan<Deep>(deep, paired);
   if (tl <= ts && tl <= td) return f(Large<EP>{}, large);
@@ -353,13 +408,13 @@ hipError_t launch_gemm(const GemmLaunch& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int EP>
+template <int EP, bool ROWS = false>
 size_t bytes_of(const GemmLaunch& g) {
-  return with_form<EP>(g, [](auto form, const GemmLaunch& planned) { return parts_bytes<decltype(form)>(planned); });
+  return with_form<EP, ROWS>(g, [](auto form, const GemmLaunch& planned) { return parts_bytes<decltype(form)>(planned); });
 }
 template <bool A_ROWK, bool B_ROWK, int EP>
 hipError_t run(const GemmLaunch& g, hipStream_t stream) {
-  return with_form<EP>(g, [&](auto form, const GemmLaunch& planned) { return launch_gemm<decltype(form), A_ROWK, B_ROWK, EP>(planned, stream); });
+  return with_form<EP, A_ROWK && B_ROWK>(g, [&](auto form, const GemmLaunch& planned) { return launch_gemm<decltype(form), A_ROWK, B_ROWK, EP>(planned, stream); });
 }
 
 static GemmProblem product(const __bf16* a, int64_t lda, const __bf16* b, int64_t ldb, __bf16* c, int64_t ldc, int M, int N, int K) {
@@ -423,7 +478,7 @@ size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward) {
   FfnArgs a{};
   a.tokens = (int)tokens; a.width = width; a.hidden = hidden;
   if (!backward && ffn_few(tokens, width, hidden)) return 0;
-  if (!backward) return std::max(bytes_of<kActForward>(up_products(a)), bytes_of<kStore>(down_product(a)));
+  if (!backward) return std::max(bytes_of<kActForward, true>(up_products(a)), bytes_of<kStore, true>(down_product(a)));
   size_t most = std::max(bytes_of<kActBackward>(hidden_gradients(a)), bytes_of<kStore>(input_gradient(a)));
   __bf16* const some = reinterpret_cast<__bf16*>(16);      // asked for, not looked at
   for (int wanted = 1; wanted < 8; ++wanted) {             // whichever gradients of weights a call wants

@@ -2,7 +2,7 @@
 // An operand either lies with k along its rows (ROWK: element (r, k) at r ld + k) or with k down its rows (element (r, k) at k ld + r), so that
 // all products of the block take their tensors as they are: nothing is transposed in memory.
 //
-// A workgroup of WM x WN waves forms a tile of BM x BN, a wave TM x TN blocks of 32 x 32.  Stages of 64 k's go through a ring of two or four buffers in
+// A workgroup of WM x WN waves forms a tile of BM x BN, a wave TM x TN blocks of 32 x 32.  Stages of 64 k's go through a ring of two to six buffers in
 // LDS, filled past the registers by asynchronous copies: [rows][64] for ROWK, whose rows are whole lines of 128 bytes, read 16 bytes a lane, and [64][128]
 // for the other, read transposed, both in layouts that neither way of reading meets a bank twice in.  A wave reads fragments one or two steps of 16 k's
 // ahead of their products.  Once a stage's last fragments are asked for, it meets the others: their reads of this buffer are behind them, so that it is
@@ -23,6 +23,7 @@
 #include "knap_kernels.h"
 
 #include <type_traits>
+#include <utility>
 
 namespace knap {
 
@@ -32,21 +33,27 @@ constexpr int kGemmNowhere = 0x7fffffe0;  // a byte offset behind every descript
 template <int BM_, int BN_, int WM_, int WN_, int BUFFERS_, int AHEAD_>
 struct GemmCfg {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
-  static constexpr int BUFFERS = BUFFERS_;                // of the ring, 2 or 4
+  static constexpr int BUFFERS = BUFFERS_;                // of the ring, 2 to 6
   static constexpr int AHEAD = AHEAD_;                    // steps of 16 k's that fragments are read ahead of their products (1 or 2)
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   static constexpr int STAGE = (BM + BN) * kGemmK;      // elements
   static constexpr int LDS_BYTES = BUFFERS * STAGE * 2;
 };
-struct GemmBuffers { __bf16 *b0, *b1, *b2, *b3; };
+struct GemmBuffers { __bf16 *b0, *b1, *b2, *b3, *b4, *b5; };
 template <int B>
 __device__ __forceinline__ __bf16* buffer_of(const GemmBuffers& s) {
   if constexpr (B == 0) return s.b0;
   else if constexpr (B == 1) return s.b1;
   else if constexpr (B == 2) return s.b2;
-  else return s.b3;
+  else if constexpr (B == 3) return s.b3;
+  else if constexpr (B == 4) return s.b4;
+  else return s.b5;
 }
+
+// f of 0, 1, ... as types, up to the first that returns false
+template <class F, int... B>
+__device__ __forceinline__ bool while_true(F& f, std::integer_sequence<int, B...>) { return (f(std::integral_constant<int, B>{}) && ...); }
 
 // Copies of R rows (columns) of an operand for one stage: instruction i of a wave fills 1 KB.
 // ROWK: 8 rows of 128 bytes.  Unit c (16 bytes) of row r lies at c ^ ((r / 2) % 8): 16 rows put one unit in 16 places of a 256-byte line.
@@ -149,14 +156,15 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
     if constexpr (PAIRED) r = (r >> 6) * 32 + (r & 31);      // which of the two matrices follows from the instruction
     off_b[i] = r * (int)p.ldb * 2 + LB::block(i, wave) * 256 + LB::unit(i, wave, lane) * 16;
   }
+  const int columns = min(p.N, n0 + p.step);      // the tile's end
   // the stage that is copied next
   OperandStream<A_ROWK> sa;
   OperandStream<B_ROWK> sb, sb2;
   int at = s0, left;
   auto enter = [&](int seg, int k0) {
     sa.aim(p.a[seg], p.lda, m0, p.M, C::BM, k0);
-    sb.aim(p.b[PAIRED ? 0 : seg], p.ldb, n0, p.N, PAIRED ? C::BN / 2 : C::BN, k0);
-    if constexpr (PAIRED) sb2.aim(p.b[1], p.ldb, n0, p.N, C::BN / 2, k0);
+    sb.aim(p.b[PAIRED ? 0 : seg], p.ldb, n0, columns, PAIRED ? C::BN / 2 : C::BN, k0);
+    if constexpr (PAIRED) sb2.aim(p.b[1], p.ldb, n0, columns, C::BN / 2, k0);
     left = p.K - k0;
   };
   const int seg = TWO && s0 >= per ? 1 : 0;
@@ -230,12 +238,12 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
   // the order of 16 k's: reads of the next fragments and copies spread over the products
   auto order = [&](auto copies) {      // at most so many of those
     constexpr int MF = C::TM * C::TN, READS = C::TM * (A_ROWK ? 1 : 2) + C::TN * (B_ROWK ? 1 : 2), EACH = (READS + MF - 1) / MF;
-    constexpr int N = decltype(copies)::value, EVERY = N ? MF / N : MF + 1;
+    constexpr int N = decltype(copies)::value, TOGETHER = (N + MF - 1) / MF, EVERY = N ? MF * TOGETHER / N : MF + 1;
 #pragma unroll
     for (int q = 0; q < MF; ++q) {
       KNAP_SGB(KNAP_SG_MFMA, 1);
       if (q * EACH < READS) KNAP_SGB(KNAP_SG_DS_READ, EACH);
-      if (N && q % EVERY == 0 && q / EVERY < N) KNAP_SGB(KNAP_SG_VMEM_READ, 1);
+      if (N && q % EVERY == 0 && q / EVERY < N) KNAP_SGB(KNAP_SG_VMEM_READ, TOGETHER);
     }
     KNAP_SCHED_FENCE();
   };
@@ -244,20 +252,14 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
   constexpr int SHARES = 3, MEET = SUB - C::AHEAD;      // MEET: the step that the waves meet in front of
   auto share = [](int i) { return L * i / SHARES; };
   prepare();
-  copy(buffer_of<0>(lds), 0, L);
-  advance();
-  prepare();
-  copy(buffer_of<1>(lds), 0, L);
-  advance();
-  prepare();
-  if constexpr (C::BUFFERS == 4) {
-    copy(buffer_of<2>(lds), 0, L);
+  auto begin = [&](auto which) {
+    copy(buffer_of<decltype(which)::value>(lds), 0, L);
     advance();
     prepare();
-    copy(buffer_of<3>(lds), 0, L);
-    advance();
-    prepare();
-  }
+    return true;
+  };
+  constexpr auto buffers = std::make_integer_sequence<int, C::BUFFERS>{};
+  while_true(begin, buffers);
   wait_vm<(C::BUFFERS - 1) * L>();
   lds_barrier();
 #pragma unroll
@@ -293,17 +295,12 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, int m0, int n0, 
   };
   int s = s0;
   stage(std::integral_constant<int, 0>{}, std::false_type{});
-  while (true) {
-    if (++s >= s1) break;
-    stage(std::integral_constant<int, 1>{}, std::true_type{});
-    if constexpr (C::BUFFERS == 4) {
-      if (++s >= s1) break;
-      stage(std::integral_constant<int, 2>{}, std::true_type{});
-      if (++s >= s1) break;
-      stage(std::integral_constant<int, 3>{}, std::true_type{});
-    }
-    if (++s >= s1) break;
-    stage(std::integral_constant<int, 0>{}, std::true_type{});
+  auto go = [&](auto before) {      // the stage behind the one in buffer `before`
+    if (++s >= s1) return false;
+    stage(std::integral_constant<int, (decltype(before)::value + 1) % C::BUFFERS>{}, std::true_type{});
+    return true;
+  };
+  while (while_true(go, buffers)) {
   }
   wait_vm<0>();
   lds_barrier();      // the buffers are free

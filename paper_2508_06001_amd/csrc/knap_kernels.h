@@ -149,6 +149,7 @@ struct GemmProblem {
   int M, N, K;
   int segments;                   // 1 or 2 products of K each, added up
   int tiles_m, tiles_n;
+  int step;                       // columns of a tile, of each of a pair
 };
 struct GemmLaunch {
   GemmProblem p[3];
@@ -171,10 +172,10 @@ struct FfnArgs {
   float* partial;
 };
 size_t ffn_partial_bytes(int64_t tokens, int width, int hidden, bool backward);
-// Whether a forward takes the form of knap_ffn_few.hip: up to 16 tokens, and up to 32 of smaller weights, whose tiles are too few for the card; larger
-// ones are the faster in tiles, which read the second 16 tokens less often (24 tokens, us, this form and tiles: 768 x 2048 12 and 21, 2048 x 5504 30 and 33,
-// 4096 x 10944 72 and 67).
-inline bool ffn_few(int64_t tokens, int64_t width, int64_t hidden) { return tokens <= 16 || (tokens <= 32 && width * hidden <= 16000000); }
+// Whether a forward takes the form of knap_ffn_few.hip: up to 16 tokens, and up to 32 of smaller weights; it reads the second 16 tokens as often as there
+// are workgroups, which tiles do not (us, this form and tiles: 768 x 2048, 32 tokens 14.7 and 21.9; 2048 x 5504, 17 tokens 30 and 34, 24 34 and 34, 32 38 and
+// 34; 4096 x 10944, 16 tokens 68.5 and 69.8, 24 80 and 70; 4096 x 16384, 16 tokens 93 and 102, 17 101 and 102).
+inline bool ffn_few(int64_t tokens, int64_t width, int64_t hidden) { return tokens <= 16 || (tokens <= 32 && tokens * width * hidden <= 270000000); }
 hipError_t launch_ffn_few(const FfnArgs& a, hipStream_t stream);
 hipError_t launch_ffn_fwd(const FfnArgs& a, hipStream_t stream);
 hipError_t launch_ffn_bwd(const FfnArgs& a, hipStream_t stream);

@@ -73,6 +73,13 @@ def test_numbers_of_tokens(T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("D,F", [(4104, 4104), (1032, 16400), (16392, 1096), (264, 8)])
+@pytest.mark.parametrize("T", [17, 24, 32, 33, 47, 64, 65])
+def test_few_tokens_of_larger_weights(T, D, F):
+    run(T, D, F, T % 2 == 0, backward=T in (24, 47))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T,D,F", [(5, 72, 136), (70, 256, 264), (300, 520, 1032), (3000, 1536, 2056)])
 def test_strides(T, D, F):
     run(T, D, F, False, pad=16)
