@@ -3,6 +3,9 @@
 // Bound by HBM: every gradient is read once for S and once more for the product, which is written once.  Workgroups take chunks of a plan
 // in turn, whose records say where they lie.  Squares and sums are in 64 bits (of which the card does as many as of 32): no gradient that is finite
 // overflows or vanishes in them, and the norm is right to its last bit in 32.  Every workgroup leaves one sum, which a second launch adds up in a fixed order.
+// The second pass goes through the plan from its end: what the first has read last is in the caches still, and stays there, since the second reads and writes
+// past them.  339.8 million elements in bf16 (2.04 GB moved), us: both passes from the front 381, the stores past the caches 364, from the end 357, the
+// loads past them as well 327 (6.2 TB/s); 34.7 million, most in 32 bits: 67.6, 55.9, 55.5, 55.0.
 #include "knap_device.h"
 #include "knap_kernels.h"
 
@@ -110,6 +113,7 @@ __global__ __launch_bounds__(1024) void grad_join_kernel(const double* __restric
   if (threadIdx.x == 0) *sum = x;
 }
 
+constexpr int kPast = 2;      // the non-temporal bit of a buffer access
 template <class T>
 __device__ __forceinline__ void chunk_scale(const T* p, T* q, int count, float c) {
   using U = Unit<T>;
@@ -119,14 +123,14 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* q, int count, float c
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, bytes), w = make_rsrc(q, bytes);
     u32x4 x[TURNS];
 #pragma unroll
-    for (int i = 0; i < TURNS; ++i) x[i] = buffer_load16(r, (threadIdx.x + i * kGradThreads) * 16u);
+    for (int i = 0; i < TURNS; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, (int)((threadIdx.x + i * kGradThreads) * 16u), 0, kPast);
 #pragma unroll
     for (int i = 0; i < TURNS; ++i) {
       float v[U::N];
       U::open(x[i], v);
 #pragma unroll
       for (int e = 0; e < U::N; ++e) v[e] *= c;
-      __builtin_amdgcn_raw_buffer_store_b128(U::close(v), w, (int)((threadIdx.x + i * kGradThreads) * 16u), 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(U::close(v), w, (int)((threadIdx.x + i * kGradThreads) * 16u), 0, kPast);
     }
     const int rest = count / U::N * U::N + threadIdx.x;
     if (rest < count) q[rest] = (T)((float)p[rest] * c);
@@ -143,10 +147,10 @@ __global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(const GradChunk
   const float c = q >= 1.0 || max_norm > 3.4028234e38f ? 1.f : (float)q;
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)length;
   if (blockIdx.x >= chunks) return;
-  GradChunk next = plan[blockIdx.x];
+  GradChunk next = plan[chunks - 1 - blockIdx.x];
   for (int64_t i = blockIdx.x; i < chunks; i += gridDim.x) {
     const GradChunk k = next;
-    if (i + gridDim.x < chunks) next = plan[i + gridDim.x];
+    if (i + gridDim.x < chunks) next = plan[chunks - 1 - i - gridDim.x];
     if (c == 1.f && k.from == k.to) continue;
     if (k.bf16) chunk_scale(static_cast<const __bf16*>(k.from), static_cast<__bf16*>(k.to), k.count, c);
     else chunk_scale(static_cast<const float*>(k.from), static_cast<float*>(k.to), k.count, c);
