@@ -93,7 +93,9 @@ __device__ __forceinline__ void finish_block(const GemmLaunch& g, const GemmProb
 // The epilogue of a whole tile.  A wave's rows of results lie across its lanes' registers, so that stores from there would write 32 bytes of 32 rows
 // each; they go through its own part of the buffers in LDS, 32 rows at a time, and out in rows, past the caches: what is written there would only
 // push out what the other workgroups multiply (256 x 256 tiles, us, from registers, through LDS, and past the caches as well: 32768 x 8192 x 1536
-// 809, 741, 640; 8192^3 858, 811, 756).
+// 809, 741, 640; 8192^3 858, 811, 756).  What the next launch reads, h, da and db, goes through them where it fits into the last one (4173 tokens, 2048 x 5504,
+// us of a forward past the caches and through them: 293 and 283, 613 tokens, 1000 x 2664, both directions 93.0 and 89.9; of 31464, 1536 x 4096, where h does
+// not fit, 3140 and 3165).
 constexpr int kPast = 2;      // the non-temporal bit of a buffer access
 template <class C, int EP>
 __device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProblem& p, int m0, int n0, const f32x16 (&acc)[C::TM][C::TN],
@@ -124,6 +126,10 @@ __device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProbl
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, pack8(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7])), to.r, at, 0, kPast);
   };
   const int columns = min(p.N, n0 + p.step);
+  auto pass_on = [&](const TileRows& to, int at, const float (&v)[8]) {      // to the next launch
+    if (g.keep) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, pack8(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7])), to.r, at, 0, 0);
+    else put(to, at, v);
+  };
   const TileRows out0(EP == kStore ? p.c : g.gate, EP == kStore ? p.ldc : p.N, g.gate || EP == kStore ? p.M : 0, columns, m0, C::BM);
   const TileRows out1(EP == kStore ? nullptr : g.up, p.N, EP != kStore && g.up ? p.M : 0, columns, m0, C::BM);
   const TileRows in0(EP == kActForward ? g.h : g.gate_in, p.N, p.M, columns, m0, C::BM), in1(g.up_in, p.N, p.M, columns, m0, C::BM);
@@ -178,7 +184,7 @@ __device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProbl
           h[e] = x[e] * s * b[e];
         }
         const int place_h = in0.at(m0 + (wm * C::TM + i) * 32 + row, n_first + 8 * unit);
-        put(in0, place_h, h);
+        pass_on(in0, place_h, h);
         put(out0, at, x);
         put(out1, at, b);
       } else {
@@ -191,8 +197,8 @@ __device__ __forceinline__ void finish_tile(const GemmLaunch& g, const GemmProbl
           const float b = __builtin_bit_cast(float, (e & 1) ? bv[e >> 1] & 0xffff0000u : bv[e >> 1] << 16);
           hidden_gradient(x[e], a, b, g.gelu, da[e], db[e]);
         }
-        put(out0, at, da);
-        put(out1, at, db);
+        pass_on(out0, at, da);
+        pass_on(out1, at, db);
       }
     }
     settle();
@@ -417,6 +423,8 @@ hipError_t run(const GemmLaunch& g, hipStream_t stream) {
   return with_form<EP, A_ROWK && B_ROWK>(g, [&](auto form, const GemmLaunch& planned) { return launch_gemm<decltype(form), A_ROWK, B_ROWK, EP>(planned, stream); });
 }
 
+constexpr int64_t kKeptBytes = 128 << 20;      // half of the card's last cache
+
 static GemmProblem product(const __bf16* a, int64_t lda, const __bf16* b, int64_t ldb, __bf16* c, int64_t ldc, int M, int N, int K) {
   GemmProblem p{};
   p.a[0] = p.a[1] = a;
@@ -434,6 +442,7 @@ static GemmLaunch up_products(const FfnArgs& a) {
   g.p[0] = product(a.x, a.x_stride, a.w_gate, a.width, nullptr, 0, a.tokens, a.hidden, a.width);
   g.p[0].b[1] = a.w_up;
   g.gate = a.gate; g.up = a.up; g.h = a.h;
+  g.keep = (int64_t)a.tokens * a.hidden * 2 <= kKeptBytes;
   g.gelu = a.gelu;
   g.partial = a.partial;
   return g;
@@ -451,6 +460,7 @@ static GemmLaunch hidden_gradients(const FfnArgs& a) {
   g.p[0] = product(a.dy, a.dy_stride, a.w_down, a.hidden, nullptr, 0, a.tokens, a.hidden, a.width);
   g.gate_in = a.gate; g.up_in = a.up;
   g.gate = a.dgate; g.up = a.dup;
+  g.keep = (int64_t)a.tokens * a.hidden * 4 <= kKeptBytes;
   g.gelu = a.gelu;
   g.partial = a.partial;
   return g;

@@ -161,6 +161,7 @@ struct GemmLaunch {
   const __bf16 *gate_in, *up_in;
   __bf16 *gate, *up, *h;
   bool gelu;
+  bool keep;                // h, da and db go through the caches
 };
 struct FfnArgs {
   const __bf16 *x, *w_gate, *w_up, *w_down, *dy;
