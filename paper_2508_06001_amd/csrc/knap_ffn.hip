@@ -4,7 +4,10 @@
 // act(a) = a s with s the logistic function of a (SiLU) or of 2 sqrt(2 / pi) (a + 0.044715 a^3) (GELU in its tanh form).
 // Five launches of the product of knap_gemm.h.  a and b are formed side by side, blocks of 32 columns of either in turn, so that a wave has both of
 // an element and act(a) b is its epilogue; da and db are the epilogue of dh, which never reaches memory; dx adds up two products over k.
-// a, b, h, da and db are rounded to 16 bits (h and da, db from 32-bit values): they are what the matrix cores multiply next.
+// a, b, h, da and db are rounded to 16 bits: h and da, db, formed from 32-bit values, because they are what the matrix cores multiply next, a and b
+// because a backward reads them (in 32 bits 515 MB more to write and as many to read at 31464 x 4096).
+// Bound by the matrix cores, the epilogue of the hidden gradients by HBM.  31464 tokens, 1536 x 4096, us and TFLOP/s: up 728 (1088), down 329 (1202), hidden
+// gradients 503 (787; 1.3 GB of a, b, da and db), dx 625 (1266), the weights' gradients 911 (1303); 4173 tokens, 2048 x 5504: up 174 (1080), down 97 (975).
 #include "knap_gemm.h"
 
 #include <algorithm>

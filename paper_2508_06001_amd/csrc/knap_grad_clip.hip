@@ -5,7 +5,7 @@
 // overflows or vanishes in them, and the norm is right to its last bit in 32.  Every workgroup leaves one sum, which a second launch adds up in a fixed order.
 // The second pass goes through the plan from its end: what the first has read last is in the caches still, and stays there, since the second reads and writes
 // past them.  339.8 million elements in bf16 (2.04 GB moved), us: both passes from the front 381, the stores past the caches 364, from the end 357, the
-// loads past them as well 327 (6.2 TB/s); 34.7 million, most in 32 bits: 67.6, 55.9, 55.5, 55.0.
+// loads past them as well 327 (6.2 TB/s; 110 and 211 the two passes); 34.7 million, most in 32 bits: 67.6, 55.9, 55.5, 55.0.
 #include "knap_device.h"
 #include "knap_kernels.h"
 

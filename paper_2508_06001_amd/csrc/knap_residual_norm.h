@@ -65,7 +65,7 @@ __device__ __forceinline__ void load_scale(const ResidualArgs& a, int seq, int g
 }
 
 // Which form a width takes: 8 columns of a thread, or 16, so that the vectors of a sequence and its sums fit the registers beside the rows; two rows
-// at a time where that leaves registers (single columns, which take a register each: 8191 rows of 1003 in 32 bits, one and two rows, forward 28 and 35 us).
+// at a time where that leaves registers (single columns, which take a register each: 7584 rows of 1003 in 32 bits, one and two rows, forward 28 and 35 us).
 template <bool WIDE, class F>
 hipError_t residual_form(int width, F f) {
   if constexpr (WIDE) {
