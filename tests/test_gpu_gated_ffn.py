@@ -73,7 +73,7 @@ def test_numbers_of_tokens(T):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("D,F", [(4104, 4104), (1032, 16400), (16392, 1096), (264, 8)])
+@pytest.mark.parametrize("D,F", [(4104, 4104), (1032, 16400), (16392, 1096), (264, 8), (768, 2048)])
 @pytest.mark.parametrize("T", [17, 24, 32, 33, 47, 64, 65])
 def test_few_tokens_of_larger_weights(T, D, F):
     run(T, D, F, T % 2 == 0, backward=T in (24, 47))
