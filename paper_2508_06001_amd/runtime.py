@@ -165,8 +165,9 @@ class GradientClip:
         self.plan = B.knap_grad_plan(self.grads, self.out)
         self.max_norm, self.eps = float(max_norm), float(eps)
         device = self.plan.device
-        self.sum_sq = torch.zeros((), dtype=torch.float64, device=device)
-        self.norm = torch.zeros((), dtype=torch.float32, device=device)
+        # not filled here: a fill would still be under way when the first call runs on another stream
+        self.sum_sq = torch.empty((), dtype=torch.float64, device=device)
+        self.norm = torch.empty((), dtype=torch.float32, device=device)
         self.workspace = torch.empty(B.KNAP_GRAD_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
     def sum_squares(self, stream=None):

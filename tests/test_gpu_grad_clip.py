@@ -164,6 +164,25 @@ def test_captured_calls_follow_the_gradients():
         assert float(a.norm) == float(b.norm) and all(torch.equal(g, e) for g, e in zip(grads, eager)), turn
 
 
+@pytest.mark.gpu
+def test_at_once_on_another_stream_than_the_current_one():
+    import torch
+    import paper_2508_06001_amd as K
+    other = torch.cuda.Stream()
+    grads = tensors([50_001, 3, 8192], ["fp32", "bf16", "bf16"])
+    before = [g.clone() for g in grads]
+    want = clip([g.clone() for g in grads], 1.0)
+    for turn in range(20):
+        for g, b in zip(grads, before):
+            g.copy_(b)
+        torch.cuda.synchronize()
+        c = K.GradientClip(grads, 1.0)
+        c.clip(stream=other)
+        torch.cuda.synchronize()
+        assert float(c.norm) == want, turn
+        check(before, grads, want, 1.0, 1e-6)
+
+
 def arrays(at, numel, types):
     import ctypes as C
     n = max(1, len(at))
