@@ -31,12 +31,13 @@ __device__ __forceinline__ void activation(float a, bool gelu, float& s, float& 
   }
 }
 
-// da and db of an element
+// da and db of an element.  What may be zero is a factor before what may be large: where the activation or its slope vanishes, a du, dh b and dh a may be
+// past the range, and infinity times zero is no number.
 __device__ __forceinline__ void hidden_gradient(float dh, float a, float b, bool gelu, float& da, float& db) {
   float s, du;
   activation(a, gelu, s, du);
-  da = dh * b * __builtin_fmaf(a * du, s * (1.f - s), s);
-  db = dh * a * s;
+  da = dh * (b * __builtin_fmaf(a * (s * (1.f - s)), du, s));
+  db = dh * (a * s);
 }
 
 // The epilogue of one block, from its registers (of tiles whose parts were added up)
