@@ -426,7 +426,7 @@ size_t knap_layer_norm_bwd_workspace_bytes(int64_t rows, int width);
  *
  * Supported: 1 <= width <= KNAP_LAYER_NORM_MAX_WIDTH, 0 <= rows < 2^31, n_seq <= KNAP_MAX_SEQS, eps finite and >= 0
  * (a row of zeros, in a layer norm a constant one, with eps = 0 gives NaN), alpha finite.  Values that are not finite stay in their row
- * but for the sums.  rows = 0 enqueues nothing in the forward and zeros in the sums in the backward.  As for the
+ * but for the sums; without a norm in front of the next branch the values of x reach no gradient.  rows = 0 enqueues nothing in the forward and zeros in the sums in the backward.  As for the
  * forward of attention, the first call of the library on a device must not be captured.
  * ------------------------------------------------------------------------ */
 #define KNAP_NORM_NONE  0

@@ -137,7 +137,8 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS > 512 ? 4 : 2) void residual
 #pragma unroll
       for (int i = 0; i < C::COLS; ++i) {
         f[k][i] = POST ? (raw_f[k].get(i) - raw_stats[k][2]) * rp[k] : raw_f[k].get(i);
-        x[k][i] = __builtin_fmaf(f[k][i], gz[i], raw_x[k].get(i));
+        // without a norm no gradient depends on x', whatever it holds: a zero by a product of it would be none of an infinity
+        x[k][i] = dy_base ? __builtin_fmaf(f[k][i], gz[i], raw_x[k].get(i)) : 0.f;
       }
     }
     const RowCursor now = at;
