@@ -1,8 +1,10 @@
-"""Gated feed-forward block on values at the ends of the range."""
+"""Gated feed-forward block on values at the ends of the range, on rows that are not finite, and between columns that are not: what a form's masks
+behind the last row, column and k have to keep apart, at sizes that no stage divides, in every form of tiles."""
 import pytest
 
 from gpu_util import say
 from oracle import gated_ffn as G
+from test_gpu_gated_ffn import Guarded, inputs
 
 HALF = 2.0 ** -8
 # gate, up and dy of a column; x is a power of two, so that a and b are exact
@@ -49,3 +51,58 @@ def test_where_the_activation_is_flat_its_gradients_are_what_the_formula_says(T,
     assert near(dx, da * g + db * u, (da * g).abs() + (db * u).abs(), 2)
     assert near(dwg, da.T @ xv, da.abs().T @ xv, 2)
     assert near(dwu, db.T @ xv, db.abs().T @ xv, 2)
+
+
+# one and two blocks of the few-token form, a row of tiles of 32 and of 64 tokens, the three forms of tiles, with parts and without, in every product
+FORMS = [(5, 72, 136), (20, 72, 136), (33, 136, 72), (24, 4104, 4104), (60, 72, 136), (60, 1032, 2056), (300, 264, 136), (613, 1000, 2664), (4173, 1032, 5512),
+         (5000, 1544, 264), (9000, 520, 2056), (12001, 1544, 4104)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,D,F", FORMS)
+def test_a_bad_row_stays_in_its_row_in_every_form(T, D, F):
+    """The other rows have the same bits as without it: neither k's behind a row's end nor rows behind a tile's meet what the next row holds."""
+    import torch
+    import paper_2508_06001_amd as K
+    say(f"[gpu] ffn, bad rows T={T} D={D} F={F}")
+    x, wg, wu, wd, dy = inputs(T, D, F)
+    f = K.GatedFeedForward(T, D, F, wg, wu, wd)
+    y = f.forward(x).clone()
+    dx = f.backward(x, dy)[0].clone()
+    bad_x, bad_dy = {T - 1, T // 2}, {1, T // 2 + 1}
+    bx, bdy = x.clone(), dy.clone()
+    bx[T - 1] = float("nan")
+    bx[T // 2, 0] = float("inf")
+    bdy[1] = float("nan")
+    bdy[T // 2 + 1, 0] = float("-inf")
+    by = f.forward(bx).clone()
+    bdx = f.backward(bx, bdy)[0].clone()
+    torch.cuda.synchronize()
+    for got, clean, bad in ((by, y, bad_x), (bdx, dx, bad_x | bad_dy)):
+        good = torch.tensor([t not in bad for t in range(T)], device="cuda")
+        assert torch.equal(got[good], clean[good])
+        assert not bool(torch.isfinite(got[~good]).all(1).any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,D,F", FORMS + [(17, 264, 520), (48, 264, 520), (64, 1032, 4104), (3000, 1536, 2056)])
+def test_columns_between_rows_are_not_looked_at(T, D, F):
+    """x and dy as columns of a wider tensor that is NaN elsewhere, y and dx as columns of another."""
+    import torch
+    import paper_2508_06001_amd as K
+    say(f"[gpu] ffn, between NaN T={T} D={D} F={F}")
+    x, wg, wu, wd, dy = inputs(T, D, F)
+    wide = [Guarded(T, D, 24) for _ in range(4)]
+    xs, dys, y, dx = (w.view for w in wide)
+    xs.copy_(x)
+    dys.copy_(dy)
+    f = K.GatedFeedForward(T, D, F, wg, wu, wd)
+    f.y, f.dx = y, dx
+    f.forward(xs)
+    f.backward(xs, dys)
+    torch.cuda.synchronize()
+    for n, w in zip(("x", "dy", "y", "dx"), wide):
+        w.check(n)
+    val, off = G.gated_ffn(*(t.double() for t in (x, wg, wu, wd)), False, dy.double())
+    for n, t in (("y", y), ("dx", dx), ("dw_gate", f.dw_gate), ("dw_up", f.dw_up), ("dw_down", f.dw_down)):
+        assert G.worst_block(t, val[n], off[n]) <= 1.0, n
