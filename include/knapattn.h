@@ -474,7 +474,8 @@ size_t knap_residual_norm_bwd_workspace_bytes(int64_t rows, int width, int n_seq
  * knap_gated_ffn_fwd_workspace_bytes / _bwd_workspace_bytes(tokens, width, hidden) bytes, 256-byte aligned (NULL where that is 0): parts of
  * sums over k and, backward, da and db; its contents on entry are ignored; one for each call that may run at the same time.
  *
- * Supported: width and hidden multiples of 8, 8 <= width, hidden <= KNAP_FFN_MAX_WIDTH, strides <= 2^20, 0 <= tokens <= 2^26; pointers aligned to 16 bytes.
+ * Supported: width and hidden multiples of 8, 8 <= width, hidden <= KNAP_FFN_MAX_WIDTH, strides <= 2^20, 0 <= tokens <= 2^26,
+ * tokens times the larger of width and hidden <= 2^37; pointers aligned to 16 bytes.
  * tokens = 0 enqueues nothing in the forward and zeros in the weights' gradients in the backward.  Rows are
  * independent of each other: a value that is not finite stays in its row of y and dx.  As for the forward of attention, the first call of
  * the library on a device must not be captured.

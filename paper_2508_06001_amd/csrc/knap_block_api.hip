@@ -168,10 +168,13 @@ int knap_residual_norm_bwd(const void* x, int x_type, int64_t x_stride, int64_t 
 namespace {
 
 constexpr int64_t kFfnMostTokens = (int64_t)1 << 26;
+constexpr int64_t kFfnMostElements = (int64_t)1 << 37;      // of x or h: what a launch's workgroups cover (launch_gemm)
 
+bool ffn_sizes(int64_t tokens, int width, int hidden) {
+  return tokens <= kFfnMostTokens && width <= KNAP_FFN_MAX_WIDTH && hidden <= KNAP_FFN_MAX_WIDTH && tokens * std::max(width, hidden) <= kFfnMostElements;
+}
 int check_ffn(int64_t tokens, int width, int hidden, const void* w_gate, const void* w_up, const void* w_down, int act) {
-  if (tokens < 0 || tokens > kFfnMostTokens || width < 8 || width > KNAP_FFN_MAX_WIDTH || width % 8 || hidden < 8 || hidden > KNAP_FFN_MAX_WIDTH || hidden % 8)
-    return KNAP_ERR_INVALID_ARG;
+  if (tokens < 0 || width < 8 || width % 8 || hidden < 8 || hidden % 8 || !ffn_sizes(tokens, width, hidden)) return KNAP_ERR_INVALID_ARG;
   if (act != KNAP_SILU && act != KNAP_GELU_TANH) return KNAP_ERR_INVALID_ARG;
   if (tokens > 0 && (!w_gate || !w_up || !w_down || !aligned(w_gate, 16) || !aligned(w_up, 16) || !aligned(w_down, 16))) return KNAP_ERR_INVALID_ARG;
   return KNAP_OK;
@@ -186,12 +189,12 @@ size_t ffn_hidden_bytes(int64_t tokens, int hidden) { return round_up((size_t)to
 extern "C" {
 
 size_t knap_gated_ffn_fwd_workspace_bytes(int64_t tokens, int width, int hidden) {
-  if (tokens <= 0 || tokens > kFfnMostTokens || width <= 0 || hidden <= 0 || width > KNAP_FFN_MAX_WIDTH || hidden > KNAP_FFN_MAX_WIDTH) return 0;
+  if (tokens <= 0 || width <= 0 || hidden <= 0 || !ffn_sizes(tokens, width, hidden)) return 0;
   return round_up(knap::ffn_partial_bytes(tokens, width, hidden, false), 256);
 }
 
 size_t knap_gated_ffn_bwd_workspace_bytes(int64_t tokens, int width, int hidden) {
-  if (tokens <= 0 || tokens > kFfnMostTokens || width <= 0 || hidden <= 0 || width > KNAP_FFN_MAX_WIDTH || hidden > KNAP_FFN_MAX_WIDTH) return 0;
+  if (tokens <= 0 || width <= 0 || hidden <= 0 || !ffn_sizes(tokens, width, hidden)) return 0;
   return 2 * ffn_hidden_bytes(tokens, hidden) + round_up(knap::ffn_partial_bytes(tokens, width, hidden, true), 256);
 }
 

@@ -410,7 +410,10 @@ auto with_form(const GemmLaunch& g, F f) {
 template <class C, bool A_ROWK, bool B_ROWK, int EP>
 hipError_t launch_gemm(const GemmLaunch& g, hipStream_t stream) {
   constexpr int BLOCKS = C::TM * C::TN / (EP == kActForward ? 2 : 1);
-  if (g.whole + (int64_t)g.tail * g.splits > 1 << 22) return hipErrorInvalidValue;      // 2^36 results, which the card does not hold
+  // A grid has fewer than 2^32 threads: 2^24 workgroups of 256.  The entry points let up to 2^37 results of a product pass, which are at most 2^22 + 2^18 + 2^9
+  // of Large's tiles.  The other forms' tiles are a quarter of those, but a form is taken by its estimate, which for many tiles is 1.7 / 256 a tile of Large,
+  // 1.05 / 512 of Small and 0.6 / 256 of Deep: where there are more than 3.3 times as many of them, Large is taken.
+  if (g.whole + (int64_t)g.tail * g.splits >= 1 << 24) return hipErrorInvalidValue;
   hipLaunchKernelGGL((gemm_kernel<C, A_ROWK, B_ROWK, EP>), dim3(g.whole + g.tail * g.splits), dim3(C::THREADS), 0, stream, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.tail == 0) return e;
