@@ -157,18 +157,29 @@ class GatedFeedForward:
 
 class GradientClip:
     """Buffers + calls of the global norm of a fixed list of gradients and clipping by it, in place or into `out`.  Ranks that hold parts of the
-    gradients call sum_squares, add up `sum_sq` (an all-reduce of one float64) and call scale; clip does both on one GPU."""
+    gradients call sum_squares, add up `sum_sq` (an all-reduce of one float64) and call scale; clip does both on one GPU.
+    The plan points to the gradients' memory as it was laid down, which this object keeps.  A program whose gradients are other tensors from step to
+    step (set to None in between) asks stands_for, or copies them to ones that stay."""
 
     def __init__(self, grads, max_norm: float, eps: float = 1e-6, out=None):
         self.grads = list(grads)
         self.out = self.grads if out is None else list(out)
         self.plan = B.knap_grad_plan(self.grads, self.out)
+        # tensors of their own on the same memory: a caller's tensor may be given other memory, and what it had would be freed under the plan
+        self._held = [t.detach() for t in self.grads]
+        self._held_out = [] if out is None else [t.detach() for t in self.out]
         self.max_norm, self.eps = float(max_norm), float(eps)
         device = self.plan.device
         # not filled here: a fill would still be under way when the first call runs on another stream
         self.sum_sq = torch.empty((), dtype=torch.float64, device=device)
         self.norm = torch.empty((), dtype=torch.float32, device=device)
         self.workspace = torch.empty(B.KNAP_GRAD_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+
+    def stands_for(self, grads) -> bool:
+        """Whether these are the gradients that the plan was laid down for, where they were then."""
+        grads = list(grads)
+        return len(grads) == len(self._held) and all(
+            g is not None and g.data_ptr() == h.data_ptr() and g.numel() == h.numel() and g.dtype is h.dtype for g, h in zip(grads, self._held))
 
     def sum_squares(self, stream=None):
         B.knap_grad_sum_squares(self.plan, self.sum_sq, self.workspace, B.KNAP_GRAD_WORKSPACE_BYTES, stream)
