@@ -24,6 +24,15 @@ def bf16_device_to_bits(t: torch.Tensor) -> np.ndarray:
     return t.detach().contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
 
 
+def _settled(values, dtype, device) -> torch.Tensor:
+    """`values` as a tensor on the device, in memory when this returns: a call may go to any stream, and a conversion of values that are on a GPU
+    runs on the current one."""
+    t = torch.as_tensor(values, dtype=dtype).to(device)
+    if t.is_cuda and t is not values and not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(t.device).synchronize()
+    return t
+
+
 class RotaryPositions:
     """Rotary positions of one packed bag: the first `rot` columns of every head turned by `frequencies` (rot / 2 of them, see
     knap_rope_frequencies) times `factor`.  `positions`: int32 (T,) or (T, axes) with the pairs of each axis in `axis_pairs`;
@@ -32,9 +41,9 @@ class RotaryPositions:
     def __init__(self, rot: int, layout: int, frequencies: Sequence[float], factor: float = 1.0, positions=None, axis_pairs=None,
                  cu_seqlens=None, device="cuda"):
         self.rot, self.layout, self.factor = int(rot), int(layout), float(factor)
-        self.freq = torch.as_tensor(frequencies, dtype=torch.float64).to(device)
+        self.freq = _settled(frequencies, torch.float64, device)
         self.positions, self.axis_pairs = positions, list(axis_pairs) if axis_pairs else None
-        self.cu = None if cu_seqlens is None else torch.as_tensor(cu_seqlens, dtype=torch.int32).to(device)
+        self.cu = None if cu_seqlens is None else _settled(cu_seqlens, torch.int32, device)
 
     def forward(self, q, k, q_out, k_out, stream=None):
         B.knap_rope_fwd(q, k, self.rot, self.layout, self.freq, self.factor, q_out, k_out, self.positions, self.axis_pairs, self.cu, stream)
@@ -86,7 +95,7 @@ class ResidualNorm:
                  train: bool = True, device="cuda"):
         self.rows, self.width, self.alpha, self.eps = int(rows), int(width), float(alpha), float(eps)
         self.norm, self.weight, self.post_norm, self.post_weight = norm, weight, post_norm, post_weight
-        self.cu = None if cu_seqlens is None else torch.as_tensor(cu_seqlens, dtype=torch.int32).to(device)
+        self.cu = None if cu_seqlens is None else _settled(cu_seqlens, torch.int32, device)
         self.n_seq = 1 if self.cu is None else self.cu.numel() - 1
         self.branch = bool(branch)
         normed = norm != B.KNAP_NORM_NONE
