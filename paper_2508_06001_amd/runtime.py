@@ -280,7 +280,9 @@ class VarlenDiffAttention:
         self.out2 = self.dq = self.dk = self.dv = self.dlam = self.workspace = None
         if train:
             self.out2, self.dq, self.dk, self.dv = new(), new(), new(), new()
-            self.dlam = torch.zeros((self.H,), dtype=torch.float32, device=self.device)
+            # not filled here, but for no sequences, where a backward writes nothing: a fill that is still under way when a backward runs on
+            # another stream would put zeros over its result
+            self.dlam = (torch.empty if self.n_seq else torch.zeros)((self.H,), dtype=torch.float32, device=self.device)
             nbytes = B.knap_varlen_diff_attn_bwd_workspace_bytes(self.T, self.n_seq, self.H, self.d)
             self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
         if rope is not None:

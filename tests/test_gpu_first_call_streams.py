@@ -43,3 +43,53 @@ def test_boundaries_and_frequencies_that_were_converted_on_the_gpu():
     torch.cuda.synchronize()
     assert torch.equal(got.x_out, want.x_out) and torch.equal(got.y, want.y)
     assert torch.equal(turned[0], turned[2]) and torch.equal(turned[1], turned[3])
+
+
+@pytest.mark.gpu
+def test_dlambda_is_not_filled_behind_the_backward():
+    import torch
+    import paper_2508_06001_amd as K
+    say("[gpu] first call on another stream: dlambda")
+    lens, H, d = [0, 70, 200], 2, 64
+    q, k, v, dout = (torch.randn((200, H, d), device="cuda").bfloat16() for _ in range(4))
+    lam = torch.full((H,), 0.5, device="cuda")
+    other = torch.cuda.Stream()
+
+    def run(stream):
+        attn = K.VarlenDiffAttention(lens, H, d, 0.125, lam)
+        attn.forward(q, k, v, stream=stream)
+        attn.backward(q, k, v, dout, stream=stream)
+        return attn
+
+    want = run(None)
+    torch.cuda.synchronize()
+    assert bool(want.dlam.all())
+    busy()
+    got = run(other)
+    torch.cuda.synchronize()
+    assert torch.equal(got.dlam, want.dlam) and torch.equal(got.dq, want.dq)
+
+
+def test_dlambda_of_no_sequences_is_zero():
+    import torch
+    import paper_2508_06001_amd as K
+    for _ in range(8):
+        keep = torch.full((64,), 7.0)
+        del keep
+        assert not bool(K.VarlenDiffAttention([0], 64, 64, 0.125, None, device="cpu").dlam.any())
+
+
+def test_what_a_backward_writes_is_not_filled_when_the_object_is_made(monkeypatch):
+    import torch
+    import paper_2508_06001_amd as K
+
+    def filled(*args, **kw):
+        raise AssertionError("a fill")
+
+    for name in ("zeros", "ones", "full"):
+        monkeypatch.setattr(torch, name, filled)
+    K.VarlenDiffAttention([0, 3], 2, 64, 0.125, None, device="cpu")
+    K.VarlenAttention([0, 3], 2, 64, 0.125, device="cpu")
+    K.LayerNorm(3, 8, device="cpu")
+    K.ResidualNorm(3, 8, [0, 3], device="cpu")
+    K.GatedFeedForward(3, 8, 8, None, None, None, device="cpu")
