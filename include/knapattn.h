@@ -406,14 +406,14 @@ size_t knap_layer_norm_bwd_workspace_bytes(int64_t rows, int width);
  *
  * x, x_out, dx_out, dx (rows, width): x_type, KNAP_BF16 or KNAP_F32.  f, y, df, dy (rows, width):
  * branch_type, the same or KNAP_BF16.  Columns are contiguous; strides count elements from a row to the
- * next, >= width (not looked at for a single row, nor for tensors that are not given).
+ * next, >= width, <= 2^30 (not looked at for a single row, nor for tensors that are not given).
  * cu_seqlens: device int32[n_seq + 1] as for attention; rows from cu_seqlens[n_seq] on (a padded
  * bag) are left as they were.  NULL: one sequence of all rows (n_seq = 1).
  * gate, scale, shift (n_seq, width): mod_type; gate_stride of gate, mod_stride of scale and shift
- * count elements from a sequence to the next, >= 0 (chunks of one projection's (n_seq, 6 width)
+ * count elements from a sequence to the next, 0 to 2^40 (chunks of one projection's (n_seq, 6 width)
  * result as they lie).  NULL for ones, zeros, zeros.  weight, post_weight: `width` values of w_type, NULL for ones.
  * x' is normed as it is before its rounding to x_type, and the backward forms it again from x and f.
- * Sums and statistics are 32-bit.  stats: fp32 (4, rows): mean and rstd of x', then of f; rows of it whose
+ * Sums and statistics are 32-bit: magnitudes in a row from about 2^64 / sqrt(width) on, whose squares' sum is past the range, norm to zeros.  stats: fp32 (4, rows): mean and rstd of x', then of f; rows of it whose
  * norm there is not are not touched; NULL in the forward where no backward follows, in the backward where there are no norms.
  * dgate, dscale, dshift: fp32 (n_seq, width), strides dgate_stride and dmod_stride >= width;
  * dweight, dpost_weight: fp32[width].  Any of them, dx and df may be NULL: not wanted.  The sums are
@@ -421,7 +421,7 @@ size_t knap_layer_norm_bwd_workspace_bytes(int64_t rows, int width);
  * the same device gives the same bits.  workspace: knap_residual_norm_bwd_workspace_bytes(rows, width, n_seq)
  * bytes, 256-byte aligned, needed where one of the sums is wanted; one for each call that may run at the same time.
  * x_out may be x and dx may be dx_out (in place, same stride; the backward takes x as it was); otherwise
- * outputs must not alias inputs or each other.  Pointers need the alignment of their type only; 16 bytes, strides and
+ * outputs must not alias inputs or each other, and f is another tensor than x.  Pointers need the alignment of their type only; 16 bytes, strides and
  * widths that are multiples of 8 give the fast form.
  *
  * Supported: 1 <= width <= KNAP_LAYER_NORM_MAX_WIDTH, 0 <= rows < 2^31, n_seq <= KNAP_MAX_SEQS, eps finite and >= 0
@@ -473,6 +473,7 @@ size_t knap_residual_norm_bwd_workspace_bytes(int64_t rows, int width, int n_seq
  * other, and have the same bits every time for the same call.  workspace: device scratch of at least
  * knap_gated_ffn_fwd_workspace_bytes / _bwd_workspace_bytes(tokens, width, hidden) bytes, 256-byte aligned (NULL where that is 0): parts of
  * sums over k and, backward, da and db; its contents on entry are ignored; one for each call that may run at the same time.
+ * Work is laid out for the card's 256 compute units; results on a device of another number are as right.
  *
  * Supported: width and hidden multiples of 8, 8 <= width, hidden <= KNAP_FFN_MAX_WIDTH, strides <= 2^20, 0 <= tokens <= 2^26,
  * tokens times the larger of width and hidden <= 2^37; pointers aligned to 16 bytes.

@@ -7,7 +7,7 @@
 // a, b, h, da and db are rounded to 16 bits: h and da, db, formed from 32-bit values, because they are what the matrix cores multiply next, a and b
 // because a backward reads them (in 32 bits 515 MB more to write and as many to read at 31464 x 4096).
 // Bound by the matrix cores, the epilogue of the hidden gradients by HBM.  31464 tokens, 1536 x 4096, us and TFLOP/s: up 728 (1088), down 329 (1202), hidden
-// gradients 503 (787; 1.3 GB of a, b, da and db), dx 625 (1266), the weights' gradients 911 (1303); 4173 tokens, 2048 x 5504: up 174 (1080), down 97 (975).
+// gradients 503 (787; 1327 MB read, where a, b, dy and Wd are 625, and 516 written), dx 625 (1266), the weights' gradients 911 (1303); 4173 tokens, 2048 x 5504: up 174 (1080), down 97 (975).
 #include "knap_gemm.h"
 
 #include <algorithm>
@@ -303,10 +303,13 @@ using Few64 = GemmCfg<64, 64, 2, 1, 5, 1>;
 // ---------------------------------------------------------------------------
 // Plans
 // ---------------------------------------------------------------------------
+// The card's, not asked of the device: a call's plan, and with it the size of its workspace, depends on its sizes alone.  On a device of other compute units (a
+// partition) results are as right, and the last round of tiles is cut for another one.
 constexpr int kGemmCus = 256;
 
 // What a form costs, in us, as measured: a stage of a round of workgroups with `fill` of the card's places taken, and what a part adds that is written
-// and read again.
+// and read again.  It compares forms of many stages.  A launch's start, a ring's first fill and the epilogue are not in it: calls of few stages take about
+// twice as long (613 tokens, 1000 x 2664, 16 stages: up 9.0 by it and 16.4 us, hidden gradients 7.5 and 19.4).
 struct FormCost {
   int places;                   // workgroups at one time
   float stage, more, part;      // a stage takes stage + more * fill
@@ -314,7 +317,7 @@ struct FormCost {
 template <class C> constexpr FormCost form_cost() { return {kGemmCus, 1.15f, 0.55f, 0.105f}; }      // Large
 template <> constexpr FormCost form_cost<Small>() { return {2 * kGemmCus, 0.62f, 0.43f, 0.026f}; }
 template <> constexpr FormCost form_cost<Deep>() { return {kGemmCus, 0.38f, 0.22f, 0.026f}; }
-constexpr float kJoin = 4.f;      // the launch that adds up parts
+constexpr float kJoin = 4.f;      // the launch that adds up parts (4.8 to 6.6 us of few, 12.6 of the weights' gradients of 1536 x 4096)
 
 // Lays down the tiles of the products in `g` in form C, and how many parts the tiles of the last round go in (which is not full: more of them take less
 // time and more bytes); returns the estimated time.

@@ -64,8 +64,12 @@ __device__ __forceinline__ void load_scale(const ResidualArgs& a, int seq, int g
   for (int i = 0; i < C::COLS; ++i) sw[i] = norm_has<C>(g, i, a.width) ? (1.f + sw[i]) * w[i] : 0.f;
 }
 
-// Which form a width takes: 8 columns of a thread, or 16, so that the vectors of a sequence and its sums fit the registers beside the rows; two rows
-// at a time where that leaves registers (single columns, which take a register each: 7584 rows of 1003 in 32 bits, one and two rows, forward 28 and 35 us).
+// Which form a width takes: 8 columns of a thread, or 16 of 513 to 1024 aligned ones and of the widest rows, so that up to 8192 columns the vectors of a sequence and its sums
+// fit the registers beside the rows (but for 2 to 4 of a backward of single columns in 32 bits with a branch of 16); two rows at a time where that leaves
+// registers (single columns, which take a register each: 7584 rows of 1003 in 32 bits, one and two rows, forward 28 and 35 us).
+// Beyond 8192 columns they do not fit: 1024 threads have 128 registers each, and a backward spills 72 to 92 of them in 16-byte accesses and 114 to 218
+// column by column, a forward up to 7 and 73 to 116.  Inputs in no cache, norms on both sides, forward and backward with its sums: 8000 rows of 5000, bf16, 92 and
+// 225 us (3.5 and 2.1 TB/s); 6000 of 9600, bf16, 114 and 990 (4.0 and 0.7); 3000 of 16384, bf16, 96 and 756; 6000 of 9601, 32 bits, no post norm, 543 and 1146.
 template <bool WIDE, class F>
 hipError_t residual_form(int width, F f) {
   if constexpr (WIDE) {
@@ -82,7 +86,7 @@ hipError_t residual_form(int width, F f) {
   if (width <= 8192) return f(NormCfg<1024, 1, 1, WIDE>{});
   return f(NormCfg<1024, 2, 1, WIDE>{});
 }
-// whether the next rows' loads are under way while these are worked on: where there are registers for both
+// whether the next rows' loads are under way while these are worked on: where there are registers for both, which 1024 lanes, of rows wider than 4096, do not have
 template <class C, class TX>
 constexpr bool residual_ahead() { return C::LANES < 1024 && (C::UNITS == 1 || sizeof(TX) == 2); }
 

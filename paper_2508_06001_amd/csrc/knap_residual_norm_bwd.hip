@@ -8,7 +8,8 @@
 // registers; at the sequence's end (or its own) they go to the workspace, row `workgroup + sequence` of them: both only ever rise along the
 // rows, so that no two meet.  A second kernel adds up each sequence's rows in a fixed order: no atomics, the same bits every time.
 // 31464 rows of 1536 in bf16, layer norm: 580 MB in 109 us (5.3 TB/s) and 5.6 for the sums; 24576 of 2048, x in 32 bits, RMS on both sides: 906 MB in 194
-// (4.7) and 8.8; 7584 of 1003 in 32 bits, columns singly: 183 MB in 42 (4.3) and 7.5.
+// (4.7) and 8.8; 7584 of 1003 in 32 bits, columns singly: 183 MB in 42 (4.3) and 7.5.  These are of one set of inputs, part of which stays in the last cache;
+// of three in turn, in no cache, with the sums: 149 us, 241 and 64.
 #include "knap_residual_norm.h"
 
 #include <algorithm>
