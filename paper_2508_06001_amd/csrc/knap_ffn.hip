@@ -32,11 +32,12 @@ __device__ __forceinline__ void activation(float a, bool gelu, float& s, float& 
 }
 
 // da and db of an element.  What may be zero is a factor before what may be large: where the activation or its slope vanishes, a du, dh b and dh a may be
-// past the range, and infinity times zero is no number.
+// past the range, and infinity times zero is no number.  Half of the slope, which may be above one, so that b times it stays in the range as well.
 __device__ __forceinline__ void hidden_gradient(float dh, float a, float b, bool gelu, float& da, float& db) {
   float s, du;
   activation(a, gelu, s, du);
-  da = dh * (b * __builtin_fmaf(a * (s * (1.f - s)), du, s));
+  const float half = 0.5f * s;
+  da = 2.f * (dh * (b * __builtin_fmaf(a * (half * (1.f - s)), du, half)));
   db = dh * (a * s);
 }
 

@@ -14,18 +14,12 @@ FLAT = [(3e38, 1e-3, 0.03), (-3e38, 1e-3, 0.03), (1e37, 1e-3, 0.03), (-1e37, 1e-
         (20.0, 1.0, 1.0), (-20.0, 1.0, 1.0), (17.0, 1.0, 1.0), (16.0, 1.0, 1.0), (-16.0, 1.0, 1.0), (0.5, 1.0, 1.0), (-0.5, 1.0, 1.0), (0.0, 1.0, 1.0)]
 
 
-@pytest.mark.gpu
-@pytest.mark.parametrize("gelu", [False, True])
-@pytest.mark.parametrize("T", [3, 24, 40, 300])
-def test_where_the_activation_is_flat_its_gradients_are_what_the_formula_says(T, gelu):
-    """Diagonal weights: every element by itself.  h, da, db and the result are rounded to bf16 once each, a half step for each; the logistic function has
-    |a| 2^-23 of its value where it is small, below 2^-17 here; what is below 1e-36 may be zero."""
+def of_single_columns(T, gelu, columns):
     import torch
     import paper_2508_06001_amd as K
-    say(f"[gpu] ffn, flat T={T} gelu={gelu}")
     D = F = 64
     act = K.KNAP_GELU_TANH if gelu else K.KNAP_SILU
-    col = torch.tensor((FLAT * 4)[:D], device="cuda").bfloat16()
+    col = torch.tensor((columns * D)[:D], device="cuda").bfloat16()
     x = (0.5 ** (torch.arange(T, device="cuda") % 3)).float()[:, None].expand(T, D).bfloat16().contiguous()
     wg, wu = torch.diag(col[:, 0]).contiguous(), torch.diag(col[:, 1]).contiguous()
     wd = (0.5 * torch.eye(D, device="cuda")).bfloat16()
@@ -51,6 +45,24 @@ def test_where_the_activation_is_flat_its_gradients_are_what_the_formula_says(T,
     assert near(dx, da * g + db * u, (da * g).abs() + (db * u).abs(), 2)
     assert near(dwg, da.T @ xv, da.abs().T @ xv, 2)
     assert near(dwu, db.T @ xv, db.abs().T @ xv, 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gelu", [False, True])
+@pytest.mark.parametrize("T", [3, 24, 40, 300])
+def test_where_the_activation_is_flat_its_gradients_are_what_the_formula_says(T, gelu):
+    """Diagonal weights: every element by itself.  h, da, db and the result are rounded to bf16 once each, a half step for each; the logistic function has
+    |a| 2^-23 of its value where it is small, below 2^-17 here; what is below 1e-36 may be zero."""
+    say(f"[gpu] ffn, flat T={T} gelu={gelu}")
+    of_single_columns(T, gelu, FLAT)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gelu", [False, True])
+def test_a_slope_above_one_at_the_end_of_the_range(gelu):
+    """dh b slope is far inside the range, b slope is not; the same bounds."""
+    say(f"[gpu] ffn, steep gelu={gelu}")
+    of_single_columns(40, gelu, [(1.0, 3.3e38, 1e-10), (0.875, 3.38e38, -1e-10), (1.0, -3.38e38, 1e-20), (1.0, 1.0, 1.0)])
 
 
 # one and two blocks of the few-token form, a row of tiles of 32 and of 64 tokens, the three forms of tiles, with parts and without, in every product
